@@ -303,7 +303,7 @@ def _inputs(case, seed):
         begun = (at // BLOCK == (start // BLOCK)[req]) & held & (n["new"] > 0)[req]
         s.update(old_place=_gpu(np.flatnonzero(begun)), new_place=_gpu(np.flatnonzero(~held)))
         s.update(old_block=s["block"][s["old_place"]], new_block=s["block"][s["new_place"]],
-                 start=_gpu(start.astype(np.int32)), max_new=int(n["new"].max()),
+                 start=_gpu(start.astype(np.int32)),
                  new_offset=_gpu(np.concatenate([[0], np.cumsum(n["new"])]).astype(np.int32)))
         h = _gpu(held)
         for name, y in (("k8", k), ("v8", v)):
@@ -379,8 +379,8 @@ def run(state):
             jet.jet_quantize_kv_e4m3(s["layout"], s["dims"], x["k"], x["v"], x["k8"], x["v8"])
             return _held(s)
         if op == "append":
-            jet.jet_append_kv_e4m3(s["layout"], s["dims"], s["start"], s["new_offset"],
-                                   s["max_new"], x["k"], x["v"], x["k8"], x["v8"])
+            jet.jet_append_kv_e4m3(s["layout"], s["dims"], s["start"], s["new_offset"], x["k"],
+                                   x["v"], x["k8"], x["v8"])
             return _held(s)
         if op == "read":
             jet.jet_dequantize_kv_e4m3(s["layout"], s["dims"], x["k8"], x["v8"], s["k"], s["v"])

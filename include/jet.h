@@ -214,6 +214,82 @@ jet_status jet_prefix_attend(const jet_layout* lay, const jet_dims* dims, const 
                              void* stream);
 
 /*
+ * The prefix K/V cache in 8 bits (Sec. 4.1: the prefix is evaluated once and its
+ * keys and values are reused by every candidate, so reading them bounds the
+ * step's attention, and holding them bounds the batch). JET_KV_BLOCK tokens of a
+ * request, counted from its first, share one exponent per key/value head, for
+ * keys and values apart. With amax the largest magnitude of the block's finite
+ * elements of the head,
+ *   X     = the least integer in [-117, 119] with amax <= 448 * 2^X (-117 for a
+ *           block of zeros)
+ *   code  = the OCP FP8 E4M3 code of x * 2^-X: nearest, ties to even, saturated at
+ *           +-448; infinite and NaN elements are held as NaN
+ *   value = code * 2^X, a number of bf16 and of float32 for every finite code
+ *
+ * Layout of a cache buffer (keys, or values; jet_kv_e4m3_bytes() bytes):
+ *   - codes [total_prefix, Hkv, d], packed like the bf16 prefix K/V, padded to a
+ *     multiple of 256 bytes;
+ *   - exponent bytes X + 127 [total_prefix / JET_KV_BLOCK + R, Hkv] (the quotient
+ *     rounded down): block b of request r at place
+ *     prefix_offset[r] / JET_KV_BLOCK + r + b (rounded down). Places past a
+ *     request's last block are unused: never written, never read.
+ */
+#define JET_KV_BLOCK 64
+
+/* Bytes of one 8-bit cache buffer (keys, or values) of a batch of these sizes and
+ * dims.Hkv, dims.d; 0 on invalid arguments. */
+size_t jet_kv_e4m3_bytes(const jet_sizes* n, const jet_dims* dims);
+
+/*
+ * jet_quantize_kv_e4m3 - write the whole prefix into 8-bit caches.
+ *   k, v    [total_prefix, Hkv, d] dims.dtype (float32 or bf16), as
+ *           jet_prefill_attend takes them
+ *   k8, v8  cache buffers of jet_kv_e4m3_bytes()
+ * Uses the layout's prefix sizes and dims.dtype, Hkv, d (64, 128 or 256) only.
+ */
+jet_status jet_quantize_kv_e4m3(const jet_layout* lay, const jet_dims* dims, const void* k,
+                                const void* v, void* k8, void* v8, void* stream);
+
+/*
+ * jet_append_kv_e4m3 - write the next tokens of each request, for prefixes that come
+ * in pieces or token by token.
+ *   start      [R] int32 (device)      tokens of request r that its cache holds
+ *   new_offset [R + 1] int32 (device)  request r's new tokens are rows
+ *              [new_offset[r], new_offset[r + 1]) of k and v (none: equal entries)
+ *   k, v       [n_new, Hkv, d] dims.dtype
+ *   k8, v8     cache buffers laid out for the whole prefix (the layout's P_r)
+ * The new tokens become positions start[r] .. of request r and must end within its
+ * prefix; a request whose words do not fit is left out and reported as
+ * JET_ERR_DEVICE. A block that holds tokens already keeps the larger of its
+ * exponent and the new tokens'; where the exponent grows, the codes it holds are
+ * rounded again to the new one. Codes past the new tokens are left as they were
+ * (a block's later tokens are to be written again after it).
+ */
+jet_status jet_append_kv_e4m3(const jet_layout* lay, const jet_dims* dims, const int32_t* start,
+                              const int32_t* new_offset, int32_t n_new, const void* k,
+                              const void* v, void* k8, void* v8, void* stream);
+
+/*
+ * jet_dequantize_kv_e4m3 - read 8-bit caches back: k, v [total_prefix, Hkv, d]
+ * dims.dtype = code * 2^X, exactly (NaN for the NaN codes).
+ */
+jet_status jet_dequantize_kv_e4m3(const jet_layout* lay, const jet_dims* dims, const void* k8,
+                                  const void* v8, void* k, void* v, void* stream);
+
+/*
+ * jet_prefix_attend_e4m3 - jet_prefix_attend over 8-bit prefix caches k8, v8: the
+ * same rows, masks, scale and outputs, the prefix keys and values being the caches'
+ * values. q, k_cand, v_cand and o are in dims.dtype (float32 or bf16). bf16: at most
+ * 128 query heads a key/value head (else JET_ERR_UNSUPPORTED). ws/ws_bytes: scratch of at least
+ * jet_attend_workspace_bytes_e4m3().
+ */
+size_t jet_attend_workspace_bytes_e4m3(const jet_sizes* n, const jet_dims* dims);
+jet_status jet_prefix_attend_e4m3(const jet_layout* lay, const jet_dims* dims, const void* q,
+                                  const void* k8, const void* v8, const void* k_cand,
+                                  const void* v_cand, void* o, void* ws, size_t ws_bytes,
+                                  void* stream);
+
+/*
  * jet_prefill_attend - the prefill before the scoring step: causal
  * self-attention over every request's prefix (Sec. 4.1: the shared prefix is
  * evaluated once and its K/V reused by every candidate; scale 1/sqrt(d), no

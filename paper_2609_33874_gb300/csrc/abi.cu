@@ -10,6 +10,7 @@
 #include "jet.h"
 
 #include "jet_internal.h"
+#include "kv_cache.h"
 
 namespace jet {
 
@@ -100,6 +101,20 @@ jet_status check_attn_dims(const jet_dims* d) {
   if (d->Hq < 1 || d->Hkv < 1 || d->Hq % d->Hkv != 0) return JET_ERR_SHAPE;
   if (d->d != 64 && d->d != 128 && d->d != 256) return JET_ERR_UNSUPPORTED;
   return JET_OK;
+}
+
+// what the 8-bit caches take of the dims
+jet_status check_kv_dims(const jet_dims* d) {
+  jet_status s = check_dtype(d);
+  if (s) return s;
+  if (d->Hkv < 1) return JET_ERR_SHAPE;
+  if (d->d != 64 && d->d != 128 && d->d != 256) return JET_ERR_UNSUPPORTED;
+  return JET_OK;
+}
+
+// places of blocks whose (keys or values, head) CTAs one grid holds
+jet_status check_kv_grid(long long places, const jet_dims* d) {
+  return places * 2 > INT32_MAX / d->Hkv ? JET_ERR_CAPACITY : JET_OK;
 }
 
 jet_status check_lm_dims(const jet_dims* d) {
@@ -230,6 +245,99 @@ extern "C" jet_status jet_prefix_attend(const jet_layout* lay, const jet_dims* d
   return cuda_status(jet::launch_prefix_attend(*lay, *dims, plan, q, k_pre, v_pre, k_cand, v_cand, o,
                                                ws, jet::device_status_ptr(),
                                                static_cast<cudaStream_t>(stream)));
+}
+
+extern "C" size_t jet_kv_e4m3_bytes(const jet_sizes* n, const jet_dims* d) {
+  if (!n || n->R < 0 || n->total_prefix < 0 || check_kv_dims(d) != JET_OK) return 0;
+  return jet::kv_size(*n, *d).bytes;
+}
+
+extern "C" jet_status jet_quantize_kv_e4m3(const jet_layout* lay, const jet_dims* dims,
+                                           const void* k, const void* v, void* k8, void* v8,
+                                           void* stream) {
+  JET_TRY(check_layout(lay));
+  JET_TRY(check_kv_dims(dims));
+  const jet_sizes& n = lay->n;
+  if (n.R == 0) return JET_OK;
+  JET_TRY(check_kv_grid(jet::kv_size(n, *dims).blocks, dims));
+  JET_TRY(check_ptr(k, n.total_prefix));
+  JET_TRY(check_ptr(v, n.total_prefix));
+  JET_TRY(check_ptr(k8, n.total_prefix));
+  JET_TRY(check_ptr(v8, n.total_prefix));
+  return cuda_status(jet::launch_kv_quantize(*lay, *dims, k, v, k8, v8, jet::device_status_ptr(),
+                                             static_cast<cudaStream_t>(stream)));
+}
+
+extern "C" jet_status jet_append_kv_e4m3(const jet_layout* lay, const jet_dims* dims,
+                                         const int32_t* start, const int32_t* new_offset,
+                                         int32_t n_new, const void* k, const void* v, void* k8,
+                                         void* v8, void* stream) {
+  JET_TRY(check_layout(lay));
+  JET_TRY(check_kv_dims(dims));
+  if (n_new < 0) return JET_ERR_ARG;
+  const jet_sizes& n = lay->n;
+  if (n.R == 0) return JET_OK;
+  if (n_new > n.total_prefix) return JET_ERR_SHAPE;
+  if (n_new == 0) return JET_OK;
+  JET_TRY(check_kv_grid(jet::kv_append_places(n, n_new), dims));
+  if (!start || !new_offset) return JET_ERR_ARG;
+  if (((reinterpret_cast<uintptr_t>(start) | reinterpret_cast<uintptr_t>(new_offset)) & 3u) != 0)
+    return JET_ERR_ALIGN;
+  JET_TRY(check_ptr(k, n_new));
+  JET_TRY(check_ptr(v, n_new));
+  JET_TRY(check_ptr(k8, n.total_prefix));
+  JET_TRY(check_ptr(v8, n.total_prefix));
+  return cuda_status(jet::launch_kv_append(*lay, *dims, start, new_offset, n_new, k, v, k8, v8,
+                                           jet::device_status_ptr(),
+                                           static_cast<cudaStream_t>(stream)));
+}
+
+extern "C" jet_status jet_dequantize_kv_e4m3(const jet_layout* lay, const jet_dims* dims,
+                                             const void* k8, const void* v8, void* k, void* v,
+                                             void* stream) {
+  JET_TRY(check_layout(lay));
+  JET_TRY(check_kv_dims(dims));
+  const jet_sizes& n = lay->n;
+  if (n.R == 0) return JET_OK;
+  JET_TRY(check_kv_grid(jet::kv_size(n, *dims).blocks, dims));
+  JET_TRY(check_ptr(k8, n.total_prefix));
+  JET_TRY(check_ptr(v8, n.total_prefix));
+  JET_TRY(check_ptr(k, n.total_prefix));
+  JET_TRY(check_ptr(v, n.total_prefix));
+  return cuda_status(jet::launch_kv_dequantize(*lay, *dims, k8, v8, k, v,
+                                               jet::device_status_ptr(),
+                                               static_cast<cudaStream_t>(stream)));
+}
+
+extern "C" size_t jet_attend_workspace_bytes_e4m3(const jet_sizes* n, const jet_dims* d) {
+  if (!n || n->R < 0 || n->N < 0 || check_attn_dims(d) != JET_OK) return 0;
+  return jet::attn_plan_kv8(*n, *d).bytes;
+}
+
+extern "C" jet_status jet_prefix_attend_e4m3(const jet_layout* lay, const jet_dims* dims,
+                                             const void* q, const void* k8, const void* v8,
+                                             const void* k_cand, const void* v_cand, void* o,
+                                             void* ws, size_t ws_bytes, void* stream) {
+  JET_TRY(check_layout(lay));
+  JET_TRY(check_attn_dims(dims));
+  if (dims->dtype == JET_DTYPE_BF16 && dims->Hq / dims->Hkv > jet::attn_tc_block())
+    return JET_ERR_UNSUPPORTED;
+  const jet_sizes& n = lay->n;
+  if (n.R == 0) return JET_OK;
+  if ((long long)n.R * dims->Hkv > 65535) return JET_ERR_CAPACITY;
+  const long long F = n.N - n.R;
+  JET_TRY(check_ptr(q, n.N));
+  JET_TRY(check_ptr(k8, n.total_prefix));
+  JET_TRY(check_ptr(v8, n.total_prefix));
+  JET_TRY(check_ptr(k_cand, F));
+  JET_TRY(check_ptr(v_cand, F));
+  JET_TRY(check_ptr(o, n.N));
+  const jet::AttnPlan plan = jet::attn_plan_kv8(n, *dims);
+  if (!ws || ws_bytes < plan.bytes) return JET_ERR_WORKSPACE;
+  if (!aligned16(ws)) return JET_ERR_ALIGN;
+  return cuda_status(jet::launch_prefix_attend_kv8(*lay, *dims, plan, q, k8, v8, k_cand, v_cand, o,
+                                                   ws, jet::device_status_ptr(),
+                                                   static_cast<cudaStream_t>(stream)));
 }
 
 extern "C" size_t jet_prefill_workspace_bytes(const jet_sizes* n, const jet_dims* d) {

@@ -16,6 +16,7 @@
 
 #include "jet_device.cuh"
 #include "jet_internal.h"
+#include "kv_cache.h"
 
 namespace jet {
 namespace {
@@ -35,18 +36,37 @@ constexpr size_t prefix_smem_bytes() {
                           size_t(kQV) * (kKT + 4));
 }
 
+// four elements: of float32 and bf16 as they are, of an 8-bit cache times f
+__device__ __forceinline__ float4 load4(const float* p, float) {
+  return *reinterpret_cast<const float4*>(p);
+}
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p, float) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u),
+                     __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
+}
+__device__ __forceinline__ float4 load4(const uint8_t* p, float f) {
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+  const float2 a = e4m3x2_to_f32(w), b = e4m3x2_to_f32(w >> 16);
+  return make_float4(a.x * f, a.y * f, b.x * f, b.y * f);
+}
+
 // One CTA: one prefix chunk of one (request, key/value head) for kQV query
 // vectors. Thread (vec = tid / 16, sub = tid % 16) scores keys sub and sub+16
 // of each tile for its vector and accumulates output dims 4 sub + 64 i .. + 3.
 // Small batches are bound by the chain of loads: the query block and a tile are
 // fetched by 16-byte loads that are all in flight at once, and chunks go down to
 // one tile (7 rows over 128 keys: 13.2 -> 4.9 us).
-template <int DH>
+// TK: float32 keys and values, or the codes of an 8-bit cache (uint8_t) with their
+// exponent bytes k_exp, v_exp: a tile lies within one block of 64 tokens, so it has one
+// scale of keys and one of values.
+template <int DH, typename T, typename TK>
 __global__ void __launch_bounds__(kThreads)
 attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* __restrict__ row_offset,
                      int R, int N, int total_prefix, int Hq, int Hkv, int chunk,
-                     const float* __restrict__ q, const float* __restrict__ k_pre,
-                     const float* __restrict__ v_pre, float* __restrict__ o_part,
+                     const T* __restrict__ q, const TK* __restrict__ k_pre,
+                     const TK* __restrict__ v_pre, const uint8_t* __restrict__ k_exp,
+                     const uint8_t* __restrict__ v_exp, float* __restrict__ o_part,
                      float2* __restrict__ ml_part, int* status) {
   pdl_begin();
   extern __shared__ __align__(16) float smem[];
@@ -83,13 +103,19 @@ attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* _
   // a tile's keys past k_end are zeros
   float4 kr[KI], vr[KI];
   auto fetch = [&](int kb) {
+    float fk = 1.f, fv = 1.f;
+    if constexpr (sizeof(TK) == 1) {
+      const size_t at = size_t(kv_place(p0, r, kb / kKvBlock)) * Hkv + kh;
+      fk = kv_scale(k_exp[at]);
+      fv = kv_scale(v_exp[at]);
+    }
 #pragma unroll
     for (int i = 0; i < KI; ++i) {
       const int e = tid + i * kThreads, j = e / C4, c = e % C4;
       const bool in = kb + j < k_end;
       const size_t idx = (size_t(p0 + kb + (in ? j : 0)) * Hkv + kh) * DH + 4 * c;
-      kr[i] = in ? *reinterpret_cast<const float4*>(k_pre + idx) : zero;
-      vr[i] = in ? *reinterpret_cast<const float4*>(v_pre + idx) : zero;
+      kr[i] = in ? load4(k_pre + idx, fk) : zero;
+      vr[i] = in ? load4(v_pre + idx, fv) : zero;
     }
   };
   if (k_begin < k_end) fetch(k_begin);
@@ -99,7 +125,7 @@ attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* _
     float4 x = zero;
     if (gv < nvec) {
       const int n = n0 + gv / g, h = kh * g + gv % g;
-      x = *reinterpret_cast<const float4*>(q + (size_t(n) * Hq + h) * DH + 4 * c);
+      x = load4(q + (size_t(n) * Hq + h) * DH + 4 * c, 1.f);
     }
     *reinterpret_cast<float4*>(Qs + vv * (DH + 4) + 4 * c) =
         make_float4(x.x * scale, x.y * scale, x.z * scale, x.w * scale);
@@ -184,17 +210,17 @@ attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* _
   }
 }
 
-// One warp per (row, query head), float32: the prefix chunks' partials, then the
+// One warp per (row, query head): the prefix chunks' partials, then the
 // row's own causal candidate keys, normalised. The loads that do not depend on
 // each other go out together: the chunks' (m, l) one a lane, their outputs and
 // the candidate's keys and values four at a time.
-template <int DH>
+template <int DH, typename T>
 __global__ void __launch_bounds__(128)
 attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restrict__ row_cand,
                     const int32_t* __restrict__ cand_row_offset, int N, int R, int C, int Hq, int Hkv,
-                    int splits, const float* __restrict__ q, const float* __restrict__ k_cand,
-                    const float* __restrict__ v_cand, const float* __restrict__ o_part,
-                    const float2* __restrict__ ml_part, float* __restrict__ o, int* status) {
+                    int splits, const T* __restrict__ q, const T* __restrict__ k_cand,
+                    const T* __restrict__ v_cand, const float* __restrict__ o_part,
+                    const float2* __restrict__ ml_part, T* __restrict__ o, int* status) {
   pdl_begin();
   const int lane = threadIdx.x & 31;
   const long long idx = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
@@ -205,7 +231,7 @@ attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restri
   constexpr int PER = DH / 32;
   float qv[PER];
 #pragma unroll
-  for (int i = 0; i < PER; ++i) qv[i] = q[(size_t(n) * Hq + h) * DH + lane + 32 * i];
+  for (int i = 0; i < PER; ++i) qv[i] = to_f32(q[(size_t(n) * Hq + h) * DH + lane + 32 * i]);
   float acc[PER];
   float m, l;
   combine_chunks<DH>(true, splits, N, Hq, n, h, lane, ml_part, o_part, m, l, acc);
@@ -222,8 +248,8 @@ attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restri
           const size_t kb = (size_t(min(n4 + t, n) - r - 1) * Hkv + kh) * DH + lane;
 #pragma unroll
           for (int i = 0; i < PER; ++i) {
-            kv[t][i] = k_cand[kb + 32 * i];
-            vv[t][i] = v_cand[kb + 32 * i];
+            kv[t][i] = to_f32(k_cand[kb + 32 * i]);
+            vv[t][i] = to_f32(v_cand[kb + 32 * i]);
           }
         }
 #pragma unroll
@@ -252,39 +278,69 @@ attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restri
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) o[(size_t(n) * Hq + h) * DH + lane + 32 * i] = acc[i] * inv;
+  for (int i = 0; i < PER; ++i)
+    o[(size_t(n) * Hq + h) * DH + lane + 32 * i] = from_f32<T>(acc[i] * inv);
+}
+
+// the prefix chunks, then their merge with the candidates' own keys
+template <int DH, typename T, typename TK>
+cudaError_t launch_simt(const jet_layout& lay, const jet_dims& d, const AttnPlan& plan,
+                        const void* q, const void* k_pre, const void* v_pre, size_t exp_off,
+                        const void* k_cand, const void* v_cand, void* o, void* ws, int* status,
+                        cudaStream_t st) {
+  const jet_sizes& n = lay.n;
+  float* o_part = static_cast<float*>(ws);
+  float2* ml_part = reinterpret_cast<float2*>(o_part + size_t(plan.splits) * n.N * d.Hq * DH);
+  const size_t smem = prefix_smem_bytes<DH>();
+  cudaError_t e = cudaFuncSetAttribute(attend_prefix_kernel<DH, T, TK>,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+  if (e != cudaSuccess) return e;
+  dim3 grid(plan.splits, plan.qgroups, unsigned(n.R * d.Hkv));
+  e = launch_pdl(attend_prefix_kernel<DH, T, TK>, grid, dim3(kThreads), smem, st,
+                 lay.prefix_offset, lay.row_offset, n.R, n.N, n.total_prefix, d.Hq, d.Hkv,
+                 plan.chunk, static_cast<const T*>(q), static_cast<const TK*>(k_pre),
+                 static_cast<const TK*>(v_pre), static_cast<const uint8_t*>(k_pre) + exp_off,
+                 static_cast<const uint8_t*>(v_pre) + exp_off, o_part, ml_part, status);
+  if (e != cudaSuccess) return e;
+  const long long warps = (long long)n.N * d.Hq;
+  return launch_pdl(attend_merge_kernel<DH, T>, dim3(unsigned((warps + 3) / 4)), dim3(128), 0, st,
+                    lay.row_req, lay.row_cand, lay.cand_row_offset, n.N, n.R, n.C, d.Hq, d.Hkv,
+                    plan.splits, static_cast<const T*>(q), static_cast<const T*>(k_cand),
+                    static_cast<const T*>(v_cand), o_part, ml_part, static_cast<T*>(o), status);
 }
 
 template <int DH>
 cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& plan,
                          const void* q, const void* k_pre, const void* v_pre, const void* k_cand,
                          const void* v_cand, void* o, void* ws, int* status, cudaStream_t st) {
-  const jet_sizes& n = lay.n;
-  float* o_part = static_cast<float*>(ws);
-  float2* ml_part = reinterpret_cast<float2*>(o_part + size_t(plan.splits) * n.N * d.Hq * DH);
-  cudaError_t e;
   if (d.dtype == JET_DTYPE_BF16) {
     // the tensor-core path covers the candidates' own keys and the combine
-    return launch_attend_tc(lay, d, plan, q, k_pre, v_pre, k_cand, v_cand, o, o_part, ml_part,
-                            status, st);
-  } else {
-    const size_t smem = prefix_smem_bytes<DH>();
-    e = cudaFuncSetAttribute(attend_prefix_kernel<DH>,
-                             cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
-    if (e != cudaSuccess) return e;
-    dim3 grid(plan.splits, plan.qgroups, unsigned(n.R * d.Hkv));
-    e = launch_pdl(attend_prefix_kernel<DH>, grid, dim3(kThreads), smem, st, lay.prefix_offset,
-                   lay.row_offset, n.R, n.N, n.total_prefix, d.Hq, d.Hkv, plan.chunk,
-                   static_cast<const float*>(q), static_cast<const float*>(k_pre),
-                   static_cast<const float*>(v_pre), o_part, ml_part, status);
+    float* o_part = static_cast<float*>(ws);
+    return launch_attend_tc(
+        lay, d, plan, q, k_pre, v_pre, k_cand, v_cand, o, o_part,
+        reinterpret_cast<float2*>(o_part + size_t(plan.splits) * lay.n.N * d.Hq * DH), status, st);
   }
-  if (e != cudaSuccess) return e;
-  const long long warps = (long long)n.N * d.Hq;
-  return launch_pdl(attend_merge_kernel<DH>, dim3(unsigned((warps + 3) / 4)), dim3(128), 0, st,
-                    lay.row_req, lay.row_cand, lay.cand_row_offset, n.N, n.R, n.C, d.Hq, d.Hkv,
-                    plan.splits, static_cast<const float*>(q), static_cast<const float*>(k_cand),
-                    static_cast<const float*>(v_cand), o_part, ml_part, static_cast<float*>(o),
-                    status);
+  return launch_simt<DH, float, float>(lay, d, plan, q, k_pre, v_pre, 0, k_cand, v_cand, o, ws,
+                                       status, st);
+}
+
+// the plan of the SIMT kernels: about four CTAs per SM
+AttnPlan attn_plan_simt(const jet_sizes& n, const jet_dims& d) {
+  AttnPlan p{};
+  if (n.R <= 0 || n.N <= 0 || d.Hkv <= 0 || d.Hq <= 0) return p;
+  const int g = d.Hq / d.Hkv;
+  p.qgroups = (n.max_rows * g + kQV - 1) / kQV;
+  const long long avg_vecs = ((long long)n.N * g + n.R - 1) / n.R;
+  const long long groups = (long long)n.R * d.Hkv * ((avg_vecs + kQV - 1) / kQV);
+  const int max_splits = std::max(1, (n.max_prefix + kKT - 1) / kKT);
+  const long long want = (kTargetCtas + groups - 1) / groups;
+  const int splits = int(std::min<long long>(std::max<long long>(want, 1), max_splits));
+  p.chunk = (n.max_prefix + splits - 1) / splits;
+  p.chunk = (p.chunk + kKT - 1) / kKT * kKT;
+  p.splits = (n.max_prefix + p.chunk - 1) / p.chunk;
+  const size_t vecs = size_t(p.splits) * n.N * d.Hq;
+  p.bytes = vecs * d.d * sizeof(float) + vecs * sizeof(float2);
+  return p;
 }
 
 }  // namespace
@@ -292,50 +348,40 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
 AttnPlan attn_plan(const jet_sizes& n, const jet_dims& d) {
   AttnPlan p{};
   if (n.R <= 0 || n.N <= 0 || d.Hkv <= 0 || d.Hq <= 0) return p;
+  if (d.dtype != JET_DTYPE_BF16) return attn_plan_simt(n, d);
   const int g = d.Hq / d.Hkv;
-  const bool tc = d.dtype == JET_DTYPE_BF16;
-  const int gran = tc ? 64 : kKT;                 // keys per tile
-  // query vectors per CTA: the tensor-core kernel takes whole rows (128 / g
-  // rows of g heads), the float32 kernel kQV vectors
-  const int qv = tc ? std::max(1, attn_tc_block() / g) * g : kQV;
+  const int gran = 64;                            // keys per tile
+  // query vectors per CTA: whole rows (128 / g rows of g heads)
+  const int qv = std::max(1, attn_tc_block() / g) * g;
   p.qgroups = (n.max_rows * g + qv - 1) / qv;
   // query blocks of an average request: blocks past a request's vectors exit
   // at once, so they do not count as work
   const long long avg_vecs = ((long long)n.N * g + n.R - 1) / n.R;
   const long long groups = (long long)n.R * d.Hkv * std::max<long long>(1, (avg_vecs + qv - 1) / qv);
   const int max_splits = std::max(1, (n.max_prefix + gran - 1) / gran);
-  int chunk;
-  if (tc) {
-    // the persistent kernel (one CTA per SM; items dealt out by their requests'
-    // lengths, or longest first from a list: `sorted` below) splits a request's
-    // prefix into near-equal chunks: no shorter than kMinChunkTc keys (an item's
-    // fixed cost - query block in, f32 partial out and read back by the combine - is
-    // worth about five 64-key tiles), and no finer than half of one SM's share of all
-    // key tiles, so that the schedule can balance
-    const double avg_tiles = double(n.total_prefix) / n.R / 64.0 + 0.5;
-    const double share = double(groups) * avg_tiles / kPlanSMs;  // tiles per SM
-    int least = kMinChunkTc;
-    // a few long prefixes leave most SMs idle at that length: then about
-    // kFewItems chunks in all, of at least kLeastChunk keys (one 6,000-key request
-    // with two kv heads: 320 keys 17.5 us, 640 keys 19.8 us, 128 keys 21.3 us). Past
-    // kFewGroups the combine costs what shorter chunks gain, and from 19 groups on in
-    // prefixes of up to 448 keys too (d 256; as here and at 640 keys: 8 groups of 1,000
-    // keys 13.2 and 17.7 us, 16 groups 15.2 and 17.9, of 400 12.9 and 13.3; 20 groups
-    // of 200 - 1,200 16.5 and 18.7, of 200 - 600 14.9 and 15.5, of 400 14.0 and 13.4;
-    // 24 groups of 400 14.0 and 13.4, of 700 to 4,000 the same)
-    if (groups <= kFewGroups && (groups <= 18 || n.max_prefix > 448)) {
-      const long long even = (long long)(double(groups) * avg_tiles / kFewItems + 0.999) * 64;
-      least = int(std::max<long long>(kLeastChunk, std::min<long long>(kMinChunkTc, even)));
-    }
-    chunk = std::max(least, int(share / 2.0 + 0.999) * 64);
-    chunk = std::min(chunk, max_splits * 64);  // one chunk holds the longest prefix
-  } else {
-    // about four CTAs per SM
-    long long want = (kTargetCtas + groups - 1) / groups;
-    int splits = int(std::min<long long>(std::max<long long>(want, 1), max_splits));
-    chunk = (n.max_prefix + splits - 1) / splits;
-    chunk = (chunk + gran - 1) / gran * gran;
+  // the persistent kernel (one CTA per SM; items dealt out by their requests'
+  // lengths, or longest first from a list: `sorted` below) splits a request's
+  // prefix into near-equal chunks: no shorter than kMinChunkTc keys (an item's
+  // fixed cost - query block in, f32 partial out and read back by the combine - is
+  // worth about five 64-key tiles), and no finer than half of one SM's share of all
+  // key tiles, so that the schedule can balance
+  const double avg_tiles = double(n.total_prefix) / n.R / 64.0 + 0.5;
+  const double share = double(groups) * avg_tiles / kPlanSMs;  // tiles per SM
+  int least = kMinChunkTc;
+  // a few long prefixes leave most SMs idle at that length: then about
+  // kFewItems chunks in all, of at least kLeastChunk keys (one 6,000-key request
+  // with two kv heads: 320 keys 17.5 us, 640 keys 19.8 us, 128 keys 21.3 us). Past
+  // kFewGroups the combine costs what shorter chunks gain, and from 19 groups on in
+  // prefixes of up to 448 keys too (d 256; as here and at 640 keys: 8 groups of 1,000
+  // keys 13.2 and 17.7 us, 16 groups 15.2 and 17.9, of 400 12.9 and 13.3; 20 groups
+  // of 200 - 1,200 16.5 and 18.7, of 200 - 600 14.9 and 15.5, of 400 14.0 and 13.4;
+  // 24 groups of 400 14.0 and 13.4, of 700 to 4,000 the same)
+  if (groups <= kFewGroups && (groups <= 18 || n.max_prefix > 448)) {
+    const long long even = (long long)(double(groups) * avg_tiles / kFewItems + 0.999) * 64;
+    least = int(std::max<long long>(kLeastChunk, std::min<long long>(kMinChunkTc, even)));
   }
+  int chunk = std::max(least, int(share / 2.0 + 0.999) * 64);
+  chunk = std::min(chunk, max_splits * 64);  // one chunk holds the longest prefix
   p.chunk = chunk;
   p.splits = (n.max_prefix + chunk - 1) / chunk;
   const size_t vecs = size_t(p.splits) * n.N * d.Hq;
@@ -348,12 +394,32 @@ AttnPlan attn_plan(const jet_sizes& n, const jet_dims& d) {
   // for their launch (requests of 2,048 - 8,192 keys, two kv heads: 128 with the list
   // 240 us, dealt 245; 90 181 and 188; 256 unsplit 438 and 426; 64 of 4,096 111 and
   // 106; 400 groups of 300 - 4,000 keys 175 and 171).
-  p.sorted = tc && p.splits > 1 && chunk >= 16 * 64 && 2 * groups <= 5 * kPlanSMs &&
+  p.sorted = p.splits > 1 && chunk >= 16 * 64 && 2 * groups <= 5 * kPlanSMs &&
              4LL * n.max_prefix * n.R > 5LL * n.total_prefix;
   // the work list: (request, kv head, query block, chunk) items plus two counters,
   // 16-byte aligned, after the partials
   if (p.sorted) p.bytes += 32 + 16 * size_t(n.R) * d.Hkv * p.qgroups * p.splits;
   return p;
+}
+
+AttnPlan attn_plan_kv8(const jet_sizes& n, const jet_dims& d) { return attn_plan_simt(n, d); }
+
+cudaError_t launch_prefix_attend_kv8(const jet_layout& lay, const jet_dims& d,
+                                     const AttnPlan& plan, const void* q, const void* k8,
+                                     const void* v8, const void* k_cand, const void* v_cand,
+                                     void* o, void* ws, int* status, cudaStream_t st) {
+  const size_t off = kv_size(lay.n, d).exp_off;
+#define JET_ATT8(DH)                                                                              \
+  return d.dtype == JET_DTYPE_BF16                                                                \
+             ? launch_simt<DH, __nv_bfloat16, uint8_t>(lay, d, plan, q, k8, v8, off, k_cand,      \
+                                                       v_cand, o, ws, status, st)                 \
+             : launch_simt<DH, float, uint8_t>(lay, d, plan, q, k8, v8, off, k_cand, v_cand, o,   \
+                                               ws, status, st)
+  if (d.d == 64) JET_ATT8(64);
+  if (d.d == 128) JET_ATT8(128);
+  if (d.d == 256) JET_ATT8(256);
+#undef JET_ATT8
+  return cudaErrorInvalidValue;
 }
 
 cudaError_t launch_prefix_attend(const jet_layout& lay, const jet_dims& d, const AttnPlan& plan,

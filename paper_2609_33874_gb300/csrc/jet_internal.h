@@ -115,6 +115,23 @@ cudaError_t launch_prefix_attend(const jet_layout& lay, const jet_dims& d, const
                                  const void* k_cand, const void* v_cand, void* o, void* ws,
                                  int* status, cudaStream_t st);
 
+// the same over an 8-bit prefix cache (codes and exponent bytes in k8, v8)
+AttnPlan attn_plan_kv8(const jet_sizes& n, const jet_dims& d);
+cudaError_t launch_prefix_attend_kv8(const jet_layout& lay, const jet_dims& d,
+                                     const AttnPlan& plan, const void* q, const void* k8,
+                                     const void* v8, const void* k_cand, const void* v_cand,
+                                     void* o, void* ws, int* status, cudaStream_t st);
+
+// the 8-bit prefix cache (kv_cache.cu): the whole prefix written, the next tokens of
+// each request, the cache read back
+cudaError_t launch_kv_quantize(const jet_layout& lay, const jet_dims& d, const void* k,
+                               const void* v, void* k8, void* v8, int* status, cudaStream_t st);
+cudaError_t launch_kv_append(const jet_layout& lay, const jet_dims& d, const int32_t* start,
+                             const int32_t* new_offset, int n_new, const void* k, const void* v,
+                             void* k8, void* v8, int* status, cudaStream_t st);
+cudaError_t launch_kv_dequantize(const jet_layout& lay, const jet_dims& d, const void* k8,
+                                 const void* v8, void* k, void* v, int* status, cudaStream_t st);
+
 // bf16 cascade attention on the tensor cores (attend_tc.cu): prefix chunks and
 // the candidates' own keys, plus the chunk combine; query vectors per CTA
 int attn_tc_block();

@@ -79,6 +79,17 @@ def _load() -> ctypes.CDLL:
         "jet_workspace_bytes": (SZ, [ctypes.POINTER(jet_sizes), ctypes.POINTER(jet_dims)]),
         "jet_prefix_attend": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
                                   P, P, P, P, P, P, P, SZ, P]),
+        "jet_kv_e4m3_bytes": (SZ, [ctypes.POINTER(jet_sizes), ctypes.POINTER(jet_dims)]),
+        "jet_quantize_kv_e4m3": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
+                                     P, P, P, P, P]),
+        "jet_append_kv_e4m3": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
+                                   P, P, I, P, P, P, P, P]),
+        "jet_dequantize_kv_e4m3": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
+                                       P, P, P, P, P]),
+        "jet_attend_workspace_bytes_e4m3": (SZ, [ctypes.POINTER(jet_sizes),
+                                                 ctypes.POINTER(jet_dims)]),
+        "jet_prefix_attend_e4m3": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
+                                       P, P, P, P, P, P, P, SZ, P]),
         "jet_prefill_workspace_bytes": (SZ, [ctypes.POINTER(jet_sizes),
                                              ctypes.POINTER(jet_dims)]),
         "jet_prefill_attend": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
@@ -127,6 +138,8 @@ def _load() -> ctypes.CDLL:
 _lib = _load()
 DECLARED = ("jet_abi_version", "jet_status_string", "jet_layout_plan", "jet_layout_words",
             "jet_layout_build", "jet_layout_bind", "jet_workspace_bytes", "jet_prefix_attend",
+            "jet_kv_e4m3_bytes", "jet_quantize_kv_e4m3", "jet_append_kv_e4m3",
+            "jet_dequantize_kv_e4m3", "jet_attend_workspace_bytes_e4m3", "jet_prefix_attend_e4m3",
             "jet_prefill_workspace_bytes", "jet_prefill_attend", "jet_prefill_state",
             "jet_fork_state", "jet_fork_state_rule", "jet_score_candidates", "jet_score_candidates_noalloc",
             "jet_quantize_rows_e4m3", "jet_workspace_bytes_e4m3", "jet_score_candidates_e4m3",
@@ -287,6 +300,66 @@ def jet_prefix_attend(layout, dims: jet_dims, q, k_pre, v_pre, k_cand, v_cand, o
                                   _addr(k_pre), _addr(v_pre), _addr(k_cand), _addr(v_cand),
                                   _addr(o), _addr(ws), int(ws_bytes), _stream(stream)),
            "jet_prefix_attend")
+
+
+def jet_kv_e4m3_bytes(sizes: jet_sizes, dims: jet_dims) -> int:
+    """Bytes of one 8-bit cache buffer, keys or values (0 if invalid)."""
+    return int(_lib.jet_kv_e4m3_bytes(ctypes.byref(sizes), ctypes.byref(dims)))
+
+
+def _kv_cache(layout, dims: jet_dims, *buffers) -> None:
+    """Cache buffers given as tensors must be uint8 and hold jet_kv_e4m3_bytes()."""
+    need = None
+    for x in buffers:
+        if x is None or isinstance(x, int):
+            continue
+        if need is None:
+            need = jet_kv_e4m3_bytes(_lay(layout).n, dims)
+        if x.element_size() != 1 or x.numel() < need:
+            raise ValueError(f"an 8-bit cache is a uint8 tensor of at least {need} bytes")
+
+
+def jet_quantize_kv_e4m3(layout, dims: jet_dims, k, v, k8, v8, stream=None) -> None:
+    """The whole prefix K/V into 8-bit caches (see include/jet.h)."""
+    _kv_cache(layout, dims, k8, v8)
+    _check(_lib.jet_quantize_kv_e4m3(ctypes.byref(_lay(layout)), ctypes.byref(dims), _addr(k),
+                                     _addr(v), _addr(k8), _addr(v8), _stream(stream)),
+           "jet_quantize_kv_e4m3")
+
+
+def jet_append_kv_e4m3(layout, dims: jet_dims, start, new_offset, k, v, k8, v8, stream=None) -> None:
+    """The next tokens of each request, k and v [n_new, Hkv, d] tensors, into 8-bit
+    caches; start [R] and new_offset [R + 1] are int32 device tensors (see
+    include/jet.h)."""
+    _kv_cache(layout, dims, k8, v8)
+    if k.shape != v.shape:
+        raise ValueError("k and v must have the same shape")
+    _check(_lib.jet_append_kv_e4m3(ctypes.byref(_lay(layout)), ctypes.byref(dims), _addr(start),
+                                   _addr(new_offset), int(k.shape[0]), _addr(k), _addr(v),
+                                   _addr(k8), _addr(v8), _stream(stream)), "jet_append_kv_e4m3")
+
+
+def jet_dequantize_kv_e4m3(layout, dims: jet_dims, k8, v8, k, v, stream=None) -> None:
+    """8-bit caches read back into k, v [total_prefix, Hkv, d] (see include/jet.h)."""
+    _kv_cache(layout, dims, k8, v8)
+    _check(_lib.jet_dequantize_kv_e4m3(ctypes.byref(_lay(layout)), ctypes.byref(dims), _addr(k8),
+                                       _addr(v8), _addr(k), _addr(v), _stream(stream)),
+           "jet_dequantize_kv_e4m3")
+
+
+def jet_attend_workspace_bytes_e4m3(sizes: jet_sizes, dims: jet_dims) -> int:
+    return int(_lib.jet_attend_workspace_bytes_e4m3(ctypes.byref(sizes), ctypes.byref(dims)))
+
+
+def jet_prefix_attend_e4m3(layout, dims: jet_dims, q, k8, v8, k_cand, v_cand, o, ws,
+                           ws_bytes: Optional[int] = None, stream=None) -> None:
+    """jet_prefix_attend over 8-bit prefix caches (see include/jet.h)."""
+    _kv_cache(layout, dims, k8, v8)
+    ws_bytes = ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    _check(_lib.jet_prefix_attend_e4m3(ctypes.byref(_lay(layout)), ctypes.byref(dims), _addr(q),
+                                       _addr(k8), _addr(v8), _addr(k_cand), _addr(v_cand),
+                                       _addr(o), _addr(ws), int(ws_bytes), _stream(stream)),
+           "jet_prefix_attend_e4m3")
 
 
 def jet_prefill_workspace_bytes(sizes: jet_sizes, dims: jet_dims) -> int:

@@ -118,6 +118,17 @@ def quantize_lm_head_mxfp8(w_lm: torch.Tensor, stream=None):
     return w_mx
 
 
+def quantize_prefix(layout, dims: "jet.jet_dims", k_pre: torch.Tensor, v_pre: torch.Tensor,
+                    stream=None):
+    """8-bit caches (uint8, jet_kv_e4m3_bytes each) of the packed prefix keys and
+    values [total_prefix, Hkv, d] (jet_quantize_kv_e4m3), for a step built with
+    kv="e4m3"; ``layout`` is the batch's :class:`jet.DeviceLayout`."""
+    nb = jet.jet_kv_e4m3_bytes(layout.sizes, dims)
+    k8, v8 = (torch.empty(nb, dtype=torch.uint8, device=k_pre.device) for _ in range(2))
+    jet.jet_quantize_kv_e4m3(layout, dims, k_pre, v_pre, k8, v8, stream=stream)
+    return k8, v8
+
+
 class ScoringStep:
     """Device state of one batch shape.
 
@@ -130,12 +141,19 @@ class ScoringStep:
     "w4" (the pair returned by :func:`quantize_lm_head_w4`) or "mxfp8" (the
     buffer returned by :func:`quantize_lm_head_mxfp8`).
     ``rule`` selects the fork's recurrence: "delta" (gated delta rule) or "gla"
-    (plain gated linear attention).
+    (plain gated linear attention). ``kv`` = "e4m3" reads the prefix from 8-bit
+    caches: the inputs k_pre and v_pre are then the uint8 buffers of
+    :func:`quantize_prefix` (half the bytes of a bf16 prefix, on the device and
+    over the host link) instead of tensors of the step's type.
     """
 
     def __init__(self, layout: "jet.HostLayout", dims: "jet.jet_dims", mode: int,
                  device="cuda", hybrid: bool = False, keep_fork_state: bool = False,
-                 chain: bool = False, lm: str = "bf16", rule: str = "delta"):
+                 chain: bool = False, lm: str = "bf16", rule: str = "delta",
+                 kv: Optional[str] = None):
+        if kv not in (None, "e4m3"):
+            raise ValueError("kv must be None or 'e4m3'")
+        self.kv = kv
         if lm not in ("bf16", "e4m3", "w4", "mxfp8"):
             raise ValueError("lm must be 'bf16', 'e4m3', 'w4' or 'mxfp8'")
         self.lm = lm
@@ -162,6 +180,8 @@ class ScoringStep:
         ws = {"bf16": jet.jet_workspace_bytes, "e4m3": jet.jet_workspace_bytes_e4m3,
               "w4": jet.jet_workspace_bytes_e4m3,
               "mxfp8": jet.jet_workspace_bytes_mxfp8}[lm](n, dims)
+        if kv:
+            ws = max(ws, jet.jet_attend_workspace_bytes_e4m3(n, dims))
         self.ws = z((ws + 15) // 16 * 4)  # float32 words, 16-byte multiple
         if hybrid:
             self.lo = z(self.F, dims.Hl, dims.dv, dtype=dt)
@@ -193,8 +213,9 @@ class ScoringStep:
         """
         d = self.dims
         lay = self.layout if layout is None else layout
-        jet.jet_prefix_attend(lay, d, x["q"], x["k_pre"], x["v_pre"], x["k_cand"], x["v_cand"],
-                              self.o, self.ws, stream=stream)
+        attend = jet.jet_prefix_attend_e4m3 if self.kv else jet.jet_prefix_attend
+        attend(lay, d, x["q"], x["k_pre"], x["v_pre"], x["k_cand"], x["v_cand"], self.o, self.ws,
+               stream=stream)
         if self.hybrid:
             jet.jet_fork_state(lay, d, x["s_prefix"], x["lq"], x["lk"], x["lv"], x["alpha"],
                                x["beta"], self.lo, self.s_fork, stream=stream, rule=self.rule)

@@ -36,14 +36,9 @@ constexpr size_t prefix_smem_bytes() {
                           size_t(kQV) * (kKT + 4));
 }
 
-// four elements: of float32 and bf16 as they are, of an 8-bit cache times f
+// four elements: of float32 as they are, of an 8-bit cache times f
 __device__ __forceinline__ float4 load4(const float* p, float) {
   return *reinterpret_cast<const float4*>(p);
-}
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p, float) {
-  const uint2 w = *reinterpret_cast<const uint2*>(p);
-  return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u),
-                     __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u));
 }
 __device__ __forceinline__ float4 load4(const uint8_t* p, float f) {
   const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
@@ -60,11 +55,11 @@ __device__ __forceinline__ float4 load4(const uint8_t* p, float f) {
 // TK: float32 keys and values, or the codes of an 8-bit cache (uint8_t) with their
 // exponent bytes k_exp, v_exp: a tile lies within one block of 64 tokens, so it has one
 // scale of keys and one of values.
-template <int DH, typename T, typename TK>
+template <int DH, typename TK>
 __global__ void __launch_bounds__(kThreads)
 attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* __restrict__ row_offset,
                      int R, int N, int total_prefix, int Hq, int Hkv, int chunk,
-                     const T* __restrict__ q, const TK* __restrict__ k_pre,
+                     const float* __restrict__ q, const TK* __restrict__ k_pre,
                      const TK* __restrict__ v_pre, const uint8_t* __restrict__ k_exp,
                      const uint8_t* __restrict__ v_exp, float* __restrict__ o_part,
                      float2* __restrict__ ml_part, int* status) {
@@ -210,17 +205,17 @@ attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* _
   }
 }
 
-// One warp per (row, query head): the prefix chunks' partials, then the
+// One warp per (row, query head), float32: the prefix chunks' partials, then the
 // row's own causal candidate keys, normalised. The loads that do not depend on
 // each other go out together: the chunks' (m, l) one a lane, their outputs and
 // the candidate's keys and values four at a time.
-template <int DH, typename T>
+template <int DH>
 __global__ void __launch_bounds__(128)
 attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restrict__ row_cand,
                     const int32_t* __restrict__ cand_row_offset, int N, int R, int C, int Hq, int Hkv,
-                    int splits, const T* __restrict__ q, const T* __restrict__ k_cand,
-                    const T* __restrict__ v_cand, const float* __restrict__ o_part,
-                    const float2* __restrict__ ml_part, T* __restrict__ o, int* status) {
+                    int splits, const float* __restrict__ q, const float* __restrict__ k_cand,
+                    const float* __restrict__ v_cand, const float* __restrict__ o_part,
+                    const float2* __restrict__ ml_part, float* __restrict__ o, int* status) {
   pdl_begin();
   const int lane = threadIdx.x & 31;
   const long long idx = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
@@ -231,7 +226,7 @@ attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restri
   constexpr int PER = DH / 32;
   float qv[PER];
 #pragma unroll
-  for (int i = 0; i < PER; ++i) qv[i] = to_f32(q[(size_t(n) * Hq + h) * DH + lane + 32 * i]);
+  for (int i = 0; i < PER; ++i) qv[i] = q[(size_t(n) * Hq + h) * DH + lane + 32 * i];
   float acc[PER];
   float m, l;
   combine_chunks<DH>(true, splits, N, Hq, n, h, lane, ml_part, o_part, m, l, acc);
@@ -248,8 +243,8 @@ attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restri
           const size_t kb = (size_t(min(n4 + t, n) - r - 1) * Hkv + kh) * DH + lane;
 #pragma unroll
           for (int i = 0; i < PER; ++i) {
-            kv[t][i] = to_f32(k_cand[kb + 32 * i]);
-            vv[t][i] = to_f32(v_cand[kb + 32 * i]);
+            kv[t][i] = k_cand[kb + 32 * i];
+            vv[t][i] = v_cand[kb + 32 * i];
           }
         }
 #pragma unroll
@@ -278,12 +273,11 @@ attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restri
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
-  for (int i = 0; i < PER; ++i)
-    o[(size_t(n) * Hq + h) * DH + lane + 32 * i] = from_f32<T>(acc[i] * inv);
+  for (int i = 0; i < PER; ++i) o[(size_t(n) * Hq + h) * DH + lane + 32 * i] = acc[i] * inv;
 }
 
 // the prefix chunks, then their merge with the candidates' own keys
-template <int DH, typename T, typename TK>
+template <int DH, typename TK>
 cudaError_t launch_simt(const jet_layout& lay, const jet_dims& d, const AttnPlan& plan,
                         const void* q, const void* k_pre, const void* v_pre, size_t exp_off,
                         const void* k_cand, const void* v_cand, void* o, void* ws, int* status,
@@ -292,21 +286,21 @@ cudaError_t launch_simt(const jet_layout& lay, const jet_dims& d, const AttnPlan
   float* o_part = static_cast<float*>(ws);
   float2* ml_part = reinterpret_cast<float2*>(o_part + size_t(plan.splits) * n.N * d.Hq * DH);
   const size_t smem = prefix_smem_bytes<DH>();
-  cudaError_t e = cudaFuncSetAttribute(attend_prefix_kernel<DH, T, TK>,
+  cudaError_t e = cudaFuncSetAttribute(attend_prefix_kernel<DH, TK>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
   dim3 grid(plan.splits, plan.qgroups, unsigned(n.R * d.Hkv));
-  e = launch_pdl(attend_prefix_kernel<DH, T, TK>, grid, dim3(kThreads), smem, st,
+  e = launch_pdl(attend_prefix_kernel<DH, TK>, grid, dim3(kThreads), smem, st,
                  lay.prefix_offset, lay.row_offset, n.R, n.N, n.total_prefix, d.Hq, d.Hkv,
-                 plan.chunk, static_cast<const T*>(q), static_cast<const TK*>(k_pre),
+                 plan.chunk, static_cast<const float*>(q), static_cast<const TK*>(k_pre),
                  static_cast<const TK*>(v_pre), static_cast<const uint8_t*>(k_pre) + exp_off,
                  static_cast<const uint8_t*>(v_pre) + exp_off, o_part, ml_part, status);
   if (e != cudaSuccess) return e;
   const long long warps = (long long)n.N * d.Hq;
-  return launch_pdl(attend_merge_kernel<DH, T>, dim3(unsigned((warps + 3) / 4)), dim3(128), 0, st,
+  return launch_pdl(attend_merge_kernel<DH>, dim3(unsigned((warps + 3) / 4)), dim3(128), 0, st,
                     lay.row_req, lay.row_cand, lay.cand_row_offset, n.N, n.R, n.C, d.Hq, d.Hkv,
-                    plan.splits, static_cast<const T*>(q), static_cast<const T*>(k_cand),
-                    static_cast<const T*>(v_cand), o_part, ml_part, static_cast<T*>(o), status);
+                    plan.splits, static_cast<const float*>(q), static_cast<const float*>(k_cand),
+                    static_cast<const float*>(v_cand), o_part, ml_part, static_cast<float*>(o), status);
 }
 
 template <int DH>
@@ -320,7 +314,7 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
         lay, d, plan, q, k_pre, v_pre, k_cand, v_cand, o, o_part,
         reinterpret_cast<float2*>(o_part + size_t(plan.splits) * lay.n.N * d.Hq * DH), status, st);
   }
-  return launch_simt<DH, float, float>(lay, d, plan, q, k_pre, v_pre, 0, k_cand, v_cand, o, ws,
+  return launch_simt<DH, float>(lay, d, plan, q, k_pre, v_pre, 0, k_cand, v_cand, o, ws,
                                        status, st);
 }
 
@@ -402,19 +396,17 @@ AttnPlan attn_plan(const jet_sizes& n, const jet_dims& d) {
   return p;
 }
 
-AttnPlan attn_plan_kv8(const jet_sizes& n, const jet_dims& d) { return attn_plan_simt(n, d); }
+AttnPlan attn_plan_kv8(const jet_sizes& n, const jet_dims& d) { return attn_plan(n, d); }
 
 cudaError_t launch_prefix_attend_kv8(const jet_layout& lay, const jet_dims& d,
                                      const AttnPlan& plan, const void* q, const void* k8,
                                      const void* v8, const void* k_cand, const void* v_cand,
                                      void* o, void* ws, int* status, cudaStream_t st) {
+  if (d.dtype == JET_DTYPE_BF16)
+    return launch_attend_kv8_tc(lay, d, plan, q, k8, v8, k_cand, v_cand, o, ws, status, st);
   const size_t off = kv_size(lay.n, d).exp_off;
 #define JET_ATT8(DH)                                                                              \
-  return d.dtype == JET_DTYPE_BF16                                                                \
-             ? launch_simt<DH, __nv_bfloat16, uint8_t>(lay, d, plan, q, k8, v8, off, k_cand,      \
-                                                       v_cand, o, ws, status, st)                 \
-             : launch_simt<DH, float, uint8_t>(lay, d, plan, q, k8, v8, off, k_cand, v_cand, o,   \
-                                               ws, status, st)
+  return launch_simt<DH, uint8_t>(lay, d, plan, q, k8, v8, off, k_cand, v_cand, o, ws, status, st)
   if (d.d == 64) JET_ATT8(64);
   if (d.d == 128) JET_ATT8(128);
   if (d.d == 256) JET_ATT8(256);

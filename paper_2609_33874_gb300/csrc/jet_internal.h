@@ -122,6 +122,12 @@ cudaError_t launch_prefix_attend_kv8(const jet_layout& lay, const jet_dims& d,
                                      const void* v8, const void* k_cand, const void* v_cand,
                                      void* o, void* ws, int* status, cudaStream_t st);
 
+// bf16 on the tensor cores (attend_kv8.cu)
+cudaError_t launch_attend_kv8_tc(const jet_layout& lay, const jet_dims& d, const AttnPlan& plan,
+                                 const void* q, const void* k8, const void* v8,
+                                 const void* k_cand, const void* v_cand, void* o, void* ws,
+                                 int* status, cudaStream_t st);
+
 // the 8-bit prefix cache (kv_cache.cu): the whole prefix written, the next tokens of
 // each request, the cache read back
 cudaError_t launch_kv_quantize(const jet_layout& lay, const jet_dims& d, const void* k,

@@ -8,10 +8,10 @@
 // the time for it (d 256: 32 KB, 0.73 us): what follows keeps each unit below that.
 //
 //   scores   S = Q K^T on the codes as they are (kind::f8f6f4). A query is held as two
-//            e4m3 numbers, q = 2^x (hi + lo), x per row: hi has the first four of a bf16
-//            number's eight digits, lo the other four, so the split is exact for
-//            elements within 2^-10 of the row's largest and leaves 2^-10 of 2^x, at
-//            most 2^-18 of that largest element, below. (Keys widened to bf16 instead
+//            e4m3 numbers, q = 2^x (hi + lo), x per row: hi is the nearest code, lo that of
+//            what is left, at most four binary digits of a bf16 number's eight, so the
+//            split is exact for elements within 2^-10 of the row's largest and leaves
+//            2^-10 of 2^x, at most 2^-17.8 of that largest element, below. (Keys widened to bf16 instead
 //            would pass shared memory twice more: 1,536 cycles a tile of d 256, 1,393
 //            at the HBM rate.) S = acc 2^(x + X), X the tile's exponent: the 64 tokens of
 //            a block are a tile.
@@ -44,15 +44,20 @@ namespace jet {
 namespace {
 
 constexpr int kBC = 32;  // candidate tokens per tile
-constexpr int kThreads = 512;
+constexpr float kWeightLog2 = 7.f;  // weights are 2^7 at a row's maximum
+// P_j's 32 columns are the second half of S_j's 64: P of the second half's keys is made
+// first, from registers, while the first half's scores are still there
+constexpr uint32_t kPOff = 32;
+constexpr int kThreads = 640;
 constexpr int kProdWarp = 0, kMmaWarp = 1, kSchedWarp = 2, kSoftWarp = 4, kWideWarp = 12;
+constexpr int kWideThreads = kThreads - 32 * kWideWarp;
 
 template <int DH>
 struct Geo {
   static constexpr uint32_t kTile = kBN * DH;             // bytes of a K or V tile
-  static constexpr int kK = DH == 256 ? 3 : 6;            // K tiles in flight
+  static constexpr int kK = DH == 256 ? 2 : 6;            // K tiles in flight
   static constexpr int kV = kK;                           // V tiles in flight
-  static constexpr int kW = DH == 256 ? 1 : 2;            // widened V tiles
+  static constexpr int kW = 2;                            // widened V tiles
   static constexpr int kS = DH == 256 ? 2 : 4;            // S buffers
   static constexpr uint32_t kOffK = kBV * DH * 2;         // after the bf16 query block
   static constexpr uint32_t kOffV = kOffK + kK * kTile;
@@ -89,6 +94,7 @@ struct Small {
   uint64_t s_full[4], p_full[4], pv_done[4];
   uint64_t m_full[2][4];                 // a tile's running maxima, per softmax warp
   uint64_t l_full[4];                    // both groups' sums of an item
+  uint64_t xc_full;                      // the candidate values' maxima of an item
   uint64_t item_full[2], item_empty[2];
   uint64_t q_full, q_free;               // the bf16 query block
   uint64_t qt_full, qt_free;             // the queries' codes in TMEM
@@ -97,10 +103,12 @@ struct Small {
   uint64_t drain;
   uint32_t tmem;
   volatile int abort;
-  volatile int bad[2][4];                // non-finite candidate values, per widening warp
+  volatile int bad[2][8];                // non-finite candidate values, per widening warp
   float m[2][kBV];                       // running maxima after an even / odd tile
   float2 ml[2][2][kBV];                  // [item parity][group] (m, l)
   int qx[2][kBV];                        // [item parity] the queries' exponents
+  int vx[2];                             // [item parity] the exponent of V and O
+  uint32_t xc[2][8];                     // [item parity] candidate maxima, per widening warp
 };
 static_assert(sizeof(Small) <= 8192, "the small part of shared memory");
 
@@ -143,38 +151,103 @@ __device__ __forceinline__ void tmem_st_16cols_u32(uint32_t taddr, const uint32_
       : "memory");
 }
 
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+// and 8 columns
+__device__ __forceinline__ void tmem_st_8cols_u32(uint32_t taddr, const uint32_t (&v)[8]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+      : "memory");
+}
+
+// the codes of a word's two halves as f16 numbers, and two f16 numbers' nearest codes
+__device__ __forceinline__ void e4m3x4_to_f16x4(uint32_t codes, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(codes));
+}
+__device__ __forceinline__ uint32_t f16x4_to_e4m3x4(uint32_t lo, uint32_t hi) {
   uint32_t d;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  asm("{\n\t.reg .b16 a, b;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f16x2 a, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, %2;\n\t"
+      "mov.b32 %0, {a, b};\n\t}"
+      : "=r"(d)
+      : "r"(lo), "r"(hi));
   return d;
 }
 
-// 2^x as a bf16 number, twice; x in [-126, 127]
-__device__ __forceinline__ uint32_t pow2_bf16x2(int x) {
-  const uint32_t h = uint32_t(x + 127) << 7;
-  return h | h << 16;
+__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
 }
 
-// Two e4m3 codes in the high bytes of the halves of w as bf16 numbers times 2^-120: the
-// four exponent and three fraction bits under bf16's exponent (subnormal codes are
-// subnormal there)
-__device__ __forceinline__ uint32_t widen2(uint32_t w) {
-  return ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u);
+// the larger magnitudes of two pairs of bf16 numbers; NaN if there is one
+__device__ __forceinline__ uint32_t max_bf16x2_nan(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
 }
 
-// 0x80 in each byte of w that is a NaN code
-__device__ __forceinline__ uint32_t nan_codes(uint32_t w) {
-  return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
 }
 
-__device__ __forceinline__ bool any_nonfinite_bf16x2(uint32_t w) {
-  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(b), "f"(a));
+  return d;
 }
 
-__device__ __forceinline__ uint32_t drop_nonfinite_bf16x2(uint32_t w) {
-  if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
-  if ((w & 0x7f800000u) == 0x7f800000u) w &= 0x0000ffffu;
-  return w;
+// f16 A and B (format 0), f32 accumulator; B is MN-major
+constexpr uint32_t idesc_f16_f32_mn(int M, int N) {
+  return (1u << 4) | (1u << 16) | (uint32_t(N >> 3) << 17) | (uint32_t(M >> 4) << 24);
+}
+
+// where a V tile's TMA copy leaves the 16 codes c of a key: slices of 128 codes under
+// 128-byte swizzling, d 64 rows of 64 bytes under 64-byte swizzling
+template <int DH>
+__device__ __forceinline__ uint32_t raw_piece(int key, int c) {
+  if constexpr (DH == 64) return uint32_t(key) * 64u + (uint32_t(c ^ ((key >> 1) & 3)) << 4);
+  return uint32_t(c >> 3) * (kBN * 128) + sw128(key, c & 7);
+}
+
+// two float32 at a time
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, c, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\t"
+      "fma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 a, b, d;\n\t"
+      "mov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\t"
+      "add.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
+__device__ __forceinline__ bool nonfinite_bf16(uint32_t h) { return (h & 0x7f80u) == 0x7f80u; }
+
+// the larger of `top` and the magnitudes of two bf16 numbers, as bits; infinities and NaN
+// do not count
+__device__ __forceinline__ uint32_t finite_max_bf16x2(uint32_t top, uint32_t w) {
+  const uint32_t a = w & 0x7fffu, b = (w >> 16) & 0x7fffu;
+  return max(top, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
 }
 
 template <int DH>
@@ -198,10 +271,10 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     }
     for (int s = 0; s < NV; ++s) {
       mbar_init(sh.v_full + s, 1);
-      mbar_init(sh.v_empty + s, 4);
+      mbar_init(sh.v_empty + s, 8);
     }
     for (int s = 0; s < NW; ++s) {
-      mbar_init(sh.w_full + s, 4);
+      mbar_init(sh.w_full + s, 8);
       mbar_init(sh.w_empty + s, 1);
     }
     for (int b = 0; b < NS; ++b) {
@@ -216,11 +289,12 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(sh.item_full + b, 1);
-      mbar_init(sh.item_empty + b, 14);  // producer, MMA thread, 8 softmax and 4 widening warps
+      mbar_init(sh.item_empty + b, 18);  // producer, MMA thread, 8 softmax and 8 widening warps
     }
+    mbar_init(&sh.xc_full, 8);
     mbar_init(&sh.q_full, 1);
-    mbar_init(&sh.q_free, 5);            // the split's four warps, the last product with it
-    mbar_init(&sh.qt_full, 4);
+    mbar_init(&sh.q_free, 9);  // the split's eight warps, the last product with it
+    mbar_init(&sh.qt_full, 8);
     mbar_init(&sh.qt_free, 1);
     mbar_init(&sh.qx_read, 8);
     mbar_init(&sh.o_free, 8);
@@ -247,10 +321,10 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem;
-  // registers to the softmax warps, which hold a tile's scores: 72 + 168 + 168 + 104 are
-  // the four warpgroups' launch share of 128 each
+  // registers to the softmax warps, which hold a tile's scores: 64 + 2 x 136 + 2 x 72 are
+  // the five warpgroups' launch share of 96 each
   if (warp < kSoftWarp) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
   if (warp == kSchedWarp) {
     // ---------------------------------------------------------------- scheduler
     const int count = a.sorted ? *a.item_count : 0;
@@ -389,8 +463,10 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                   tma_load_3d(vs + sl * (kBC * 128), &tmVc, sh.v_full + s, sl * 64, e.kh,
                               e.f_begin + jv * kBC, pol);
               } else {
-                tma_load_3d(vs, &tmV, sh.v_full + s, 0, e.kh,
-                            e.p0 + e.k_begin + (jv - e.nct) * kBN, pol);
+                const int key = e.p0 + e.k_begin + (jv - e.nct) * kBN;
+#pragma unroll
+                for (int sl = 0; sl < (DH + 127) / 128; ++sl)
+                  tma_load_3d(vs + sl * (kBN * 128), &tmV, sh.v_full + s, sl * 128, e.kh, key, pol);
               }
               v_issued |= 1u << s;
               v_par = (v_par & ~(1u << s)) | (ph << s);
@@ -398,6 +474,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
               progressed = true;
             }
           }
+          if (!progressed) __nanosleep(100);
           if (clk.expired(progressed, abort_flag, a.wait_ns)) {
             ok = false;
             break;
@@ -423,7 +500,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     if (elect_one()) {
       constexpr uint32_t id_s = idesc_e4m3_f32(kBV, kBN);
       constexpr uint32_t id_c = idesc_bf16_f32(kBV, kBC);
-      constexpr uint32_t id_o = idesc_bf16_f32(kBV, DH) | (1u << 16);  // B (V) is MN-major
+      constexpr uint32_t id_o = idesc_f16_f32_mn(kBV, DH);
       const uint32_t qs = smem_u32(smem);
       bool ok = true;
       int T = 0;
@@ -482,7 +559,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 mbar_test(sh.p_full + b, (Tj / NS) & 1) &&
                 mbar_test(sh.w_full + w, (Tj / NW) & 1)) {
               tc_fence_after();
-              const uint32_t pt = tmem + G::kSCol + b * kBN;
+              const uint32_t pt = tmem + G::kSCol + b * kBN + kPOff;
               const uint32_t vs = smem_u32(smem + G::kOffW + w * 2 * G::kTile);
               if (jo < nct) {
 #pragma unroll
@@ -519,10 +596,17 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     }
   }
   } else if (warp >= kWideWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     // ---------------------------------------------------------------- queries and V
-    const int q4 = warp - kWideWarp, t = threadIdx.x - kWideWarp * 32;  // row, thread of 128
+    const int wi = warp - kWideWarp, q4 = wi & 3, half = wi >> 2;
+    const int t = threadIdx.x - kWideWarp * 32;
+    const int row = q4 * 32 + lane;  // of the queries, in two halves of their elements
     const uint32_t lane_off = uint32_t(q4 * 32) << 16;
+    // of a V tile: one key's pieces of 16 codes, every fourth one. Eight lanes are eight
+    // keys, whose swizzled places differ in their banks, before and after.
+    constexpr int kMine = DH / 64;
+    const int key = t & (kBN - 1), c0 = t >> 6;
+    int n_fed = 0;  // items with candidates so far
     bool ok = true;
     int T = 0;
     for (int u = 0; ok; ++u) {
@@ -533,29 +617,55 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       }
       if (!sh.ring[slot].live) break;
       const ItemGeo e = sh.ring[slot].e;
-      const int fed = sh.ring[slot].fed;
-      const size_t ex = size_t(kv_place(e.p0, e.r, e.k_begin / kBN)) * a.Hkv + e.kh;
-      int byte = a.v_exp[ex];
-      if (lane == 0) sh.bad[slot][q4] = 0;  // item u - 2's output is out (below)
+      const int fed = sh.ring[slot].fed, keys = e.k_end - e.k_begin;
+      // V's unit of this item: the largest exponent of its tiles and of its candidates'
+      // values (the loads fly while the queries are split)
+      const uint8_t* ex = a.v_exp + size_t(kv_place(e.p0, e.r, e.k_begin / kBN)) * a.Hkv + e.kh;
+      int byte = *ex, vx = kKvLow + 127;
+      for (int pt = lane; pt < e.npt; pt += 32) vx = max(vx, int(ex[size_t(pt) * a.Hkv]));
+      if (fed > 0) {
+        uint32_t top = 0;
+        const __nv_bfloat16* vc = a.v_cand + (size_t(e.f_begin) * a.Hkv + e.kh) * DH;
+        for (int i = t; i < fed * (DH / 8); i += kWideThreads) {
+          const uint4 v = *reinterpret_cast<const uint4*>(
+              vc + size_t(i / (DH / 8)) * a.Hkv * DH + 8 * (i % (DH / 8)));
+          top = finite_max_bf16x2(finite_max_bf16x2(top, v.x), v.y);
+          top = finite_max_bf16x2(finite_max_bf16x2(top, v.z), v.w);
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (lane == 0) {
+          sh.xc[slot][wi] = top;
+          mbar_arrive(&sh.xc_full);
+        }
+        if (!warp_mbar_wait(&sh.xc_full, n_fed & 1, a.wait_ns, abort_flag)) {
+          ok = false;
+          break;
+        }
+        ++n_fed;
+        vx = max(vx, kv_exponent(__reduce_max_sync(0xffffffffu, sh.xc[slot][lane & 7]) << 16) + 127);
+      }
+      if (lane == 0) sh.bad[slot][wi] = 0;  // item u - 2's output is out (below)
       if (!warp_mbar_wait(&sh.q_full, u & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
-      // the row's largest magnitude (NaN and infinities lie above all): rows past the
-      // block's vectors hold what an earlier block left and go unread
-      {
+      vx = min(max(__reduce_max_sync(0xffffffffu, vx) - 127, kKvLow), kKvHigh);
+      if (t == 0) sh.vx[slot] = vx;
+      if (q4 * 32 < e.nv) {
+        // the row's largest magnitude (NaN and infinities lie above all): rows past the
+        // block's vectors hold what an earlier block left and go unread
         uint32_t top = 0;
-#pragma unroll 4
+#pragma unroll 8
         for (int c = 0; c < DH / 8; ++c) {
-          const uint4 x = *reinterpret_cast<const uint4*>(smem + (c >> 3) * (kBV * 128) +
-                                                          sw128(t, c & 7));
-          top = __vmaxu2(top, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu),
-                                       __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
+          const uint4 q = *reinterpret_cast<const uint4*>(smem + (c >> 3) * (kBV * 128) +
+                                                          sw128(row, c & 7));
+          top = max_bf16x2_nan(max_bf16x2_nan(top, q.x & 0x7fff7fffu), q.y & 0x7fff7fffu);
+          top = max_bf16x2_nan(max_bf16x2_nan(top, q.z & 0x7fff7fffu), q.w & 0x7fff7fffu);
         }
-        top = max(top & 0xffffu, top >> 16);
+        top = max(top & 0x7fffu, (top >> 16) & 0x7fffu);
         const bool finite = top < 0x7f80u;
-        const int x = finite ? kv_exponent(top << 16) : 0;
-        const float inv = pow2(-x);
+        const int qx = finite ? kv_exponent(top << 16) : 0;
+        const float inv = pow2(-qx);
         // the codes of the item before are read by its last product with the keys; a
         // softmax warp must not find qt_full two items on
         if (u >= 1 && (!warp_mbar_wait(&sh.qt_free, (u - 1) & 1, a.wait_ns, abort_flag) ||
@@ -563,63 +673,56 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           ok = false;
           break;
         }
-        sh.qx[slot][t] = x;
+        if (half == 0) sh.qx[slot][row] = qx;
         tc_fence_after();
+        // 32 elements at a time: eight columns of four codes
 #pragma unroll 1
-        for (int sl = 0; sl < DH / 64; ++sl) {
-          uint32_t hi[16], lo[16];
+        for (int k32 = half; k32 < DH / 32; k32 += 2) {
+          uint32_t hi[8], lo[8];
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            const uint4 xv = *reinterpret_cast<const uint4*>(smem + sl * (kBV * 128) + sw128(t, c));
+          for (int c = 0; c < 4; ++c) {
+            const uint4 xv = *reinterpret_cast<const uint4*>(
+                smem + (k32 >> 1) * (kBV * 128) + sw128(row, 4 * (k32 & 1) + c));
             const uint32_t w[4] = {xv.x, xv.y, xv.z, xv.w};
+            uint32_t y[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)  // (f16 holds a bf16 number's eight digits)
+              y[k] = pack_f16(__uint_as_float(w[k] << 16) * inv,
+                              __uint_as_float(w[k] & 0xffff0000u) * inv);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              uint32_t hw = 0, lw = 0;
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const uint32_t p = w[2 * i + k];
-                const float q0 = __uint_as_float(p << 16) * inv;
-                const float q1 = __uint_as_float(p & 0xffff0000u) * inv;
-                // the first four digits by their bits, the rest exactly
-                const float h0 = __uint_as_float(__float_as_uint(q0) & 0xfff00000u);
-                const float h1 = __uint_as_float(__float_as_uint(q1) & 0xfff00000u);
-                const uint32_t ph = __nv_cvt_float2_to_fp8x2(make_float2(h0, h1), __NV_SATFINITE,
-                                                             __NV_E4M3);
-                const float2 back = e4m3x2_to_f32(ph);  // below 2^-6 the code is shorter
-                const uint32_t pl = __nv_cvt_float2_to_fp8x2(
-                    make_float2(q0 - back.x, q1 - back.y), __NV_SATFINITE, __NV_E4M3);
-                hw |= ph << (16 * k);
-                lw |= pl << (16 * k);
-              }
-              if (!finite) hw = 0x7f7f7f7fu;  // the whole row's output is NaN
-              hi[2 * c + i] = hw;
-              lo[2 * c + i] = lw;
+              uint32_t h0, h1;
+              const uint32_t h = f16x4_to_e4m3x4(y[2 * i], y[2 * i + 1]);
+              e4m3x4_to_f16x4(h, h0, h1);
+              hi[2 * c + i] = finite ? h : 0x7f7f7f7fu;
+              lo[2 * c + i] =
+                  f16x4_to_e4m3x4(sub_f16x2(y[2 * i], h0), sub_f16x2(y[2 * i + 1], h1));
             }
           }
-          const uint32_t at = tmem + lane_off + G::kQCol + uint32_t(16 * sl);
-          tmem_st_16cols_u32(at, hi);
-          tmem_st_16cols_u32(at + DH / 4, lo);
+          const uint32_t at = tmem + lane_off + G::kQCol + uint32_t(8 * k32);
+          tmem_st_8cols_u32(at, hi);
+          tmem_st_8cols_u32(at + DH / 4, lo);
         }
         tmem_wait_st();
         tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&sh.qt_full);
-          mbar_arrive(&sh.q_free);
-        }
+      } else if (u >= 1 && (!warp_mbar_wait(&sh.qt_free, (u - 1) & 1, a.wait_ns, abort_flag) ||
+                            !warp_mbar_wait(&sh.qx_read, (u - 1) & 1, a.wait_ns, abort_flag))) {
+        ok = false;
+        break;
       }
-      // V tiles: 16 codes to 16 bf16 numbers at a time
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&sh.qt_full);
+        mbar_arrive(&sh.q_free);
+      }
       for (int j = 0; j < e.ntiles; ++j) {
         const int Tj = T + j;
         const int s = Tj % NV, w = Tj % NW;
-        // before item u can end: item u - 1's output is out, so that item u + 1 may take
+        // before item u can end, item u - 1's output is out, so that item u + 1 may take
         // its places (a wait past the end could miss the phase)
-        if (j == e.ntiles - 1 && u >= 1 &&
-            !warp_mbar_wait(&sh.o_free, (u - 1) & 1, a.wait_ns, abort_flag)) {
-          ok = false;
-          break;
-        }
-        if (!warp_mbar_wait(sh.v_full + s, (Tj / NV) & 1, a.wait_ns, abort_flag) ||
+        if ((j == e.ntiles - 1 && u >= 1 &&
+             !warp_mbar_wait(&sh.o_free, (u - 1) & 1, a.wait_ns, abort_flag)) ||
+            !warp_mbar_wait(sh.v_full + s, (Tj / NV) & 1, a.wait_ns, abort_flag) ||
             !warp_mbar_wait(sh.w_empty + w, ((Tj / NW) & 1) ^ 1u, a.wait_ns, abort_flag)) {
           ok = false;
           break;
@@ -627,68 +730,59 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         const uint8_t* vs = smem + G::kOffV + s * G::kTile;
         uint8_t* ws = smem + G::kOffW + w * 2 * G::kTile;
         if (j < e.nct) {
-          // candidate values: bf16 already, in the places the product reads
+          // candidate values, in the places the product reads
           const int left = fed - j * kBC;
+          const float inv = pow2(-vx);
           bool found = false;
-#pragma unroll 4
-          for (int i = t; i < int(G::kTile) / 16; i += 128) {
-            uint4 x = *reinterpret_cast<const uint4*>(vs + 16 * i);
-            if (((i >> 3) & (kBC - 1)) >= left) x = make_uint4(0u, 0u, 0u, 0u);
-            if (any_nonfinite_bf16x2(x.x) || any_nonfinite_bf16x2(x.y) ||
-                any_nonfinite_bf16x2(x.z) || any_nonfinite_bf16x2(x.w)) {
-              found = true;
-              x = make_uint4(drop_nonfinite_bf16x2(x.x), drop_nonfinite_bf16x2(x.y),
-                             drop_nonfinite_bf16x2(x.z), drop_nonfinite_bf16x2(x.w));
+#pragma unroll
+          for (int k = 0; k < kMine; ++k) {
+            const int i = t + k * kWideThreads;
+            const uint4 v = *reinterpret_cast<const uint4*>(vs + 16 * i);
+            const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+            uint32_t y[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const bool n0 = nonfinite_bf16(in[q]), n1 = nonfinite_bf16(in[q] >> 16);
+              found |= n0 | n1;
+              y[q] = pack_f16(n0 ? 0.f : __uint_as_float(in[q] << 16) * inv,
+                              n1 ? 0.f : __uint_as_float(in[q] & 0xffff0000u) * inv);
+              if (((i >> 3) & (kBC - 1)) >= left) y[q] = 0u;
             }
-            *reinterpret_cast<uint4*>(ws + 16 * i) = x;
+            *reinterpret_cast<uint4*>(ws + 16 * i) = make_uint4(y[0], y[1], y[2], y[3]);
           }
-          if (__any_sync(0xffffffffu, found) && lane == 0) sh.bad[slot][q4] = 1;
+          if (__any_sync(0xffffffffu, found) && lane == 0) sh.bad[slot][wi] = 1;
         } else {
           const int pt = j - e.nct;
-          const int X = min(max(byte - 127, kKvLow), kKvHigh);
-          if (pt + 1 < e.npt) byte = a.v_exp[ex + size_t(pt + 1) * a.Hkv];
-          const int left = e.k_end - (e.k_begin + pt * kBN);
-          // 2^(120 + X) in one factor, or two where bf16 does not hold it
-          const uint32_t f = pow2_bf16x2(min(120 + X, 127));
-          const uint32_t f2 = pow2_bf16x2(max(X - 7, 0));
-          constexpr int kC = DH / 16;  // 16-code pieces of a key
+          // 2^(X - vx): below 2^-24 f16 holds no product with a code
+          const int k2 = max(min(max(byte - 127, kKvLow), kKvHigh) - vx, -24);
+          if (pt + 1 < e.npt) byte = ex[size_t(pt + 1) * a.Hkv];
+          const uint32_t h2 = k2 > -15 ? uint32_t(k2 + 15) << 10 : 1u << (k2 + 24);
+          const uint32_t f = h2 | h2 << 16;
+          const int left = keys - pt * kBN;  // the tile's keys past it are another request's
+          uint4 x[kMine];
 #pragma unroll
-          for (int i = 0; i < kBN * kC / 128; ++i) {
-            const int key = (t + i * 128) / kC, c = t % kC;
-            const uint4 x = *reinterpret_cast<const uint4*>(vs + key * DH + c * 16);
-            const uint32_t in[4] = {x.x, x.y, x.z, x.w};
+          for (int i = 0; i < kMine; ++i)
+            x[i] = *reinterpret_cast<const uint4*>(vs + raw_piece<DH>(key, c0 + 4 * i));
+          if (left < kBN && key >= left) {
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
+          }
+#pragma unroll
+          for (int i = 0; i < kMine; ++i) {
+            const uint32_t in[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
             uint32_t y[8];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-              y[2 * q] = mul_bf16x2(widen2(__byte_perm(in[q], 0u, 0x1404)), f);
-              y[2 * q + 1] = mul_bf16x2(widen2(__byte_perm(in[q], 0u, 0x3424)), f);
+              e4m3x4_to_f16x4(in[q], y[2 * q], y[2 * q + 1]);
+              y[2 * q] = mul_f16x2(y[2 * q], f);
+              y[2 * q + 1] = mul_f16x2(y[2 * q + 1], f);
             }
-            if (X > 7) {
-#pragma unroll
-              for (int q = 0; q < 8; ++q) y[q] = mul_bf16x2(y[q], f2);
-            }
-            if (nan_codes(x.x) | nan_codes(x.y) | nan_codes(x.z) | nan_codes(x.w)) {
-#pragma unroll
-              for (int q = 0; q < 4; ++q) {
-                const uint32_t n = nan_codes(in[q]);
-                if (n & 0x80u) y[2 * q] = (y[2 * q] & 0xffff0000u) | 0x7fffu;
-                if (n & 0x8000u) y[2 * q] = (y[2 * q] & 0xffffu) | 0x7fff0000u;
-                if (n & 0x800000u) y[2 * q + 1] = (y[2 * q + 1] & 0xffff0000u) | 0x7fffu;
-                if (n & 0x80000000u) y[2 * q + 1] = (y[2 * q + 1] & 0xffffu) | 0x7fff0000u;
-              }
-            }
-            if (key >= left) {  // other requests' keys
-#pragma unroll
-              for (int q = 0; q < 8; ++q) y[q] = 0u;
-            }
-            // pieces 2 c and 2 c + 1 of the key's row; odd slices in the other order,
-            // so that eight lanes' 16-byte stores fall in different banks
-            uint8_t* row = ws + (c >> 2) * (kBN * 128);
-            const int first = (c >> 2) & 1;
-            const uint4 p0 = make_uint4(y[0], y[1], y[2], y[3]);
-            const uint4 p1 = make_uint4(y[4], y[5], y[6], y[7]);
-            *reinterpret_cast<uint4*>(row + sw128(key, (2 * c + first) & 7)) = first ? p1 : p0;
-            *reinterpret_cast<uint4*>(row + sw128(key, (2 * c + 1 - first) & 7)) = first ? p0 : p1;
+            const int c = c0 + 4 * i;  // pieces 2 c and 2 c + 1 of the f16 row
+            uint8_t* to = ws + (c >> 2) * (kBN * 128);
+            *reinterpret_cast<uint4*>(to + sw128(key, (2 * c) & 7)) =
+                make_uint4(y[0], y[1], y[2], y[3]);
+            *reinterpret_cast<uint4*>(to + sw128(key, (2 * c + 1) & 7)) =
+                make_uint4(y[4], y[5], y[6], y[7]);
           }
         }
         fence_proxy_async_smem();
@@ -707,7 +801,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       flag(a.status, JET_ERR_TIMEOUT);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
     // ---------------------------------------------------------------- softmax
     const int q4 = warp & 3, grp = (warp - kSoftWarp) >> 2;
     const int i = q4 * 32 + lane;  // query vector within the block = TMEM lane
@@ -722,11 +816,12 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         break;
       }
       if (!sh.ring[slot].live) break;
-      const ItemGeo e = sh.ring[slot].e;
+      const ItemGeo& e = sh.ring[slot].e;  // (read again where needed: registers are few)
+      const int nct = e.nct, ntiles = e.ntiles, keys = e.k_end - e.k_begin, f_begin = e.f_begin;
       const bool valid = i < e.nv;
       const bool some = q4 * 32 < e.nv;  // a warp without vectors only keeps the barriers going
       int fa = 1, fb = 0;                // fed tokens this vector sees (none: shared row)
-      if (valid && e.nct > 0) {
+      if (valid && nct > 0) {
         const int n = e.n0 + (e.vbase + i) / g;
         const int c = a.row_cand[n];
         if (c >= 0 && c < a.C) {
@@ -737,7 +832,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       const uint8_t* ex = a.k_exp + size_t(kv_place(e.p0, e.r, e.k_begin / kBN)) * a.Hkv + e.kh;
       const int j0 = (grp ^ T) & 1;  // this group's tiles: j0, j0 + 2, ..
       int byte = 0;
-      if (j0 >= e.nct && j0 < e.ntiles) byte = ex[size_t(j0 - e.nct) * a.Hkv];
+      if (j0 >= nct && j0 < ntiles) byte = ex[size_t(j0 - nct) * a.Hkv];
       int qx = 0;
       bool qx_read = false;
       auto read_qx = [&]() -> bool {
@@ -750,34 +845,35 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       };
       float m_own = -INFINITY, l = 0.f;  // l: the sum over this group's tiles, relative to m_own
 
-      // scores of W keys in columns klo .. khi, times mul in base 2, to weights
-      auto tile = [&](auto width, int j, float mul, int klo, int khi) -> bool {
-        constexpr int W = decltype(width)::value;
+      // scores of 32 nh keys in columns klo .. khi, times mul in base 2, to weights: 32
+      // scores at a time in registers, the last of them from their maximum to their
+      // weights, the others read twice
+      auto tile = [&](int nh, int j, float mul, int klo, int khi) -> bool {
         const int Tj = T + j, b = Tj % NS;
         const uint32_t at = tmem + lane_off + G::kSCol + b * kBN;
-        float sv[W];
-        if (some) {
-          float t0[W / 32][32];
-#pragma unroll
-          for (int k = 0; k < W / 32; ++k) tmem_ld_32cols(at + 32 * k, t0[k]);
+        float sv[32];
+        const bool cut = __any_sync(0xffffffffu, klo > 0 || khi < 32 * nh);
+        auto load = [&](int k) {
+          tmem_ld_32cols(at + 32 * k, sv);
           tmem_wait_ld();
+          if (cut) {
 #pragma unroll
-          for (int c = 0; c < W; ++c) sv[c] = t0[c >> 5][c & 31];
-          if (__any_sync(0xffffffffu, klo > 0 || khi < W)) {
-#pragma unroll
-            for (int c = 0; c < W; ++c)
-              if (c < klo || c >= khi) sv[c] = -INFINITY;
+            for (int c = 0; c < 32; ++c)
+              if (c < klo - 32 * k || c >= khi - 32 * k) sv[c] = -INFINITY;
           }
-        }
+        };
         float mt = -INFINITY;
         if (some) {
-          float mq[8];
+          float mq[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+          for (int k = 0; k < nh; ++k) {
+            load(k);
 #pragma unroll
-          for (int q = 0; q < 8; ++q) mq[q] = sv[q];
+            for (int c = 0; c < 32; c += 8)
 #pragma unroll
-          for (int c = 8; c < W; ++c) mq[c & 7] = fmaxf(mq[c & 7], sv[c]);
-          mt = mul * fmaxf(fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])),
-                           fmaxf(fmaxf(mq[4], mq[5]), fmaxf(mq[6], mq[7])));
+              for (int q = 0; q < 4; ++q) mq[q] = max3(mq[q], sv[c + q], sv[c + 4 + q]);
+          }
+          mt = mul * fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3]));
         }
         // the row's maximum after the tile before, which the other group has
         if (Tj > 0 && !warp_mbar_wait(&sh.m_full[(Tj - 1) & 1][q4], ((Tj - 1) >> 1) & 1, a.wait_ns,
@@ -798,38 +894,42 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             tc_fence_after();
             const float f = grow ? ex2(m_prev - m_new) : 1.f;
 #pragma unroll 1
-            for (int c0 = 0; c0 < DH; c0 += 32) {
-              float ov[32];
-              tmem_ld_32cols(tmem + lane_off + c0, ov);
+            for (int c0 = 0; c0 < DH; c0 += 16) {
+              float ov[16];
+              tmem_ld_16cols(tmem + lane_off + c0, ov);
               tmem_wait_ld();
 #pragma unroll
-              for (int c = 0; c < 32; ++c) ov[c] *= f;
-              tmem_st_32cols(tmem + lane_off + c0, ov);
+              for (int c = 0; c < 16; ++c) ov[c] *= f;
+              tmem_st_16cols(tmem + lane_off + c0, ov);
             }
+            if (nh > 1) load(nh - 1);  // the registers' scores again
           }
           if (m_new != m_own) {
             l = m_own == -INFINITY ? 0.f : l * ex2(m_own - m_new);
             m_own = m_new;
           }
-          const float sub = m_new == -INFINITY ? 0.f : m_new;  // no key seen yet: weights of 0
-          float ps[8];
+          // weights 2^(s - m + 7): f16 holds them from 2^-24 to the 2^15 that a maximum not
+          // yet taken over may give; no key seen yet: weights of 0
+          const float sub = m_new == -INFINITY ? 0.f : m_new - kWeightLog2;
+          const float2 mul2 = make_float2(mul, mul), sub2 = make_float2(-sub, -sub);
+          float2 ps[4];
 #pragma unroll
-          for (int q = 0; q < 8; ++q) ps[q] = 0.f;
-          // the row sum uses the rounded values, which are what the tensor core multiplies
-          auto weights = [&](int c) {
-            const float x0 = ex2(fmaf(sv[c], mul, -sub)), x1 = ex2(fmaf(sv[c + 1], mul, -sub));
-            const uint32_t w = pack_bf16(x0, x1);
-            ps[(c >> 1) & 7] += __uint_as_float(w << 16) + __uint_as_float(w & 0xffff0000u);
-            return w;
-          };
-#pragma unroll
-          for (int k = 0; k < W / 32; ++k) {
+          for (int q = 0; q < 4; ++q) ps[q] = make_float2(0.f, 0.f);
+#pragma unroll 1
+          for (int k = nh - 1; k >= 0; --k) {
+            if (k < nh - 1) load(k);
             uint32_t pw[16];
 #pragma unroll
-            for (int c = 0; c < 16; ++c) pw[c] = weights(32 * k + 2 * c);
-            tmem_st_16cols_u32(at + 16 * k, pw);
+            for (int c = 0; c < 16; ++c) {
+              const float2 y = fma2(make_float2(sv[2 * c], sv[2 * c + 1]), mul2, sub2);
+              const float2 x = make_float2(ex2(y.x), ex2(y.y));
+              ps[c & 3] = add2(ps[c & 3], x);
+              pw[c] = pack_f16(x.x, x.y);
+            }
+            tmem_st_16cols_u32(at + kPOff + 16 * k, pw);
           }
-          l += ((ps[0] + ps[1]) + (ps[2] + ps[3])) + ((ps[4] + ps[5]) + (ps[6] + ps[7]));
+          const float2 p = add2(add2(ps[0], ps[1]), add2(ps[2], ps[3]));
+          l += p.x + p.y;
           tmem_wait_st();
         }
         tc_fence_before();
@@ -838,9 +938,9 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         return true;
       };
 
-      for (int j = j0; j < e.ntiles; j += 2) {
+      for (int j = j0; j < ntiles; j += 2) {
         const int Tj = T + j, b = Tj % NS;
-        if (j >= e.nct && !qx_read && !read_qx()) {
+        if (j >= nct && !qx_read && !read_qx()) {
           ok = false;
           break;
         }
@@ -851,17 +951,20 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         tc_fence_after();
         const int held = byte;
         // the exponent of this group's next tile, a tile ahead of its use
-        if (j + 2 >= e.nct && j + 2 < e.ntiles) byte = ex[size_t(j + 2 - e.nct) * a.Hkv];
-        if (j < e.nct) {
-          const int f0 = e.f_begin + j * kBC;
-          ok = tile(std::integral_constant<int, kBC>(), j, a.scale_log2, max(0, fa - f0),
-                    min(kBC, fb - f0 + 1));
+        if (j + 2 >= nct && j + 2 < ntiles) byte = ex[size_t(j + 2 - nct) * a.Hkv];
+        int nh = kBN / 32, klo = 0, khi;
+        float mul = a.scale_log2;
+        if (j < nct) {
+          const int f0 = f_begin + j * kBC;
+          nh = kBC / 32;
+          klo = max(0, fa - f0);
+          khi = min(kBC, fb - f0 + 1);
         } else {
           const int X = min(max(held - 127, kKvLow), kKvHigh);
-          const float mul = a.scale_log2 * pow2(min(max(qx + X, -126), 126));
-          ok = tile(std::integral_constant<int, kBN>(), j, mul, 0,
-                    min(kBN, e.k_end - (e.k_begin + (j - e.nct) * kBN)));
+          mul *= pow2(min(max(qx + X, -126), 126));
+          khi = min(kBN, keys - (j - nct) * kBN);
         }
+        ok = tile(nh, j, mul, klo, khi);
         if (!ok) break;
       }
       if (!ok) break;
@@ -877,7 +980,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         ok = false;
         break;
       }
-      const int Tl = T + e.ntiles - 1;
+      const int Tl = T + ntiles - 1;
       const float m_fin = sh.m[Tl & 1][i];
       const float2 x0 = sh.ml[slot][0][i], x1 = sh.ml[slot][1][i];
       l = (x0.x == -INFINITY && x0.y == 0.f ? 0.f : x0.y * ex2(x0.x - m_fin)) +
@@ -896,25 +999,29 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
       }
       if (valid && a.splits > 1 && grp == 0) {
-        // as the bf16 kernel leaves them for the combine
+        // as the bf16 kernel leaves them for the combine, but with the partial divided by
+        // its sum (l 1, the sum in m), as a sum of large values may pass float32
         const int gv = e.vbase + i;
         const size_t at = size_t(e.n0 + gv / g) * a.Hq + e.kh * g + gv % g;
         const size_t step = size_t(a.N) * a.Hq;
         a.ml_part[at + (direct ? 0 : e.split * step)] =
-            direct ? make_float2(0.f, -1.f) : make_float2(m_fin, l);
+            direct ? make_float2(0.f, -1.f) : make_float2(m_fin + log2f(l), l > 0.f ? 1.f : l);
         if (!direct && e.split == e.splits_r - 1)
           for (int sp = e.splits_r; sp < a.splits; ++sp)
             a.ml_part[at + sp * step] = make_float2(-INFINITY, 0.f);
       }
-      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const float inv = l > 0.f ? 1.f / l : 0.f, unit = pow2(sh.vx[slot]);
       if (!warp_mbar_wait(sh.pv_done + Tl % NS, (Tl / NS) & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
       tc_fence_after();
       if (some) {
-        const bool bad = e.nct > 0 && (sh.bad[slot][0] | sh.bad[slot][1] | sh.bad[slot][2] |
-                                       sh.bad[slot][3]) != 0;
+        bool bad = false;
+        if (nct > 0) {
+#pragma unroll
+          for (int w = 0; w < 8; ++w) bad |= sh.bad[slot][w] != 0;
+        }
         // 64 bytes of each vector at a time through this warp's 2 KB stage: four 16-byte
         // pieces a row, rotated so that eight lanes meet different banks
         auto put = [&](const uint4(&x)[4], char* base, size_t esize, int col) {
@@ -936,8 +1043,10 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           float ov[32];
           tmem_ld_32cols(tmem + lane_off + c0, ov);
           tmem_wait_ld();
+#pragma unroll
+          for (int c = 0; c < 32; ++c) ov[c] = ov[c] * inv * unit;
           if (bad) {  // the non-finite values of the tokens this row sees
-            for (int f = max(fa, e.f_begin); f <= fb; ++f) {
+            for (int f = max(fa, f_begin); f <= fb; ++f) {
               const __nv_bfloat16* v = a.v_cand + (size_t(f) * a.Hkv + e.kh) * DH + c0;
 #pragma unroll
               for (int c = 0; c < 32; ++c) {
@@ -951,8 +1060,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               const float* y = ov + 8 * q;
-              x[q] = make_uint4(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
-                                pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv));
+              x[q] = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]),
+                                pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
             }
             put(x, reinterpret_cast<char*>(a.o), 2, c0);
           } else {
@@ -977,7 +1086,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         mbar_arrive(&sh.o_free);
         mbar_arrive(sh.item_empty + slot);
       }
-      T += e.ntiles;
+      T += ntiles;
     }
     if (!ok) {
       sh.abort = 1;
@@ -993,18 +1102,18 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   }
 }
 
-// codes [keys, heads, DH]: box of box_d codes x 1 head x kBN keys
-bool encode_codes(CUtensorMap* map, const void* base, int rows, int heads, int DH, int box_d,
-                  CUtensorMapSwizzle swizzle) {
+// codes [keys, heads, DH]: box of 128 (or all 64) codes x 1 head x kBN keys
+bool encode_codes(CUtensorMap* map, const void* base, int rows, int heads, int DH) {
   auto fn = encode_fn();
   if (!fn) return false;
   const cuuint64_t dims[3] = {cuuint64_t(DH), cuuint64_t(heads), cuuint64_t(rows)};
   const cuuint64_t strides[2] = {cuuint64_t(DH), cuuint64_t(heads) * DH};
-  const cuuint32_t box[3] = {cuuint32_t(box_d), 1, cuuint32_t(kBN)};
+  const cuuint32_t box[3] = {cuuint32_t(std::min(DH, 128)), 1, cuuint32_t(kBN)};
   const cuuint32_t estr[3] = {1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box,
-            estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+            estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            DH == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int DH>
@@ -1017,9 +1126,8 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
   if (g > kBV) return cudaErrorInvalidValue;
   CUtensorMap tmQ, tmK, tmV, tmKc, tmVc;
   if (!encode_3d(&tmQ, q, n.N, d.Hq, DH, g, kBV / g) ||
-      !encode_codes(&tmK, k8, n.total_prefix, d.Hkv, DH, std::min(DH, 128),
-                    DH == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B) ||
-      !encode_codes(&tmV, v8, n.total_prefix, d.Hkv, DH, DH, CU_TENSOR_MAP_SWIZZLE_NONE))
+      !encode_codes(&tmK, k8, n.total_prefix, d.Hkv, DH) ||
+      !encode_codes(&tmV, v8, n.total_prefix, d.Hkv, DH))
     return cudaErrorInvalidValue;
   if (F > 0) {
     if (!encode_3d(&tmKc, k_cand, F, d.Hkv, DH, 1, kBC) ||

@@ -20,13 +20,13 @@
 //            to a large one).
 //
 //   warp 0       TMA producer: rings of K tiles, of V tiles, and the query block
-//   warp 1       TMEM allocator, MMA issuer
+//   warp 1       TMEM allocator, issues S_j = Q K_j^T
 //   warp 2       scheduler: work items one ahead
-//   warps 4..11  softmax, two groups of four on alternating tiles: thread = query
-//                vector = TMEM lane. The running maximum of a row passes from group to
-//                group through shared memory, ahead of the exponentials. P_j overwrites
-//                S_j in TMEM.
-//   warps 12..15 per item the queries' split into TMEM, per tile V to bf16. Values of
+//   warp 3       issues O += P_j V_j
+//   warps 4..11  softmax: two threads a query vector (TMEM lane), each with half of a
+//                tile's columns; they exchange their maxima through shared memory. P_j
+//                overwrites S_j in TMEM.
+//   warps 12..19 per item the queries' split into TMEM, per tile V to f16. Values of
 //                keys past the chunk (other requests') become zeros there.
 // The candidates' own tokens come first in a request's last chunk, as 32-key tiles of
 // bf16 keys and values (the same bytes as a cache tile) against the bf16 queries; their
@@ -45,22 +45,18 @@ namespace {
 
 constexpr int kBC = 32;  // candidate tokens per tile
 constexpr float kWeightLog2 = 7.f;  // weights are 2^7 at a row's maximum
-// P_j's 32 columns are the second half of S_j's 64: P of the second half's keys is made
-// first, from registers, while the first half's scores are still there
-constexpr uint32_t kPOff = 32;
 constexpr int kThreads = 640;
-constexpr int kProdWarp = 0, kMmaWarp = 1, kSchedWarp = 2, kSoftWarp = 4, kWideWarp = 12;
+constexpr int kProdWarp = 0, kMmaWarp = 1, kSchedWarp = 2, kPvWarp = 3, kSoftWarp = 4, kWideWarp = 12;
 constexpr int kWideThreads = kThreads - 32 * kWideWarp;
 
 template <int DH>
 struct Geo {
   static constexpr uint32_t kTile = kBN * DH;             // bytes of a K or V tile
-  static constexpr int kK = DH == 256 ? 2 : 6;            // K tiles in flight
-  static constexpr int kV = kK;                           // V tiles in flight
+  static constexpr int kS = DH == 256 ? 2 : 4;            // S buffers, and K tiles in flight
+  static constexpr int kV = DH == 256 ? 2 : 6;            // V tiles in flight
   static constexpr int kW = 2;                            // widened V tiles
-  static constexpr int kS = DH == 256 ? 2 : 4;            // S buffers
   static constexpr uint32_t kOffK = kBV * DH * 2;         // after the bf16 query block
-  static constexpr uint32_t kOffV = kOffK + kK * kTile;
+  static constexpr uint32_t kOffV = kOffK + kS * kTile;
   static constexpr uint32_t kOffW = kOffV + kV * kTile;
   static constexpr uint32_t kOffStage = kOffW + kW * 2 * kTile;  // 2 KB per softmax warp
   static constexpr uint32_t kOffSmall = kOffStage + 8 * 2048;
@@ -89,10 +85,10 @@ struct __align__(16) KvItem {
 
 struct Small {
   KvItem ring[2];
-  uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6];
-  uint64_t w_full[2], w_empty[2];        // widened V tiles
+  uint64_t k_full[4], v_full[6], v_empty[6];
+  uint64_t w_full[2];                    // widened V tiles
   uint64_t s_full[4], p_full[4], pv_done[4];
-  uint64_t m_full[2][4];                 // a tile's running maxima, per softmax warp
+  uint64_t m_full[2][4];                 // both halves' maxima of an even / odd tile
   uint64_t l_full[4];                    // both groups' sums of an item
   uint64_t xc_full;                      // the candidate values' maxima of an item
   uint64_t item_full[2], item_empty[2];
@@ -100,12 +96,12 @@ struct Small {
   uint64_t qt_full, qt_free;             // the queries' codes in TMEM
   uint64_t qx_read;                      // their exponents are in the softmax's registers
   uint64_t o_free;                       // an item's O is out of TMEM
-  uint64_t drain;
+  uint64_t drain[2];
   uint32_t tmem;
   volatile int abort;
   volatile int bad[2][8];                // non-finite candidate values, per widening warp
-  float m[2][kBV];                       // running maxima after an even / odd tile
-  float2 ml[2][2][kBV];                  // [item parity][group] (m, l)
+  float m[2][2][kBV];                    // [tile parity][half] maxima
+  float l[2][2][kBV];                    // [item parity][half] sums
   int qx[2][kBV];                        // [item parity] the queries' exponents
   int vx[2];                             // [item parity] the exponent of V and O
   uint32_t xc[2][8];                     // [item parity] candidate maxima, per widening warp
@@ -256,7 +252,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                   const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmKc,
                   const __grid_constant__ CUtensorMap tmVc, const Kv8Args a) {
   using G = Geo<DH>;
-  constexpr int NK = G::kK, NV = G::kV, NW = G::kW, NS = G::kS;
+  constexpr int NV = G::kV, NW = G::kW, NS = G::kS;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
@@ -265,31 +261,25 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = a.g, rb = a.rb;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < NK; ++s) {
-      mbar_init(sh.k_full + s, 1);
-      mbar_init(sh.k_empty + s, 1);
-    }
     for (int s = 0; s < NV; ++s) {
       mbar_init(sh.v_full + s, 1);
       mbar_init(sh.v_empty + s, 8);
     }
-    for (int s = 0; s < NW; ++s) {
-      mbar_init(sh.w_full + s, 8);
-      mbar_init(sh.w_empty + s, 1);
-    }
+    for (int s = 0; s < NW; ++s) mbar_init(sh.w_full + s, 8);
     for (int b = 0; b < NS; ++b) {
+      mbar_init(sh.k_full + b, 1);
       mbar_init(sh.s_full + b, 1);
-      mbar_init(sh.p_full + b, 4);
+      mbar_init(sh.p_full + b, 8);
       mbar_init(sh.pv_done + b, 1);
     }
     for (int q = 0; q < 4; ++q) {
-      mbar_init(&sh.m_full[0][q], 1);
-      mbar_init(&sh.m_full[1][q], 1);
+      mbar_init(&sh.m_full[0][q], 2);
+      mbar_init(&sh.m_full[1][q], 2);
       mbar_init(sh.l_full + q, 2);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(sh.item_full + b, 1);
-      mbar_init(sh.item_empty + b, 18);  // producer, MMA thread, 8 softmax and 8 widening warps
+      mbar_init(sh.item_empty + b, 19);  // producer, two MMA threads, 8 softmax, 8 widening warps
     }
     mbar_init(&sh.xc_full, 8);
     mbar_init(&sh.q_full, 1);
@@ -298,7 +288,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     mbar_init(&sh.qt_free, 1);
     mbar_init(&sh.qx_read, 8);
     mbar_init(&sh.o_free, 8);
-    mbar_init(&sh.drain, 1);
+    mbar_init(sh.drain, 1);
+    mbar_init(sh.drain + 1, 1);
     sh.abort = 0;
     fence_barrier_init();
   }
@@ -321,10 +312,10 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem;
-  // registers to the softmax warps, which hold a tile's scores: 64 + 2 x 136 + 2 x 72 are
+  // registers to the softmax warps, which hold a tile's scores: 80 + 2 x 128 + 2 x 72 are
   // the five warpgroups' launch share of 96 each
   if (warp < kSoftWarp) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
   if (warp == kSchedWarp) {
     // ---------------------------------------------------------------- scheduler
     const int count = a.sorted ? *a.item_count : 0;
@@ -429,9 +420,10 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             q_sent = progressed = true;
           }
           if (jk < e.ntiles) {
-            const int s = (T + jk) % NK;
-            const uint32_t ph = ((T + jk) / NK) & 1;
-            if (mbar_test(sh.k_empty + s, ph ^ 1u)) {
+            // (a K tile's place is free when its scores are there)
+            const int s = (T + jk) % NS;
+            const uint32_t ph = ((T + jk) / NS) & 1;
+            if (mbar_test(sh.s_full + s, ph ^ 1u)) {
               uint8_t* ks = smem + G::kOffK + s * G::kTile;
               mbar_arrive_expect_tx(sh.k_full + s, G::kTile);
               if (jk < e.nct) {
@@ -489,99 +481,58 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         flag(a.status, JET_ERR_TIMEOUT);
         // let every copy already issued land before the CTA can exit
         if (q_issued) mbar_wait(&sh.q_full, q_par, kDrainNs, nullptr);
-        for (int t = 0; t < NK; ++t)
+        for (int t = 0; t < NS; ++t)
           if (k_issued & (1u << t)) mbar_wait(sh.k_full + t, (k_par >> t) & 1u, kDrainNs, nullptr);
         for (int t = 0; t < NV; ++t)
           if (v_issued & (1u << t)) mbar_wait(sh.v_full + t, (v_par >> t) & 1u, kDrainNs, nullptr);
       }
     }
   } else if (warp == kMmaWarp) {
-    // ---------------------------------------------------------------- MMA issuer
+    // ---------------------------------------------------------------- scores
     if (elect_one()) {
       constexpr uint32_t id_s = idesc_e4m3_f32(kBV, kBN);
       constexpr uint32_t id_c = idesc_bf16_f32(kBV, kBC);
-      constexpr uint32_t id_o = idesc_f16_f32_mn(kBV, DH);
       const uint32_t qs = smem_u32(smem);
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        return mbar_wait(bar, parity, a.wait_ns, abort_flag);
+      };
       bool ok = true;
       int T = 0;
       for (int u = 0; ok; ++u) {
         const int slot = u & 1;
-        if (!mbar_wait(sh.item_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
-          ok = false;
-          break;
-        }
-        if (!sh.ring[slot].live) break;
+        ok = wait(sh.item_full + slot, (u >> 1) & 1);
+        if (!ok || !sh.ring[slot].live) break;
         const int nct = sh.ring[slot].e.nct, ntiles = sh.ring[slot].e.ntiles;
         if (nct == 0) mbar_arrive(&sh.q_free);  // only the split reads the bf16 block
-        int js = 0, jo = 0;
-        IdleClock clk;
-        while (jo < ntiles) {
-          bool progressed = false;
-          if (js < ntiles) {
-            const int Tj = T + js;
-            const int s = Tj % NK, b = Tj % NS;
-            if (mbar_test(sh.k_full + s, (Tj / NK) & 1) &&
-                mbar_test(sh.pv_done + b, ((Tj / NS) & 1) ^ 1u) &&
-                mbar_test(js < nct ? &sh.q_full : &sh.qt_full, u & 1)) {
-              tc_fence_after();
-              const uint32_t ks = smem_u32(smem + G::kOffK + s * G::kTile);
-              const uint32_t d = tmem + G::kSCol + b * kBN;
-              if (js < nct) {
+        for (int j = 0; j < ntiles; ++j) {
+          const int Tj = T + j, b = Tj % NS;
+          ok = (j > 0 && j != nct) || wait(j < nct ? &sh.q_full : &sh.qt_full, u & 1);
+          ok = ok && wait(sh.k_full + b, (Tj / NS) & 1) &&
+               wait(sh.pv_done + b, ((Tj / NS) & 1) ^ 1u);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t ks = smem_u32(smem + G::kOffK + b * G::kTile);
+          const uint32_t d = tmem + G::kSCol + b * kBN;
+          if (j < nct) {
 #pragma unroll
-                for (int st = 0; st < DH / 16; ++st) {
-                  const int sl = st >> 2, k = st & 3;
-                  mma_f16(d, desc_k_sw128(qs + sl * (kBV * 128) + 32 * k),
-                          desc_k_sw128(ks + sl * (kBC * 128) + 32 * k), id_c, st != 0);
-                }
-                if (js == nct - 1) mma_commit(&sh.q_free);
-              } else {
+            for (int st = 0; st < DH / 16; ++st) {
+              const int sl = st >> 2, k = st & 3;
+              mma_f16(d, desc_k_sw128(qs + sl * (kBV * 128) + 32 * k),
+                      desc_k_sw128(ks + sl * (kBC * 128) + 32 * k), id_c, st != 0);
+            }
+            if (j == nct - 1) mma_commit(&sh.q_free);
+          } else {
 #pragma unroll
-                for (int st = 0; st < DH / 16; ++st) {  // hi, then lo, over the same keys
-                  const int kk = st % (DH / 32);
-                  const uint64_t kd = DH == 64 ? desc_k_sw64(ks + 32 * kk)
-                                               : desc_k_sw128(ks + (kk >> 2) * (kBN * 128) +
-                                                              32 * (kk & 3));
-                  mma_e4m3_ta(d, tmem + G::kQCol + uint32_t(8 * st), kd, id_s, st != 0);
-                }
-                if (js == ntiles - 1) mma_commit(&sh.qt_free);
-              }
-              mma_commit(sh.s_full + b);
-              mma_commit(sh.k_empty + s);
-              ++js;
-              progressed = true;
+            for (int st = 0; st < DH / 16; ++st) {  // hi, then lo, over the same keys
+              const int kk = st % (DH / 32);
+              const uint64_t kd = DH == 64 ? desc_k_sw64(ks + 32 * kk)
+                                           : desc_k_sw128(ks + (kk >> 2) * (kBN * 128) +
+                                                          32 * (kk & 3));
+              mma_e4m3_ta(d, tmem + G::kQCol + uint32_t(8 * st), kd, id_s, st != 0);
             }
           }
-          if (jo < js) {
-            const int Tj = T + jo;
-            const int w = Tj % NW, b = Tj % NS;
-            // the item's first P V overwrites O: the previous item's O must be out
-            if ((jo > 0 || u == 0 || mbar_test(&sh.o_free, (u - 1) & 1)) &&
-                mbar_test(sh.p_full + b, (Tj / NS) & 1) &&
-                mbar_test(sh.w_full + w, (Tj / NW) & 1)) {
-              tc_fence_after();
-              const uint32_t pt = tmem + G::kSCol + b * kBN + kPOff;
-              const uint32_t vs = smem_u32(smem + G::kOffW + w * 2 * G::kTile);
-              if (jo < nct) {
-#pragma unroll
-                for (int k = 0; k < kBC / 16; ++k)
-                  mma_f16_ta(tmem, pt + uint32_t(8 * k), desc_mn_sw128(vs + k * 2048, kBC * 128),
-                             id_o, (jo | k) != 0);
-              } else {
-#pragma unroll
-                for (int k = 0; k < kBN / 16; ++k)
-                  mma_f16_ta(tmem, pt + uint32_t(8 * k), desc_mn_sw128(vs + k * 2048, kBN * 128),
-                             id_o, (jo | k) != 0);
-              }
-              mma_commit(sh.pv_done + b);
-              mma_commit(sh.w_empty + w);
-              ++jo;
-              progressed = true;
-            }
-          }
-          if (clk.expired(progressed, abort_flag, a.wait_ns)) {
-            ok = false;
-            break;
-          }
+          mma_commit(sh.s_full + b);
+          if (j == ntiles - 1) mma_commit(&sh.qt_free);
         }
         if (!ok) break;
         mbar_arrive(sh.item_empty + slot);
@@ -590,8 +541,55 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       if (!ok) {
         sh.abort = 1;
         flag(a.status, JET_ERR_TIMEOUT);
-        mma_commit(&sh.drain);
-        mbar_wait(&sh.drain, 0, kDrainNs, nullptr);
+        mma_commit(sh.drain);
+        mbar_wait(sh.drain, 0, kDrainNs, nullptr);
+      }
+    }
+  } else if (warp == kPvWarp) {
+    // ---------------------------------------------------------------- outputs
+    if (elect_one()) {
+      constexpr uint32_t id_o = idesc_f16_f32_mn(kBV, DH);
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        return mbar_wait(bar, parity, a.wait_ns, abort_flag);
+      };
+      bool ok = true;
+      int T = 0;
+      for (int u = 0; ok; ++u) {
+        const int slot = u & 1;
+        ok = wait(sh.item_full + slot, (u >> 1) & 1);
+        if (!ok || !sh.ring[slot].live) break;
+        const int nct = sh.ring[slot].e.nct, ntiles = sh.ring[slot].e.ntiles;
+        for (int j = 0; j < ntiles; ++j) {
+          const int Tj = T + j, b = Tj % NS, w = Tj % NW;
+          // the item's first P V overwrites O: the previous item's O must be out
+          ok = j > 0 || u == 0 || wait(&sh.o_free, (u - 1) & 1);
+          ok = ok && wait(sh.w_full + w, (Tj / NW) & 1) && wait(sh.p_full + b, (Tj / NS) & 1);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t pt = tmem + G::kSCol + b * kBN;
+          const uint32_t vs = smem_u32(smem + G::kOffW + w * 2 * G::kTile);
+          if (j < nct) {
+#pragma unroll
+            for (int k = 0; k < kBC / 16; ++k)
+              mma_f16_ta(tmem, pt + uint32_t(8 * k), desc_mn_sw128(vs + k * 2048, kBC * 128), id_o,
+                         (j | k) != 0);
+          } else {
+#pragma unroll
+            for (int k = 0; k < kBN / 16; ++k)
+              mma_f16_ta(tmem, pt + uint32_t(8 * k), desc_mn_sw128(vs + k * 2048, kBN * 128), id_o,
+                         (j | k) != 0);
+          }
+          mma_commit(sh.pv_done + b);
+        }
+        if (!ok) break;
+        mbar_arrive(sh.item_empty + slot);
+        T += ntiles;
+      }
+      if (!ok) {
+        sh.abort = 1;
+        flag(a.status, JET_ERR_TIMEOUT);
+        mma_commit(sh.drain + 1);
+        mbar_wait(sh.drain + 1, 0, kDrainNs, nullptr);
       }
     }
   }
@@ -723,7 +721,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         if ((j == e.ntiles - 1 && u >= 1 &&
              !warp_mbar_wait(&sh.o_free, (u - 1) & 1, a.wait_ns, abort_flag)) ||
             !warp_mbar_wait(sh.v_full + s, (Tj / NV) & 1, a.wait_ns, abort_flag) ||
-            !warp_mbar_wait(sh.w_empty + w, ((Tj / NW) & 1) ^ 1u, a.wait_ns, abort_flag)) {
+            (Tj >= NW && !warp_mbar_wait(sh.pv_done + (Tj - NW) % NS, ((Tj - NW) / NS) & 1,
+                                         a.wait_ns, abort_flag))) {
           ok = false;
           break;
         }
@@ -801,14 +800,14 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       flag(a.status, JET_ERR_TIMEOUT);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
     // ---------------------------------------------------------------- softmax
-    const int q4 = warp & 3, grp = (warp - kSoftWarp) >> 2;
+    const int q4 = warp & 3, half = (warp - kSoftWarp) >> 2;
     const int i = q4 * 32 + lane;  // query vector within the block = TMEM lane
     const uint32_t lane_off = uint32_t(q4 * 32) << 16;
     uint4* stage = reinterpret_cast<uint4*>(smem + G::kOffStage + (warp - kSoftWarp) * 2048);
     bool ok = true;
-    int T = 0;
+    int T = 0, x = 0;  // tiles of earlier items; tiles that this warp has worked on
     for (int u = 0; ok; ++u) {
       const int slot = u & 1;
       if (!warp_mbar_wait(sh.item_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
@@ -830,104 +829,111 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
       }
       const uint8_t* ex = a.k_exp + size_t(kv_place(e.p0, e.r, e.k_begin / kBN)) * a.Hkv + e.kh;
-      const int j0 = (grp ^ T) & 1;  // this group's tiles: j0, j0 + 2, ..
-      int byte = 0;
-      if (j0 >= nct && j0 < ntiles) byte = ex[size_t(j0 - nct) * a.Hkv];
+      int byte = *ex;
       int qx = 0;
-      bool qx_read = false;
-      auto read_qx = [&]() -> bool {
-        if (!warp_mbar_wait(&sh.qt_full, u & 1, a.wait_ns, abort_flag)) return false;
-        qx = sh.qx[slot][i];
-        qx_read = true;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.qx_read);
-        return true;
-      };
-      float m_own = -INFINITY, l = 0.f;  // l: the sum over this group's tiles, relative to m_own
-
-      // scores of 32 nh keys in columns klo .. khi, times mul in base 2, to weights: 32
-      // scores at a time in registers, the last of them from their maximum to their
-      // weights, the others read twice
-      auto tile = [&](int nh, int j, float mul, int klo, int khi) -> bool {
+      float m = -INFINITY, l = 0.f;  // the running maximum; the sum over this half's columns
+      for (int j = 0; j < ntiles; ++j) {
         const int Tj = T + j, b = Tj % NS;
-        const uint32_t at = tmem + lane_off + G::kSCol + b * kBN;
-        float sv[32];
-        const bool cut = __any_sync(0xffffffffu, klo > 0 || khi < 32 * nh);
-        auto load = [&](int k) {
-          tmem_ld_32cols(at + 32 * k, sv);
+        if (j == nct) {
+          if (!warp_mbar_wait(&sh.qt_full, u & 1, a.wait_ns, abort_flag)) {
+            ok = false;
+            break;
+          }
+          qx = sh.qx[slot][i];
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.qx_read);
+        }
+        if (!warp_mbar_wait(sh.s_full + b, (Tj / NS) & 1, a.wait_ns, abort_flag)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        // this half's 32 columns [klo, khi) of the tile, and the scores' factor in base 2
+        float mul = a.scale_log2;
+        int klo = 0, khi;
+        if (j < nct) {
+          const int f0 = f_begin + j * kBC + 32 * half;
+          klo = fa - f0;
+          khi = half == 0 ? min(32, fb - f0 + 1) : 0;
+        } else {
+          const int X = min(max(byte - 127, kKvLow), kKvHigh);
+          mul *= pow2(min(max(qx + X, -126), 126));
+          khi = min(32, keys - (j - nct) * kBN - 32 * half);
+          // the exponent of the next tile, a tile ahead of its use
+          if (j + 1 < ntiles) byte = ex[size_t(j + 1 - nct) * a.Hkv];
+        }
+        if (some) {
+          float sv[32];
+          tmem_ld_32cols(tmem + lane_off + G::kSCol + b * kBN + 32 * half, sv);
           tmem_wait_ld();
-          if (cut) {
+          if (__any_sync(0xffffffffu, klo > 0 || khi < 32)) {
 #pragma unroll
             for (int c = 0; c < 32; ++c)
-              if (c < klo - 32 * k || c >= khi - 32 * k) sv[c] = -INFINITY;
+              if (c < klo || c >= khi) sv[c] = -INFINITY;
           }
-        };
-        float mt = -INFINITY;
-        if (some) {
-          float mq[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-          for (int k = 0; k < nh; ++k) {
-            load(k);
+          float mq[4];
 #pragma unroll
-            for (int c = 0; c < 32; c += 8)
+          for (int q = 0; q < 4; ++q) mq[q] = max3(sv[q], sv[4 + q], sv[8 + q]);
 #pragma unroll
-              for (int q = 0; q < 4; ++q) mq[q] = max3(mq[q], sv[c + q], sv[c + 4 + q]);
+          for (int c = 12; c < 28; c += 8)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mq[q] = max3(mq[q], sv[c + q], sv[c + 4 + q]);
+          float mt = max3(max3(mq[0], sv[28], sv[29]), max3(mq[1], sv[30], sv[31]),
+                          fmaxf(mq[2], mq[3]));
+          mt *= mul;
+          // the other half's: then both know the row's maximum over the tile
+          sh.m[x & 1][half][i] = mt;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.m_full[x & 1][q4]);
+          if (!warp_mbar_wait(&sh.m_full[x & 1][q4], (x >> 1) & 1, a.wait_ns, abort_flag)) {
+            ok = false;
+            break;
           }
-          mt = mul * fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3]));
-        }
-        // the row's maximum after the tile before, which the other group has
-        if (Tj > 0 && !warp_mbar_wait(&sh.m_full[(Tj - 1) & 1][q4], ((Tj - 1) >> 1) & 1, a.wait_ns,
-                                      abort_flag))
-          return false;
-        const float m_prev = j > 0 ? sh.m[(Tj - 1) & 1][i] : -INFINITY;
-        const bool grow = j == 0 || (valid && mt > m_prev + kRescaleLog2);
-        const float m_new = grow ? mt : m_prev;
-        sh.m[Tj & 1][i] = m_new;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.m_full[Tj & 1][q4]);
-        if (some) {
-          if (j > 0 && __any_sync(0xffffffffu, grow)) {
-            // O holds this item's P V so far: wait for the last one, rescale in TMEM
-            const int b1 = (Tj - 1) % NS;
-            if (!warp_mbar_wait(sh.pv_done + b1, ((Tj - 1) / NS) & 1, a.wait_ns, abort_flag))
-              return false;
-            tc_fence_after();
-            const float f = grow ? ex2(m_prev - m_new) : 1.f;
+          mt = fmaxf(mt, sh.m[x & 1][half ^ 1][i]);
+          ++x;
+          const bool grow = j == 0 || (valid && mt > m + kRescaleLog2);
+          if (__any_sync(0xffffffffu, grow)) {
+            const float m_new = grow ? mt : m;
+            if (j > 0) {
+              // O holds this item's P V so far: wait for the last one, rescale this half of
+              // its columns in TMEM
+              if (!warp_mbar_wait(sh.pv_done + (Tj - 1) % NS, ((Tj - 1) / NS) & 1, a.wait_ns,
+                                  abort_flag)) {
+                ok = false;
+                break;
+              }
+              tc_fence_after();
+              const float f = !grow ? 1.f : m == -INFINITY ? 0.f : ex2(m - m_new);
 #pragma unroll 1
-            for (int c0 = 0; c0 < DH; c0 += 16) {
-              float ov[16];
-              tmem_ld_16cols(tmem + lane_off + c0, ov);
-              tmem_wait_ld();
+              for (int c0 = half * (DH / 2); c0 < (half + 1) * (DH / 2); c0 += 16) {
+                float ov[16];
+                tmem_ld_16cols(tmem + lane_off + c0, ov);
+                tmem_wait_ld();
 #pragma unroll
-              for (int c = 0; c < 16; ++c) ov[c] *= f;
-              tmem_st_16cols(tmem + lane_off + c0, ov);
+                for (int c = 0; c < 16; ++c) ov[c] *= f;
+                tmem_st_16cols(tmem + lane_off + c0, ov);
+              }
+              l *= f;
             }
-            if (nh > 1) load(nh - 1);  // the registers' scores again
-          }
-          if (m_new != m_own) {
-            l = m_own == -INFINITY ? 0.f : l * ex2(m_own - m_new);
-            m_own = m_new;
+            m = m_new;
           }
           // weights 2^(s - m + 7): f16 holds them from 2^-24 to the 2^15 that a maximum not
           // yet taken over may give; no key seen yet: weights of 0
-          const float sub = m_new == -INFINITY ? 0.f : m_new - kWeightLog2;
-          const float2 mul2 = make_float2(mul, mul), sub2 = make_float2(-sub, -sub);
+          const float sub = m == -INFINITY ? 0.f : kWeightLog2 - m;
+          const float2 mul2 = make_float2(mul, mul), sub2 = make_float2(sub, sub);
           float2 ps[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) ps[q] = make_float2(0.f, 0.f);
-#pragma unroll 1
-          for (int k = nh - 1; k >= 0; --k) {
-            if (k < nh - 1) load(k);
-            uint32_t pw[16];
+          uint32_t pw[16];
 #pragma unroll
-            for (int c = 0; c < 16; ++c) {
-              const float2 y = fma2(make_float2(sv[2 * c], sv[2 * c + 1]), mul2, sub2);
-              const float2 x = make_float2(ex2(y.x), ex2(y.y));
-              ps[c & 3] = add2(ps[c & 3], x);
-              pw[c] = pack_f16(x.x, x.y);
-            }
-            tmem_st_16cols_u32(at + kPOff + 16 * k, pw);
+          for (int c = 0; c < 16; ++c) {
+            const float2 y = fma2(make_float2(sv[2 * c], sv[2 * c + 1]), mul2, sub2);
+            const float2 p = make_float2(ex2(y.x), ex2(y.y));
+            ps[c & 3] = add2(ps[c & 3], p);
+            pw[c] = pack_f16(p.x, p.y);
           }
+          // both halves' scores are in registers by now: P takes the place of S
+          tmem_st_16cols_u32(tmem + lane_off + G::kSCol + b * kBN + 16 * half, pw);
           const float2 p = add2(add2(ps[0], ps[1]), add2(ps[2], ps[3]));
           l += p.x + p.y;
           tmem_wait_st();
@@ -935,57 +941,18 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(sh.p_full + b);
-        return true;
-      };
-
-      for (int j = j0; j < ntiles; j += 2) {
-        const int Tj = T + j, b = Tj % NS;
-        if (j >= nct && !qx_read && !read_qx()) {
-          ok = false;
-          break;
-        }
-        if (!warp_mbar_wait(sh.s_full + b, (Tj / NS) & 1, a.wait_ns, abort_flag)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-        const int held = byte;
-        // the exponent of this group's next tile, a tile ahead of its use
-        if (j + 2 >= nct && j + 2 < ntiles) byte = ex[size_t(j + 2 - nct) * a.Hkv];
-        int nh = kBN / 32, klo = 0, khi;
-        float mul = a.scale_log2;
-        if (j < nct) {
-          const int f0 = f_begin + j * kBC;
-          nh = kBC / 32;
-          klo = max(0, fa - f0);
-          khi = min(kBC, fb - f0 + 1);
-        } else {
-          const int X = min(max(held - 127, kKvLow), kKvHigh);
-          mul *= pow2(min(max(qx + X, -126), 126));
-          khi = min(kBN, keys - (j - nct) * kBN);
-        }
-        ok = tile(nh, j, mul, klo, khi);
-        if (!ok) break;
       }
       if (!ok) break;
-      if (!qx_read && !read_qx()) {
-        ok = false;
-        break;
-      }
-      // both groups' sums, relative to the maximum after the last tile
-      sh.ml[slot][grp][i] = make_float2(m_own, l);
+      // both halves' sums
+      sh.l[slot][half][i] = l;
       __syncwarp();
       if (lane == 0) mbar_arrive(sh.l_full + q4);
       if (!warp_mbar_wait(sh.l_full + q4, u & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
+      l += sh.l[slot][half ^ 1][i];
       const int Tl = T + ntiles - 1;
-      const float m_fin = sh.m[Tl & 1][i];
-      const float2 x0 = sh.ml[slot][0][i], x1 = sh.ml[slot][1][i];
-      l = (x0.x == -INFINITY && x0.y == 0.f ? 0.f : x0.y * ex2(x0.x - m_fin)) +
-          (x1.x == -INFINITY && x1.y == 0.f ? 0.f : x1.y * ex2(x1.x - m_fin));
-      if (valid && (m_fin == -INFINITY)) l = x0.y + x1.y;
       const bool direct = e.splits_r == 1;
       long long dst[4];  // of the vectors this lane stores (8 s + lane / 4, 16 bytes each)
 #pragma unroll
@@ -998,14 +965,14 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           dst[s] = (long long)(size_t(direct ? n : e.split * (long long)a.N + n) * a.Hq + h) * DH;
         }
       }
-      if (valid && a.splits > 1 && grp == 0) {
+      if (valid && a.splits > 1 && half == 0) {
         // as the bf16 kernel leaves them for the combine, but with the partial divided by
         // its sum (l 1, the sum in m), as a sum of large values may pass float32
         const int gv = e.vbase + i;
         const size_t at = size_t(e.n0 + gv / g) * a.Hq + e.kh * g + gv % g;
         const size_t step = size_t(a.N) * a.Hq;
         a.ml_part[at + (direct ? 0 : e.split * step)] =
-            direct ? make_float2(0.f, -1.f) : make_float2(m_fin + log2f(l), l > 0.f ? 1.f : l);
+            direct ? make_float2(0.f, -1.f) : make_float2(m + log2f(l), l > 0.f ? 1.f : l);
         if (!direct && e.split == e.splits_r - 1)
           for (int sp = e.splits_r; sp < a.splits; ++sp)
             a.ml_part[at + sp * step] = make_float2(-INFINITY, 0.f);
@@ -1037,9 +1004,9 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           }
           __syncwarp();
         };
-        // each group writes half of the columns
+        // each of a row's two warps writes half of the columns
 #pragma unroll 1
-        for (int c0 = grp * (DH / 2); c0 < (grp + 1) * (DH / 2); c0 += 32) {
+        for (int c0 = half * (DH / 2); c0 < (half + 1) * (DH / 2); c0 += 32) {
           float ov[32];
           tmem_ld_32cols(tmem + lane_off + c0, ov);
           tmem_wait_ld();

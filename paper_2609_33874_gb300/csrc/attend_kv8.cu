@@ -43,7 +43,6 @@
 namespace jet {
 namespace {
 
-constexpr int kBC = 32;  // candidate tokens per tile
 constexpr float kWeightLog2 = 7.f;  // weights are 2^7 at a row's maximum
 constexpr int kThreads = 640;
 constexpr int kProdWarp = 0, kMmaWarp = 1, kSchedWarp = 2, kPvWarp = 3, kSoftWarp = 4, kWideWarp = 12;
@@ -51,9 +50,14 @@ constexpr int kWideThreads = kThreads - 32 * kWideWarp;
 
 template <int DH>
 struct Geo {
-  static constexpr uint32_t kTile = kBN * DH;             // bytes of a K or V tile
-  static constexpr int kS = DH == 256 ? 2 : 4;            // S buffers, and K tiles in flight
-  static constexpr int kV = DH == 256 ? 2 : 6;            // V tiles in flight
+  // A tile of 64 keys for d 256, whose O leaves TMEM no more; else of 128, so that half as
+  // many steps of the pipeline carry the same bytes
+  static constexpr int kT = DH == 256 ? 64 : 128;
+  static constexpr int kHalf = kT / 2;                    // columns of a softmax warp
+  static constexpr int kC = kT / 2;                       // candidate tokens per tile
+  static constexpr uint32_t kTile = kT * DH;              // bytes of a K or V tile
+  static constexpr int kS = DH == 64 ? 3 : 2;             // S buffers, and K tiles in flight
+  static constexpr int kV = DH == 256 ? 2 : DH == 128 ? 3 : 6;  // V tiles in flight
   static constexpr int kW = 2;                            // widened V tiles
   static constexpr uint32_t kOffK = kBV * DH * 2;         // after the bf16 query block
   static constexpr uint32_t kOffV = kOffK + kS * kTile;
@@ -64,7 +68,7 @@ struct Geo {
   // TMEM: O, the S buffers (P in place of S), the queries' hi and lo codes
   static constexpr uint32_t kTmemCols = 512;
   static constexpr uint32_t kSCol = DH;
-  static constexpr uint32_t kQCol = kSCol + kS * kBN;
+  static constexpr uint32_t kQCol = kSCol + kS * kT;
   static_assert(kQCol + DH / 2 <= kTmemCols, "TMEM columns");
   static_assert(kBytes + 1024 <= 232448, "shared memory");
 };
@@ -204,10 +208,22 @@ constexpr uint32_t idesc_f16_f32_mn(int M, int N) {
 
 // where a V tile's TMA copy leaves the 16 codes c of a key: slices of 128 codes under
 // 128-byte swizzling, d 64 rows of 64 bytes under 64-byte swizzling
-template <int DH>
+template <int DH, int KT>
 __device__ __forceinline__ uint32_t raw_piece(int key, int c) {
   if constexpr (DH == 64) return uint32_t(key) * 64u + (uint32_t(c ^ ((key >> 1) & 3)) << 4);
-  return uint32_t(c >> 3) * (kBN * 128) + sw128(key, c & 7);
+  return uint32_t(c >> 3) * (KT * 128) + sw128(key, c & 7);
+}
+
+// An exponent byte, asked for a tile ahead of its use: the compiler is not to touch the
+// register in between, as that would wait for the load (1,000 cycles a tile of d 128)
+__device__ __forceinline__ uint32_t load_ahead(const uint8_t* p) {
+  uint32_t v;
+  asm volatile("ld.global.nc.u8 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ int exponent_of(uint32_t byte) {
+  asm volatile("" : "+r"(byte));
+  return min(max(int(byte) - 127, kKvLow), kKvHigh);
 }
 
 // two float32 at a time
@@ -252,7 +268,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                   const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmKc,
                   const __grid_constant__ CUtensorMap tmVc, const Kv8Args a) {
   using G = Geo<DH>;
-  constexpr int NV = G::kV, NW = G::kW, NS = G::kS;
+  constexpr int NV = G::kV, NW = G::kW, NS = G::kS, KT = G::kT, KC = G::kC;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
@@ -363,7 +379,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             // from the first of its first row's candidate on
             fed = e.row0 + e.nv / g - 1;
             int lo = 0;
-            if (fed > kBC && e.row0 > 0) {
+            if (fed > KC && e.row0 > 0) {
               const int c = a.row_cand[e.n0 + e.row0];
               if (c >= 0 && c < a.C)
                 lo = min(max(a.cand_row_offset[c] - e.n0 - 1, 0), fed);
@@ -371,7 +387,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             e.f_begin += lo;
             fed -= lo;
           }
-          e.nct = (fed + kBC - 1) / kBC;
+          e.nct = (fed + KC - 1) / KC;
+          e.npt = (e.k_end - e.k_begin + KT - 1) / KT;
           e.ntiles = e.npt + e.nct;
         }
         sh.ring[slot].e = e;
@@ -429,13 +446,13 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
               if (jk < e.nct) {
 #pragma unroll
                 for (int sl = 0; sl < DH / 64; ++sl)
-                  tma_load_3d(ks + sl * (kBC * 128), &tmKc, sh.k_full + s, sl * 64, e.kh,
-                              e.f_begin + jk * kBC, pol);
+                  tma_load_3d(ks + sl * (KC * 128), &tmKc, sh.k_full + s, sl * 64, e.kh,
+                              e.f_begin + jk * KC, pol);
               } else {
-                const int key = e.p0 + e.k_begin + (jk - e.nct) * kBN;
+                const int key = e.p0 + e.k_begin + (jk - e.nct) * KT;
 #pragma unroll
                 for (int sl = 0; sl < (DH + 127) / 128; ++sl)
-                  tma_load_3d(ks + sl * (kBN * 128), &tmK, sh.k_full + s, sl * 128, e.kh, key, pol);
+                  tma_load_3d(ks + sl * (KT * 128), &tmK, sh.k_full + s, sl * 128, e.kh, key, pol);
               }
               k_issued |= 1u << s;
               k_par = (k_par & ~(1u << s)) | (ph << s);
@@ -452,13 +469,13 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
               if (jv < e.nct) {
 #pragma unroll
                 for (int sl = 0; sl < DH / 64; ++sl)
-                  tma_load_3d(vs + sl * (kBC * 128), &tmVc, sh.v_full + s, sl * 64, e.kh,
-                              e.f_begin + jv * kBC, pol);
+                  tma_load_3d(vs + sl * (KC * 128), &tmVc, sh.v_full + s, sl * 64, e.kh,
+                              e.f_begin + jv * KC, pol);
               } else {
-                const int key = e.p0 + e.k_begin + (jv - e.nct) * kBN;
+                const int key = e.p0 + e.k_begin + (jv - e.nct) * KT;
 #pragma unroll
                 for (int sl = 0; sl < (DH + 127) / 128; ++sl)
-                  tma_load_3d(vs + sl * (kBN * 128), &tmV, sh.v_full + s, sl * 128, e.kh, key, pol);
+                  tma_load_3d(vs + sl * (KT * 128), &tmV, sh.v_full + s, sl * 128, e.kh, key, pol);
               }
               v_issued |= 1u << s;
               v_par = (v_par & ~(1u << s)) | (ph << s);
@@ -490,8 +507,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   } else if (warp == kMmaWarp) {
     // ---------------------------------------------------------------- scores
     if (elect_one()) {
-      constexpr uint32_t id_s = idesc_e4m3_f32(kBV, kBN);
-      constexpr uint32_t id_c = idesc_bf16_f32(kBV, kBC);
+      constexpr uint32_t id_s = idesc_e4m3_f32(kBV, KT);
+      constexpr uint32_t id_c = idesc_bf16_f32(kBV, KC);
       const uint32_t qs = smem_u32(smem);
       auto wait = [&](uint64_t* bar, uint32_t parity) {
         return mbar_wait(bar, parity, a.wait_ns, abort_flag);
@@ -512,13 +529,13 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           if (!ok) break;
           tc_fence_after();
           const uint32_t ks = smem_u32(smem + G::kOffK + b * G::kTile);
-          const uint32_t d = tmem + G::kSCol + b * kBN;
+          const uint32_t d = tmem + G::kSCol + b * KT;
           if (j < nct) {
 #pragma unroll
             for (int st = 0; st < DH / 16; ++st) {
               const int sl = st >> 2, k = st & 3;
               mma_f16(d, desc_k_sw128(qs + sl * (kBV * 128) + 32 * k),
-                      desc_k_sw128(ks + sl * (kBC * 128) + 32 * k), id_c, st != 0);
+                      desc_k_sw128(ks + sl * (KC * 128) + 32 * k), id_c, st != 0);
             }
             if (j == nct - 1) mma_commit(&sh.q_free);
           } else {
@@ -526,7 +543,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             for (int st = 0; st < DH / 16; ++st) {  // hi, then lo, over the same keys
               const int kk = st % (DH / 32);
               const uint64_t kd = DH == 64 ? desc_k_sw64(ks + 32 * kk)
-                                           : desc_k_sw128(ks + (kk >> 2) * (kBN * 128) +
+                                           : desc_k_sw128(ks + (kk >> 2) * (KT * 128) +
                                                           32 * (kk & 3));
               mma_e4m3_ta(d, tmem + G::kQCol + uint32_t(8 * st), kd, id_s, st != 0);
             }
@@ -566,17 +583,17 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           ok = ok && wait(sh.w_full + w, (Tj / NW) & 1) && wait(sh.p_full + b, (Tj / NS) & 1);
           if (!ok) break;
           tc_fence_after();
-          const uint32_t pt = tmem + G::kSCol + b * kBN;
+          const uint32_t pt = tmem + G::kSCol + b * KT;
           const uint32_t vs = smem_u32(smem + G::kOffW + w * 2 * G::kTile);
           if (j < nct) {
 #pragma unroll
-            for (int k = 0; k < kBC / 16; ++k)
-              mma_f16_ta(tmem, pt + uint32_t(8 * k), desc_mn_sw128(vs + k * 2048, kBC * 128), id_o,
+            for (int k = 0; k < KC / 16; ++k)
+              mma_f16_ta(tmem, pt + uint32_t(8 * k), desc_mn_sw128(vs + k * 2048, KC * 128), id_o,
                          (j | k) != 0);
           } else {
 #pragma unroll
-            for (int k = 0; k < kBN / 16; ++k)
-              mma_f16_ta(tmem, pt + uint32_t(8 * k), desc_mn_sw128(vs + k * 2048, kBN * 128), id_o,
+            for (int k = 0; k < KT / 16; ++k)
+              mma_f16_ta(tmem, pt + uint32_t(8 * k), desc_mn_sw128(vs + k * 2048, KT * 128), id_o,
                          (j | k) != 0);
           }
           mma_commit(sh.pv_done + b);
@@ -600,10 +617,11 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     const int t = threadIdx.x - kWideWarp * 32;
     const int row = q4 * 32 + lane;  // of the queries, in two halves of their elements
     const uint32_t lane_off = uint32_t(q4 * 32) << 16;
-    // of a V tile: one key's pieces of 16 codes, every fourth one. Eight lanes are eight
+    // of a V tile: one key's pieces of 16 codes, every kPer-th one. Eight lanes are eight
     // keys, whose swizzled places differ in their banks, before and after.
-    constexpr int kMine = DH / 64;
-    const int key = t & (kBN - 1), c0 = t >> 6;
+    constexpr int kPer = kWideThreads / KT, kMine = DH / 16 / kPer;
+    const int key = t & (KT - 1), c0 = t / KT;
+    const int block = key / kKvBlock;  // of the tile's, the key's: the same for a warp
     int n_fed = 0;  // items with candidates so far
     bool ok = true;
     int T = 0;
@@ -619,8 +637,10 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       // V's unit of this item: the largest exponent of its tiles and of its candidates'
       // values (the loads fly while the queries are split)
       const uint8_t* ex = a.v_exp + size_t(kv_place(e.p0, e.r, e.k_begin / kBN)) * a.Hkv + e.kh;
-      int byte = *ex, vx = kKvLow + 127;
-      for (int pt = lane; pt < e.npt; pt += 32) vx = max(vx, int(ex[size_t(pt) * a.Hkv]));
+      const int blocks = (keys + kKvBlock - 1) / kKvBlock;
+      uint32_t byte = block < blocks ? load_ahead(ex + size_t(block) * a.Hkv) : 0;
+      int vx = kKvLow + 127;
+      for (int b = lane; b < blocks; b += 32) vx = max(vx, int(ex[size_t(b) * a.Hkv]));
       if (fed > 0) {
         uint32_t top = 0;
         const __nv_bfloat16* vc = a.v_cand + (size_t(e.f_begin) * a.Hkv + e.kh) * DH;
@@ -730,7 +750,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         uint8_t* ws = smem + G::kOffW + w * 2 * G::kTile;
         if (j < e.nct) {
           // candidate values, in the places the product reads
-          const int left = fed - j * kBC;
+          const int left = fed - j * KC;
           const float inv = pow2(-vx);
           bool found = false;
 #pragma unroll
@@ -745,7 +765,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
               found |= n0 | n1;
               y[q] = pack_f16(n0 ? 0.f : __uint_as_float(in[q] << 16) * inv,
                               n1 ? 0.f : __uint_as_float(in[q] & 0xffff0000u) * inv);
-              if (((i >> 3) & (kBC - 1)) >= left) y[q] = 0u;
+              if (((i >> 3) & (KC - 1)) >= left) y[q] = 0u;
             }
             *reinterpret_cast<uint4*>(ws + 16 * i) = make_uint4(y[0], y[1], y[2], y[3]);
           }
@@ -753,16 +773,17 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         } else {
           const int pt = j - e.nct;
           // 2^(X - vx): below 2^-24 f16 holds no product with a code
-          const int k2 = max(min(max(byte - 127, kKvLow), kKvHigh) - vx, -24);
-          if (pt + 1 < e.npt) byte = ex[size_t(pt + 1) * a.Hkv];
+          const int k2 = max(exponent_of(byte) - vx, -24);
+          const int next = (pt + 1) * (KT / kKvBlock) + block;
+          if (next < blocks) byte = load_ahead(ex + size_t(next) * a.Hkv);
           const uint32_t h2 = k2 > -15 ? uint32_t(k2 + 15) << 10 : 1u << (k2 + 24);
           const uint32_t f = h2 | h2 << 16;
-          const int left = keys - pt * kBN;  // the tile's keys past it are another request's
+          const int left = keys - pt * KT;  // the tile's keys past it are another request's
           uint4 x[kMine];
 #pragma unroll
           for (int i = 0; i < kMine; ++i)
-            x[i] = *reinterpret_cast<const uint4*>(vs + raw_piece<DH>(key, c0 + 4 * i));
-          if (left < kBN && key >= left) {
+            x[i] = *reinterpret_cast<const uint4*>(vs + raw_piece<DH, KT>(key, c0 + kPer * i));
+          if (left < KT && key >= left) {
 #pragma unroll
             for (int i = 0; i < kMine; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
           }
@@ -776,8 +797,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
               y[2 * q] = mul_f16x2(y[2 * q], f);
               y[2 * q + 1] = mul_f16x2(y[2 * q + 1], f);
             }
-            const int c = c0 + 4 * i;  // pieces 2 c and 2 c + 1 of the f16 row
-            uint8_t* to = ws + (c >> 2) * (kBN * 128);
+            const int c = c0 + kPer * i;  // pieces 2 c and 2 c + 1 of the f16 row
+            uint8_t* to = ws + (c >> 2) * (KT * 128);
             *reinterpret_cast<uint4*>(to + sw128(key, (2 * c) & 7)) =
                 make_uint4(y[0], y[1], y[2], y[3]);
             *reinterpret_cast<uint4*>(to + sw128(key, (2 * c + 1) & 7)) =
@@ -829,7 +850,12 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
       }
       const uint8_t* ex = a.k_exp + size_t(kv_place(e.p0, e.r, e.k_begin / kBN)) * a.Hkv + e.kh;
-      int byte = *ex;
+      constexpr int kCols = G::kHalf;
+      // this half's blocks of the tiles: every tile's (d 256), or every second block
+      constexpr int kBlocks = KT / kKvBlock;
+      const int first = kBlocks == 2 ? half : 0;
+      const int blocks = (keys + kKvBlock - 1) / kKvBlock;
+      uint32_t byte = first < blocks ? load_ahead(ex + size_t(first) * a.Hkv) : 0;
       int qx = 0;
       float m = -INFINITY, l = 0.f;  // the running maximum; the sum over this half's columns
       for (int j = 0; j < ntiles; ++j) {
@@ -843,43 +869,45 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.qx_read);
         }
+        // this half's columns [klo, khi) of the tile, and the scores' factor in base 2
+        float mul = a.scale_log2;
+        int klo = 0, khi;
+        if (j < nct) {
+          const int f0 = f_begin + j * KC;
+          klo = fa - f0;
+          khi = half == 0 ? min(kCols, fb - f0 + 1) : 0;
+        } else {
+          mul *= pow2(min(max(qx + exponent_of(byte), -126), 126));
+          khi = min(kCols, keys - (j - nct) * KT - kCols * half);
+          const int next = (j + 1 - nct) * kBlocks + first;
+          if (next < blocks) byte = load_ahead(ex + size_t(next) * a.Hkv);
+        }
+        const bool cut = __any_sync(0xffffffffu, klo > 0 || khi < kCols);
         if (!warp_mbar_wait(sh.s_full + b, (Tj / NS) & 1, a.wait_ns, abort_flag)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        // this half's 32 columns [klo, khi) of the tile, and the scores' factor in base 2
-        float mul = a.scale_log2;
-        int klo = 0, khi;
-        if (j < nct) {
-          const int f0 = f_begin + j * kBC + 32 * half;
-          klo = fa - f0;
-          khi = half == 0 ? min(32, fb - f0 + 1) : 0;
-        } else {
-          const int X = min(max(byte - 127, kKvLow), kKvHigh);
-          mul *= pow2(min(max(qx + X, -126), 126));
-          khi = min(32, keys - (j - nct) * kBN - 32 * half);
-          // the exponent of the next tile, a tile ahead of its use
-          if (j + 1 < ntiles) byte = ex[size_t(j + 1 - nct) * a.Hkv];
-        }
         if (some) {
-          float sv[32];
-          tmem_ld_32cols(tmem + lane_off + G::kSCol + b * kBN + 32 * half, sv);
-          tmem_wait_ld();
-          if (__any_sync(0xffffffffu, klo > 0 || khi < 32)) {
+          float sv[kCols];
 #pragma unroll
-            for (int c = 0; c < 32; ++c)
+          for (int k = 0; k < kCols / 32; ++k)
+            tmem_ld_32cols(tmem + lane_off + G::kSCol + b * KT + kCols * half + 32 * k,
+                           *reinterpret_cast<float(*)[32]>(sv + 32 * k));
+          tmem_wait_ld();
+          if (cut) {
+#pragma unroll
+            for (int c = 0; c < kCols; ++c)
               if (c < klo || c >= khi) sv[c] = -INFINITY;
           }
           float mq[4];
 #pragma unroll
-          for (int q = 0; q < 4; ++q) mq[q] = max3(sv[q], sv[4 + q], sv[8 + q]);
+          for (int q = 0; q < 4; ++q) mq[q] = fmaxf(sv[q], sv[4 + q]);
 #pragma unroll
-          for (int c = 12; c < 28; c += 8)
+          for (int c = 8; c < kCols; c += 8)
 #pragma unroll
             for (int q = 0; q < 4; ++q) mq[q] = max3(mq[q], sv[c + q], sv[c + 4 + q]);
-          float mt = max3(max3(mq[0], sv[28], sv[29]), max3(mq[1], sv[30], sv[31]),
-                          fmaxf(mq[2], mq[3]));
+          float mt = max3(mq[0], mq[1], fmaxf(mq[2], mq[3]));
           mt *= mul;
           // the other half's: then both know the row's maximum over the tile
           sh.m[x & 1][half][i] = mt;
@@ -924,16 +952,20 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           float2 ps[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) ps[q] = make_float2(0.f, 0.f);
-          uint32_t pw[16];
+          // P takes the place of scores that are in registers by now
 #pragma unroll
-          for (int c = 0; c < 16; ++c) {
-            const float2 y = fma2(make_float2(sv[2 * c], sv[2 * c + 1]), mul2, sub2);
-            const float2 p = make_float2(ex2(y.x), ex2(y.y));
-            ps[c & 3] = add2(ps[c & 3], p);
-            pw[c] = pack_f16(p.x, p.y);
+          for (int k = 0; k < kCols / 32; ++k) {
+            uint32_t pw[16];
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+              const int at = 32 * k + 2 * c;
+              const float2 y = fma2(make_float2(sv[at], sv[at + 1]), mul2, sub2);
+              const float2 p = make_float2(ex2(y.x), ex2(y.y));
+              ps[c & 3] = add2(ps[c & 3], p);
+              pw[c] = pack_f16(p.x, p.y);
+            }
+            tmem_st_16cols_u32(tmem + lane_off + G::kSCol + b * KT + kCols / 2 * half + 16 * k, pw);
           }
-          // both halves' scores are in registers by now: P takes the place of S
-          tmem_st_16cols_u32(tmem + lane_off + G::kSCol + b * kBN + 16 * half, pw);
           const float2 p = add2(add2(ps[0], ps[1]), add2(ps[2], ps[3]));
           l += p.x + p.y;
           tmem_wait_st();
@@ -1069,13 +1101,13 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   }
 }
 
-// codes [keys, heads, DH]: box of 128 (or all 64) codes x 1 head x kBN keys
-bool encode_codes(CUtensorMap* map, const void* base, int rows, int heads, int DH) {
+// codes [keys, heads, DH]: box of 128 (or all 64) codes x 1 head x box_keys keys
+bool encode_codes(CUtensorMap* map, const void* base, int rows, int heads, int DH, int box_keys) {
   auto fn = encode_fn();
   if (!fn) return false;
   const cuuint64_t dims[3] = {cuuint64_t(DH), cuuint64_t(heads), cuuint64_t(rows)};
   const cuuint64_t strides[2] = {cuuint64_t(DH), cuuint64_t(heads) * DH};
-  const cuuint32_t box[3] = {cuuint32_t(std::min(DH, 128)), 1, cuuint32_t(kBN)};
+  const cuuint32_t box[3] = {cuuint32_t(std::min(DH, 128)), 1, cuuint32_t(box_keys)};
   const cuuint32_t estr[3] = {1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box,
             estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -1093,12 +1125,12 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
   if (g > kBV) return cudaErrorInvalidValue;
   CUtensorMap tmQ, tmK, tmV, tmKc, tmVc;
   if (!encode_3d(&tmQ, q, n.N, d.Hq, DH, g, kBV / g) ||
-      !encode_codes(&tmK, k8, n.total_prefix, d.Hkv, DH) ||
-      !encode_codes(&tmV, v8, n.total_prefix, d.Hkv, DH))
+      !encode_codes(&tmK, k8, n.total_prefix, d.Hkv, DH, Geo<DH>::kT) ||
+      !encode_codes(&tmV, v8, n.total_prefix, d.Hkv, DH, Geo<DH>::kT))
     return cudaErrorInvalidValue;
   if (F > 0) {
-    if (!encode_3d(&tmKc, k_cand, F, d.Hkv, DH, 1, kBC) ||
-        !encode_3d(&tmVc, v_cand, F, d.Hkv, DH, 1, kBC))
+    if (!encode_3d(&tmKc, k_cand, F, d.Hkv, DH, 1, Geo<DH>::kC) ||
+        !encode_3d(&tmVc, v_cand, F, d.Hkv, DH, 1, Geo<DH>::kC))
       return cudaErrorInvalidValue;
   } else {
     tmKc = tmK;  // never read: no request has candidate tiles

@@ -64,7 +64,7 @@ struct Geo {
   static constexpr uint32_t kOffW = kOffV + kV * kTile;
   static constexpr uint32_t kOffStage = kOffW + kW * 2 * kTile;  // 2 KB per softmax warp
   static constexpr uint32_t kOffSmall = kOffStage + 8 * 2048;
-  static constexpr uint32_t kBytes = kOffSmall + 8192;
+  static constexpr uint32_t kBytes = kOffSmall + 9216;
   // TMEM: O, the S buffers (P in place of S), the queries' hi and lo codes
   static constexpr uint32_t kTmemCols = 512;
   static constexpr uint32_t kSCol = DH;
@@ -94,7 +94,8 @@ struct Small {
   uint64_t s_full[4], p_full[4], pv_done[4];
   uint64_t m_full[2][4];                 // both halves' maxima of an even / odd tile
   uint64_t l_full[4];                    // both groups' sums of an item
-  uint64_t xc_full;                      // the candidate values' maxima of an item
+  uint64_t aux_full[2];                  // sees, vx of an item
+  uint64_t a_full[4];                    // both halves' maxima of the queries
   uint64_t item_full[2], item_empty[2];
   uint64_t q_full, q_free;               // the bf16 query block
   uint64_t qt_full, qt_free;             // the queries' codes in TMEM
@@ -108,9 +109,11 @@ struct Small {
   float l[2][2][kBV];                    // [item parity][half] sums
   int qx[2][kBV];                        // [item parity] the queries' exponents
   int vx[2];                             // [item parity] the exponent of V and O
-  uint32_t xc[2][8];                     // [item parity] candidate maxima, per widening warp
+  uint32_t qmax[2][kBV];                 // [half] largest magnitudes of the queries
+  int2 sees[2][kBV];                     // [item parity] the fed tokens a vector sees, from
+                                         // f_begin on: first, end
 };
-static_assert(sizeof(Small) <= 8192, "the small part of shared memory");
+static_assert(sizeof(Small) <= 9216, "the small part of shared memory");
 
 // D[tmem] (+)= A[tmem] B[smem]^T, e4m3 inputs, f32 accumulation; four A elements per
 // 32-bit TMEM column
@@ -292,12 +295,13 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       mbar_init(&sh.m_full[0][q], 2);
       mbar_init(&sh.m_full[1][q], 2);
       mbar_init(sh.l_full + q, 2);
+      mbar_init(sh.a_full + q, 2);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(sh.item_full + b, 1);
+      mbar_init(sh.aux_full + b, 1);
       mbar_init(sh.item_empty + b, 19);  // producer, two MMA threads, 8 softmax, 8 widening warps
     }
-    mbar_init(&sh.xc_full, 8);
     mbar_init(&sh.q_full, 1);
     mbar_init(&sh.q_free, 9);  // the split's eight warps, the last product with it
     mbar_init(&sh.qt_full, 8);
@@ -328,7 +332,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem;
-  // registers to the softmax warps, which hold a tile's scores: 80 + 2 x 128 + 2 x 72 are
+  // registers to the softmax warps, which hold a tile's scores: 80 + 2 x 112 + 2 x 88 are
   // the five warpgroups' launch share of 96 each
   if (warp < kSoftWarp) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
@@ -371,8 +375,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           if (!live && lane == 0) flag(a.status, JET_ERR_DEVICE);
         }
       }
+      int fed = 0;
       if (lane == 0) {
-        int fed = 0;
         if (live) {
           if (e.nct > 0) {
             // the fed tokens that a row of this block sees: up to its last row's own,
@@ -402,6 +406,43 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
       }
       if (!__shfl_sync(0xffffffffu, live ? 1 : 0, 0)) break;
+      // What the other warps need a little later, and would wait for memory to know: the
+      // fed tokens that each vector sees, and V's unit, the largest exponent of the
+      // item's blocks and of its candidates' values
+      {
+        __syncwarp();
+        const ItemGeo& it = sh.ring[slot].e;
+        fed = __shfl_sync(0xffffffffu, fed, 0);
+        const int f_begin = it.f_begin, blocks = (it.k_end - it.k_begin + kKvBlock - 1) / kKvBlock;
+        if (fed > 0) {
+          for (int i = lane; i < it.nv; i += 32) {
+            const int n = it.n0 + (it.vbase + i) / g;
+            const int c = a.row_cand[n];
+            int from = 0, end = 0;  // none: shared row
+            if (c >= 0 && c < a.C) {
+              from = min(max(a.cand_row_offset[c] - it.r - 1 - f_begin, 0), fed);  // y_{c,1}
+              end = min(n - it.r - f_begin, fed);  // past the row's own fed token
+            }
+            sh.sees[slot][i] = make_int2(from, end);
+          }
+        }
+        const uint8_t* ex = a.v_exp + size_t(kv_place(it.p0, it.r, it.k_begin / kBN)) * a.Hkv + it.kh;
+        int vx = kKvLow + 127;
+        for (int b = lane; b < blocks; b += 32) vx = max(vx, int(ex[size_t(b) * a.Hkv]));
+        uint32_t top = 0;
+        const __nv_bfloat16* vc = a.v_cand + (size_t(f_begin) * a.Hkv + it.kh) * DH;
+#pragma unroll 4
+        for (int i = lane; i < fed * (DH / 8); i += 32) {
+          const uint4 v = *reinterpret_cast<const uint4*>(
+              vc + size_t(i / (DH / 8)) * a.Hkv * DH + 8 * (i % (DH / 8)));
+          top = finite_max_bf16x2(finite_max_bf16x2(top, v.x), v.y);
+          top = finite_max_bf16x2(finite_max_bf16x2(top, v.z), v.w);
+        }
+        vx = __reduce_max_sync(0xffffffffu, max(vx, top ? kv_exponent(top << 16) + 127 : 0));
+        if (lane == 0) sh.vx[slot] = min(max(vx - 127, kKvLow), kKvHigh);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sh.aux_full + slot);
+      }
     }
   } else if (warp == kProdWarp) {
     // ---------------------------------------------------------------- producer
@@ -611,7 +652,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     }
   }
   } else if (warp >= kWideWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     // ---------------------------------------------------------------- queries and V
     const int wi = warp - kWideWarp, q4 = wi & 3, half = wi >> 2;
     const int t = threadIdx.x - kWideWarp * 32;
@@ -622,9 +663,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     constexpr int kPer = kWideThreads / KT, kMine = DH / 16 / kPer;
     const int key = t & (KT - 1), c0 = t / KT;
     const int block = key / kKvBlock;  // of the tile's, the key's: the same for a warp
-    int n_fed = 0;  // items with candidates so far
     bool ok = true;
-    int T = 0;
+    int T = 0, n_q = 0;  // tiles of earlier items; items whose queries this warp split
     for (int u = 0; ok; ++u) {
       const int slot = u & 1;
       if (!warp_mbar_wait(sh.item_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
@@ -634,53 +674,40 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       if (!sh.ring[slot].live) break;
       const ItemGeo e = sh.ring[slot].e;
       const int fed = sh.ring[slot].fed, keys = e.k_end - e.k_begin;
-      // V's unit of this item: the largest exponent of its tiles and of its candidates'
-      // values (the loads fly while the queries are split)
       const uint8_t* ex = a.v_exp + size_t(kv_place(e.p0, e.r, e.k_begin / kBN)) * a.Hkv + e.kh;
       const int blocks = (keys + kKvBlock - 1) / kKvBlock;
       uint32_t byte = block < blocks ? load_ahead(ex + size_t(block) * a.Hkv) : 0;
-      int vx = kKvLow + 127;
-      for (int b = lane; b < blocks; b += 32) vx = max(vx, int(ex[size_t(b) * a.Hkv]));
-      if (fed > 0) {
-        uint32_t top = 0;
-        const __nv_bfloat16* vc = a.v_cand + (size_t(e.f_begin) * a.Hkv + e.kh) * DH;
-        for (int i = t; i < fed * (DH / 8); i += kWideThreads) {
-          const uint4 v = *reinterpret_cast<const uint4*>(
-              vc + size_t(i / (DH / 8)) * a.Hkv * DH + 8 * (i % (DH / 8)));
-          top = finite_max_bf16x2(finite_max_bf16x2(top, v.x), v.y);
-          top = finite_max_bf16x2(finite_max_bf16x2(top, v.z), v.w);
-        }
-        top = __reduce_max_sync(0xffffffffu, top);
-        if (lane == 0) {
-          sh.xc[slot][wi] = top;
-          mbar_arrive(&sh.xc_full);
-        }
-        if (!warp_mbar_wait(&sh.xc_full, n_fed & 1, a.wait_ns, abort_flag)) {
-          ok = false;
-          break;
-        }
-        ++n_fed;
-        vx = max(vx, kv_exponent(__reduce_max_sync(0xffffffffu, sh.xc[slot][lane & 7]) << 16) + 127);
-      }
-      if (lane == 0) sh.bad[slot][wi] = 0;  // item u - 2's output is out (below)
+      if (lane == 0) sh.bad[slot][wi] = 0;
       if (!warp_mbar_wait(&sh.q_full, u & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
-      vx = min(max(__reduce_max_sync(0xffffffffu, vx) - 127, kKvLow), kKvHigh);
-      if (t == 0) sh.vx[slot] = vx;
       if (q4 * 32 < e.nv) {
-        // the row's largest magnitude (NaN and infinities lie above all): rows past the
-        // block's vectors hold what an earlier block left and go unread
-        uint32_t top = 0;
-#pragma unroll 8
-        for (int c = 0; c < DH / 8; ++c) {
+        // the row's largest magnitude (NaN and infinities lie above all), this half's and
+        // the other's: rows past the block's vectors hold what an earlier block left and
+        // go unread
+        constexpr int kMyPieces = DH / 16;  // of eight elements
+        uint32_t mx[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kMyPieces; ++i) {
+          const int c = kMyPieces * half + i;
           const uint4 q = *reinterpret_cast<const uint4*>(smem + (c >> 3) * (kBV * 128) +
                                                           sw128(row, c & 7));
-          top = max_bf16x2_nan(max_bf16x2_nan(top, q.x & 0x7fff7fffu), q.y & 0x7fff7fffu);
-          top = max_bf16x2_nan(max_bf16x2_nan(top, q.z & 0x7fff7fffu), q.w & 0x7fff7fffu);
+          mx[0] = __vmaxu2(mx[0], q.x & 0x7fff7fffu);
+          mx[1] = __vmaxu2(mx[1], q.y & 0x7fff7fffu);
+          mx[2] = __vmaxu2(mx[2], q.z & 0x7fff7fffu);
+          mx[3] = __vmaxu2(mx[3], q.w & 0x7fff7fffu);
         }
-        top = max(top & 0x7fffu, (top >> 16) & 0x7fffu);
+        mx[0] = __vmaxu2(__vmaxu2(mx[0], mx[1]), __vmaxu2(mx[2], mx[3]));
+        sh.qmax[half][row] = max(mx[0] & 0xffffu, mx[0] >> 16);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sh.a_full + q4);
+        if (!warp_mbar_wait(sh.a_full + q4, n_q & 1, a.wait_ns, abort_flag)) {
+          ok = false;
+          break;
+        }
+        ++n_q;
+        const uint32_t top = max(sh.qmax[0][row], sh.qmax[1][row]);
         const bool finite = top < 0x7f80u;
         const int qx = finite ? kv_exponent(top << 16) : 0;
         const float inv = pow2(-qx);
@@ -695,7 +722,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         tc_fence_after();
         // 32 elements at a time: eight columns of four codes
 #pragma unroll 1
-        for (int k32 = half; k32 < DH / 32; k32 += 2) {
+        for (int k32 = DH / 64 * half; k32 < DH / 64 * (half + 1); ++k32) {
           uint32_t hi[8], lo[8];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
@@ -733,14 +760,15 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         mbar_arrive(&sh.qt_full);
         mbar_arrive(&sh.q_free);
       }
+      if (!warp_mbar_wait(sh.aux_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
+        ok = false;
+        break;
+      }
+      const int vx = sh.vx[slot];
       for (int j = 0; j < e.ntiles; ++j) {
         const int Tj = T + j;
         const int s = Tj % NV, w = Tj % NW;
-        // before item u can end, item u - 1's output is out, so that item u + 1 may take
-        // its places (a wait past the end could miss the phase)
-        if ((j == e.ntiles - 1 && u >= 1 &&
-             !warp_mbar_wait(&sh.o_free, (u - 1) & 1, a.wait_ns, abort_flag)) ||
-            !warp_mbar_wait(sh.v_full + s, (Tj / NV) & 1, a.wait_ns, abort_flag) ||
+        if (!warp_mbar_wait(sh.v_full + s, (Tj / NV) & 1, a.wait_ns, abort_flag) ||
             (Tj >= NW && !warp_mbar_wait(sh.pv_done + (Tj - NW) % NS, ((Tj - NW) / NS) & 1,
                                          a.wait_ns, abort_flag))) {
           ok = false;
@@ -794,8 +822,10 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               e4m3x4_to_f16x4(in[q], y[2 * q], y[2 * q + 1]);
-              y[2 * q] = mul_f16x2(y[2 * q], f);
-              y[2 * q + 1] = mul_f16x2(y[2 * q + 1], f);
+            }
+            if (k2 != 0) {
+#pragma unroll
+              for (int q = 0; q < 8; ++q) y[q] = mul_f16x2(y[q], f);
             }
             const int c = c0 + kPer * i;  // pieces 2 c and 2 c + 1 of the f16 row
             uint8_t* to = ws + (c >> 2) * (KT * 128);
@@ -821,7 +851,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       flag(a.status, JET_ERR_TIMEOUT);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 128;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
     // ---------------------------------------------------------------- softmax
     const int q4 = warp & 3, half = (warp - kSoftWarp) >> 2;
     const int i = q4 * 32 + lane;  // query vector within the block = TMEM lane
@@ -840,22 +870,19 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       const int nct = e.nct, ntiles = e.ntiles, keys = e.k_end - e.k_begin, f_begin = e.f_begin;
       const bool valid = i < e.nv;
       const bool some = q4 * 32 < e.nv;  // a warp without vectors only keeps the barriers going
-      int fa = 1, fb = 0;                // fed tokens this vector sees (none: shared row)
-      if (valid && nct > 0) {
-        const int n = e.n0 + (e.vbase + i) / g;
-        const int c = a.row_cand[n];
-        if (c >= 0 && c < a.C) {
-          fa = a.cand_row_offset[c] - e.r - 1;  // y_{c,1}
-          fb = n - e.r - 1;                     // the row's own fed token, inclusive
-        }
+      if (nct > 0 && !warp_mbar_wait(sh.aux_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
+        ok = false;
+        break;
       }
       const uint8_t* ex = a.k_exp + size_t(kv_place(e.p0, e.r, e.k_begin / kBN)) * a.Hkv + e.kh;
       constexpr int kCols = G::kHalf;
       // this half's blocks of the tiles: every tile's (d 256), or every second block
       constexpr int kBlocks = KT / kKvBlock;
-      const int first = kBlocks == 2 ? half : 0;
       const int blocks = (keys + kKvBlock - 1) / kKvBlock;
-      uint32_t byte = first < blocks ? load_ahead(ex + size_t(first) * a.Hkv) : 0;
+      int next = kBlocks == 2 ? half : 0;
+      ex += size_t(next) * a.Hkv;
+      const size_t ex_step = size_t(kBlocks) * a.Hkv;
+      uint32_t byte = next < blocks ? load_ahead(ex) : 0;
       int qx = 0;
       float m = -INFINITY, l = 0.f;  // the running maximum; the sum over this half's columns
       for (int j = 0; j < ntiles; ++j) {
@@ -869,20 +896,26 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.qx_read);
         }
-        // this half's columns [klo, khi) of the tile, and the scores' factor in base 2
+        // the scores' factor in base 2, and this half's columns [klo, khi) of the tile
+        // where not all of them count
         float mul = a.scale_log2;
-        int klo = 0, khi;
+        bool cut = false;
+        int klo = 0, khi = kCols;
         if (j < nct) {
-          const int f0 = f_begin + j * KC;
-          klo = fa - f0;
-          khi = half == 0 ? min(kCols, fb - f0 + 1) : 0;
+          const int2 sees = sh.sees[slot][i];
+          klo = sees.x - j * KC;
+          khi = half == 0 && valid ? sees.y - j * KC : 0;
+          cut = true;
         } else {
           mul *= pow2(min(max(qx + exponent_of(byte), -126), 126));
-          khi = min(kCols, keys - (j - nct) * KT - kCols * half);
-          const int next = (j + 1 - nct) * kBlocks + first;
-          if (next < blocks) byte = load_ahead(ex + size_t(next) * a.Hkv);
+          next += kBlocks;
+          ex += ex_step;
+          if (next < blocks) byte = load_ahead(ex);
+          if (j == ntiles - 1) {
+            khi = keys - (j - nct) * KT - kCols * half;
+            cut = khi < kCols;
+          }
         }
-        const bool cut = __any_sync(0xffffffffu, klo > 0 || khi < kCols);
         if (!warp_mbar_wait(sh.s_full + b, (Tj / NS) & 1, a.wait_ns, abort_flag)) {
           ok = false;
           break;
@@ -986,15 +1019,20 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       l += sh.l[slot][half ^ 1][i];
       const int Tl = T + ntiles - 1;
       const bool direct = e.splits_r == 1;
-      long long dst[4];  // of the vectors this lane stores (8 s + lane / 4, 16 bytes each)
+      char* dst[4];  // of the vectors this lane stores (8 s + lane / 4, 16 bytes each)
+      {
+        char* base = direct ? reinterpret_cast<char*>(a.o) : reinterpret_cast<char*>(a.o_part);
+        const int esize = direct ? 2 : 4;
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const int gi = q4 * 32 + 8 * s + (lane >> 2);
-        dst[s] = -1;
-        if (gi < e.nv) {
-          const int gv = e.vbase + gi;
-          const int n = e.n0 + gv / g, h = e.kh * g + gv % g;
-          dst[s] = (long long)(size_t(direct ? n : e.split * (long long)a.N + n) * a.Hq + h) * DH;
+        for (int s = 0; s < 4; ++s) {
+          const int gi = q4 * 32 + 8 * s + (lane >> 2);
+          dst[s] = nullptr;
+          if (gi < e.nv) {
+            const int gv = e.vbase + gi;
+            const int n = e.n0 + gv / g, h = e.kh * g + gv % g;
+            const size_t row = size_t(direct ? n : e.split * (long long)a.N + n) * a.Hq + h;
+            dst[s] = base + (row * DH + half * (DH / 2)) * esize + (lane & 3) * 16;
+          }
         }
       }
       if (valid && a.splits > 1 && half == 0) {
@@ -1009,7 +1047,13 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           for (int sp = e.splits_r; sp < a.splits; ++sp)
             a.ml_part[at + sp * step] = make_float2(-INFINITY, 0.f);
       }
+      if (!warp_mbar_wait(sh.aux_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
+        ok = false;
+        break;
+      }
       const float inv = l > 0.f ? 1.f / l : 0.f, unit = pow2(sh.vx[slot]);
+      // 1 / l and V's unit in one factor, unless the factor would not be a normal number
+      const bool plain = __all_sync(0xffffffffu, fabsf(inv * unit) > 0x1p-100f) != 0;
       if (!warp_mbar_wait(sh.pv_done + Tl % NS, (Tl / NS) & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
@@ -1023,29 +1067,46 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
         // 64 bytes of each vector at a time through this warp's 2 KB stage: four 16-byte
         // pieces a row, rotated so that eight lanes meet different banks
-        auto put = [&](const uint4(&x)[4], char* base, size_t esize, int col) {
+        auto put = [&](const uint4(&x)[4]) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) stage[lane * 4 + (q ^ ((lane >> 1) & 3))] = x[q];
           __syncwarp();
+          uint4 val[4];
 #pragma unroll
           for (int s = 0; s < 4; ++s) {
             const int iv = 8 * s + (lane >> 2), c = lane & 3;
-            const uint4 val = stage[iv * 4 + (c ^ ((iv >> 1) & 3))];
-            if (dst[s] >= 0)
-              *reinterpret_cast<uint4*>(base + (dst[s] + col) * esize + c * 16) = val;
+            val[s] = stage[iv * 4 + (c ^ ((iv >> 1) & 3))];
+          }
+#pragma unroll
+          for (int s = 0; s < 4; ++s) {
+            if (dst[s]) {
+              *reinterpret_cast<uint4*>(dst[s]) = val[s];
+              dst[s] += 64;
+            }
           }
           __syncwarp();
         };
         // each of a row's two warps writes half of the columns
+        const float2 scale = make_float2(inv * (plain ? unit : 1.f), inv * (plain ? unit : 1.f));
+        const float2 zero = make_float2(0.f, 0.f);
 #pragma unroll 1
         for (int c0 = half * (DH / 2); c0 < (half + 1) * (DH / 2); c0 += 32) {
           float ov[32];
           tmem_ld_32cols(tmem + lane_off + c0, ov);
           tmem_wait_ld();
 #pragma unroll
-          for (int c = 0; c < 32; ++c) ov[c] = ov[c] * inv * unit;
+          for (int c = 0; c < 32; c += 2) {
+            const float2 y = fma2(make_float2(ov[c], ov[c + 1]), scale, zero);
+            ov[c] = y.x;
+            ov[c + 1] = y.y;
+          }
+          if (!plain) {
+#pragma unroll
+            for (int c = 0; c < 32; ++c) ov[c] *= unit;
+          }
           if (bad) {  // the non-finite values of the tokens this row sees
-            for (int f = max(fa, f_begin); f <= fb; ++f) {
+            const int2 sees = sh.sees[slot][i];
+            for (int f = f_begin + sees.x; f < f_begin + sees.y; ++f) {
               const __nv_bfloat16* v = a.v_cand + (size_t(f) * a.Hkv + e.kh) * DH + c0;
 #pragma unroll
               for (int c = 0; c < 32; ++c) {
@@ -1062,7 +1123,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
               x[q] = make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]),
                                 pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
             }
-            put(x, reinterpret_cast<char*>(a.o), 2, c0);
+            put(x);
           } else {
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -1073,7 +1134,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 x[q] = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]),
                                   __float_as_uint(y[2]), __float_as_uint(y[3]));
               }
-              put(x, reinterpret_cast<char*>(a.o_part), 4, c0 + 16 * k);
+              put(x);
             }
           }
         }

@@ -396,7 +396,22 @@ AttnPlan attn_plan(const jet_sizes& n, const jet_dims& d) {
   return p;
 }
 
-AttnPlan attn_plan_kv8(const jet_sizes& n, const jet_dims& d) { return attn_plan(n, d); }
+AttnPlan attn_plan_kv8(const jet_sizes& n, const jet_dims& d) {
+  AttnPlan p = attn_plan(n, d);
+  p.copies = 1;
+  if (d.dtype != JET_DTYPE_BF16 || n.R <= 0 || n.N <= 0) return p;
+  // Few query vectors leave softmax warps without any. Then a block holds its vectors two
+  // or four times over, and each copy takes its part of a tile's keys: the copies leave
+  // partials that the combine joins like chunks.
+  const int vecs = n.max_rows * (d.Hq / d.Hkv);
+  if (vecs <= 32) p.copies = 4;
+  else if (vecs <= 64) p.copies = 2;
+  if (p.copies > 1) {
+    const size_t v = size_t(p.splits) * n.N * d.Hq;
+    p.bytes += (p.copies - 1) * v * (d.d * sizeof(float) + sizeof(float2));
+  }
+  return p;
+}
 
 cudaError_t launch_prefix_attend_kv8(const jet_layout& lay, const jet_dims& d,
                                      const AttnPlan& plan, const void* q, const void* k8,

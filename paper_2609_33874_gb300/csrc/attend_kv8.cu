@@ -56,11 +56,12 @@ struct Geo {
   static constexpr int kHalf = kT / 2;                    // columns of a softmax warp
   static constexpr int kC = kT / 2;                       // candidate tokens per tile
   static constexpr uint32_t kTile = kT * DH;              // bytes of a K or V tile
-  static constexpr int kS = DH == 64 ? 3 : 2;             // S buffers, and K tiles in flight
+  static constexpr int kS = DH == 64 ? 3 : 2;             // S buffers
+  static constexpr int kK = DH == 256 ? 2 : DH == 128 ? 3 : 4;  // K tiles in flight
   static constexpr int kV = DH == 256 ? 2 : DH == 128 ? 3 : 6;  // V tiles in flight
   static constexpr int kW = 2;                            // widened V tiles
   static constexpr uint32_t kOffK = kBV * DH * 2;         // after the bf16 query block
-  static constexpr uint32_t kOffV = kOffK + kS * kTile;
+  static constexpr uint32_t kOffV = kOffK + kK * kTile;
   static constexpr uint32_t kOffW = kOffV + kV * kTile;
   static constexpr uint32_t kOffStage = kOffW + kW * 2 * kTile;  // 2 KB per softmax warp
   static constexpr uint32_t kOffSmall = kOffStage + 8 * 2048;
@@ -89,7 +90,7 @@ struct __align__(16) KvItem {
 
 struct Small {
   KvItem ring[2];
-  uint64_t k_full[4], v_full[6], v_empty[6];
+  uint64_t k_full[6], k_empty[6], v_full[6], v_empty[6];
   uint64_t w_full[2];                    // widened V tiles
   uint64_t s_full[4], p_full[4], pv_done[4];
   uint64_t m_full[2][4];                 // both halves' maxima of an even / odd tile
@@ -160,6 +161,40 @@ __device__ __forceinline__ void tmem_st_8cols_u32(uint32_t taddr, const uint32_t
       "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
       "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
       : "memory");
+}
+
+// and 4 columns
+__device__ __forceinline__ void tmem_st_4cols_u32(uint32_t taddr, const uint32_t (&v)[4]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr),
+               "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
+               : "memory");
+}
+
+template <int N>
+__device__ __forceinline__ void tmem_st_cols(uint32_t taddr, const uint32_t (&v)[N]) {
+  if constexpr (N == 16) tmem_st_16cols_u32(taddr, v);
+  if constexpr (N == 8) tmem_st_8cols_u32(taddr, v);
+  if constexpr (N == 4) tmem_st_4cols_u32(taddr, v);
+}
+
+// 8 consecutive f32 columns of this warp's 32 TMEM lanes
+__device__ __forceinline__ void tmem_ld_8cols(uint32_t taddr, float (&v)[8]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]),
+        "=f"(v[7])
+      : "r"(taddr));
+}
+
+template <int N>
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, float (&v)[N]) {
+  if constexpr (N == 64) {
+    tmem_ld_32cols(taddr, *reinterpret_cast<float(*)[32]>(v));
+    tmem_ld_32cols(taddr + 32, *reinterpret_cast<float(*)[32]>(v + 32));
+  }
+  if constexpr (N == 32) tmem_ld_32cols(taddr, v);
+  if constexpr (N == 16) tmem_ld_16cols(taddr, v);
+  if constexpr (N == 8) tmem_ld_8cols(taddr, v);
 }
 
 // the codes of a word's two halves as f16 numbers, and two f16 numbers' nearest codes
@@ -265,13 +300,14 @@ __device__ __forceinline__ uint32_t finite_max_bf16x2(uint32_t top, uint32_t w) 
   return max(top, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
 }
 
-template <int DH>
+template <int DH, int R>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                   const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmKc,
                   const __grid_constant__ CUtensorMap tmVc, const Kv8Args a) {
   using G = Geo<DH>;
-  constexpr int NV = G::kV, NW = G::kW, NS = G::kS, KT = G::kT, KC = G::kC;
+  constexpr int NK = G::kK, NV = G::kV, NW = G::kW, NS = G::kS, KT = G::kT, KC = G::kC;
+  constexpr int RV = kBV / R;  // vectors of an item; R copies of them fill the lanes
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
@@ -280,13 +316,16 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = a.g, rb = a.rb;
   if (threadIdx.x == 0) {
+    for (int s = 0; s < NK; ++s) {
+      mbar_init(sh.k_full + s, 1);
+      mbar_init(sh.k_empty + s, 1);
+    }
     for (int s = 0; s < NV; ++s) {
       mbar_init(sh.v_full + s, 1);
       mbar_init(sh.v_empty + s, 8);
     }
     for (int s = 0; s < NW; ++s) mbar_init(sh.w_full + s, 8);
     for (int b = 0; b < NS; ++b) {
-      mbar_init(sh.k_full + b, 1);
       mbar_init(sh.s_full + b, 1);
       mbar_init(sh.p_full + b, 8);
       mbar_init(sh.pv_done + b, 1);
@@ -467,21 +506,22 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           bool progressed = false;
           if (!q_sent && (u == 0 || mbar_test(&sh.q_free, (u - 1) & 1))) {
             if (!(u == 0 && a.hold_first)) {  // test hook: the first block never lands
-              mbar_arrive_expect_tx(&sh.q_full, uint32_t(DH / 64) * 64 * 2 * g * rb);
+              mbar_arrive_expect_tx(&sh.q_full, uint32_t(R * (DH / 64)) * 64 * 2 * g * rb);
 #pragma unroll
-              for (int sl = 0; sl < DH / 64; ++sl)
-                tma_load_3d(smem + sl * (kBV * 128), &tmQ, &sh.q_full, sl * 64, e.kh * g,
-                            e.n0 + e.row0, pol);
+              for (int c = 0; c < R; ++c)
+#pragma unroll
+                for (int sl = 0; sl < DH / 64; ++sl)
+                  tma_load_3d(smem + sl * (kBV * 128) + c * RV * 128, &tmQ, &sh.q_full, sl * 64,
+                              e.kh * g, e.n0 + e.row0, pol);
               q_issued = 1;
               q_par = u & 1;
             }
             q_sent = progressed = true;
           }
           if (jk < e.ntiles) {
-            // (a K tile's place is free when its scores are there)
-            const int s = (T + jk) % NS;
-            const uint32_t ph = ((T + jk) / NS) & 1;
-            if (mbar_test(sh.s_full + s, ph ^ 1u)) {
+            const int s = (T + jk) % NK;
+            const uint32_t ph = ((T + jk) / NK) & 1;
+            if (mbar_test(sh.k_empty + s, ph ^ 1u)) {
               uint8_t* ks = smem + G::kOffK + s * G::kTile;
               mbar_arrive_expect_tx(sh.k_full + s, G::kTile);
               if (jk < e.nct) {
@@ -539,7 +579,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         flag(a.status, JET_ERR_TIMEOUT);
         // let every copy already issued land before the CTA can exit
         if (q_issued) mbar_wait(&sh.q_full, q_par, kDrainNs, nullptr);
-        for (int t = 0; t < NS; ++t)
+        for (int t = 0; t < NK; ++t)
           if (k_issued & (1u << t)) mbar_wait(sh.k_full + t, (k_par >> t) & 1u, kDrainNs, nullptr);
         for (int t = 0; t < NV; ++t)
           if (v_issued & (1u << t)) mbar_wait(sh.v_full + t, (v_par >> t) & 1u, kDrainNs, nullptr);
@@ -563,13 +603,13 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         const int nct = sh.ring[slot].e.nct, ntiles = sh.ring[slot].e.ntiles;
         if (nct == 0) mbar_arrive(&sh.q_free);  // only the split reads the bf16 block
         for (int j = 0; j < ntiles; ++j) {
-          const int Tj = T + j, b = Tj % NS;
+          const int Tj = T + j, b = Tj % NS, kb = Tj % NK;
           ok = (j > 0 && j != nct) || wait(j < nct ? &sh.q_full : &sh.qt_full, u & 1);
-          ok = ok && wait(sh.k_full + b, (Tj / NS) & 1) &&
+          ok = ok && wait(sh.k_full + kb, (Tj / NK) & 1) &&
                wait(sh.pv_done + b, ((Tj / NS) & 1) ^ 1u);
           if (!ok) break;
           tc_fence_after();
-          const uint32_t ks = smem_u32(smem + G::kOffK + b * G::kTile);
+          const uint32_t ks = smem_u32(smem + G::kOffK + kb * G::kTile);
           const uint32_t d = tmem + G::kSCol + b * KT;
           if (j < nct) {
 #pragma unroll
@@ -590,6 +630,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             }
           }
           mma_commit(sh.s_full + b);
+          mma_commit(sh.k_empty + kb);
           if (j == ntiles - 1) mma_commit(&sh.qt_free);
         }
         if (!ok) break;
@@ -682,7 +723,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         ok = false;
         break;
       }
-      if (q4 * 32 < e.nv) {
+      if (q4 * 32 % RV < e.nv) {
         // the row's largest magnitude (NaN and infinities lie above all), this half's and
         // the other's: rows past the block's vectors hold what an earlier block left and
         // go unread
@@ -854,7 +895,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     asm volatile("setmaxnreg.inc.sync.aligned.u32 112;");
     // ---------------------------------------------------------------- softmax
     const int q4 = warp & 3, half = (warp - kSoftWarp) >> 2;
-    const int i = q4 * 32 + lane;  // query vector within the block = TMEM lane
+    // the query vector of this TMEM lane, and which of its copies
+    const int i = q4 * 32 % RV + lane, copy = q4 * 32 / RV;
     const uint32_t lane_off = uint32_t(q4 * 32) << 16;
     uint4* stage = reinterpret_cast<uint4*>(smem + G::kOffStage + (warp - kSoftWarp) * 2048);
     bool ok = true;
@@ -869,13 +911,14 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       const ItemGeo& e = sh.ring[slot].e;  // (read again where needed: registers are few)
       const int nct = e.nct, ntiles = e.ntiles, keys = e.k_end - e.k_begin, f_begin = e.f_begin;
       const bool valid = i < e.nv;
-      const bool some = q4 * 32 < e.nv;  // a warp without vectors only keeps the barriers going
+      const bool some = q4 * 32 % RV < e.nv;  // a warp without vectors only keeps the barriers going
       if (nct > 0 && !warp_mbar_wait(sh.aux_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
       const uint8_t* ex = a.k_exp + size_t(kv_place(e.p0, e.r, e.k_begin / kBN)) * a.Hkv + e.kh;
-      constexpr int kCols = G::kHalf;
+      constexpr int kCols = G::kHalf / R;
+      const int col0 = kCols * copy;  // of this half's
       // this half's blocks of the tiles: every tile's (d 256), or every second block
       constexpr int kBlocks = KT / kKvBlock;
       const int blocks = (keys + kKvBlock - 1) / kKvBlock;
@@ -892,7 +935,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             ok = false;
             break;
           }
-          qx = sh.qx[slot][i];
+          qx = sh.qx[slot][q4 * 32 + lane];
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.qx_read);
         }
@@ -903,8 +946,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         int klo = 0, khi = kCols;
         if (j < nct) {
           const int2 sees = sh.sees[slot][i];
-          klo = sees.x - j * KC;
-          khi = half == 0 && valid ? sees.y - j * KC : 0;
+          klo = sees.x - j * KC - col0;
+          khi = half == 0 && valid ? sees.y - j * KC - col0 : 0;
           cut = true;
         } else {
           mul *= pow2(min(max(qx + exponent_of(byte), -126), 126));
@@ -912,7 +955,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           ex += ex_step;
           if (next < blocks) byte = load_ahead(ex);
           if (j == ntiles - 1) {
-            khi = keys - (j - nct) * KT - kCols * half;
+            khi = keys - (j - nct) * KT - G::kHalf * half - col0;
             cut = khi < kCols;
           }
         }
@@ -923,10 +966,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         tc_fence_after();
         if (some) {
           float sv[kCols];
-#pragma unroll
-          for (int k = 0; k < kCols / 32; ++k)
-            tmem_ld_32cols(tmem + lane_off + G::kSCol + b * KT + kCols * half + 32 * k,
-                           *reinterpret_cast<float(*)[32]>(sv + 32 * k));
+          tmem_ld_cols(tmem + lane_off + G::kSCol + b * KT + G::kHalf * half + col0, sv);
           tmem_wait_ld();
           if (cut) {
 #pragma unroll
@@ -943,14 +983,14 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           float mt = max3(mq[0], mq[1], fmaxf(mq[2], mq[3]));
           mt *= mul;
           // the other half's: then both know the row's maximum over the tile
-          sh.m[x & 1][half][i] = mt;
+          sh.m[x & 1][half][q4 * 32 + lane] = mt;
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.m_full[x & 1][q4]);
           if (!warp_mbar_wait(&sh.m_full[x & 1][q4], (x >> 1) & 1, a.wait_ns, abort_flag)) {
             ok = false;
             break;
           }
-          mt = fmaxf(mt, sh.m[x & 1][half ^ 1][i]);
+          mt = fmaxf(mt, sh.m[x & 1][half ^ 1][q4 * 32 + lane]);
           ++x;
           const bool grow = j == 0 || (valid && mt > m + kRescaleLog2);
           if (__any_sync(0xffffffffu, grow)) {
@@ -985,19 +1025,29 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           float2 ps[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) ps[q] = make_float2(0.f, 0.f);
-          // P takes the place of scores that are in registers by now
+          // P takes the place of scores that are in registers by now; where the vectors are
+          // there R times, each copy has weights in its own columns and zeros in the others'
+          constexpr int kWords = G::kHalf / 2;
+          const uint32_t pt = tmem + lane_off + G::kSCol + b * KT + kWords * half;
+          if constexpr (R > 1) {
+            const uint32_t zeros[16] = {};
 #pragma unroll
-          for (int k = 0; k < kCols / 32; ++k) {
-            uint32_t pw[16];
+            for (int k = 0; k < kWords; k += 16) tmem_st_16cols_u32(pt + k, zeros);
+            tmem_wait_st();
+          }
+          constexpr int kStep = kCols / 2 < 16 ? kCols / 2 : 16;
 #pragma unroll
-            for (int c = 0; c < 16; ++c) {
-              const int at = 32 * k + 2 * c;
+          for (int k = 0; k < kCols / 2; k += kStep) {
+            uint32_t pw[kStep];
+#pragma unroll
+            for (int c = 0; c < kStep; ++c) {
+              const int at = 2 * (k + c);
               const float2 y = fma2(make_float2(sv[at], sv[at + 1]), mul2, sub2);
               const float2 p = make_float2(ex2(y.x), ex2(y.y));
               ps[c & 3] = add2(ps[c & 3], p);
               pw[c] = pack_f16(p.x, p.y);
             }
-            tmem_st_16cols_u32(tmem + lane_off + G::kSCol + b * KT + kCols / 2 * half + 16 * k, pw);
+            tmem_st_cols(pt + col0 / 2 + k, pw);
           }
           const float2 p = add2(add2(ps[0], ps[1]), add2(ps[2], ps[3]));
           l += p.x + p.y;
@@ -1009,42 +1059,43 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       }
       if (!ok) break;
       // both halves' sums
-      sh.l[slot][half][i] = l;
+      sh.l[slot][half][q4 * 32 + lane] = l;
       __syncwarp();
       if (lane == 0) mbar_arrive(sh.l_full + q4);
       if (!warp_mbar_wait(sh.l_full + q4, u & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
-      l += sh.l[slot][half ^ 1][i];
+      l += sh.l[slot][half ^ 1][q4 * 32 + lane];
       const int Tl = T + ntiles - 1;
-      const bool direct = e.splits_r == 1;
+      const bool direct = R == 1 && e.splits_r == 1;
+      const int part = e.split * R + copy;  // the partial that is written
       char* dst[4];  // of the vectors this lane stores (8 s + lane / 4, 16 bytes each)
       {
         char* base = direct ? reinterpret_cast<char*>(a.o) : reinterpret_cast<char*>(a.o_part);
         const int esize = direct ? 2 : 4;
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-          const int gi = q4 * 32 + 8 * s + (lane >> 2);
+          const int gi = q4 * 32 % RV + 8 * s + (lane >> 2);
           dst[s] = nullptr;
           if (gi < e.nv) {
             const int gv = e.vbase + gi;
             const int n = e.n0 + gv / g, h = e.kh * g + gv % g;
-            const size_t row = size_t(direct ? n : e.split * (long long)a.N + n) * a.Hq + h;
+            const size_t row = size_t(direct ? n : part * (long long)a.N + n) * a.Hq + h;
             dst[s] = base + (row * DH + half * (DH / 2)) * esize + (lane & 3) * 16;
           }
         }
       }
-      if (valid && a.splits > 1 && half == 0) {
+      if (valid && a.splits * R > 1 && half == 0) {
         // as the bf16 kernel leaves them for the combine, but with the partial divided by
         // its sum (l 1, the sum in m), as a sum of large values may pass float32
         const int gv = e.vbase + i;
         const size_t at = size_t(e.n0 + gv / g) * a.Hq + e.kh * g + gv % g;
         const size_t step = size_t(a.N) * a.Hq;
-        a.ml_part[at + (direct ? 0 : e.split * step)] =
+        a.ml_part[at + (direct ? 0 : part * step)] =
             direct ? make_float2(0.f, -1.f) : make_float2(m + log2f(l), l > 0.f ? 1.f : l);
-        if (!direct && e.split == e.splits_r - 1)
-          for (int sp = e.splits_r; sp < a.splits; ++sp)
+        if (!direct && part == e.splits_r * R - 1)
+          for (int sp = e.splits_r * R; sp < a.splits * R; ++sp)
             a.ml_part[at + sp * step] = make_float2(-INFINITY, 0.f);
       }
       if (!warp_mbar_wait(sh.aux_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
@@ -1176,16 +1227,16 @@ bool encode_codes(CUtensorMap* map, const void* base, int rows, int heads, int D
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int DH>
+template <int DH, int R>
 cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& plan,
                       const void* q, const void* k8, const void* v8, const void* k_cand,
                       const void* v_cand, void* o, void* ws, int* status, cudaStream_t st) {
   const jet_sizes& n = lay.n;
   const int F = n.N - n.R;
   const int g = d.Hq / d.Hkv;
-  if (g > kBV) return cudaErrorInvalidValue;
+  if (g > kBV / R) return cudaErrorInvalidValue;
   CUtensorMap tmQ, tmK, tmV, tmKc, tmVc;
-  if (!encode_3d(&tmQ, q, n.N, d.Hq, DH, g, kBV / g) ||
+  if (!encode_3d(&tmQ, q, n.N, d.Hq, DH, g, kBV / R / g) ||
       !encode_codes(&tmK, k8, n.total_prefix, d.Hkv, DH, Geo<DH>::kT) ||
       !encode_codes(&tmV, v8, n.total_prefix, d.Hkv, DH, Geo<DH>::kT))
     return cudaErrorInvalidValue;
@@ -1197,7 +1248,7 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
     tmKc = tmK;  // never read: no request has candidate tiles
     tmVc = tmV;
   }
-  const size_t vecs = size_t(plan.splits) * n.N * d.Hq;
+  const size_t vecs = size_t(plan.splits) * R * n.N * d.Hq;
   const size_t exp_off = kv_size(n, d).exp_off;
   Kv8Args a{};
   a.wait_ns = wait_budget_ns();
@@ -1219,7 +1270,7 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
   a.Hkv = d.Hkv;
   a.chunk = plan.chunk;
   a.g = g;
-  a.rb = kBV / g;
+  a.rb = kBV / R / g;
   a.has_cand = F > 0;
   a.scale_log2 = 1.4426950408889634f / sqrtf(float(DH));
   a.k_exp = static_cast<const uint8_t*>(k8) + exp_off;
@@ -1244,15 +1295,15 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
                    plan.qgroups, plan.splits);
   if (e != cudaSuccess) return e;
   const size_t smem = Geo<DH>::kBytes + 1024;
-  e = cudaFuncSetAttribute(attend_kv8_kernel<DH>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  e = cudaFuncSetAttribute(attend_kv8_kernel<DH, R>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            int(smem));
   if (e != cudaSuccess) return e;
-  e = launch_pdl(attend_kv8_kernel<DH>, dim3(grid), dim3(kThreads), smem, st, tmQ, tmK, tmV, tmKc,
+  e = launch_pdl(attend_kv8_kernel<DH, R>, dim3(grid), dim3(kThreads), smem, st, tmQ, tmK, tmV, tmKc,
                  tmVc, a);
-  if (e != cudaSuccess || plan.splits <= 1) return e;
+  if (e != cudaSuccess || plan.splits * R <= 1) return e;
   const long long blocks = ((long long)n.N * d.Hq + 3) / 4;
   return launch_pdl(attend_combine_kernel<DH>, dim3(unsigned(blocks)), dim3(128), 0, st,
-                    lay.row_req, n.N, n.R, d.Hq, plan.splits, blocks <= 8LL * sms, a.o_part,
+                    lay.row_req, n.N, n.R, d.Hq, plan.splits * R, blocks <= 8LL * sms, a.o_part,
                     a.ml_part, a.o, status);
 }
 
@@ -1262,11 +1313,18 @@ cudaError_t launch_attend_kv8_tc(const jet_layout& lay, const jet_dims& d, const
                                  const void* q, const void* k8, const void* v8,
                                  const void* k_cand, const void* v_cand, void* o, void* ws,
                                  int* status, cudaStream_t st) {
-#define JET_KV8(DH) \
-  return launch_dh<DH>(lay, d, plan, q, k8, v8, k_cand, v_cand, o, ws, status, st)
-  if (d.d == 64) JET_KV8(64);
-  if (d.d == 128) JET_KV8(128);
-  if (d.d == 256) JET_KV8(256);
+#define JET_KV8(DH, R)                                                                     \
+  if (d.d == DH && plan.copies == R)                                                       \
+  return launch_dh<DH, R>(lay, d, plan, q, k8, v8, k_cand, v_cand, o, ws, status, st)
+  JET_KV8(64, 1);
+  JET_KV8(64, 2);
+  JET_KV8(64, 4);
+  JET_KV8(128, 1);
+  JET_KV8(128, 2);
+  JET_KV8(128, 4);
+  JET_KV8(256, 1);
+  JET_KV8(256, 2);
+  JET_KV8(256, 4);
 #undef JET_KV8
   return cudaErrorInvalidValue;
 }

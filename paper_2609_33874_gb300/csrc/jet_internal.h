@@ -31,6 +31,7 @@ struct AttnPlan {
   int chunk;     // prefix keys per chunk (multiple of 32)
   int qgroups;   // query-vector groups per (request, key/value head)
   bool sorted;   // tensor-core path: items from a longest-first work list
+  int copies;    // 8-bit cache: how often a query block holds its vectors (1, 2 or 4)
   size_t bytes;  // workspace bytes
 };
 AttnPlan attn_plan(const jet_sizes& n, const jet_dims& d);

@@ -116,6 +116,28 @@ struct Small {
 };
 static_assert(sizeof(Small) <= 9216, "the small part of shared memory");
 
+// The bounded waits of this kernel, in few instructions: two dozen of them stand between
+// the roles' working code, which the instruction caches barely hold. (try_wait itself
+// sleeps for a while, so the clock is read seldom enough.)
+__device__ __forceinline__ bool poll(uint64_t* bar, uint32_t parity, uint64_t budget_ns,
+                                     volatile int* abort) {
+  const uint64_t t0 = global_timer_ns();
+#pragma unroll 1
+  while (!mbar_try_wait(bar, parity))
+    if (*abort || global_timer_ns() - t0 > budget_ns) return false;
+  return true;
+}
+__device__ __forceinline__ bool wait1(uint64_t* bar, uint32_t parity, uint64_t budget_ns,
+                                      volatile int* abort) {
+  return mbar_try_wait(bar, parity) || poll(bar, parity, budget_ns, abort);
+}
+// by every lane of a warp, with one outcome for the whole warp
+__device__ __forceinline__ bool wait32(uint64_t* bar, uint32_t parity, uint64_t budget_ns,
+                                       volatile int* abort) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, poll(bar, parity, budget_ns, abort));
+}
+
 // D[tmem] (+)= A[tmem] B[smem]^T, e4m3 inputs, f32 accumulation; four A elements per
 // 32-bit TMEM column
 __device__ __forceinline__ void mma_e4m3_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc,
@@ -381,7 +403,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     ItemWindow window{};
     for (int u = 0;; ++u) {
       const int slot = u & 1;
-      if (!warp_mbar_wait(sh.item_empty + slot, ((u >> 1) & 1) ^ 1u, a.wait_ns, abort_flag)) {
+      if (!wait32(sh.item_empty + slot, ((u >> 1) & 1) ^ 1u, a.wait_ns, abort_flag)) {
         if (lane == 0) {
           sh.abort = 1;
           flag(a.status, JET_ERR_TIMEOUT);
@@ -492,7 +514,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       bool ok = true;
       for (int u = 0; ok; ++u) {
         const int slot = u & 1;
-        if (!mbar_wait(sh.item_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
+        if (!wait1(sh.item_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
           ok = false;
           break;
         }
@@ -592,7 +614,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       constexpr uint32_t id_c = idesc_bf16_f32(kBV, KC);
       const uint32_t qs = smem_u32(smem);
       auto wait = [&](uint64_t* bar, uint32_t parity) {
-        return mbar_wait(bar, parity, a.wait_ns, abort_flag);
+        return wait1(bar, parity, a.wait_ns, abort_flag);
       };
       bool ok = true;
       int T = 0;
@@ -649,7 +671,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     if (elect_one()) {
       constexpr uint32_t id_o = idesc_f16_f32_mn(kBV, DH);
       auto wait = [&](uint64_t* bar, uint32_t parity) {
-        return mbar_wait(bar, parity, a.wait_ns, abort_flag);
+        return wait1(bar, parity, a.wait_ns, abort_flag);
       };
       bool ok = true;
       int T = 0;
@@ -708,7 +730,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     int T = 0, n_q = 0;  // tiles of earlier items; items whose queries this warp split
     for (int u = 0; ok; ++u) {
       const int slot = u & 1;
-      if (!warp_mbar_wait(sh.item_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
+      if (!wait32(sh.item_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
@@ -719,7 +741,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       const int blocks = (keys + kKvBlock - 1) / kKvBlock;
       uint32_t byte = block < blocks ? load_ahead(ex + size_t(block) * a.Hkv) : 0;
       if (lane == 0) sh.bad[slot][wi] = 0;
-      if (!warp_mbar_wait(&sh.q_full, u & 1, a.wait_ns, abort_flag)) {
+      if (!wait32(&sh.q_full, u & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
@@ -743,7 +765,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         sh.qmax[half][row] = max(mx[0] & 0xffffu, mx[0] >> 16);
         __syncwarp();
         if (lane == 0) mbar_arrive(sh.a_full + q4);
-        if (!warp_mbar_wait(sh.a_full + q4, n_q & 1, a.wait_ns, abort_flag)) {
+        if (!wait32(sh.a_full + q4, n_q & 1, a.wait_ns, abort_flag)) {
           ok = false;
           break;
         }
@@ -754,8 +776,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         const float inv = pow2(-qx);
         // the codes of the item before are read by its last product with the keys; a
         // softmax warp must not find qt_full two items on
-        if (u >= 1 && (!warp_mbar_wait(&sh.qt_free, (u - 1) & 1, a.wait_ns, abort_flag) ||
-                       !warp_mbar_wait(&sh.qx_read, (u - 1) & 1, a.wait_ns, abort_flag))) {
+        if (u >= 1 && (!wait32(&sh.qt_free, (u - 1) & 1, a.wait_ns, abort_flag) ||
+                       !wait32(&sh.qx_read, (u - 1) & 1, a.wait_ns, abort_flag))) {
           ok = false;
           break;
         }
@@ -791,8 +813,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
         tmem_wait_st();
         tc_fence_before();
-      } else if (u >= 1 && (!warp_mbar_wait(&sh.qt_free, (u - 1) & 1, a.wait_ns, abort_flag) ||
-                            !warp_mbar_wait(&sh.qx_read, (u - 1) & 1, a.wait_ns, abort_flag))) {
+      } else if (u >= 1 && (!wait32(&sh.qt_free, (u - 1) & 1, a.wait_ns, abort_flag) ||
+                            !wait32(&sh.qx_read, (u - 1) & 1, a.wait_ns, abort_flag))) {
         ok = false;
         break;
       }
@@ -801,7 +823,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         mbar_arrive(&sh.qt_full);
         mbar_arrive(&sh.q_free);
       }
-      if (!warp_mbar_wait(sh.aux_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
+      if (!wait32(sh.aux_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
@@ -809,8 +831,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       for (int j = 0; j < e.ntiles; ++j) {
         const int Tj = T + j;
         const int s = Tj % NV, w = Tj % NW;
-        if (!warp_mbar_wait(sh.v_full + s, (Tj / NV) & 1, a.wait_ns, abort_flag) ||
-            (Tj >= NW && !warp_mbar_wait(sh.pv_done + (Tj - NW) % NS, ((Tj - NW) / NS) & 1,
+        if (!wait32(sh.v_full + s, (Tj / NV) & 1, a.wait_ns, abort_flag) ||
+            (Tj >= NW && !wait32(sh.pv_done + (Tj - NW) % NS, ((Tj - NW) / NS) & 1,
                                          a.wait_ns, abort_flag))) {
           ok = false;
           break;
@@ -903,7 +925,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     int T = 0, x = 0;  // tiles of earlier items; tiles that this warp has worked on
     for (int u = 0; ok; ++u) {
       const int slot = u & 1;
-      if (!warp_mbar_wait(sh.item_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
+      if (!wait32(sh.item_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
@@ -912,7 +934,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       const int nct = e.nct, ntiles = e.ntiles, keys = e.k_end - e.k_begin, f_begin = e.f_begin;
       const bool valid = i < e.nv;
       const bool some = q4 * 32 % RV < e.nv;  // a warp without vectors only keeps the barriers going
-      if (nct > 0 && !warp_mbar_wait(sh.aux_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
+      if (nct > 0 && !wait32(sh.aux_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
@@ -931,7 +953,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       for (int j = 0; j < ntiles; ++j) {
         const int Tj = T + j, b = Tj % NS;
         if (j == nct) {
-          if (!warp_mbar_wait(&sh.qt_full, u & 1, a.wait_ns, abort_flag)) {
+          if (!wait32(&sh.qt_full, u & 1, a.wait_ns, abort_flag)) {
             ok = false;
             break;
           }
@@ -959,7 +981,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             cut = khi < kCols;
           }
         }
-        if (!warp_mbar_wait(sh.s_full + b, (Tj / NS) & 1, a.wait_ns, abort_flag)) {
+        if (!wait32(sh.s_full + b, (Tj / NS) & 1, a.wait_ns, abort_flag)) {
           ok = false;
           break;
         }
@@ -986,7 +1008,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           sh.m[x & 1][half][q4 * 32 + lane] = mt;
           __syncwarp();
           if (lane == 0) mbar_arrive(&sh.m_full[x & 1][q4]);
-          if (!warp_mbar_wait(&sh.m_full[x & 1][q4], (x >> 1) & 1, a.wait_ns, abort_flag)) {
+          if (!wait32(&sh.m_full[x & 1][q4], (x >> 1) & 1, a.wait_ns, abort_flag)) {
             ok = false;
             break;
           }
@@ -998,7 +1020,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             if (j > 0) {
               // O holds this item's P V so far: wait for the last one, rescale this half of
               // its columns in TMEM
-              if (!warp_mbar_wait(sh.pv_done + (Tj - 1) % NS, ((Tj - 1) / NS) & 1, a.wait_ns,
+              if (!wait32(sh.pv_done + (Tj - 1) % NS, ((Tj - 1) / NS) & 1, a.wait_ns,
                                   abort_flag)) {
                 ok = false;
                 break;
@@ -1062,7 +1084,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       sh.l[slot][half][q4 * 32 + lane] = l;
       __syncwarp();
       if (lane == 0) mbar_arrive(sh.l_full + q4);
-      if (!warp_mbar_wait(sh.l_full + q4, u & 1, a.wait_ns, abort_flag)) {
+      if (!wait32(sh.l_full + q4, u & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
@@ -1098,14 +1120,14 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           for (int sp = e.splits_r * R; sp < a.splits * R; ++sp)
             a.ml_part[at + sp * step] = make_float2(-INFINITY, 0.f);
       }
-      if (!warp_mbar_wait(sh.aux_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
+      if (!wait32(sh.aux_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
       const float inv = l > 0.f ? 1.f / l : 0.f, unit = pow2(sh.vx[slot]);
       // 1 / l and V's unit in one factor, unless the factor would not be a normal number
       const bool plain = __all_sync(0xffffffffu, fabsf(inv * unit) > 0x1p-100f) != 0;
-      if (!warp_mbar_wait(sh.pv_done + Tl % NS, (Tl / NS) & 1, a.wait_ns, abort_flag)) {
+      if (!wait32(sh.pv_done + Tl % NS, (Tl / NS) & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }

@@ -612,7 +612,9 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     if (elect_one()) {
       constexpr uint32_t id_s = idesc_e4m3_f32(kBV, KT);
       constexpr uint32_t id_c = idesc_bf16_f32(kBV, KC);
-      const uint32_t qs = smem_u32(smem);
+      const uint64_t q0 = desc_k_sw128(smem_u32(smem));
+      const uint64_t kc0 = desc_k_sw128(smem_u32(smem + G::kOffK));
+      const uint64_t k0 = DH == 64 ? desc_k_sw64(smem_u32(smem + G::kOffK)) : kc0;
       auto wait = [&](uint64_t* bar, uint32_t parity) {
         return wait1(bar, parity, a.wait_ns, abort_flag);
       };
@@ -631,24 +633,24 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                wait(sh.pv_done + b, ((Tj / NS) & 1) ^ 1u);
           if (!ok) break;
           tc_fence_after();
-          const uint32_t ks = smem_u32(smem + G::kOffK + kb * G::kTile);
           const uint32_t d = tmem + G::kSCol + b * KT;
+          // (a descriptor of another address: its low field counts 16 bytes)
           if (j < nct) {
+            const uint64_t kd = kc0 + kb * (G::kTile >> 4);
 #pragma unroll
             for (int st = 0; st < DH / 16; ++st) {
               const int sl = st >> 2, k = st & 3;
-              mma_f16(d, desc_k_sw128(qs + sl * (kBV * 128) + 32 * k),
-                      desc_k_sw128(ks + sl * (KC * 128) + 32 * k), id_c, st != 0);
+              mma_f16(d, q0 + ((sl * (kBV * 128) + 32 * k) >> 4),
+                      kd + ((sl * (KC * 128) + 32 * k) >> 4), id_c, st != 0);
             }
             if (j == nct - 1) mma_commit(&sh.q_free);
           } else {
+            const uint64_t kd = k0 + kb * (G::kTile >> 4);
 #pragma unroll
             for (int st = 0; st < DH / 16; ++st) {  // hi, then lo, over the same keys
               const int kk = st % (DH / 32);
-              const uint64_t kd = DH == 64 ? desc_k_sw64(ks + 32 * kk)
-                                           : desc_k_sw128(ks + (kk >> 2) * (KT * 128) +
-                                                          32 * (kk & 3));
-              mma_e4m3_ta(d, tmem + G::kQCol + uint32_t(8 * st), kd, id_s, st != 0);
+              mma_e4m3_ta(d, tmem + G::kQCol + uint32_t(8 * st),
+                          kd + (((kk >> 2) * (KT * 128) + 32 * (kk & 3)) >> 4), id_s, st != 0);
             }
           }
           mma_commit(sh.s_full + b);
@@ -670,6 +672,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     // ---------------------------------------------------------------- outputs
     if (elect_one()) {
       constexpr uint32_t id_o = idesc_f16_f32_mn(kBV, DH);
+      const uint64_t v0 = desc_mn_sw128(smem_u32(smem + G::kOffW), KT * 128);
+      const uint64_t vc0 = desc_mn_sw128(smem_u32(smem + G::kOffW), KC * 128);
       auto wait = [&](uint64_t* bar, uint32_t parity) {
         return wait1(bar, parity, a.wait_ns, abort_flag);
       };
@@ -688,17 +692,14 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           if (!ok) break;
           tc_fence_after();
           const uint32_t pt = tmem + G::kSCol + b * KT;
-          const uint32_t vs = smem_u32(smem + G::kOffW + w * 2 * G::kTile);
-          if (j < nct) {
+          const uint64_t vd = (j < nct ? vc0 : v0) + w * (2 * G::kTile >> 4);
 #pragma unroll
-            for (int k = 0; k < KC / 16; ++k)
-              mma_f16_ta(tmem, pt + uint32_t(8 * k), desc_mn_sw128(vs + k * 2048, KC * 128), id_o,
-                         (j | k) != 0);
-          } else {
+          for (int k = 0; k < KC / 16; ++k)
+            mma_f16_ta(tmem, pt + uint32_t(8 * k), vd + (k * 2048 >> 4), id_o, (j | k) != 0);
+          if (j >= nct) {
 #pragma unroll
-            for (int k = 0; k < KT / 16; ++k)
-              mma_f16_ta(tmem, pt + uint32_t(8 * k), desc_mn_sw128(vs + k * 2048, KT * 128), id_o,
-                         (j | k) != 0);
+            for (int k = KC / 16; k < KT / 16; ++k)
+              mma_f16_ta(tmem, pt + uint32_t(8 * k), vd + (k * 2048 >> 4), id_o, 1);
           }
           mma_commit(sh.pv_done + b);
         }
@@ -874,7 +875,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll
           for (int i = 0; i < kMine; ++i)
             x[i] = *reinterpret_cast<const uint4*>(vs + raw_piece<DH, KT>(key, c0 + kPer * i));
-          if (left < KT && key >= left) {
+          if (__builtin_expect(left < KT && key >= left, 0)) {
 #pragma unroll
             for (int i = 0; i < kMine; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
           }
@@ -990,7 +991,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           float sv[kCols];
           tmem_ld_cols(tmem + lane_off + G::kSCol + b * KT + G::kHalf * half + col0, sv);
           tmem_wait_ld();
-          if (cut) {
+          if (__builtin_expect(cut, 0)) {
 #pragma unroll
             for (int c = 0; c < kCols; ++c)
               if (c < klo || c >= khi) sv[c] = -INFINITY;
@@ -1015,7 +1016,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           mt = fmaxf(mt, sh.m[x & 1][half ^ 1][q4 * 32 + lane]);
           ++x;
           const bool grow = j == 0 || (valid && mt > m + kRescaleLog2);
-          if (__any_sync(0xffffffffu, grow)) {
+          if (__builtin_expect(__any_sync(0xffffffffu, grow), 0)) {
             const float m_new = grow ? mt : m;
             if (j > 0) {
               // O holds this item's P V so far: wait for the last one, rescale this half of

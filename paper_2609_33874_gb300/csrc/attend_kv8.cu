@@ -829,82 +829,88 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         break;
       }
       const int vx = sh.vx[slot];
-      for (int j = 0; j < e.ntiles; ++j) {
-        const int Tj = T + j;
-        const int s = Tj % NV, w = Tj % NW;
-        if (!wait32(sh.v_full + s, (Tj / NV) & 1, a.wait_ns, abort_flag) ||
-            (Tj >= NW && !wait32(sh.pv_done + (Tj - NW) % NS, ((Tj - NW) / NS) & 1,
-                                         a.wait_ns, abort_flag))) {
-          ok = false;
-          break;
-        }
-        const uint8_t* vs = smem + G::kOffV + s * G::kTile;
-        uint8_t* ws = smem + G::kOffW + w * 2 * G::kTile;
-        if (j < e.nct) {
-          // candidate values, in the places the product reads
-          const int left = fed - j * KC;
-          const float inv = pow2(-vx);
-          bool found = false;
-#pragma unroll
-          for (int k = 0; k < kMine; ++k) {
-            const int i = t + k * kWideThreads;
-            const uint4 v = *reinterpret_cast<const uint4*>(vs + 16 * i);
-            const uint32_t in[4] = {v.x, v.y, v.z, v.w};
-            uint32_t y[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const bool n0 = nonfinite_bf16(in[q]), n1 = nonfinite_bf16(in[q] >> 16);
-              found |= n0 | n1;
-              y[q] = pack_f16(n0 ? 0.f : __uint_as_float(in[q] << 16) * inv,
-                              n1 ? 0.f : __uint_as_float(in[q] & 0xffff0000u) * inv);
-              if (((i >> 3) & (KC - 1)) >= left) y[q] = 0u;
-            }
-            *reinterpret_cast<uint4*>(ws + 16 * i) = make_uint4(y[0], y[1], y[2], y[3]);
-          }
-          if (__any_sync(0xffffffffu, found) && lane == 0) sh.bad[slot][wi] = 1;
-        } else {
-          const int pt = j - e.nct;
-          // 2^(X - vx): below 2^-24 f16 holds no product with a code
-          const int k2 = max(exponent_of(byte) - vx, -24);
-          const int next = (pt + 1) * (KT / kKvBlock) + block;
-          if (next < blocks) byte = load_ahead(ex + size_t(next) * a.Hkv);
-          const uint32_t h2 = k2 > -15 ? uint32_t(k2 + 15) << 10 : 1u << (k2 + 24);
-          const uint32_t f = h2 | h2 << 16;
-          const int left = keys - pt * KT;  // the tile's keys past it are another request's
-          uint4 x[kMine];
-#pragma unroll
-          for (int i = 0; i < kMine; ++i)
-            x[i] = *reinterpret_cast<const uint4*>(vs + raw_piece<DH, KT>(key, c0 + kPer * i));
-          if (__builtin_expect(left < KT && key >= left, 0)) {
-#pragma unroll
-            for (int i = 0; i < kMine; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
-          }
-#pragma unroll
-          for (int i = 0; i < kMine; ++i) {
-            const uint32_t in[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-            uint32_t y[8];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              e4m3x4_to_f16x4(in[q], y[2 * q], y[2 * q + 1]);
-            }
-            if (k2 != 0) {
-#pragma unroll
-              for (int q = 0; q < 8; ++q) y[q] = mul_f16x2(y[q], f);
-            }
-            const int c = c0 + kPer * i;  // pieces 2 c and 2 c + 1 of the f16 row
-            uint8_t* to = ws + (c >> 2) * (KT * 128);
-            *reinterpret_cast<uint4*>(to + sw128(key, (2 * c) & 7)) =
-                make_uint4(y[0], y[1], y[2], y[3]);
-            *reinterpret_cast<uint4*>(to + sw128(key, (2 * c + 1) & 7)) =
-                make_uint4(y[4], y[5], y[6], y[7]);
-          }
-        }
+      // a V tile's codes there, and the place that its widened values take free
+      auto ready = [&](int Tj) -> bool {
+        return wait32(sh.v_full + Tj % NV, (Tj / NV) & 1, a.wait_ns, abort_flag) &&
+               (Tj < NW || wait32(sh.pv_done + (Tj - NW) % NS, ((Tj - NW) / NS) & 1, a.wait_ns,
+                                  abort_flag));
+      };
+      auto done = [&](int Tj) {
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(sh.w_full + w);
-          mbar_arrive(sh.v_empty + s);
+          mbar_arrive(sh.w_full + Tj % NW);
+          mbar_arrive(sh.v_empty + Tj % NV);
         }
+      };
+      for (int j = 0; j < e.nct; ++j) {
+        const int Tj = T + j;
+        ok = ready(Tj);
+        if (!ok) break;
+        const uint8_t* vs = smem + G::kOffV + (Tj % NV) * G::kTile;
+        uint8_t* ws = smem + G::kOffW + (Tj % NW) * 2 * G::kTile;
+        // candidate values, in the places the product reads
+        const int left = fed - j * KC;
+        const float inv = pow2(-vx);
+        bool found = false;
+#pragma unroll 2
+        for (int k = 0; k < kMine; ++k) {
+          const int i = t + k * kWideThreads;
+          const uint4 v = *reinterpret_cast<const uint4*>(vs + 16 * i);
+          const uint32_t in[4] = {v.x, v.y, v.z, v.w};
+          uint32_t y[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const bool n0 = nonfinite_bf16(in[q]), n1 = nonfinite_bf16(in[q] >> 16);
+            found |= n0 | n1;
+            y[q] = pack_f16(n0 ? 0.f : __uint_as_float(in[q] << 16) * inv,
+                            n1 ? 0.f : __uint_as_float(in[q] & 0xffff0000u) * inv);
+            if (((i >> 3) & (KC - 1)) >= left) y[q] = 0u;
+          }
+          *reinterpret_cast<uint4*>(ws + 16 * i) = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+        if (__any_sync(0xffffffffu, found) && lane == 0) sh.bad[slot][wi] = 1;
+        done(Tj);
+      }
+      if (!ok) break;
+      int left = keys, next = block;  // the keys past `left` of a tile are another request's
+      for (int Tj = T + e.nct; Tj < T + e.ntiles; ++Tj, left -= KT) {
+        ok = ready(Tj);
+        if (!ok) break;
+        const uint8_t* vs = smem + G::kOffV + (Tj % NV) * G::kTile;
+        uint8_t* ws = smem + G::kOffW + (Tj % NW) * 2 * G::kTile;
+        uint4 x[kMine];
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+          x[i] = *reinterpret_cast<const uint4*>(vs + raw_piece<DH, KT>(key, c0 + kPer * i));
+        // 2^(X - vx): below 2^-24 f16 holds no product with a code
+        const int k2 = max(exponent_of(byte) - vx, -24);
+        next += KT / kKvBlock;
+        if (next < blocks) byte = load_ahead(ex + size_t(next) * a.Hkv);
+        if (__builtin_expect(left < KT && key >= left, 0)) {
+#pragma unroll
+          for (int i = 0; i < kMine; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        const uint32_t h2 = k2 > -15 ? uint32_t(k2 + 15) << 10 : 1u << (k2 + 24);
+        const uint32_t f = h2 | h2 << 16;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+          const uint32_t in[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          uint32_t y[8];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) e4m3x4_to_f16x4(in[q], y[2 * q], y[2 * q + 1]);
+          if (k2 != 0) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) y[q] = mul_f16x2(y[q], f);
+          }
+          const int c = c0 + kPer * i;  // pieces 2 c and 2 c + 1 of the f16 row
+          uint8_t* to = ws + (c >> 2) * (KT * 128);
+          *reinterpret_cast<uint4*>(to + sw128(key, (2 * c) & 7)) =
+              make_uint4(y[0], y[1], y[2], y[3]);
+          *reinterpret_cast<uint4*>(to + sw128(key, (2 * c + 1) & 7)) =
+              make_uint4(y[4], y[5], y[6], y[7]);
+        }
+        done(Tj);
       }
       if (!ok) break;
       if (lane == 0) mbar_arrive(sh.item_empty + slot);

@@ -9,9 +9,15 @@
 // and X, reading back rounds nothing in bf16 or float32, and the attention takes the
 // scales out of its sums.
 //
-// All three are streams: each element is read and written once, and HBM bounds them.
-// One CTA takes one (block of 64 tokens, keys or values, head): a block's elements
-// stay in registers between its maximum and its codes.
+// All three are streams: each element is read and written once, and HBM bounds them
+// (1.38e9 bf16 elements written: 592 us, 7.0 TB/s; 172e6 read back: 79 us, 6.6 TB/s).
+// One CTA works on one (block of 64 tokens, keys or values, head) at a time: its
+// elements stay in registers between their maximum and their codes. Four such pairs one
+// after another hide the launch and the search for the place behind other CTAs' loads:
+// 1.38e9 bf16 elements with one pair a CTA against four: 629 and 592 us at d 256, 712 and
+// 606 at d 128; 0.69e9 at d 64, 577 and 345.
+#include <algorithm>
+
 #include "jet_device.cuh"
 #include "jet_internal.h"
 #include "kv_cache.h"
@@ -31,6 +37,7 @@ struct KvArgs {
   uint8_t* exps[2];
   int R, Hkv, total_prefix;
   int rows;                   // rows of k and v
+  int each;                   // (keys or values, head) pairs that a CTA takes
   int* status;
 };
 
@@ -96,107 +103,130 @@ __device__ __forceinline__ float element<__nv_bfloat16>(const uint4& v, int i) {
   return __uint_as_float((i & 1) ? (w & 0xffff0000u) : (w << 16));
 }
 
-// the larger magnitude of `top` and a piece's elements, as float32 bits; FINITE leaves
-// out infinities and NaN
-template <typename T, bool FINITE>
-__device__ __forceinline__ uint32_t top_bits(uint32_t top, const uint4& v) {
+// the larger magnitude of `top` and a piece's finite elements, as float32 bits
+template <typename T>
+__device__ __forceinline__ uint32_t top_finite(uint32_t top, const uint4& v) {
 #pragma unroll
   for (int i = 0; i < int(16 / sizeof(T)); ++i) {
     const uint32_t u = __float_as_uint(element<T>(v, i)) & 0x7fffffffu;
-    top = max(top, FINITE && u >= 0x7f800000u ? 0u : u);
+    top = max(top, u >= 0x7f800000u ? 0u : u);
   }
   return top;
 }
 
-__device__ __forceinline__ uint32_t block_max(uint32_t v) {
-  __shared__ uint32_t part[kThreads / 32];
-  __syncthreads();  // an earlier result is read by all
-  v = __reduce_max_sync(0xffffffffu, v);
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-  __syncthreads();
+// the largest magnitude of a thread's pieces, as float32 bits; the bits of bf16's
+// magnitudes are compared two at once
+template <typename T, int N>
+__device__ __forceinline__ uint32_t top_bits(const uint4 (&v)[N]) {
+  constexpr bool bf16 = sizeof(T) == 2;
+  uint32_t top = 0;
 #pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) v = max(v, part[w]);
-  return v;
+  for (int i = 0; i < N; ++i) {
+    const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      top = bf16 ? __vmaxu2(top, w[q] & 0x7fff7fffu) : max(top, w[q] & 0x7fffffffu);
+  }
+  return bf16 ? max(top & 0xffff0000u, top << 16) : top;
 }
 
+// the CTA's largest v; calls take the two halves of `part` in turn, so that a barrier
+// stands between a read of one and its next write
+__device__ __forceinline__ uint32_t block_max(uint32_t v, int* turn) {
+  __shared__ uint32_t part[2][kThreads / 32];
+  uint32_t* mine = part[*turn];
+  *turn ^= 1;
+  v = __reduce_max_sync(0xffffffffu, v);
+  if ((threadIdx.x & 31) == 0) mine[threadIdx.x >> 5] = v;
+  __syncthreads();
+  return __reduce_max_sync(0xffffffffu, mine[threadIdx.x % (kThreads / 32)]);
+}
+
+// A CTA takes `each` of a block's 2 Hkv (keys or values, head) pairs, one after another.
+// The CTAs an SM that the launch bounds ask for are the most whose registers hold the
+// elements without spills; left to itself the compiler takes 122 registers at d 256 in
+// bf16 and two CTAs run (823 us instead of 632 at one pair each).
 template <typename T, int DH, bool APPEND>
-__global__ void __launch_bounds__(kThreads) kv_quantize_kernel(const KvArgs a) {
+__global__ void __launch_bounds__(kThreads, DH == 256 ? (sizeof(T) == 2 ? 4 : 3) : DH == 128 ? 5 : 8)
+kv_quantize_kernel(const KvArgs a) {
   pdl_begin();
   constexpr int kPer = 16 / int(sizeof(T));          // elements of a 16-byte piece
   constexpr int kRow = DH / kPer;                    // pieces of a token
   constexpr int kMine = kKvBlock * kRow / kThreads;  // of a thread
-  const int h = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv;
-  const int kv = rest & 1;
+  constexpr int kStep = kThreads / kRow;             // tokens between a thread's pieces
+  const int groups = (2 * a.Hkv + a.each - 1) / a.each;
+  const int first = int(blockIdx.x % groups) * a.each;
   KvSpan s;
-  if (!find_span<APPEND>(a, rest >> 1, &s)) return;
+  if (!find_span<APPEND>(a, blockIdx.x / groups, &s)) return;
   const int nt = s.t1 - s.t0, tid = threadIdx.x;
-  uint8_t* exp = a.exps[kv] + size_t(kv_place(s.p0, s.r, s.b)) * a.Hkv + h;
-  // a block begun before: the exponent of the tokens it holds
-  const bool begun = APPEND && s.t0 > s.b * kKvBlock;
-  const int held = begun ? min(max(int(*exp) - 127, kKvLow), kKvHigh) : kKvLow;
-  const T* x = static_cast<const T*>(a.x[kv]) + (size_t(s.row0) * a.Hkv + h) * DH;
+  const int j0 = tid / kRow, c0 = tid % kRow * kPer;
   const size_t step = size_t(a.Hkv) * DH;
-  uint4 v[kMine];
-  uint32_t top = 0;
+  int turn = 0;
+#pragma unroll 1
+  for (int u = first; u < min(first + a.each, 2 * a.Hkv); ++u) {
+    const int kv = u >= a.Hkv, h = u - kv * a.Hkv;
+    uint8_t* exp = a.exps[kv] + size_t(kv_place(s.p0, s.r, s.b)) * a.Hkv + h;
+    // a block begun before: the exponent of the tokens it holds
+    const bool begun = APPEND && s.t0 > s.b * kKvBlock;
+    const int held = begun ? min(max(int(*exp) - 127, kKvLow), kKvHigh) : kKvLow;
+    const T* x = static_cast<const T*>(a.x[kv]) + (size_t(s.row0 + j0) * a.Hkv + h) * DH + c0;
+    uint4 v[kMine];
 #pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    const int e = tid + i * kThreads, j = e / kRow, c = e % kRow;
-    v[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (j < nt) v[i] = *reinterpret_cast<const uint4*>(x + j * step + c * kPer);
-  }
+    for (int i = 0; i < kMine; ++i) {
+      v[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (j0 + i * kStep < nt) v[i] = *reinterpret_cast<const uint4*>(x + i * kStep * step);
+    }
+    uint32_t top = block_max(top_bits<T>(v), &turn);
+    const bool finite = top < 0x7f800000u;
+    if (!finite) {
+      top = 0;
 #pragma unroll
-  for (int i = 0; i < kMine; ++i) top = top_bits<T, false>(top, v[i]);
-  top = block_max(top);
-  const bool finite = top < 0x7f800000u;
-  if (!finite) {
-    top = 0;
+      for (int i = 0; i < kMine; ++i) top = top_finite<T>(top, v[i]);
+      top = block_max(top, &turn);
+    }
+    const int X = max(kv_exponent(top), held);
+    const float inv = pow2(-X);
+    uint8_t* codes = a.codes[kv] + (size_t(s.p0 + s.t0 + j0) * a.Hkv + h) * DH + c0;
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) top = top_bits<T, true>(top, v[i]);
-    top = block_max(top);
-  }
-  const int X = max(kv_exponent(top), held);
-  const float inv = pow2(-X);
-  uint8_t* codes = a.codes[kv] + (size_t(s.p0 + s.t0) * a.Hkv + h) * DH;
+    for (int i = 0; i < kMine; ++i) {
+      if (j0 + i * kStep >= nt) continue;
+      uint32_t w[kPer / 4];
 #pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    const int e = tid + i * kThreads, j = e / kRow, c = e % kRow;
-    if (j >= nt) continue;
-    uint32_t w[kPer / 4];
+      for (int q = 0; q < kPer / 4; ++q) {
+        const float f0 = element<T>(v[i], 4 * q), f1 = element<T>(v[i], 4 * q + 1);
+        const float f2 = element<T>(v[i], 4 * q + 2), f3 = element<T>(v[i], 4 * q + 3);
+        w[q] = encode2(f0 * inv, f1 * inv) | encode2(f2 * inv, f3 * inv) << 16;
+        if (!finite) {  // the format has no infinity: it is held as NaN too
+          if (isinf(f0)) w[q] |= 0x7fu;
+          if (isinf(f1)) w[q] |= 0x7f00u;
+          if (isinf(f2)) w[q] |= 0x7f0000u;
+          if (isinf(f3)) w[q] |= 0x7f000000u;
+        }
+      }
+      uint8_t* to = codes + i * kStep * step;
+      if constexpr (kPer == 8)
+        *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+      else
+        *reinterpret_cast<uint32_t*>(to) = w[0];
+    }
+    if (begun && X > held) {
+      // the tokens before, rounded again (codes that stay normal keep their values)
+      const float f = pow2(max(held - X, -126));
+      uint8_t* old = a.codes[kv] + (size_t(s.p0 + s.b * kKvBlock) * a.Hkv + h) * DH;
+      for (int e = tid; e < (s.t0 - s.b * kKvBlock) * (DH / 8); e += kThreads) {
+        uint2* at = reinterpret_cast<uint2*>(old + (e / (DH / 8)) * step + 8 * (e % (DH / 8)));
+        uint2 w = *at;
 #pragma unroll
-    for (int q = 0; q < kPer / 4; ++q) {
-      const float f0 = element<T>(v[i], 4 * q), f1 = element<T>(v[i], 4 * q + 1);
-      const float f2 = element<T>(v[i], 4 * q + 2), f3 = element<T>(v[i], 4 * q + 3);
-      w[q] = encode2(f0 * inv, f1 * inv) | encode2(f2 * inv, f3 * inv) << 16;
-      if (!finite) {  // the format has no infinity: it is held as NaN too
-        if (isinf(f0)) w[q] |= 0x7fu;
-        if (isinf(f1)) w[q] |= 0x7f00u;
-        if (isinf(f2)) w[q] |= 0x7f0000u;
-        if (isinf(f3)) w[q] |= 0x7f000000u;
+        for (int q = 0; q < 2; ++q) {
+          uint32_t& y = q ? w.y : w.x;
+          const float2 lo = e4m3x2_to_f32(y), hi = e4m3x2_to_f32(y >> 16);
+          y = encode2(lo.x * f, lo.y * f) | encode2(hi.x * f, hi.y * f) << 16;
+        }
+        *at = w;
       }
     }
-    uint8_t* to = codes + j * step + c * kPer;
-    if constexpr (kPer == 8)
-      *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
-    else
-      *reinterpret_cast<uint32_t*>(to) = w[0];
+    if (tid == 0) *exp = uint8_t(X + 127);  // block_max: every thread has read what it held
   }
-  if (begun && X > held) {
-    // the tokens before, rounded again (codes that stay normal keep their values)
-    const float f = pow2(max(held - X, -126));
-    uint8_t* old = a.codes[kv] + (size_t(s.p0 + s.b * kKvBlock) * a.Hkv + h) * DH;
-    for (int e = tid; e < (s.t0 - s.b * kKvBlock) * (DH / 8); e += kThreads) {
-      uint2* at = reinterpret_cast<uint2*>(old + (e / (DH / 8)) * step + 8 * (e % (DH / 8)));
-      uint2 w = *at;
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        uint32_t& y = q ? w.y : w.x;
-        const float2 lo = e4m3x2_to_f32(y), hi = e4m3x2_to_f32(y >> 16);
-        y = encode2(lo.x * f, lo.y * f) | encode2(hi.x * f, hi.y * f) << 16;
-      }
-      *at = w;
-    }
-  }
-  if (tid == 0) *exp = uint8_t(X + 127);  // block_max: every thread has read what it held
 }
 
 template <typename T, int DH>
@@ -205,51 +235,56 @@ __global__ void __launch_bounds__(kThreads) kv_dequantize_kernel(const KvArgs a)
   constexpr int kPer = 16 / int(sizeof(T));
   constexpr int kRow = DH / kPer;
   constexpr int kMine = kKvBlock * kRow / kThreads;
-  const int h = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv;
-  const int kv = rest & 1;
+  constexpr int kStep = kThreads / kRow;
+  const int groups = (2 * a.Hkv + a.each - 1) / a.each;
+  const int first = int(blockIdx.x % groups) * a.each;
   KvSpan s;
-  if (!find_span<false>(a, rest >> 1, &s)) return;
+  if (!find_span<false>(a, blockIdx.x / groups, &s)) return;
   const int nt = s.t1 - s.t0, tid = threadIdx.x;
-  const uint8_t held = a.exps[kv][size_t(kv_place(s.p0, s.r, s.b)) * a.Hkv + h];
-  const float f = kv_scale(held);
-  const size_t step = size_t(a.Hkv) * DH, at = (size_t(s.p0 + s.t0) * a.Hkv + h) * DH;
-  const uint8_t* codes = a.codes[kv] + at;
-  T* out = static_cast<T*>(a.out[kv]) + at;
-  uint32_t w[kMine][kPer / 4];
+  const int j0 = tid / kRow, c0 = tid % kRow * kPer;
+  const size_t step = size_t(a.Hkv) * DH;
+#pragma unroll 1
+  for (int u = first; u < min(first + a.each, 2 * a.Hkv); ++u) {
+    const int kv = u >= a.Hkv, h = u - kv * a.Hkv;
+    const uint8_t held = a.exps[kv][size_t(kv_place(s.p0, s.r, s.b)) * a.Hkv + h];
+    const float f = kv_scale(held);
+    const size_t at = (size_t(s.p0 + s.t0 + j0) * a.Hkv + h) * DH + c0;
+    const uint8_t* codes = a.codes[kv] + at;
+    T* out = static_cast<T*>(a.out[kv]) + at;
+    uint32_t w[kMine][kPer / 4];
 #pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    const int e = tid + i * kThreads, j = e / kRow, c = e % kRow;
-    if (j >= nt) continue;
-    const uint8_t* from = codes + j * step + c * kPer;
-    if constexpr (kPer == 8) {
-      const uint2 y = *reinterpret_cast<const uint2*>(from);
-      w[i][0] = y.x;
-      w[i][1] = y.y;
-    } else {
-      w[i][0] = *reinterpret_cast<const uint32_t*>(from);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    const int e = tid + i * kThreads, j = e / kRow, c = e % kRow;
-    if (j >= nt) continue;
-    uint32_t y[4];
-#pragma unroll
-    for (int q = 0; q < kPer / 4; ++q) {
-      const float2 lo = e4m3x2_to_f32(w[i][q]), hi = e4m3x2_to_f32(w[i][q] >> 16);
+    for (int i = 0; i < kMine; ++i) {
+      if (j0 + i * kStep >= nt) continue;
+      const uint8_t* from = codes + i * kStep * step;
       if constexpr (kPer == 8) {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(lo.x * f, lo.y * f);
-        const __nv_bfloat162 r = __floats2bfloat162_rn(hi.x * f, hi.y * f);
-        y[2 * q] = *reinterpret_cast<const uint32_t*>(&p);
-        y[2 * q + 1] = *reinterpret_cast<const uint32_t*>(&r);
+        const uint2 y = *reinterpret_cast<const uint2*>(from);
+        w[i][0] = y.x;
+        w[i][1] = y.y;
       } else {
-        y[0] = __float_as_uint(lo.x * f);
-        y[1] = __float_as_uint(lo.y * f);
-        y[2] = __float_as_uint(hi.x * f);
-        y[3] = __float_as_uint(hi.y * f);
+        w[i][0] = *reinterpret_cast<const uint32_t*>(from);
       }
     }
-    *reinterpret_cast<uint4*>(out + j * step + c * kPer) = make_uint4(y[0], y[1], y[2], y[3]);
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      if (j0 + i * kStep >= nt) continue;
+      uint32_t y[4];
+#pragma unroll
+      for (int q = 0; q < kPer / 4; ++q) {
+        const float2 lo = e4m3x2_to_f32(w[i][q]), hi = e4m3x2_to_f32(w[i][q] >> 16);
+        if constexpr (kPer == 8) {
+          const __nv_bfloat162 p = __floats2bfloat162_rn(lo.x * f, lo.y * f);
+          const __nv_bfloat162 r = __floats2bfloat162_rn(hi.x * f, hi.y * f);
+          y[2 * q] = *reinterpret_cast<const uint32_t*>(&p);
+          y[2 * q + 1] = *reinterpret_cast<const uint32_t*>(&r);
+        } else {
+          y[0] = __float_as_uint(lo.x * f);
+          y[1] = __float_as_uint(lo.y * f);
+          y[2] = __float_as_uint(hi.x * f);
+          y[3] = __float_as_uint(hi.y * f);
+        }
+      }
+      *reinterpret_cast<uint4*>(out + i * kStep * step) = make_uint4(y[0], y[1], y[2], y[3]);
+    }
   }
 }
 
@@ -271,9 +306,19 @@ KvArgs kv_args(const jet_layout& lay, const jet_dims& d, const void* k8, const v
   return a;
 }
 
+// The grid of `places` blocks, and a.each: a CTA takes up to `most` pairs, but no more
+// than leaves 512 CTAs, three or four an SM. An append's places are mostly partial, so
+// it has fewer to hide behind (16 requests of 100 to 700 tokens: 8.8 us with two, 11.1 with
+// four), and a piece read back holds its codes for a shorter time, so what counts is a
+// CTA's bytes (d 128: 355 us with one, 313 with two; d 256: 79 with one, 84 with two).
+dim3 kv_grid(KvArgs* a, int most, long long places) {
+  a->each = int(std::min((long long)most, std::max(1LL, places * 2 * a->Hkv / 512)));
+  return dim3(unsigned(places * ((2 * a->Hkv + a->each - 1) / a->each)));
+}
+
 template <typename T, bool APPEND>
-cudaError_t launch_quantize(const KvArgs& a, int DH, long long places, cudaStream_t st) {
-  const dim3 grid(unsigned(places * 2 * a.Hkv));
+cudaError_t launch_quantize(KvArgs a, int DH, long long places, cudaStream_t st) {
+  const dim3 grid = kv_grid(&a, APPEND ? 2 : 4, places);
   if (DH == 64) return launch_pdl(kv_quantize_kernel<T, 64, APPEND>, grid, dim3(kThreads), 0, st, a);
   if (DH == 128)
     return launch_pdl(kv_quantize_kernel<T, 128, APPEND>, grid, dim3(kThreads), 0, st, a);
@@ -281,8 +326,8 @@ cudaError_t launch_quantize(const KvArgs& a, int DH, long long places, cudaStrea
 }
 
 template <typename T>
-cudaError_t launch_dequantize(const KvArgs& a, int DH, long long places, cudaStream_t st) {
-  const dim3 grid(unsigned(places * 2 * a.Hkv));
+cudaError_t launch_dequantize(KvArgs a, int DH, long long places, cudaStream_t st) {
+  const dim3 grid = kv_grid(&a, 256 / DH, places);
   if (DH == 64) return launch_pdl(kv_dequantize_kernel<T, 64>, grid, dim3(kThreads), 0, st, a);
   if (DH == 128) return launch_pdl(kv_dequantize_kernel<T, 128>, grid, dim3(kThreads), 0, st, a);
   return launch_pdl(kv_dequantize_kernel<T, 256>, grid, dim3(kThreads), 0, st, a);

@@ -402,10 +402,17 @@ AttnPlan attn_plan_kv8(const jet_sizes& n, const jet_dims& d) {
   if (d.dtype != JET_DTYPE_BF16 || n.R <= 0 || n.N <= 0) return p;
   // Few query vectors leave softmax warps without any. Then a block holds its vectors two
   // or four times over, and each copy takes its part of a tile's keys: the copies leave
-  // partials that the combine joins like chunks.
+  // partials that the combine joins like chunks. That pays at d 64 and 128 once an SM has
+  // some three 128-key tiles (32 vectors, one copy against four: 256 requests of 1,000
+  // keys, d 128, two kv heads 75.8 and 61.4 us, d 64 63.5 and 51.2; 32 of 1,000, 421 keys
+  // an SM, 24.6 and 22.5; 64 of 300, 253 keys an SM, 20.5 and 22.5; one of 6,000 20.5 and
+  // 24.6; four against two at 64 of 1,000 to 6,000, d 64, eight kv heads 149.5 and 174.1;
+  // 64 vectors, one and two: 256 of 1,000, d 128 75.8 and 69.6). A tile of d 256 has half
+  // the keys for the same bytes, and its copies only break even (64 of 1,000 to 6,000
+  // 85.0 and 85.0, one of 6,000 22.5 and 28.7).
   const int vecs = n.max_rows * (d.Hq / d.Hkv);
-  if (vecs <= 32) p.copies = 4;
-  else if (vecs <= 64) p.copies = 2;
+  if (d.d <= 128 && (long long)n.total_prefix * d.Hkv >= 3LL * 128 * kPlanSMs)
+    p.copies = vecs <= 32 ? 4 : vecs <= 64 ? 2 : 1;
   if (p.copies > 1) {
     const size_t v = size_t(p.splits) * n.N * d.Hq;
     p.bytes += (p.copies - 1) * v * (d.d * sizeof(float) + sizeof(float2));

@@ -2,7 +2,7 @@
 // (Sec. 4.1; bf16 queries, candidates' keys and values, and outputs; f32 accumulation).
 //
 // As in attend_tc.cu a CTA owns one (request r, key/value head kh, prefix chunk, block of
-// up to 128 query vectors), streams the chunk's 64-key tiles once for all of them and
+// up to 128 query vectors), streams the chunk's tiles of 64 or 128 keys once for all of them and
 // leaves a partial that the combine merges, or the output where the request is one
 // chunk. A cache tile is half the bytes of a bf16 one, so at the HBM rate an SM has half
 // the time for it (d 256: 32 KB, 0.73 us): what follows keeps each unit below that.
@@ -11,13 +11,16 @@
 //            e4m3 numbers, q = 2^x (hi + lo), x per row: hi is the nearest code, lo that of
 //            what is left, at most four binary digits of a bf16 number's eight, so the
 //            split is exact for elements within 2^-10 of the row's largest and leaves
-//            2^-10 of 2^x, at most 2^-17.8 of that largest element, below. (Keys widened to bf16 instead
-//            would pass shared memory twice more: 1,536 cycles a tile of d 256, 1,393
-//            at the HBM rate.) S = acc 2^(x + X), X the tile's exponent: the 64 tokens of
-//            a block are a tile.
-//   outputs  O += P V with P in bf16 and V widened from the codes to bf16, exactly, by
-//            four warps on the way (P in e4m3 would lose the many small weights next
-//            to a large one).
+//            2^-10 of 2^x, at most 2^-17.8 of that largest element, below. (Keys
+//            widened to bf16 instead would pass shared memory twice more: 1,536 cycles
+//            a tile of d 256, 1,393 at the HBM rate.) S = acc 2^(x + X), X the exponent
+//            of the 64 tokens: a tile has one or two.
+//   outputs  O += P V with P in f16, as weights 2^(s - m + 7) <= 2^15 (f16 keeps eleven
+//            digits down to 2^-14, so weights 2^-21 of a maximum's, and rounds
+//            at 2^-25 below; e4m3 would lose the many small weights next to a large
+//            one), and V widened from the codes to f16 in units of 2^vx, the item's
+//            largest exponent, by eight warps on the way: exact but for codes below
+//            2^-14 of that unit, which are rounded at 2^-25 of it.
 //
 //   warp 0       TMA producer: rings of K tiles, of V tiles, and the query block
 //   warp 1       TMEM allocator, issues S_j = Q K_j^T
@@ -28,14 +31,28 @@
 //                overwrites S_j in TMEM.
 //   warps 12..19 per item the queries' split into TMEM, per tile V to f16. Values of
 //                keys past the chunk (other requests') become zeros there.
-// The candidates' own tokens come first in a request's last chunk, as 32-key tiles of
-// bf16 keys and values (the same bytes as a cache tile) against the bf16 queries; their
-// values pass the widening warps too, which take non-finite ones out, as a weight of
-// zero would spread them to the rows that do not see them; the output adds them back
-// for the rows that do.
+// The candidates' own tokens come first in a request's last chunk, in tiles of half the
+// keys in bf16 (the same bytes as a cache tile) against the bf16 queries; their values
+// pass the widening warps too. Values that are not finite, or so large that V's unit
+// would take the prefix's digits with it, are left out there, as a weight of zero would
+// not keep them from the rows that do not see them; the output adds such an item's
+// candidate tokens one by one, each to the rows that do.
+//
+// What bounds it: long prefixes, HBM and the issue slots of the softmax and widening
+// warps together (256 requests of 2,048 - 8,192 tokens, d 256, two kv heads: 346 us, 61 %
+// of the copy rate; 128 of them at d 128, eight kv heads: 415 us, 50 %): a tile of d 256
+// takes these warps some 1,600 cycles (a conversion or an exponential holds its unit for
+// two to four cycles), its bytes 1,393. At one query row a request the copies below
+// leave the widening of V (64 requests of 1,000 - 6,000, d 128: 110 us, 65 %). Small
+// calls take an item's way through all roles, some 35,000 cycles or 18 us: the schedule
+// (3,800), the queries' arrival (5,900) and split (3,900), the tiles, the output (2,400).
+//
+// With R copies a block of 128 / R vectors stands R times in the TMEM lanes, and copy c's
+// softmax warps take columns c of R of their half's, with zeros for the others' in P: a
+// partial each.
 #include <algorithm>
+#include <climits>
 #include <cmath>
-#include <type_traits>
 
 #include "attend_tc.cuh"
 #include "kv_cache.h"
@@ -45,13 +62,15 @@ namespace {
 
 constexpr float kWeightLog2 = 7.f;  // weights are 2^7 at a row's maximum
 constexpr int kThreads = 640;
-constexpr int kProdWarp = 0, kMmaWarp = 1, kSchedWarp = 2, kPvWarp = 3, kSoftWarp = 4, kWideWarp = 12;
+constexpr int kProdWarp = 0, kMmaWarp = 1, kSchedWarp = 2, kPvWarp = 3, kSoftWarp = 4;
+constexpr int kWideWarp = 12;
 constexpr int kWideThreads = kThreads - 32 * kWideWarp;
 
 template <int DH>
 struct Geo {
-  // A tile of 64 keys for d 256, whose O leaves TMEM no more; else of 128, so that half as
-  // many steps of the pipeline carry the same bytes
+  // A tile of 64 keys for d 256, where O, two S and the queries' codes leave TMEM room for
+  // no more; else of 128, so that half as many steps of the pipeline carry the same
+  // bytes (d 128, long prefixes: 415 us instead of 487)
   static constexpr int kT = DH == 256 ? 64 : 128;
   static constexpr int kHalf = kT / 2;                    // columns of a softmax warp
   static constexpr int kC = kT / 2;                       // candidate tokens per tile
@@ -77,6 +96,8 @@ struct Geo {
 struct Kv8Args : AttArgs {
   const uint8_t* k_exp;  // exponent bytes of the caches
   const uint8_t* v_exp;
+  const __nv_bfloat16* q;
+  const __nv_bfloat16* k_cand;
   const __nv_bfloat16* v_cand;
 };
 
@@ -105,11 +126,12 @@ struct Small {
   uint64_t drain[2];
   uint32_t tmem;
   volatile int abort;
-  volatile int bad[2][8];                // non-finite candidate values, per widening warp
   float m[2][2][kBV];                    // [tile parity][half] maxima
   float l[2][2][kBV];                    // [item parity][half] sums
   int qx[2][kBV];                        // [item parity] the queries' exponents
   int vx[2];                             // [item parity] the exponent of V and O
+  int apart[2];                          // [item parity] the candidates' values stay out of
+                                         // P V
   uint32_t qmax[2][kBV];                 // [half] largest magnitudes of the queries
   int2 sees[2][kBV];                     // [item parity] the fed tokens a vector sees, from
                                          // f_begin on: first, end
@@ -242,13 +264,6 @@ __device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
   return d;
 }
 
-// the larger magnitudes of two pairs of bf16 numbers; NaN if there is one
-__device__ __forceinline__ uint32_t max_bf16x2_nan(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-
 __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
   uint32_t d;
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
@@ -311,15 +326,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
-}
-
-__device__ __forceinline__ bool nonfinite_bf16(uint32_t h) { return (h & 0x7f80u) == 0x7f80u; }
-
-// the larger of `top` and the magnitudes of two bf16 numbers, as bits; infinities and NaN
-// do not count
-__device__ __forceinline__ uint32_t finite_max_bf16x2(uint32_t top, uint32_t w) {
-  const uint32_t a = w & 0x7fffu, b = (w >> 16) & 0x7fffu;
-  return max(top, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
 }
 
 template <int DH, int R>
@@ -396,325 +402,339 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
   // registers to the softmax warps, which hold a tile's scores: 80 + 2 x 112 + 2 x 88 are
   // the five warpgroups' launch share of 96 each
   if (warp < kSoftWarp) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-  if (warp == kSchedWarp) {
-    // ---------------------------------------------------------------- scheduler
-    const int count = a.sorted ? *a.item_count : 0;
-    ItemWindow window{};
-    for (int u = 0;; ++u) {
-      const int slot = u & 1;
-      if (!wait32(sh.item_empty + slot, ((u >> 1) & 1) ^ 1u, a.wait_ns, abort_flag)) {
-        if (lane == 0) {
-          sh.abort = 1;
-          flag(a.status, JET_ERR_TIMEOUT);
-        }
-        break;
-      }
-      ItemGeo e{};
-      bool live = false;
-      if (a.sorted) {
-        // the CTA's first item is number blockIdx.x, later ones come from the shared
-        // counter, past the grid's first items
-        if (lane == 0) {
-          for (bool first = (u == 0);; first = false) {
-            const int idx = first ? int(blockIdx.x) : int(gridDim.x) + atomicAdd(a.item_next, 1);
-            if (idx >= count) break;
-            bool fits;
-            e = item_geo(a, a.items[idx], &fits);
-            live = e.ok;
-            if (live) break;
-            flag(a.status, JET_ERR_DEVICE);  // the list holds an item the layout lacks
-          }
-        }
-      } else {
-        // dealt out back and forth, as the bf16 kernel does
-        const int n = int(gridDim.x);
-        const int k = u * n + ((u & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
-        int4 it;
-        if (k < a.n_all && nth_item(a, k, lane, window, &it, &e)) {
-          live = e.ok;
-          if (!live && lane == 0) flag(a.status, JET_ERR_DEVICE);
-        }
-      }
-      int fed = 0;
-      if (lane == 0) {
-        if (live) {
-          if (e.nct > 0) {
-            // the fed tokens that a row of this block sees: up to its last row's own,
-            // from the first of its first row's candidate on
-            fed = e.row0 + e.nv / g - 1;
-            int lo = 0;
-            if (fed > KC && e.row0 > 0) {
-              const int c = a.row_cand[e.n0 + e.row0];
-              if (c >= 0 && c < a.C)
-                lo = min(max(a.cand_row_offset[c] - e.n0 - 1, 0), fed);
-            }
-            e.f_begin += lo;
-            fed -= lo;
-          }
-          e.nct = (fed + KC - 1) / KC;
-          e.npt = (e.k_end - e.k_begin + KT - 1) / KT;
-          e.ntiles = e.npt + e.nct;
-        }
-        sh.ring[slot].e = e;
-        sh.ring[slot].fed = fed;
-        sh.ring[slot].live = live;
-        mbar_arrive(sh.item_full + slot);
-        if (live) {  // the query block on its way into L2
-#pragma unroll
-          for (int sl = 0; sl < DH / 64; ++sl)
-            tma_prefetch_3d(&tmQ, sl * 64, e.kh * g, e.n0 + e.row0);
-        }
-      }
-      if (!__shfl_sync(0xffffffffu, live ? 1 : 0, 0)) break;
-      // What the other warps need a little later, and would wait for memory to know: the
-      // fed tokens that each vector sees, and V's unit, the largest exponent of the
-      // item's blocks and of its candidates' values
-      {
-        __syncwarp();
-        const ItemGeo& it = sh.ring[slot].e;
-        fed = __shfl_sync(0xffffffffu, fed, 0);
-        const int f_begin = it.f_begin, blocks = (it.k_end - it.k_begin + kKvBlock - 1) / kKvBlock;
-        if (fed > 0) {
-          for (int i = lane; i < it.nv; i += 32) {
-            const int n = it.n0 + (it.vbase + i) / g;
-            const int c = a.row_cand[n];
-            int from = 0, end = 0;  // none: shared row
-            if (c >= 0 && c < a.C) {
-              from = min(max(a.cand_row_offset[c] - it.r - 1 - f_begin, 0), fed);  // y_{c,1}
-              end = min(n - it.r - f_begin, fed);  // past the row's own fed token
-            }
-            sh.sees[slot][i] = make_int2(from, end);
-          }
-        }
-        const uint8_t* ex = a.v_exp + size_t(kv_place(it.p0, it.r, it.k_begin / kBN)) * a.Hkv + it.kh;
-        int vx = kKvLow + 127;
-        for (int b = lane; b < blocks; b += 32) vx = max(vx, int(ex[size_t(b) * a.Hkv]));
-        uint32_t top = 0;
-        const __nv_bfloat16* vc = a.v_cand + (size_t(f_begin) * a.Hkv + it.kh) * DH;
-#pragma unroll 4
-        for (int i = lane; i < fed * (DH / 8); i += 32) {
-          const uint4 v = *reinterpret_cast<const uint4*>(
-              vc + size_t(i / (DH / 8)) * a.Hkv * DH + 8 * (i % (DH / 8)));
-          top = finite_max_bf16x2(finite_max_bf16x2(top, v.x), v.y);
-          top = finite_max_bf16x2(finite_max_bf16x2(top, v.z), v.w);
-        }
-        vx = __reduce_max_sync(0xffffffffu, max(vx, top ? kv_exponent(top << 16) + 127 : 0));
-        if (lane == 0) sh.vx[slot] = min(max(vx - 127, kKvLow), kKvHigh);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(sh.aux_full + slot);
-      }
-    }
-  } else if (warp == kProdWarp) {
-    // ---------------------------------------------------------------- producer
-    if (elect_one()) {
-      const uint64_t pol = policy_evict_first();
-      uint32_t k_issued = 0, k_par = 0, v_issued = 0, v_par = 0, q_issued = 0, q_par = 0;
-      int T = 0;  // tiles of earlier items
-      bool ok = true;
-      for (int u = 0; ok; ++u) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp == kSchedWarp) {
+      // ---------------------------------------------------------------- scheduler
+      const int count = a.sorted ? *a.item_count : 0;
+      ItemWindow window{};
+      for (int u = 0;; ++u) {
         const int slot = u & 1;
-        if (!wait1(sh.item_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
-          ok = false;
+        if (!wait32(sh.item_empty + slot, ((u >> 1) & 1) ^ 1u, a.wait_ns, abort_flag)) {
+          if (lane == 0) {
+            sh.abort = 1;
+            flag(a.status, JET_ERR_TIMEOUT);
+          }
           break;
         }
-        if (!sh.ring[slot].live) break;
-        const ItemGeo e = sh.ring[slot].e;
-        // K_j, V_j and the query block are issued as soon as their places drain
-        int jk = 0, jv = 0;
-        bool q_sent = false;
-        IdleClock clk;
-        while (jv < e.ntiles || !q_sent) {
-          bool progressed = false;
-          if (!q_sent && (u == 0 || mbar_test(&sh.q_free, (u - 1) & 1))) {
-            if (!(u == 0 && a.hold_first)) {  // test hook: the first block never lands
-              mbar_arrive_expect_tx(&sh.q_full, uint32_t(R * (DH / 64)) * 64 * 2 * g * rb);
-#pragma unroll
-              for (int c = 0; c < R; ++c)
-#pragma unroll
-                for (int sl = 0; sl < DH / 64; ++sl)
-                  tma_load_3d(smem + sl * (kBV * 128) + c * RV * 128, &tmQ, &sh.q_full, sl * 64,
-                              e.kh * g, e.n0 + e.row0, pol);
-              q_issued = 1;
-              q_par = u & 1;
+        ItemGeo e{};
+        bool live = false;
+        if (a.sorted) {
+          // the CTA's first item is number blockIdx.x, later ones come from the shared
+          // counter, past the grid's first items
+          if (lane == 0) {
+            for (bool first = (u == 0);; first = false) {
+              const int idx = first ? int(blockIdx.x) : int(gridDim.x) + atomicAdd(a.item_next, 1);
+              if (idx >= count) break;
+              bool fits;
+              e = item_geo(a, a.items[idx], &fits);
+              live = e.ok;
+              if (live) break;
+              flag(a.status, JET_ERR_DEVICE);  // the list holds an item the layout lacks
             }
-            q_sent = progressed = true;
           }
-          if (jk < e.ntiles) {
-            const int s = (T + jk) % NK;
-            const uint32_t ph = ((T + jk) / NK) & 1;
-            if (mbar_test(sh.k_empty + s, ph ^ 1u)) {
-              uint8_t* ks = smem + G::kOffK + s * G::kTile;
-              mbar_arrive_expect_tx(sh.k_full + s, G::kTile);
-              if (jk < e.nct) {
-#pragma unroll
-                for (int sl = 0; sl < DH / 64; ++sl)
-                  tma_load_3d(ks + sl * (KC * 128), &tmKc, sh.k_full + s, sl * 64, e.kh,
-                              e.f_begin + jk * KC, pol);
-              } else {
-                const int key = e.p0 + e.k_begin + (jk - e.nct) * KT;
-#pragma unroll
-                for (int sl = 0; sl < (DH + 127) / 128; ++sl)
-                  tma_load_3d(ks + sl * (KT * 128), &tmK, sh.k_full + s, sl * 128, e.kh, key, pol);
+        } else {
+          // dealt out back and forth, as the bf16 kernel does
+          const int n = int(gridDim.x);
+          const int k = u * n + ((u & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
+          int4 it;
+          if (k < a.n_all && nth_item(a, k, lane, window, &it, &e)) {
+            live = e.ok;
+            if (!live && lane == 0) flag(a.status, JET_ERR_DEVICE);
+          }
+        }
+        int fed = 0;
+        if (lane == 0) {
+          if (live) {
+            if (e.nct > 0) {
+              // the fed tokens that a row of this block sees: up to its last row's own,
+              // from the first of its first row's candidate on
+              fed = e.row0 + e.nv / g - 1;
+              int lo = 0;
+              if (fed > KC && e.row0 > 0) {
+                const int c = a.row_cand[e.n0 + e.row0];
+                if (c >= 0 && c < a.C)
+                  lo = min(max(a.cand_row_offset[c] - e.n0 - 1, 0), fed);
               }
-              k_issued |= 1u << s;
-              k_par = (k_par & ~(1u << s)) | (ph << s);
-              ++jk;
-              progressed = true;
+              e.f_begin += lo;
+              fed -= lo;
             }
+            e.nct = (fed + KC - 1) / KC;
+            e.npt = (e.k_end - e.k_begin + KT - 1) / KT;
+            e.ntiles = e.npt + e.nct;
           }
-          if (jv < jk) {
-            const int s = (T + jv) % NV;
-            const uint32_t ph = ((T + jv) / NV) & 1;
-            if (mbar_test(sh.v_empty + s, ph ^ 1u)) {
-              uint8_t* vs = smem + G::kOffV + s * G::kTile;
-              mbar_arrive_expect_tx(sh.v_full + s, G::kTile);
-              if (jv < e.nct) {
-#pragma unroll
-                for (int sl = 0; sl < DH / 64; ++sl)
-                  tma_load_3d(vs + sl * (KC * 128), &tmVc, sh.v_full + s, sl * 64, e.kh,
-                              e.f_begin + jv * KC, pol);
-              } else {
-                const int key = e.p0 + e.k_begin + (jv - e.nct) * KT;
-#pragma unroll
-                for (int sl = 0; sl < (DH + 127) / 128; ++sl)
-                  tma_load_3d(vs + sl * (KT * 128), &tmV, sh.v_full + s, sl * 128, e.kh, key, pol);
+          sh.ring[slot].e = e;
+          sh.ring[slot].fed = fed;
+          sh.ring[slot].live = live;
+          mbar_arrive(sh.item_full + slot);
+          if (live) {  // the query block on its way into L2
+  #pragma unroll
+            for (int sl = 0; sl < DH / 64; ++sl)
+              tma_prefetch_3d(&tmQ, sl * 64, e.kh * g, e.n0 + e.row0);
+          }
+        }
+        if (!__shfl_sync(0xffffffffu, live ? 1 : 0, 0)) break;
+        // What the other warps need a little later, and would wait for memory to know: the
+        // fed tokens that each vector sees, and V's unit, the largest exponent of the
+        // item's blocks and of its candidates' values
+        {
+          __syncwarp();
+          const ItemGeo& it = sh.ring[slot].e;
+          fed = __shfl_sync(0xffffffffu, fed, 0);
+          const int f_begin = it.f_begin;
+          const int blocks = (it.k_end - it.k_begin + kKvBlock - 1) / kKvBlock;
+          if (fed > 0) {
+            for (int i = lane; i < it.nv; i += 32) {
+              const int n = it.n0 + (it.vbase + i) / g;
+              const int c = a.row_cand[n];
+              int from = 0, end = 0;  // none: shared row
+              if (c >= 0 && c < a.C) {
+                from = min(max(a.cand_row_offset[c] - it.r - 1 - f_begin, 0), fed);  // y_{c,1}
+                end = min(n - it.r - f_begin, fed);  // past the row's own fed token
               }
-              v_issued |= 1u << s;
-              v_par = (v_par & ~(1u << s)) | (ph << s);
-              ++jv;
-              progressed = true;
+              sh.sees[slot][i] = make_int2(from, end);
             }
           }
-          if (!progressed) __nanosleep(100);
-          if (clk.expired(progressed, abort_flag, a.wait_ns)) {
+          const uint8_t* ex =
+              a.v_exp + size_t(kv_place(it.p0, it.r, it.k_begin / kKvBlock)) * a.Hkv + it.kh;
+          int vx = kKvLow + 127;
+          for (int b = lane; b < blocks; b += 32) vx = max(vx, int(ex[size_t(b) * a.Hkv]));
+          vx = __reduce_max_sync(0xffffffffu, vx);
+          uint32_t top = 0;  // two magnitudes
+          const __nv_bfloat16* vc = a.v_cand + (size_t(f_begin) * a.Hkv + it.kh) * DH;
+#pragma unroll 4
+          for (int i = lane; i < fed * (DH / 8); i += 32) {
+            const uint4 v = *reinterpret_cast<const uint4*>(
+                vc + size_t(i / (DH / 8)) * a.Hkv * DH + 8 * (i % (DH / 8)));
+            top = __vmaxu2(__vmaxu2(top, v.x & 0x7fff7fffu), v.y & 0x7fff7fffu);
+            top = __vmaxu2(__vmaxu2(top, v.z & 0x7fff7fffu), v.w & 0x7fff7fffu);
+          }
+          top = __reduce_max_sync(0xffffffffu, max(top & 0xffff0000u, top << 16));
+          const int cx = top ? kv_exponent(top) + 127 : 0;
+          // Every row of the block sees the chunk's keys, but not every candidate: values
+          // that would cost the others digits (f16 has room for 2^8 of the prefix's
+          // largest), or are not finite, stay out of the product
+          const bool apart = top >= 0x7f800000u || cx > vx + 8;
+          if (lane == 0) {
+            sh.vx[slot] = min(max((apart ? vx : max(vx, cx)) - 127, kKvLow), kKvHigh);
+            sh.apart[slot] = apart;
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(sh.aux_full + slot);
+        }
+      }
+    } else if (warp == kProdWarp) {
+      // ---------------------------------------------------------------- producer
+      if (elect_one()) {
+        const uint64_t pol = policy_evict_first();
+        uint32_t k_issued = 0, k_par = 0, v_issued = 0, v_par = 0, q_issued = 0, q_par = 0;
+        int T = 0;  // tiles of earlier items
+        bool ok = true;
+        for (int u = 0; ok; ++u) {
+          const int slot = u & 1;
+          if (!wait1(sh.item_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
             ok = false;
             break;
           }
+          if (!sh.ring[slot].live) break;
+          const ItemGeo e = sh.ring[slot].e;
+          // K_j, V_j and the query block are issued as soon as their places drain
+          int jk = 0, jv = 0;
+          bool q_sent = false;
+          IdleClock clk;
+          while (jv < e.ntiles || !q_sent) {
+            bool progressed = false;
+            if (!q_sent && (u == 0 || mbar_test(&sh.q_free, (u - 1) & 1))) {
+              if (!(u == 0 && a.hold_first)) {  // test hook: the first block never lands
+                mbar_arrive_expect_tx(&sh.q_full, uint32_t(R * (DH / 64)) * 64 * 2 * g * rb);
+  #pragma unroll
+                for (int c = 0; c < R; ++c)
+  #pragma unroll
+                  for (int sl = 0; sl < DH / 64; ++sl)
+                    tma_load_3d(smem + sl * (kBV * 128) + c * RV * 128, &tmQ, &sh.q_full, sl * 64,
+                                e.kh * g, e.n0 + e.row0, pol);
+                q_issued = 1;
+                q_par = u & 1;
+              }
+              q_sent = progressed = true;
+            }
+            if (jk < e.ntiles) {
+              const int s = (T + jk) % NK;
+              const uint32_t ph = ((T + jk) / NK) & 1;
+              if (mbar_test(sh.k_empty + s, ph ^ 1u)) {
+                uint8_t* ks = smem + G::kOffK + s * G::kTile;
+                mbar_arrive_expect_tx(sh.k_full + s, G::kTile);
+                if (jk < e.nct) {
+  #pragma unroll
+                  for (int sl = 0; sl < DH / 64; ++sl)
+                    tma_load_3d(ks + sl * (KC * 128), &tmKc, sh.k_full + s, sl * 64, e.kh,
+                                e.f_begin + jk * KC, pol);
+                } else {
+                  const int key = e.p0 + e.k_begin + (jk - e.nct) * KT;
+  #pragma unroll
+                  for (int sl = 0; sl < (DH + 127) / 128; ++sl)
+                    tma_load_3d(ks + sl * (KT * 128), &tmK, sh.k_full + s, sl * 128, e.kh, key,
+                                pol);
+                }
+                k_issued |= 1u << s;
+                k_par = (k_par & ~(1u << s)) | (ph << s);
+                ++jk;
+                progressed = true;
+              }
+            }
+            if (jv < jk) {
+              const int s = (T + jv) % NV;
+              const uint32_t ph = ((T + jv) / NV) & 1;
+              if (mbar_test(sh.v_empty + s, ph ^ 1u)) {
+                uint8_t* vs = smem + G::kOffV + s * G::kTile;
+                mbar_arrive_expect_tx(sh.v_full + s, G::kTile);
+                if (jv < e.nct) {
+  #pragma unroll
+                  for (int sl = 0; sl < DH / 64; ++sl)
+                    tma_load_3d(vs + sl * (KC * 128), &tmVc, sh.v_full + s, sl * 64, e.kh,
+                                e.f_begin + jv * KC, pol);
+                } else {
+                  const int key = e.p0 + e.k_begin + (jv - e.nct) * KT;
+  #pragma unroll
+                  for (int sl = 0; sl < (DH + 127) / 128; ++sl)
+                    tma_load_3d(vs + sl * (KT * 128), &tmV, sh.v_full + s, sl * 128, e.kh, key,
+                                pol);
+                }
+                v_issued |= 1u << s;
+                v_par = (v_par & ~(1u << s)) | (ph << s);
+                ++jv;
+                progressed = true;
+              }
+            }
+            if (!progressed) __nanosleep(100);
+            if (clk.expired(progressed, abort_flag, a.wait_ns)) {
+              ok = false;
+              break;
+            }
+          }
+          if (!ok) break;
+          mbar_arrive(sh.item_empty + slot);
+          T += e.ntiles;
         }
-        if (!ok) break;
-        mbar_arrive(sh.item_empty + slot);
-        T += e.ntiles;
-      }
-      if (!ok) {
-        sh.abort = 1;
-        flag(a.status, JET_ERR_TIMEOUT);
-        // let every copy already issued land before the CTA can exit
+        if (!ok) {
+          sh.abort = 1;
+          flag(a.status, JET_ERR_TIMEOUT);
+        }
+        // let every copy issued land before the CTA can exit (where no wait ran out they are
+        // used by now)
         if (q_issued) mbar_wait(&sh.q_full, q_par, kDrainNs, nullptr);
         for (int t = 0; t < NK; ++t)
           if (k_issued & (1u << t)) mbar_wait(sh.k_full + t, (k_par >> t) & 1u, kDrainNs, nullptr);
         for (int t = 0; t < NV; ++t)
           if (v_issued & (1u << t)) mbar_wait(sh.v_full + t, (v_par >> t) & 1u, kDrainNs, nullptr);
       }
-    }
-  } else if (warp == kMmaWarp) {
-    // ---------------------------------------------------------------- scores
-    if (elect_one()) {
-      constexpr uint32_t id_s = idesc_e4m3_f32(kBV, KT);
-      constexpr uint32_t id_c = idesc_bf16_f32(kBV, KC);
-      const uint64_t q0 = desc_k_sw128(smem_u32(smem));
-      const uint64_t kc0 = desc_k_sw128(smem_u32(smem + G::kOffK));
-      const uint64_t k0 = DH == 64 ? desc_k_sw64(smem_u32(smem + G::kOffK)) : kc0;
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        return wait1(bar, parity, a.wait_ns, abort_flag);
-      };
-      bool ok = true;
-      int T = 0;
-      for (int u = 0; ok; ++u) {
-        const int slot = u & 1;
-        ok = wait(sh.item_full + slot, (u >> 1) & 1);
-        if (!ok || !sh.ring[slot].live) break;
-        const int nct = sh.ring[slot].e.nct, ntiles = sh.ring[slot].e.ntiles;
-        if (nct == 0) mbar_arrive(&sh.q_free);  // only the split reads the bf16 block
-        for (int j = 0; j < ntiles; ++j) {
-          const int Tj = T + j, b = Tj % NS, kb = Tj % NK;
-          ok = (j > 0 && j != nct) || wait(j < nct ? &sh.q_full : &sh.qt_full, u & 1);
-          ok = ok && wait(sh.k_full + kb, (Tj / NK) & 1) &&
-               wait(sh.pv_done + b, ((Tj / NS) & 1) ^ 1u);
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t d = tmem + G::kSCol + b * KT;
-          // (a descriptor of another address: its low field counts 16 bytes)
-          if (j < nct) {
-            const uint64_t kd = kc0 + kb * (G::kTile >> 4);
-#pragma unroll
-            for (int st = 0; st < DH / 16; ++st) {
-              const int sl = st >> 2, k = st & 3;
-              mma_f16(d, q0 + ((sl * (kBV * 128) + 32 * k) >> 4),
-                      kd + ((sl * (KC * 128) + 32 * k) >> 4), id_c, st != 0);
+    } else if (warp == kMmaWarp) {
+      // ---------------------------------------------------------------- scores
+      if (elect_one()) {
+        constexpr uint32_t id_s = idesc_e4m3_f32(kBV, KT);
+        constexpr uint32_t id_c = idesc_bf16_f32(kBV, KC);
+        const uint64_t q0 = desc_k_sw128(smem_u32(smem));
+        const uint64_t kc0 = desc_k_sw128(smem_u32(smem + G::kOffK));
+        const uint64_t k0 = DH == 64 ? desc_k_sw64(smem_u32(smem + G::kOffK)) : kc0;
+        auto wait = [&](uint64_t* bar, uint32_t parity) {
+          return wait1(bar, parity, a.wait_ns, abort_flag);
+        };
+        bool ok = true;
+        int T = 0;
+        for (int u = 0; ok; ++u) {
+          const int slot = u & 1;
+          ok = wait(sh.item_full + slot, (u >> 1) & 1);
+          if (!ok || !sh.ring[slot].live) break;
+          const int nct = sh.ring[slot].e.nct, ntiles = sh.ring[slot].e.ntiles;
+          if (nct == 0) mbar_arrive(&sh.q_free);  // only the split reads the bf16 block
+          for (int j = 0; j < ntiles; ++j) {
+            const int Tj = T + j, b = Tj % NS, kb = Tj % NK;
+            ok = (j > 0 && j != nct) || wait(j < nct ? &sh.q_full : &sh.qt_full, u & 1);
+            ok = ok && wait(sh.k_full + kb, (Tj / NK) & 1) &&
+                 wait(sh.pv_done + b, ((Tj / NS) & 1) ^ 1u);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t d = tmem + G::kSCol + b * KT;
+            // (a descriptor of another address: its low field counts 16 bytes)
+            if (j < nct) {
+              const uint64_t kd = kc0 + kb * (G::kTile >> 4);
+  #pragma unroll
+              for (int st = 0; st < DH / 16; ++st) {
+                const int sl = st >> 2, k = st & 3;
+                mma_f16(d, q0 + ((sl * (kBV * 128) + 32 * k) >> 4),
+                        kd + ((sl * (KC * 128) + 32 * k) >> 4), id_c, st != 0);
+              }
+              if (j == nct - 1) mma_commit(&sh.q_free);
+            } else {
+              const uint64_t kd = k0 + kb * (G::kTile >> 4);
+  #pragma unroll
+              for (int st = 0; st < DH / 16; ++st) {  // hi, then lo, over the same keys
+                const int kk = st % (DH / 32);
+                mma_e4m3_ta(d, tmem + G::kQCol + uint32_t(8 * st),
+                            kd + (((kk >> 2) * (KT * 128) + 32 * (kk & 3)) >> 4), id_s, st != 0);
+              }
             }
-            if (j == nct - 1) mma_commit(&sh.q_free);
-          } else {
-            const uint64_t kd = k0 + kb * (G::kTile >> 4);
-#pragma unroll
-            for (int st = 0; st < DH / 16; ++st) {  // hi, then lo, over the same keys
-              const int kk = st % (DH / 32);
-              mma_e4m3_ta(d, tmem + G::kQCol + uint32_t(8 * st),
-                          kd + (((kk >> 2) * (KT * 128) + 32 * (kk & 3)) >> 4), id_s, st != 0);
-            }
+            mma_commit(sh.s_full + b);
+            mma_commit(sh.k_empty + kb);
+            if (j == ntiles - 1) mma_commit(&sh.qt_free);
           }
-          mma_commit(sh.s_full + b);
-          mma_commit(sh.k_empty + kb);
-          if (j == ntiles - 1) mma_commit(&sh.qt_free);
+          if (!ok) break;
+          mbar_arrive(sh.item_empty + slot);
+          T += ntiles;
         }
-        if (!ok) break;
-        mbar_arrive(sh.item_empty + slot);
-        T += ntiles;
-      }
-      if (!ok) {
-        sh.abort = 1;
-        flag(a.status, JET_ERR_TIMEOUT);
-        mma_commit(sh.drain);
+        if (!ok) {
+          sh.abort = 1;
+          flag(a.status, JET_ERR_TIMEOUT);
+        }
+        mma_commit(sh.drain);  // nor may its products outlive it
         mbar_wait(sh.drain, 0, kDrainNs, nullptr);
       }
-    }
-  } else if (warp == kPvWarp) {
-    // ---------------------------------------------------------------- outputs
-    if (elect_one()) {
-      constexpr uint32_t id_o = idesc_f16_f32_mn(kBV, DH);
-      const uint64_t v0 = desc_mn_sw128(smem_u32(smem + G::kOffW), KT * 128);
-      const uint64_t vc0 = desc_mn_sw128(smem_u32(smem + G::kOffW), KC * 128);
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        return wait1(bar, parity, a.wait_ns, abort_flag);
-      };
-      bool ok = true;
-      int T = 0;
-      for (int u = 0; ok; ++u) {
-        const int slot = u & 1;
-        ok = wait(sh.item_full + slot, (u >> 1) & 1);
-        if (!ok || !sh.ring[slot].live) break;
-        const int nct = sh.ring[slot].e.nct, ntiles = sh.ring[slot].e.ntiles;
-        for (int j = 0; j < ntiles; ++j) {
-          const int Tj = T + j, b = Tj % NS, w = Tj % NW;
-          // the item's first P V overwrites O: the previous item's O must be out
-          ok = j > 0 || u == 0 || wait(&sh.o_free, (u - 1) & 1);
-          ok = ok && wait(sh.w_full + w, (Tj / NW) & 1) && wait(sh.p_full + b, (Tj / NS) & 1);
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t pt = tmem + G::kSCol + b * KT;
-          const uint64_t vd = (j < nct ? vc0 : v0) + w * (2 * G::kTile >> 4);
-#pragma unroll
-          for (int k = 0; k < KC / 16; ++k)
-            mma_f16_ta(tmem, pt + uint32_t(8 * k), vd + (k * 2048 >> 4), id_o, (j | k) != 0);
-          if (j >= nct) {
-#pragma unroll
-            for (int k = KC / 16; k < KT / 16; ++k)
-              mma_f16_ta(tmem, pt + uint32_t(8 * k), vd + (k * 2048 >> 4), id_o, 1);
+    } else if (warp == kPvWarp) {
+      // ---------------------------------------------------------------- outputs
+      if (elect_one()) {
+        constexpr uint32_t id_o = idesc_f16_f32_mn(kBV, DH);
+        const uint64_t v0 = desc_mn_sw128(smem_u32(smem + G::kOffW), KT * 128);
+        const uint64_t vc0 = desc_mn_sw128(smem_u32(smem + G::kOffW), KC * 128);
+        auto wait = [&](uint64_t* bar, uint32_t parity) {
+          return wait1(bar, parity, a.wait_ns, abort_flag);
+        };
+        bool ok = true;
+        int T = 0;
+        for (int u = 0; ok; ++u) {
+          const int slot = u & 1;
+          ok = wait(sh.item_full + slot, (u >> 1) & 1);
+          if (!ok || !sh.ring[slot].live) break;
+          const int nct = sh.ring[slot].e.nct, ntiles = sh.ring[slot].e.ntiles;
+          for (int j = 0; j < ntiles; ++j) {
+            const int Tj = T + j, b = Tj % NS, w = Tj % NW;
+            // the item's first P V overwrites O: the previous item's O must be out
+            ok = j > 0 || u == 0 || wait(&sh.o_free, (u - 1) & 1);
+            ok = ok && wait(sh.w_full + w, (Tj / NW) & 1) && wait(sh.p_full + b, (Tj / NS) & 1);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t pt = tmem + G::kSCol + b * KT;
+            const uint64_t vd = (j < nct ? vc0 : v0) + w * (2 * G::kTile >> 4);
+  #pragma unroll
+            for (int k = 0; k < KC / 16; ++k)
+              mma_f16_ta(tmem, pt + uint32_t(8 * k), vd + (k * 2048 >> 4), id_o, (j | k) != 0);
+            if (j >= nct) {
+  #pragma unroll
+              for (int k = KC / 16; k < KT / 16; ++k)
+                mma_f16_ta(tmem, pt + uint32_t(8 * k), vd + (k * 2048 >> 4), id_o, 1);
+            }
+            mma_commit(sh.pv_done + b);
           }
-          mma_commit(sh.pv_done + b);
+          if (!ok) break;
+          mbar_arrive(sh.item_empty + slot);
+          T += ntiles;
         }
-        if (!ok) break;
-        mbar_arrive(sh.item_empty + slot);
-        T += ntiles;
-      }
-      if (!ok) {
-        sh.abort = 1;
-        flag(a.status, JET_ERR_TIMEOUT);
-        mma_commit(sh.drain + 1);
+        if (!ok) {
+          sh.abort = 1;
+          flag(a.status, JET_ERR_TIMEOUT);
+        }
+        mma_commit(sh.drain + 1);  // nor may its products outlive it
         mbar_wait(sh.drain + 1, 0, kDrainNs, nullptr);
       }
     }
-  }
   } else if (warp >= kWideWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     // ---------------------------------------------------------------- queries and V
@@ -738,10 +758,9 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       if (!sh.ring[slot].live) break;
       const ItemGeo e = sh.ring[slot].e;
       const int fed = sh.ring[slot].fed, keys = e.k_end - e.k_begin;
-      const uint8_t* ex = a.v_exp + size_t(kv_place(e.p0, e.r, e.k_begin / kBN)) * a.Hkv + e.kh;
+      const uint8_t* ex = a.v_exp + size_t(kv_place(e.p0, e.r, e.k_begin / kKvBlock)) * a.Hkv + e.kh;
       const int blocks = (keys + kKvBlock - 1) / kKvBlock;
       uint32_t byte = block < blocks ? load_ahead(ex + size_t(block) * a.Hkv) : 0;
-      if (lane == 0) sh.bad[slot][wi] = 0;
       if (!wait32(&sh.q_full, u & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
@@ -850,9 +869,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         const uint8_t* vs = smem + G::kOffV + (Tj % NV) * G::kTile;
         uint8_t* ws = smem + G::kOffW + (Tj % NW) * 2 * G::kTile;
         // candidate values, in the places the product reads
-        const int left = fed - j * KC;
+        const int left = sh.apart[slot] ? 0 : fed - j * KC;
         const float inv = pow2(-vx);
-        bool found = false;
 #pragma unroll 2
         for (int k = 0; k < kMine; ++k) {
           const int i = t + k * kWideThreads;
@@ -861,15 +879,12 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           uint32_t y[4];
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const bool n0 = nonfinite_bf16(in[q]), n1 = nonfinite_bf16(in[q] >> 16);
-            found |= n0 | n1;
-            y[q] = pack_f16(n0 ? 0.f : __uint_as_float(in[q] << 16) * inv,
-                            n1 ? 0.f : __uint_as_float(in[q] & 0xffff0000u) * inv);
+            y[q] = pack_f16(__uint_as_float(in[q] << 16) * inv,
+                            __uint_as_float(in[q] & 0xffff0000u) * inv);
             if (((i >> 3) & (KC - 1)) >= left) y[q] = 0u;
           }
           *reinterpret_cast<uint4*>(ws + 16 * i) = make_uint4(y[0], y[1], y[2], y[3]);
         }
-        if (__any_sync(0xffffffffu, found) && lane == 0) sh.bad[slot][wi] = 1;
         done(Tj);
       }
       if (!ok) break;
@@ -940,12 +955,13 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       const ItemGeo& e = sh.ring[slot].e;  // (read again where needed: registers are few)
       const int nct = e.nct, ntiles = e.ntiles, keys = e.k_end - e.k_begin, f_begin = e.f_begin;
       const bool valid = i < e.nv;
-      const bool some = q4 * 32 % RV < e.nv;  // a warp without vectors only keeps the barriers going
+      // a warp without vectors only keeps the barriers going
+      const bool some = q4 * 32 % RV < e.nv;
       if (nct > 0 && !wait32(sh.aux_full + slot, (u >> 1) & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
       }
-      const uint8_t* ex = a.k_exp + size_t(kv_place(e.p0, e.r, e.k_begin / kBN)) * a.Hkv + e.kh;
+      const uint8_t* ex = a.k_exp + size_t(kv_place(e.p0, e.r, e.k_begin / kKvBlock)) * a.Hkv + e.kh;
       constexpr int kCols = G::kHalf / R;
       const int col0 = kCols * copy;  // of this half's
       // this half's blocks of the tiles: every tile's (d 256), or every second block
@@ -1140,10 +1156,62 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       }
       tc_fence_after();
       if (some) {
-        bool bad = false;
-        if (nct > 0) {
+        float2 scale = make_float2(inv * (plain ? unit : 1.f), inv * (plain ? unit : 1.f));
+        bool rest = !plain;  // V's unit still to come
+        if (__builtin_expect(nct > 0 && sh.apart[slot], 0)) {
+          // O normalised where it is, then the candidates' tokens one by one, each weight
+          // from its key and the row's query
+#pragma unroll 1
+          for (int c0 = half * (DH / 2); c0 < (half + 1) * (DH / 2); c0 += 16) {
+            float ov[16];
+            tmem_ld_16cols(tmem + lane_off + c0, ov);
+            tmem_wait_ld();
 #pragma unroll
-          for (int w = 0; w < 8; ++w) bad |= sh.bad[slot][w] != 0;
+            for (int c = 0; c < 16; ++c) ov[c] = ov[c] * inv * unit;
+            tmem_st_16cols(tmem + lane_off + c0, ov);
+          }
+          scale = make_float2(1.f, 1.f);
+          rest = false;
+          const int2 sees = valid ? sh.sees[slot][i] : make_int2(0, 0);
+          const int first = __reduce_min_sync(0xffffffffu, sees.x < sees.y ? sees.x : INT_MAX);
+          const int end = __reduce_max_sync(0xffffffffu, sees.y);
+          const int gv = e.vbase + min(i, e.nv - 1);
+          const uint4* q = reinterpret_cast<const uint4*>(
+              a.q + (size_t(e.n0 + gv / g) * a.Hq + e.kh * g + gv % g) * DH);
+          const float sub = m == -INFINITY ? 0.f : kWeightLog2 - m;
+#pragma unroll 1
+          for (int f = first; f < end; ++f) {
+            const size_t at = (size_t(f_begin + f) * a.Hkv + e.kh) * DH;
+            const uint4* kc = reinterpret_cast<const uint4*>(a.k_cand + at);
+            float s = 0.f;
+#pragma unroll 1
+            for (int c = 0; c < DH / 8; ++c) {
+              const uint4 x = q[c], y = kc[c];
+              const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                s = fmaf(__uint_as_float(xw[k] << 16), __uint_as_float(yw[k] << 16), s);
+                s = fmaf(__uint_as_float(xw[k] & 0xffff0000u),
+                         __uint_as_float(yw[k] & 0xffff0000u), s);
+              }
+            }
+            const bool mine = f >= sees.x && f < sees.y && f % KC / kCols == copy;
+            const float w = ex2(fmaf(s, a.scale_log2, sub)) * inv;
+#pragma unroll 1
+            for (int c0 = half * (DH / 2); c0 < (half + 1) * (DH / 2); c0 += 16) {
+              float ov[16];
+              tmem_wait_st();
+              tmem_ld_16cols(tmem + lane_off + c0, ov);
+              tmem_wait_ld();
+#pragma unroll
+              for (int c = 0; c < 16; ++c) {
+                const float x = __bfloat162float(a.v_cand[at + c0 + c]);
+                if (mine) ov[c] += isfinite(x) ? w * x : x;
+              }
+              tmem_st_16cols(tmem + lane_off + c0, ov);
+            }
+          }
+          tmem_wait_st();
         }
         // 64 bytes of each vector at a time through this warp's 2 KB stage: four 16-byte
         // pieces a row, rotated so that eight lanes meet different banks
@@ -1167,7 +1235,6 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           __syncwarp();
         };
         // each of a row's two warps writes half of the columns
-        const float2 scale = make_float2(inv * (plain ? unit : 1.f), inv * (plain ? unit : 1.f));
         const float2 zero = make_float2(0.f, 0.f);
 #pragma unroll 1
         for (int c0 = half * (DH / 2); c0 < (half + 1) * (DH / 2); c0 += 32) {
@@ -1180,20 +1247,9 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
             ov[c] = y.x;
             ov[c + 1] = y.y;
           }
-          if (!plain) {
+          if (rest) {
 #pragma unroll
             for (int c = 0; c < 32; ++c) ov[c] *= unit;
-          }
-          if (bad) {  // the non-finite values of the tokens this row sees
-            const int2 sees = sh.sees[slot][i];
-            for (int f = f_begin + sees.x; f < f_begin + sees.y; ++f) {
-              const __nv_bfloat16* v = a.v_cand + (size_t(f) * a.Hkv + e.kh) * DH + c0;
-#pragma unroll
-              for (int c = 0; c < 32; ++c) {
-                const float x = __bfloat162float(v[c]);
-                if (!isfinite(x)) ov[c] += x;
-              }
-            }
           }
           if (direct) {
             uint4 x[4];
@@ -1304,6 +1360,8 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
   a.scale_log2 = 1.4426950408889634f / sqrtf(float(DH));
   a.k_exp = static_cast<const uint8_t*>(k8) + exp_off;
   a.v_exp = static_cast<const uint8_t*>(v8) + exp_off;
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.k_cand = static_cast<const __nv_bfloat16*>(k_cand);
   a.v_cand = static_cast<const __nv_bfloat16*>(v_cand);
   // the work list follows the (m, l) partials in the workspace
   uintptr_t ctrl = reinterpret_cast<uintptr_t>(a.ml_part + vecs);
@@ -1327,8 +1385,8 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
   e = cudaFuncSetAttribute(attend_kv8_kernel<DH, R>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            int(smem));
   if (e != cudaSuccess) return e;
-  e = launch_pdl(attend_kv8_kernel<DH, R>, dim3(grid), dim3(kThreads), smem, st, tmQ, tmK, tmV, tmKc,
-                 tmVc, a);
+  e = launch_pdl(attend_kv8_kernel<DH, R>, dim3(grid), dim3(kThreads), smem, st, tmQ, tmK, tmV,
+                 tmKc, tmVc, a);
   if (e != cudaSuccess || plan.splits * R <= 1) return e;
   const long long blocks = ((long long)n.N * d.Hq + 3) / 4;
   return launch_pdl(attend_combine_kernel<DH>, dim3(unsigned(blocks)), dim3(128), 0, st,
@@ -1352,8 +1410,6 @@ cudaError_t launch_attend_kv8_tc(const jet_layout& lay, const jet_dims& d, const
   JET_KV8(128, 2);
   JET_KV8(128, 4);
   JET_KV8(256, 1);
-  JET_KV8(256, 2);
-  JET_KV8(256, 4);
 #undef JET_KV8
   return cudaErrorInvalidValue;
 }

@@ -13,6 +13,7 @@
 // exp-weighted values) that the merge kernel combines with the short causal
 // candidate part by the usual log-sum-exp rescaling.
 #include <algorithm>
+#include <cmath>
 
 #include "jet_device.cuh"
 #include "jet_internal.h"
@@ -396,10 +397,49 @@ AttnPlan attn_plan(const jet_sizes& n, const jet_dims& d) {
   return p;
 }
 
+// The 8-bit cache's plan. A request's prefix is cut in as many near-equal chunks as give
+// the least estimated time, in us: an item (2 us, and per 64 keys 0.6 at d 256, 0.3 at 64
+// and 128) bounds it from below; with more items than SMs their sum's share of an SM counts,
+// and what the schedule leaves uneven (0.3 of an item where chunks are whole requests in
+// the order of their lengths, 0.7 else); chunks cost the combine's launch (1 us) and their
+// partials' way out and back (0.3 us a MB). Fitted to 58 batches of 1 to 120 requests of
+// 200 to 8,192 keys at up to 11 chunk lengths each: the chosen ones take 3.5 % (d 256)
+// and 1 % (64 and 128) more than the best, the bf16 cache's plan 25 % more (64 requests of
+// 1,500 keys, four kv heads: 75.8 us unsplit, 103.3 in its chunks; eight of 300 - 1,200:
+// 24.2 and 29.1; one of 6,000, two kv heads: 22.0 and 23.0).
 AttnPlan attn_plan_kv8(const jet_sizes& n, const jet_dims& d) {
-  AttnPlan p = attn_plan(n, d);
+  AttnPlan p{};
   p.copies = 1;
-  if (d.dtype != JET_DTYPE_BF16 || n.R <= 0 || n.N <= 0) return p;
+  if (d.dtype != JET_DTYPE_BF16 || n.R <= 0 || n.N <= 0 || d.Hkv <= 0 || d.Hq <= 0) {
+    p = attn_plan(n, d);
+    p.copies = 1;
+    return p;
+  }
+  const int g = d.Hq / d.Hkv;
+  const int qv = std::max(1, attn_tc_block() / g) * g;  // query vectors per CTA: whole rows
+  p.qgroups = (n.max_rows * g + qv - 1) / qv;
+  const double avg = double(n.total_prefix) / n.R;
+  const double vecs = double(n.N) * g / n.R;
+  const double groups = double(n.R) * d.Hkv * std::max(1.0, std::ceil(vecs / qv));
+  const double key_us = (d.d == 256 ? 0.6 : 0.3) / 64;
+  const double partial_us = 0.3e-6 * 8 * double(n.N) * d.Hq * d.d;
+  const int tiles = std::max(1, (n.max_prefix + 63) / 64);
+  double best = 0;
+  for (int s = 1; s <= std::max(1, tiles / 3); ++s) {  // chunks of 192 keys or more
+    const int chunk = (tiles + s - 1) / s * 64, splits = (tiles * 64 + chunk - 1) / chunk;
+    if (splits != s) continue;  // as with fewer, longer chunks
+    const double per = s > 1 ? std::max(1.0, avg / chunk + 0.5) : 1.0;  // of a request
+    const double item = 2 + std::min(chunk, n.max_prefix) * key_us, items = groups * per;
+    double t = item;
+    if (items > kPlanSMs)
+      t = std::max(t, (groups * avg * key_us + items * 2) / kPlanSMs + (s > 1 ? 0.7 : 0.3) * item);
+    if (s > 1) t += 1 + per * partial_us;
+    if (s == 1 || t < best) {
+      best = t;
+      p.chunk = chunk;
+      p.splits = splits;
+    }
+  }
   // Few query vectors leave softmax warps without any. Then a block holds its vectors two
   // or four times over, and each copy takes its part of a tile's keys: the copies leave
   // partials that the combine joins like chunks. That pays at d 64 and 128 once an SM has
@@ -410,13 +450,11 @@ AttnPlan attn_plan_kv8(const jet_sizes& n, const jet_dims& d) {
   // 64 vectors, one and two: 256 of 1,000, d 128 75.8 and 69.6). A tile of d 256 has half
   // the keys for the same bytes, and its copies only break even (64 of 1,000 to 6,000
   // 85.0 and 85.0, one of 6,000 22.5 and 28.7).
-  const int vecs = n.max_rows * (d.Hq / d.Hkv);
+  const int most = n.max_rows * g;
   if (d.d <= 128 && (long long)n.total_prefix * d.Hkv >= 3LL * 128 * kPlanSMs)
-    p.copies = vecs <= 32 ? 4 : vecs <= 64 ? 2 : 1;
-  if (p.copies > 1) {
-    const size_t v = size_t(p.splits) * n.N * d.Hq;
-    p.bytes += (p.copies - 1) * v * (d.d * sizeof(float) + sizeof(float2));
-  }
+    p.copies = most <= 32 ? 4 : most <= 64 ? 2 : 1;
+  const size_t partials = size_t(p.splits) * p.copies * n.N * d.Hq;
+  p.bytes = partials * d.d * sizeof(float) + partials * sizeof(float2);
   return p;
 }
 

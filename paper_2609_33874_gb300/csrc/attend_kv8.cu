@@ -405,7 +405,6 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     if (warp == kSchedWarp) {
       // ---------------------------------------------------------------- scheduler
-      const int count = a.sorted ? *a.item_count : 0;
       ItemWindow window{};
       for (int u = 0;; ++u) {
         const int slot = u & 1;
@@ -418,29 +417,13 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         }
         ItemGeo e{};
         bool live = false;
-        if (a.sorted) {
-          // the CTA's first item is number blockIdx.x, later ones come from the shared
-          // counter, past the grid's first items
-          if (lane == 0) {
-            for (bool first = (u == 0);; first = false) {
-              const int idx = first ? int(blockIdx.x) : int(gridDim.x) + atomicAdd(a.item_next, 1);
-              if (idx >= count) break;
-              bool fits;
-              e = item_geo(a, a.items[idx], &fits);
-              live = e.ok;
-              if (live) break;
-              flag(a.status, JET_ERR_DEVICE);  // the list holds an item the layout lacks
-            }
-          }
-        } else {
-          // dealt out back and forth, as the bf16 kernel does
-          const int n = int(gridDim.x);
-          const int k = u * n + ((u & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
-          int4 it;
-          if (k < a.n_all && nth_item(a, k, lane, window, &it, &e)) {
-            live = e.ok;
-            if (!live && lane == 0) flag(a.status, JET_ERR_DEVICE);
-          }
+        // dealt out back and forth, as the bf16 kernel does
+        const int n = int(gridDim.x);
+        const int k = u * n + ((u & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
+        int4 it;
+        if (k < a.n_all && nth_item(a, k, lane, window, &it, &e)) {
+          live = e.ok;
+          if (!live && lane == 0) flag(a.status, JET_ERR_DEVICE);
         }
         int fed = 0;
         if (lane == 0) {
@@ -1363,27 +1346,15 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
   a.q = static_cast<const __nv_bfloat16*>(q);
   a.k_cand = static_cast<const __nv_bfloat16*>(k_cand);
   a.v_cand = static_cast<const __nv_bfloat16*>(v_cand);
-  // the work list follows the (m, l) partials in the workspace
-  uintptr_t ctrl = reinterpret_cast<uintptr_t>(a.ml_part + vecs);
-  ctrl = (ctrl + 15) & ~uintptr_t(15);
-  a.item_next = reinterpret_cast<int*>(ctrl);
-  a.item_count = a.item_next + 1;
-  a.items = reinterpret_cast<int4*>(ctrl + 16);
   a.splits = plan.splits;
   a.qgroups = plan.qgroups;
   a.n_all = (long long)n.R * d.Hkv * plan.qgroups * plan.splits;
-  a.sorted = plan.sorted;
   const int sms = sm_count();
   if (sms < 1) return cudaErrorInvalidValue;
   const int grid = int(std::max<long long>(1, std::min<long long>(sms, a.n_all)));
-  cudaError_t e = cudaSuccess;
-  if (a.sorted)
-    e = launch_pdl(attend_items_kernel, dim3(1), dim3(1024), 0, st, static_cast<const AttArgs&>(a),
-                   plan.qgroups, plan.splits);
-  if (e != cudaSuccess) return e;
   const size_t smem = Geo<DH>::kBytes + 1024;
-  e = cudaFuncSetAttribute(attend_kv8_kernel<DH, R>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           int(smem));
+  cudaError_t e = cudaFuncSetAttribute(attend_kv8_kernel<DH, R>,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
   e = launch_pdl(attend_kv8_kernel<DH, R>, dim3(grid), dim3(kThreads), smem, st, tmQ, tmK, tmV,
                  tmKc, tmVc, a);

@@ -120,76 +120,6 @@ __device__ __forceinline__ ItemGeo item_geo(const AttArgs& a, int4 it, bool* fit
   return e;
 }
 
-// The work list: every (request, kv head, query block, chunk) that has keys
-// and vectors, longest first (counting sort on the tile count), for the
-// persistent kernel's dynamic schedule. One block.
-constexpr int kBuckets = 256;
-
-constexpr int kItemCache = 16384;  // candidate items whose bucket stays in shared memory
-
-__device__ __forceinline__ int4 item_of(const AttArgs& a, long long idx, int splits) {
-  const int split = int(idx % splits);
-  const long long rest = idx / splits;
-  const int rk = int(rest % (a.R * a.Hkv));
-  const int qb = int(rest / (a.R * a.Hkv));
-  return make_int4(rk / a.Hkv, rk % a.Hkv, qb, split);
-}
-
-__global__ void __launch_bounds__(1024)
-attend_items_kernel(const AttArgs a, int qgroups, int splits) {
-  pdl_begin();
-  __shared__ int hist[kBuckets];
-  __shared__ int cursor[kBuckets];
-  __shared__ int wsum[kBuckets / 32];
-  __shared__ uint8_t bucket[kItemCache];  // 0: no item, else min(tiles, 255)
-  for (int b = threadIdx.x; b < kBuckets; b += blockDim.x) hist[b] = 0;
-  __syncthreads();
-  const long long n_all = (long long)a.R * a.Hkv * qgroups * splits;
-  for (long long idx = threadIdx.x; idx < n_all; idx += blockDim.x) {
-    bool fits;
-    const ItemGeo e = item_geo(a, item_of(a, idx, splits), &fits);
-    if (!fits) flag(a.status, JET_ERR_DEVICE);  // the request is left out
-    const int b = e.ok ? min(e.ntiles, kBuckets - 1) : 0;
-    if (idx < kItemCache) bucket[idx] = uint8_t(b);
-    if (b > 0) atomicAdd(&hist[b], 1);
-  }
-  __syncthreads();
-  // exclusive scan of the buckets from the longest down (longest items first)
-  if (threadIdx.x < kBuckets) {
-    const int t = threadIdx.x, lane = t & 31, w = t >> 5;
-    const int val = hist[kBuckets - 1 - t];
-    int inc = val;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += y;
-    }
-    if (lane == 31) wsum[w] = inc;
-    __syncwarp();
-    asm volatile("bar.sync 1, %0;" ::"r"(kBuckets) : "memory");
-    int base = 0;
-    for (int i = 0; i < w; ++i) base += wsum[i];
-    cursor[kBuckets - 1 - t] = base + inc - val;
-    if (t == kBuckets - 1) {
-      *a.item_count = base + inc;
-      *a.item_next = 0;
-    }
-  }
-  __syncthreads();
-  for (long long idx = threadIdx.x; idx < n_all; idx += blockDim.x) {
-    const int4 it = item_of(a, idx, splits);
-    int b;
-    if (idx < kItemCache) {
-      b = bucket[idx];
-    } else {
-      bool fits;
-      const ItemGeo e = item_geo(a, it, &fits);
-      b = e.ok ? min(e.ntiles, kBuckets - 1) : 0;
-    }
-    if (b > 0) a.items[atomicAdd(&cursor[b], 1)] = it;
-  }
-}
-
 // The offsets of the requests a lane stands for: its request in the order, its
 // rows [n0, n0 + nr), its prefix [p0, p0 + P) and how it is cut.
 struct LaneReq {

@@ -129,9 +129,8 @@ struct Small {
   float m[2][2][kBV];                    // [tile parity][half] maxima
   float l[2][2][kBV];                    // [item parity][half] sums
   int qx[2][kBV];                        // [item parity] the queries' exponents
-  int vx[2];                             // [item parity] the exponent of V and O
-  int apart[2];                          // [item parity] the candidates' values stay out of
-                                         // P V
+  int vx[2];                             // [item parity] the chunk's largest exponent of V
+  uint32_t vtop[2];                      // [item parity] the candidates' largest value's bits
   uint32_t qmax[2][kBV];                 // [half] largest magnitudes of the queries
   int2 sees[2][kBV];                     // [item parity] the fed tokens a vector sees, from
                                          // f_begin on: first, end
@@ -328,6 +327,34 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
+// The bits of the largest magnitude of the candidate values at tokens [f, f + n), by a
+// warp (of several that step together): the largest that it meets
+template <int DH>
+__device__ __forceinline__ uint32_t cand_top(const Kv8Args& a, int kh, int f, int n, int first,
+                                             int step) {
+  const __nv_bfloat16* v = a.v_cand + (size_t(f) * a.Hkv + kh) * DH;
+  uint32_t top = 0;  // two magnitudes
+#pragma unroll 4
+  for (int i = first; i < n * (DH / 8); i += step) {
+    const uint4 x = *reinterpret_cast<const uint4*>(v + size_t(i / (DH / 8)) * a.Hkv * DH +
+                                                    8 * (i % (DH / 8)));
+    top = __vmaxu2(__vmaxu2(top, x.x & 0x7fff7fffu), x.y & 0x7fff7fffu);
+    top = __vmaxu2(__vmaxu2(top, x.z & 0x7fff7fffu), x.w & 0x7fff7fffu);
+  }
+  return __reduce_max_sync(0xffffffffu, max(top & 0xffff0000u, top << 16));
+}
+
+// The unit of V and O of an item, from its chunk's largest exponent byte and its
+// candidates' largest magnitude, and whether the candidates' values stay out of P V: every
+// row of the block sees the chunk's keys, but not every candidate, so values that would
+// cost the others digits (f16 has room for 2^8 of the prefix's largest), or are not
+// finite, do.
+__device__ __forceinline__ int2 value_unit(int vx, uint32_t top) {
+  const int cx = top ? kv_exponent(top) + 127 : 0;
+  const int apart = top >= 0x7f800000u || cx > vx + 8;
+  return make_int2(min(max((apart ? vx : max(vx, cx)) - 127, kKvLow), kKvHigh), apart);
+}
+
 template <int DH, int R>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -366,7 +393,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(sh.item_full + b, 1);
-      mbar_init(sh.aux_full + b, 1);
+      mbar_init(sh.aux_full + b, 9);     // the scheduler, 8 widening warps
       mbar_init(sh.item_empty + b, 19);  // producer, two MMA threads, 8 softmax, 8 widening warps
     }
     mbar_init(&sh.q_full, 1);
@@ -448,6 +475,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           sh.ring[slot].e = e;
           sh.ring[slot].fed = fed;
           sh.ring[slot].live = live;
+          sh.vtop[slot] = 0;
           mbar_arrive(sh.item_full + slot);
           if (live) {  // the query block on its way into L2
   #pragma unroll
@@ -466,15 +494,15 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           const int f_begin = it.f_begin;
           const int blocks = (it.k_end - it.k_begin + kKvBlock - 1) / kKvBlock;
           if (fed > 0) {
-            for (int i = lane; i < it.nv; i += 32) {
-              const int n = it.n0 + (it.vbase + i) / g;
+            for (int row = lane; row < it.nv / g; row += 32) {
+              const int n = it.n0 + it.row0 + row;
               const int c = a.row_cand[n];
               int from = 0, end = 0;  // none: shared row
               if (c >= 0 && c < a.C) {
                 from = min(max(a.cand_row_offset[c] - it.r - 1 - f_begin, 0), fed);  // y_{c,1}
                 end = min(n - it.r - f_begin, fed);  // past the row's own fed token
               }
-              sh.sees[slot][i] = make_int2(from, end);
+              for (int i = 0; i < g; ++i) sh.sees[slot][row * g + i] = make_int2(from, end);
             }
           }
           const uint8_t* ex =
@@ -482,25 +510,13 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
           int vx = kKvLow + 127;
           for (int b = lane; b < blocks; b += 32) vx = max(vx, int(ex[size_t(b) * a.Hkv]));
           vx = __reduce_max_sync(0xffffffffu, vx);
-          uint32_t top = 0;  // two magnitudes
-          const __nv_bfloat16* vc = a.v_cand + (size_t(f_begin) * a.Hkv + it.kh) * DH;
-#pragma unroll 4
-          for (int i = lane; i < fed * (DH / 8); i += 32) {
-            const uint4 v = *reinterpret_cast<const uint4*>(
-                vc + size_t(i / (DH / 8)) * a.Hkv * DH + 8 * (i % (DH / 8)));
-            top = __vmaxu2(__vmaxu2(top, v.x & 0x7fff7fffu), v.y & 0x7fff7fffu);
-            top = __vmaxu2(__vmaxu2(top, v.z & 0x7fff7fffu), v.w & 0x7fff7fffu);
+          // (the first item's candidates are looked over by the widening warps, which have
+          // nothing else to do yet)
+          if (u > 0) {
+            const uint32_t top = cand_top<DH>(a, it.kh, f_begin, fed, lane, 32);
+            if (lane == 0) sh.vtop[slot] = top;
           }
-          top = __reduce_max_sync(0xffffffffu, max(top & 0xffff0000u, top << 16));
-          const int cx = top ? kv_exponent(top) + 127 : 0;
-          // Every row of the block sees the chunk's keys, but not every candidate: values
-          // that would cost the others digits (f16 has room for 2^8 of the prefix's
-          // largest), or are not finite, stay out of the product
-          const bool apart = top >= 0x7f800000u || cx > vx + 8;
-          if (lane == 0) {
-            sh.vx[slot] = min(max((apart ? vx : max(vx, cx)) - 127, kKvLow), kKvHigh);
-            sh.apart[slot] = apart;
-          }
+          if (lane == 0) sh.vx[slot] = vx;
           __syncwarp();
           if (lane == 0) mbar_arrive(sh.aux_full + slot);
         }
@@ -744,6 +760,11 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       const uint8_t* ex = a.v_exp + size_t(kv_place(e.p0, e.r, e.k_begin / kKvBlock)) * a.Hkv + e.kh;
       const int blocks = (keys + kKvBlock - 1) / kKvBlock;
       uint32_t byte = block < blocks ? load_ahead(ex + size_t(block) * a.Hkv) : 0;
+      if (u == 0 && fed > 0) {
+        const uint32_t top = cand_top<DH>(a, e.kh, e.f_begin, fed, t, kWideThreads);
+        if (lane == 0) atomicMax(&sh.vtop[slot], top);
+      }
+      if (lane == 0) mbar_arrive(sh.aux_full + slot);
       if (!wait32(&sh.q_full, u & 1, a.wait_ns, abort_flag)) {
         ok = false;
         break;
@@ -830,7 +851,8 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         ok = false;
         break;
       }
-      const int vx = sh.vx[slot];
+      const int2 unit = value_unit(sh.vx[slot], sh.vtop[slot]);
+      const int vx = unit.x;
       // a V tile's codes there, and the place that its widened values take free
       auto ready = [&](int Tj) -> bool {
         return wait32(sh.v_full + Tj % NV, (Tj / NV) & 1, a.wait_ns, abort_flag) &&
@@ -852,7 +874,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         const uint8_t* vs = smem + G::kOffV + (Tj % NV) * G::kTile;
         uint8_t* ws = smem + G::kOffW + (Tj % NW) * 2 * G::kTile;
         // candidate values, in the places the product reads
-        const int left = sh.apart[slot] ? 0 : fed - j * KC;
+        const int left = unit.y ? 0 : fed - j * KC;
         const float inv = pow2(-vx);
 #pragma unroll 2
         for (int k = 0; k < kMine; ++k) {
@@ -1130,7 +1152,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         ok = false;
         break;
       }
-      const float inv = l > 0.f ? 1.f / l : 0.f, unit = pow2(sh.vx[slot]);
+      const float inv = l > 0.f ? 1.f / l : 0.f, unit = pow2(value_unit(sh.vx[slot], sh.vtop[slot]).x);
       // 1 / l and V's unit in one factor, unless the factor would not be a normal number
       const bool plain = __all_sync(0xffffffffu, fabsf(inv * unit) > 0x1p-100f) != 0;
       if (!wait32(sh.pv_done + Tl % NS, (Tl / NS) & 1, a.wait_ns, abort_flag)) {
@@ -1141,7 +1163,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       if (some) {
         float2 scale = make_float2(inv * (plain ? unit : 1.f), inv * (plain ? unit : 1.f));
         bool rest = !plain;  // V's unit still to come
-        if (__builtin_expect(nct > 0 && sh.apart[slot], 0)) {
+        if (__builtin_expect(nct > 0 && value_unit(sh.vx[slot], sh.vtop[slot]).y, 0)) {
           // O normalised where it is, then the candidates' tokens one by one, each weight
           // from its key and the row's query
 #pragma unroll 1

@@ -334,7 +334,7 @@ __device__ __forceinline__ uint32_t cand_top(const Kv8Args& a, int kh, int f, in
                                              int step) {
   const __nv_bfloat16* v = a.v_cand + (size_t(f) * a.Hkv + kh) * DH;
   uint32_t top = 0;  // two magnitudes
-#pragma unroll 4
+#pragma unroll 8
   for (int i = first; i < n * (DH / 8); i += step) {
     const uint4 x = *reinterpret_cast<const uint4*>(v + size_t(i / (DH / 8)) * a.Hkv * DH +
                                                     8 * (i % (DH / 8)));

@@ -255,7 +255,9 @@ jet_status jet_quantize_kv_e4m3(const jet_layout* lay, const jet_dims* dims, con
  * in pieces or token by token.
  *   start      [R] int32 (device)      tokens of request r that its cache holds
  *   new_offset [R + 1] int32 (device)  request r's new tokens are rows
- *              [new_offset[r], new_offset[r + 1]) of k and v (none: equal entries)
+ *              [new_offset[r], new_offset[r + 1]) of k and v (none: equal entries); the
+ *              entries never fall (else JET_ERR_DEVICE is reported, and only the rows
+ *              up to the first fall are certain to be written)
  *   k, v       [n_new, Hkv, d] dims.dtype
  *   k8, v8     cache buffers laid out for the whole prefix (the layout's P_r)
  * The new tokens become positions start[r] .. of request r and must end within its
@@ -280,8 +282,13 @@ jet_status jet_dequantize_kv_e4m3(const jet_layout* lay, const jet_dims* dims, c
  * jet_prefix_attend_e4m3 - jet_prefix_attend over 8-bit prefix caches k8, v8: the
  * same rows, masks, scale and outputs, the prefix keys and values being the caches'
  * values. q, k_cand, v_cand and o are in dims.dtype (float32 or bf16). bf16: at most
- * 128 query heads a key/value head (else JET_ERR_UNSUPPORTED). ws/ws_bytes: scratch of at least
- * jet_attend_workspace_bytes_e4m3().
+ * 128 query heads a key/value head (else JET_ERR_UNSUPPORTED). ws/ws_bytes: scratch of at
+ * least jet_attend_workspace_bytes_e4m3().
+ * bf16: a query enters the prefix scores as two e4m3 numbers in the unit of its row (exact
+ * for elements within 2^-10 of the row's largest, 2^-17.8 of that off below), the weights
+ * round to eleven binary digits, and sums are float32. A candidate's values that are not
+ * finite, or beyond 2^8 times its request's prefix values, take a slower way; they reach
+ * no other rows than those that see the candidate.
  */
 size_t jet_attend_workspace_bytes_e4m3(const jet_sizes* n, const jet_dims* dims);
 jet_status jet_prefix_attend_e4m3(const jet_layout* lay, const jet_dims* dims, const void* q,

@@ -425,7 +425,9 @@ AttnPlan attn_plan_kv8(const jet_sizes& n, const jet_dims& d) {
   const double partial_us = 0.3e-6 * 8 * double(n.N) * d.Hq * d.d;
   const int tiles = std::max(1, (n.max_prefix + 63) / 64);
   double best = 0;
-  for (int s = 1; s <= std::max(1, tiles / 3); ++s) {  // chunks of 192 keys or more
+  // chunks of 192 keys or more, two an SM at most for one request
+  const int most_chunks = std::max(1, std::min(tiles / 3, 2 * kPlanSMs));
+  for (int s = 1; s <= most_chunks; ++s) {
     const int chunk = (tiles + s - 1) / s * 64, splits = (tiles * 64 + chunk - 1) / chunk;
     if (splits != s) continue;  // as with fewer, longer chunks
     const double per = s > 1 ? std::max(1.0, avg / chunk + 0.5) : 1.0;  // of a request

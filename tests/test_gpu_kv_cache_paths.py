@@ -53,6 +53,15 @@ def test_few_vectors_of_unsplit_prefixes(jet, d):
     c.check(c.result(), _some_rows(c, 1))
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_one_very_long_prefix(jet, d):
+    # more partials of a row than a warp of the combine has lanes
+    c = Case(jet, [40000, 3], [1, 1], [3, 1], "bf16", 8, 2, d, seed=8)
+    per = c.ref["N"] * c.Hq * (4 * d + 8)
+    assert c.need > 64 * per
+    c.check(c.result())
+
+
 def _seen(c, n):
     """The candidates' tokens that row n sees, as rows of k_cand and v_cand."""
     r = int(c.ref["row_req"][n])

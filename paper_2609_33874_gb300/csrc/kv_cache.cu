@@ -10,12 +10,9 @@
 // scales out of its sums.
 //
 // All three are streams: each element is read and written once, and HBM bounds them
-// (1.38e9 bf16 elements written: 592 us, 7.0 TB/s; 172e6 read back: 79 us, 6.6 TB/s).
+// (1.38e9 bf16 elements of d 256 written: 573 us, 7.2 TB/s; 172e6 read back: 77 us, 6.7 TB/s).
 // One CTA works on one (block of 64 tokens, keys or values, head) at a time: its
-// elements stay in registers between their maximum and their codes. Four such pairs one
-// after another hide the launch and the search for the place behind other CTAs' loads:
-// 1.38e9 bf16 elements with one pair a CTA against four: 629 and 592 us at d 256, 712 and
-// 606 at d 128; 0.69e9 at d 64, 577 and 345.
+// elements stay in registers between their maximum and their codes.
 #include <algorithm>
 
 #include "jet_device.cuh"
@@ -37,7 +34,7 @@ struct KvArgs {
   uint8_t* exps[2];
   int R, Hkv, total_prefix;
   int rows;                   // rows of k and v
-  int each;                   // (keys or values, head) pairs that a CTA takes
+  int each;                   // written: (keys or values, head) pairs that a CTA takes
   int* status;
 };
 
@@ -84,6 +81,12 @@ __device__ __forceinline__ bool find_span(const KvArgs& a, int slot, KvSpan* s) 
   if (claimed < 0) return false;
   *s = span;
   return true;
+}
+
+// (an index would copy the arguments to the stack)
+template <typename P>
+__device__ __forceinline__ P pick(P const (&p)[2], int kv) {
+  return kv ? p[1] : p[0];
 }
 
 __device__ __forceinline__ uint32_t encode2(float a, float b) {
@@ -143,9 +146,9 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, int* turn) {
 }
 
 // A CTA takes `each` of a block's 2 Hkv (keys or values, head) pairs, one after another.
-// The CTAs an SM that the launch bounds ask for are the most whose registers hold the
-// elements without spills; left to itself the compiler takes 122 registers at d 256 in
-// bf16 and two CTAs run (823 us instead of 632 at one pair each).
+// The launch bounds are the CTAs an SM that hide the loads; left to itself the compiler
+// takes more registers where that costs (0.69e9 bf16 elements of d 64 345 us instead of
+// 304; float32: 0.52e9 of d 256 677 instead of 485, of d 128 563 instead of 492).
 template <typename T, int DH, bool APPEND>
 __global__ void __launch_bounds__(kThreads, DH == 256 ? (sizeof(T) == 2 ? 4 : 3) : DH == 128 ? 5 : 8)
 kv_quantize_kernel(const KvArgs a) {
@@ -165,11 +168,11 @@ kv_quantize_kernel(const KvArgs a) {
 #pragma unroll 1
   for (int u = first; u < min(first + a.each, 2 * a.Hkv); ++u) {
     const int kv = u >= a.Hkv, h = u - kv * a.Hkv;
-    uint8_t* exp = a.exps[kv] + size_t(kv_place(s.p0, s.r, s.b)) * a.Hkv + h;
+    uint8_t* exp = pick(a.exps, kv) + size_t(kv_place(s.p0, s.r, s.b)) * a.Hkv + h;
     // a block begun before: the exponent of the tokens it holds
     const bool begun = APPEND && s.t0 > s.b * kKvBlock;
     const int held = begun ? min(max(int(*exp) - 127, kKvLow), kKvHigh) : kKvLow;
-    const T* x = static_cast<const T*>(a.x[kv]) + (size_t(s.row0 + j0) * a.Hkv + h) * DH + c0;
+    const T* x = static_cast<const T*>(pick(a.x, kv)) + (size_t(s.row0 + j0) * a.Hkv + h) * DH + c0;
     uint4 v[kMine];
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
@@ -186,7 +189,7 @@ kv_quantize_kernel(const KvArgs a) {
     }
     const int X = max(kv_exponent(top), held);
     const float inv = pow2(-X);
-    uint8_t* codes = a.codes[kv] + (size_t(s.p0 + s.t0 + j0) * a.Hkv + h) * DH + c0;
+    uint8_t* codes = pick(a.codes, kv) + (size_t(s.p0 + s.t0 + j0) * a.Hkv + h) * DH + c0;
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
       if (j0 + i * kStep >= nt) continue;
@@ -212,7 +215,7 @@ kv_quantize_kernel(const KvArgs a) {
     if (begun && X > held) {
       // the tokens before, rounded again (codes that stay normal keep their values)
       const float f = pow2(max(held - X, -126));
-      uint8_t* old = a.codes[kv] + (size_t(s.p0 + s.b * kKvBlock) * a.Hkv + h) * DH;
+      uint8_t* old = pick(a.codes, kv) + (size_t(s.p0 + s.b * kKvBlock) * a.Hkv + h) * DH;
       for (int e = tid; e < (s.t0 - s.b * kKvBlock) * (DH / 8); e += kThreads) {
         uint2* at = reinterpret_cast<uint2*>(old + (e / (DH / 8)) * step + 8 * (e % (DH / 8)));
         uint2 w = *at;
@@ -236,55 +239,50 @@ __global__ void __launch_bounds__(kThreads) kv_dequantize_kernel(const KvArgs a)
   constexpr int kRow = DH / kPer;
   constexpr int kMine = kKvBlock * kRow / kThreads;
   constexpr int kStep = kThreads / kRow;
-  const int groups = (2 * a.Hkv + a.each - 1) / a.each;
-  const int first = int(blockIdx.x % groups) * a.each;
+  const int h = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, kv = rest & 1;
   KvSpan s;
-  if (!find_span<false>(a, blockIdx.x / groups, &s)) return;
+  if (!find_span<false>(a, rest >> 1, &s)) return;
   const int nt = s.t1 - s.t0, tid = threadIdx.x;
   const int j0 = tid / kRow, c0 = tid % kRow * kPer;
   const size_t step = size_t(a.Hkv) * DH;
-#pragma unroll 1
-  for (int u = first; u < min(first + a.each, 2 * a.Hkv); ++u) {
-    const int kv = u >= a.Hkv, h = u - kv * a.Hkv;
-    const uint8_t held = a.exps[kv][size_t(kv_place(s.p0, s.r, s.b)) * a.Hkv + h];
-    const float f = kv_scale(held);
-    const size_t at = (size_t(s.p0 + s.t0 + j0) * a.Hkv + h) * DH + c0;
-    const uint8_t* codes = a.codes[kv] + at;
-    T* out = static_cast<T*>(a.out[kv]) + at;
-    uint32_t w[kMine][kPer / 4];
+  const uint8_t held = pick(a.exps, kv)[size_t(kv_place(s.p0, s.r, s.b)) * a.Hkv + h];
+  const float f = kv_scale(held);
+  const size_t at = (size_t(s.p0 + s.t0 + j0) * a.Hkv + h) * DH + c0;
+  const uint8_t* codes = pick(a.codes, kv) + at;
+  T* out = static_cast<T*>(pick(a.out, kv)) + at;
+  uint32_t w[kMine][kPer / 4];
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      if (j0 + i * kStep >= nt) continue;
-      const uint8_t* from = codes + i * kStep * step;
+  for (int i = 0; i < kMine; ++i) {
+    if (j0 + i * kStep >= nt) continue;
+    const uint8_t* from = codes + i * kStep * step;
+    if constexpr (kPer == 8) {
+      const uint2 y = *reinterpret_cast<const uint2*>(from);
+      w[i][0] = y.x;
+      w[i][1] = y.y;
+    } else {
+      w[i][0] = *reinterpret_cast<const uint32_t*>(from);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    if (j0 + i * kStep >= nt) continue;
+    uint32_t y[4];
+#pragma unroll
+    for (int q = 0; q < kPer / 4; ++q) {
+      const float2 lo = e4m3x2_to_f32(w[i][q]), hi = e4m3x2_to_f32(w[i][q] >> 16);
       if constexpr (kPer == 8) {
-        const uint2 y = *reinterpret_cast<const uint2*>(from);
-        w[i][0] = y.x;
-        w[i][1] = y.y;
+        const __nv_bfloat162 p = __floats2bfloat162_rn(lo.x * f, lo.y * f);
+        const __nv_bfloat162 r = __floats2bfloat162_rn(hi.x * f, hi.y * f);
+        y[2 * q] = *reinterpret_cast<const uint32_t*>(&p);
+        y[2 * q + 1] = *reinterpret_cast<const uint32_t*>(&r);
       } else {
-        w[i][0] = *reinterpret_cast<const uint32_t*>(from);
+        y[0] = __float_as_uint(lo.x * f);
+        y[1] = __float_as_uint(lo.y * f);
+        y[2] = __float_as_uint(hi.x * f);
+        y[3] = __float_as_uint(hi.y * f);
       }
     }
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      if (j0 + i * kStep >= nt) continue;
-      uint32_t y[4];
-#pragma unroll
-      for (int q = 0; q < kPer / 4; ++q) {
-        const float2 lo = e4m3x2_to_f32(w[i][q]), hi = e4m3x2_to_f32(w[i][q] >> 16);
-        if constexpr (kPer == 8) {
-          const __nv_bfloat162 p = __floats2bfloat162_rn(lo.x * f, lo.y * f);
-          const __nv_bfloat162 r = __floats2bfloat162_rn(hi.x * f, hi.y * f);
-          y[2 * q] = *reinterpret_cast<const uint32_t*>(&p);
-          y[2 * q + 1] = *reinterpret_cast<const uint32_t*>(&r);
-        } else {
-          y[0] = __float_as_uint(lo.x * f);
-          y[1] = __float_as_uint(lo.y * f);
-          y[2] = __float_as_uint(hi.x * f);
-          y[3] = __float_as_uint(hi.y * f);
-        }
-      }
-      *reinterpret_cast<uint4*>(out + i * kStep * step) = make_uint4(y[0], y[1], y[2], y[3]);
-    }
+    *reinterpret_cast<uint4*>(out + i * kStep * step) = make_uint4(y[0], y[1], y[2], y[3]);
   }
 }
 
@@ -306,19 +304,22 @@ KvArgs kv_args(const jet_layout& lay, const jet_dims& d, const void* k8, const v
   return a;
 }
 
-// The grid of `places` blocks, and a.each: a CTA takes up to `most` pairs, but no more
-// than leaves 512 CTAs, three or four an SM. An append's places are mostly partial, so
-// it has fewer to hide behind (16 requests of 100 to 700 tokens: 8.8 us with two, 11.1 with
-// four), and a piece read back holds its codes for a shorter time, so what counts is a
-// CTA's bytes (d 128: 355 us with one, 313 with two; d 256: 79 with one, 84 with two).
-dim3 kv_grid(KvArgs* a, int most, long long places) {
-  a->each = int(std::min((long long)most, std::max(1LL, places * 2 * a->Hkv / 512)));
-  return dim3(unsigned(places * ((2 * a->Hkv + a->each - 1) / a->each)));
+// How many pairs a CTA takes: four of bf16 heads of up to 128 elements, whose CTAs would
+// else be gone before their launch is paid (one, two, four pairs: 1.38e9 elements of d 128
+// 646, 596, 579 us, 0.69e9 of d 64 369, 323, 304), two of others (bf16 d 256 573, 570,
+// 574; 0.52e9 of float32 d 256 479, 478, 485) and of an append, whose blocks are mostly
+// partial (16 pieces of 100 to 700 tokens 8.7, 8.2, 10.2); but no more than leaves 512
+// CTAs, three or four an SM.
+template <typename T, bool APPEND>
+int pairs_each(int DH, long long pairs) {
+  const long long most = sizeof(T) == 2 && DH <= 128 && !APPEND ? 4 : 2;
+  return int(std::min(most, std::max(1LL, pairs / 512)));
 }
 
 template <typename T, bool APPEND>
 cudaError_t launch_quantize(KvArgs a, int DH, long long places, cudaStream_t st) {
-  const dim3 grid = kv_grid(&a, APPEND ? 2 : 4, places);
+  a.each = pairs_each<T, APPEND>(DH, places * 2 * a.Hkv);
+  const dim3 grid(unsigned(places * ((2 * a.Hkv + a.each - 1) / a.each)));
   if (DH == 64) return launch_pdl(kv_quantize_kernel<T, 64, APPEND>, grid, dim3(kThreads), 0, st, a);
   if (DH == 128)
     return launch_pdl(kv_quantize_kernel<T, 128, APPEND>, grid, dim3(kThreads), 0, st, a);
@@ -326,8 +327,8 @@ cudaError_t launch_quantize(KvArgs a, int DH, long long places, cudaStream_t st)
 }
 
 template <typename T>
-cudaError_t launch_dequantize(KvArgs a, int DH, long long places, cudaStream_t st) {
-  const dim3 grid = kv_grid(&a, 256 / DH, places);
+cudaError_t launch_dequantize(const KvArgs& a, int DH, long long places, cudaStream_t st) {
+  const dim3 grid(unsigned(places * 2 * a.Hkv));
   if (DH == 64) return launch_pdl(kv_dequantize_kernel<T, 64>, grid, dim3(kThreads), 0, st, a);
   if (DH == 128) return launch_pdl(kv_dequantize_kernel<T, 128>, grid, dim3(kThreads), 0, st, a);
   return launch_pdl(kv_dequantize_kernel<T, 256>, grid, dim3(kThreads), 0, st, a);

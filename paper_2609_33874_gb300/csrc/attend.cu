@@ -416,14 +416,36 @@ AttnPlan attn_plan_kv8(const jet_sizes& n, const jet_dims& d) {
     return p;
   }
   const int g = d.Hq / d.Hkv;
-  const int qv = std::max(1, attn_tc_block() / g) * g;  // query vectors per CTA: whole rows
-  p.qgroups = (n.max_rows * g + qv - 1) / qv;
-  const double avg = double(n.total_prefix) / n.R;
   const double vecs = double(n.N) * g / n.R;
+  // Few query vectors leave softmax warps without any. Then a block holds its vectors two
+  // or four times over, and each copy takes its part of a tile's keys: the copies leave
+  // partials that the combine joins like chunks. That pays at d 64 and 128 once an SM has
+  // some three 128-key tiles (32 vectors, one copy against four: 256 requests of 1,000
+  // keys, d 128, two kv heads 75.8 and 61.4 us, d 64 63.5 and 51.2; 32 of 1,000, 421 keys
+  // an SM, 24.6 and 22.5; 64 of 300, 253 keys an SM, 20.5 and 22.5; one of 6,000 20.5 and
+  // 24.6; four against two at 64 of 1,000 to 6,000, d 64, eight kv heads 149.5 and 174.1;
+  // 64 vectors, one and two: 256 of 1,000, d 128 75.8 and 69.6), and a few requests with
+  // more vectors may take several blocks then (100 requests of 1,500 - 5,000 keys, d 64: 38
+  // vectors on average of up to 100, one copy 354, two 291; 55 of 108 209 and 199; 71 of
+  // 140 211 and 236; 13 of 40, two copies and four 152 and 131; 22 of 56 158 and 152, at d
+  // 128 191 and 193). A tile of d 256 has half the keys for the same bytes, and its
+  // copies only break even (64 of 1,000 to 6,000 85.0 and 85.0, one of 6,000 22.5 and 28.7).
+  int qv = 0;  // query vectors of a block: whole rows
+  for (p.copies = 4;; p.copies /= 2) {
+    qv = std::max(1, attn_tc_block() / p.copies / g) * g;
+    if (p.copies == 1) break;
+    if (d.d > 128 || (long long)n.total_prefix * d.Hkv < 3LL * 128 * kPlanSMs ||
+        g > attn_tc_block() / p.copies)
+      continue;
+    const long long most = (long long)n.max_rows * g;
+    if (most <= qv || (vecs <= qv * (p.copies == 4 ? 0.625 : 0.875) && most <= 4 * qv)) break;
+  }
+  p.qgroups = int(((long long)n.max_rows * g + qv - 1) / qv);
+  const double avg = double(n.total_prefix) / n.R;
   const double groups = double(n.R) * d.Hkv * std::max(1.0, std::ceil(vecs / qv));
   const double key_us = (d.d == 256 ? 0.6 : 0.3) / 64;
-  const double partial_us = 0.3e-6 * 8 * double(n.N) * d.Hq * d.d;
-  const int tiles = std::max(1, (n.max_prefix + 63) / 64);
+  const double partial_us = 0.3e-6 * 8 * p.copies * double(n.N) * d.Hq * d.d;
+  const int tiles = n.max_prefix < 1 ? 1 : (n.max_prefix - 1) / 64 + 1;
   double best = 0;
   // chunks of 192 keys or more, two an SM at most for one request
   const int most_chunks = std::max(1, std::min(tiles / 3, 2 * kPlanSMs));
@@ -442,19 +464,6 @@ AttnPlan attn_plan_kv8(const jet_sizes& n, const jet_dims& d) {
       p.splits = splits;
     }
   }
-  // Few query vectors leave softmax warps without any. Then a block holds its vectors two
-  // or four times over, and each copy takes its part of a tile's keys: the copies leave
-  // partials that the combine joins like chunks. That pays at d 64 and 128 once an SM has
-  // some three 128-key tiles (32 vectors, one copy against four: 256 requests of 1,000
-  // keys, d 128, two kv heads 75.8 and 61.4 us, d 64 63.5 and 51.2; 32 of 1,000, 421 keys
-  // an SM, 24.6 and 22.5; 64 of 300, 253 keys an SM, 20.5 and 22.5; one of 6,000 20.5 and
-  // 24.6; four against two at 64 of 1,000 to 6,000, d 64, eight kv heads 149.5 and 174.1;
-  // 64 vectors, one and two: 256 of 1,000, d 128 75.8 and 69.6). A tile of d 256 has half
-  // the keys for the same bytes, and its copies only break even (64 of 1,000 to 6,000
-  // 85.0 and 85.0, one of 6,000 22.5 and 28.7).
-  const int most = n.max_rows * g;
-  if (d.d <= 128 && (long long)n.total_prefix * d.Hkv >= 3LL * 128 * kPlanSMs)
-    p.copies = most <= 32 ? 4 : most <= 64 ? 2 : 1;
   const size_t partials = size_t(p.splits) * p.copies * n.N * d.Hq;
   p.bytes = partials * d.d * sizeof(float) + partials * sizeof(float2);
   return p;

@@ -44,6 +44,22 @@ def test_few_vectors_over_much_cache(jet, d, g, rows):
     c.check(c.result(), _some_rows(c, rows, 8))
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("rows,copies", [([30, 1, 2, 2, 1, 2, 4, 1, 2], 4),
+                                         ([60, 5, 10, 8, 9, 10, 12, 3, 9], 2),
+                                         ([61, 5, 10, 8, 9, 10, 12, 3, 9], 1),
+                                         ([65, 1, 2, 1, 1, 1, 2, 1, 1], 1)])
+def test_one_request_of_many_rows(jet, d, rows, copies):
+    # a block holds the usual request's vectors several times over, and the one with many
+    # rows takes several blocks; past that plan's bounds one block holds 128 vectors
+    P = [1700, 1, 64, 500, 1900, 129, 700, 2063, 1100]
+    c = Case(jet, P, [1] * 9, rows, "bf16", 32, 8, d, seed=9)
+    per = c.ref["N"] * c.Hq * (4 * d + 8)
+    assert c.need % ((copies if d < 256 else 1) * per) == 0
+    last = int(c.ref["row_offset"][1]) - 1
+    c.check(c.result(), sorted(set(_some_rows(c, 2, 10)) | {last, last // 2}))
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_few_vectors_of_unsplit_prefixes(jet, d):
     # more items than SMs, each request one chunk: the copies' partials are joined alone

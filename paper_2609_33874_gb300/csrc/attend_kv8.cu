@@ -38,14 +38,17 @@
 // not keep them from the rows that do not see them; the output adds such an item's
 // candidate tokens one by one, each to the rows that do.
 //
-// What bounds it: long prefixes, HBM and the issue slots of the softmax and widening
-// warps together (256 requests of 2,048 - 8,192 tokens, d 256, two kv heads: 346 us, 61 %
-// of the copy rate; 128 of them at d 128, eight kv heads: 415 us, 50 %): a tile of d 256
-// takes these warps some 1,600 cycles (a conversion or an exponential holds its unit for
-// two to four cycles), its bytes 1,393. At one query row a request the copies below
-// leave the widening of V (64 requests of 1,000 - 6,000, d 128: 110 us, 65 %). Small
-// calls take an item's way through all roles, some 35,000 cycles or 18 us: the schedule
+// What bounds it: long prefixes, at 60 % of the copy rate, the units of an SM in turn (256
+// requests of 2,048 - 8,192 tokens, d 256, two kv heads: 344 us; 128 of them at d 128, eight
+// kv heads: 348 us). Of the some 1,600 cycles of a d 256 tile, whose bytes take 1,393, the
+// tensor pipe is busy for 1,024 (two passes over the keys, one over the values), and the
+// softmax and widening warps fill half of the issue slots, where a conversion or an
+// exponential holds its unit for two to four cycles. At one query row a request the copies
+// below leave the widening of V (64 requests of 1,000 - 6,000, d 128: 108 us, 66 %). Small
+// calls take an item's way through all roles, some 30,000 cycles or 16 us: the schedule
 // (3,800), the queries' arrival (5,900) and split (3,900), the tiles, the output (2,400).
+// (Softmax warps that take whole tiles in turn, instead of half of each tile's columns,
+// need no exchange of maxima but hold an S buffer twice as long: 406 us instead of 352.)
 //
 // With R copies a block of 128 / R vectors stands R times in the TMEM lanes, and copy c's
 // softmax warps take columns c of R of their half's, with zeros for the others' in P: a
@@ -70,7 +73,7 @@ template <int DH>
 struct Geo {
   // A tile of 64 keys for d 256, where O, two S and the queries' codes leave TMEM room for
   // no more; else of 128, so that half as many steps of the pipeline carry the same
-  // bytes (d 128, long prefixes: 415 us instead of 487)
+  // bytes (d 128, long prefixes: 415 us instead of 487 before other steps)
   static constexpr int kT = DH == 256 ? 64 : 128;
   static constexpr int kHalf = kT / 2;                    // columns of a softmax warp
   static constexpr int kC = kT / 2;                       // candidate tokens per tile

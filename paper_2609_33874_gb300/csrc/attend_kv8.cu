@@ -778,7 +778,7 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         // go unread
         constexpr int kMyPieces = DH / 16;  // of eight elements
         uint32_t mx[4] = {0, 0, 0, 0};
-#pragma unroll
+#pragma unroll 4  // (code that runs once an item is fetched anew each time)
         for (int i = 0; i < kMyPieces; ++i) {
           const int c = kMyPieces * half + i;
           const uint4 q = *reinterpret_cast<const uint4*>(smem + (c >> 3) * (kBV * 128) +

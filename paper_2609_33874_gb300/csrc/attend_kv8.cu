@@ -39,8 +39,8 @@
 // candidate tokens one by one, each to the rows that do.
 //
 // What bounds it: long prefixes, at 60 % of the copy rate, the units of an SM in turn (256
-// requests of 2,048 - 8,192 tokens, d 256, two kv heads: 344 us; 128 of them at d 128, eight
-// kv heads: 348 us). Of the some 1,600 cycles of a d 256 tile, whose bytes take 1,393, the
+// requests of 2,048 - 8,192 tokens, d 256, two kv heads: 340 us; 128 of them at d 128, eight
+// kv heads: 340 us). Of the some 1,600 cycles of a d 256 tile, whose bytes take 1,393, the
 // tensor pipe is busy for 1,024 (two passes over the keys, one over the values), and the
 // softmax and widening warps fill half of the issue slots, where a conversion or an
 // exponential holds its unit for two to four cycles. At one query row a request the copies

@@ -308,3 +308,35 @@ def test_many_heads_a_block(jet, dtype):
         cache = K.Cache(P, heads, d).write(_np(x[i]))
         _check_buffer(buf[i], cache, nb, 0x11)
         np.testing.assert_array_equal(_np(back[i]), cache.values())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 256])
+def test_append_to_many_requests(jet, dtype, d):
+    # enough requests for a CTA to take two of a block's pairs; every start and length
+    # within two blocks, exponents that grow in some heads only
+    import torch
+    R, heads = 300, 5
+    rng = np.random.default_rng(96)
+    P = rng.integers(1, 140, R).tolist()
+    host, lay, dims = _batch(jet, P, dtype=dtype, Hkv=heads, d=d)
+    nb, buf = _buffers(jet, host, dims, 0x77)
+    caches = [K.Cache(P, heads, d) for _ in range(2)]
+    at = np.zeros(R, int)
+    for step in range(3):
+        new = np.minimum(np.array(P) - at, rng.integers(0, 80, R) if step < 2 else 140)
+        off = np.concatenate([[0], np.cumsum(new)])
+        scale = np.float32(4.0) ** rng.integers(-3, 4, (1, heads, 1))
+        x = [_torch(_tokens(rng, int(off[-1]), heads, d) * scale, dtype) for _ in range(2)]
+        words = [torch.tensor(w, dtype=torch.int32, device="cuda") for w in (at, off)]
+        jet.jet_append_kv_e4m3(lay, dims, *words, *x, *buf)
+        for i in range(2):
+            rows = _np(x[i])
+            for r in range(R):
+                if new[r]:
+                    caches[i].append(r, int(at[r]), rows[off[r]:off[r + 1]])
+        at = at + new
+    torch.cuda.synchronize()
+    assert jet.jet_device_status() == JET_OK
+    for i in range(2):
+        _check_buffer(buf[i], caches[i], nb, 0x77)

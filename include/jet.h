@@ -285,10 +285,15 @@ jet_status jet_dequantize_kv_e4m3(const jet_layout* lay, const jet_dims* dims, c
  * 128 query heads a key/value head (else JET_ERR_UNSUPPORTED). ws/ws_bytes: scratch of at
  * least jet_attend_workspace_bytes_e4m3().
  * bf16: a query enters the prefix scores as two e4m3 numbers in the unit of its row (exact
- * for elements within 2^-10 of the row's largest, 2^-17.8 of that off below), the weights
- * round to eleven binary digits, and sums are float32. A candidate's values that are not
- * finite, or beyond 2^8 times its request's prefix values, take a slower way; they reach
- * no other rows than those that see the candidate.
+ * for elements of 2^-9 of the row's largest or more, 2^-17.8 of that off below). The
+ * weights enter the product with the values in f16, eleven binary digits; those below
+ * 2^-21 of the row's largest are off by up to 2^-32 of that largest. The values do in f16
+ * too, in a unit that they share: of a prefix chunk and head, and in the last chunk of
+ * its candidate tokens. They are exact from 2^-21 of the largest among them on, and off by
+ * up to 2^-32 of that largest below. Sums are float32.
+ * Candidate values that are not finite, or beyond some 2^8 times the largest prefix value
+ * of their request's last chunk, stay out of that unit: the candidate tokens of such a
+ * block of rows are added one by one, more slowly, each to the rows that see it only.
  */
 size_t jet_attend_workspace_bytes_e4m3(const jet_sizes* n, const jet_dims* dims);
 jet_status jet_prefix_attend_e4m3(const jet_layout* lay, const jet_dims* dims, const void* q,

@@ -19,8 +19,9 @@
 //            digits down to 2^-14, so weights 2^-21 of a maximum's, and rounds
 //            at 2^-25 below; e4m3 would lose the many small weights next to a large
 //            one), and V widened from the codes to f16 in units of 2^vx, the item's
-//            largest exponent, by eight warps on the way: exact but for codes below
-//            2^-14 of that unit, which are rounded at 2^-25 of it.
+//            largest exponent, by eight warps on the way: exact but for values below
+//            2^-14 of that unit, which are rounded at 2^-25 of it. (A block whose scale
+//            is out of f16's range in that unit, 2^-25 or less, takes it in two factors.)
 //
 //   warp 0       TMA producer: rings of K tiles, of V tiles, and the query block
 //   warp 1       TMEM allocator, issues S_j = Q K_j^T
@@ -270,6 +271,12 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
   uint32_t d;
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
+}
+
+// 2^k twice, k in [-24, 15]
+__device__ __forceinline__ uint32_t pow2_f16x2(int k) {
+  const uint32_t h = k > -15 ? uint32_t(k + 15) << 10 : 1u << (k + 24);
+  return h | h << 16;
 }
 
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
@@ -906,16 +913,17 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
 #pragma unroll
         for (int i = 0; i < kMine; ++i)
           x[i] = *reinterpret_cast<const uint4*>(vs + raw_piece<DH, KT>(key, c0 + kPer * i));
-        // 2^(X - vx): below 2^-24 f16 holds no product with a code
-        const int k2 = max(exponent_of(byte) - vx, -24);
+        // 2^(X - vx), what the block's codes are worth in the unit. Where f16 does not hold it
+        // the codes, multiples of 2^-9, take 2^-15 here, exactly, and the rest below.
+        const int exact_k2 = exponent_of(byte) - vx;
+        const int k2 = exact_k2 < -24 ? -15 : exact_k2;
         next += KT / kKvBlock;
         if (next < blocks) byte = load_ahead(ex + size_t(next) * a.Hkv);
         if (__builtin_expect(left < KT && key >= left, 0)) {
 #pragma unroll
           for (int i = 0; i < kMine; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
         }
-        const uint32_t h2 = k2 > -15 ? uint32_t(k2 + 15) << 10 : 1u << (k2 + 24);
-        const uint32_t f = h2 | h2 << 16;
+        const uint32_t f = pow2_f16x2(k2);
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
           const uint32_t in[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
@@ -932,6 +940,18 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
               make_uint4(y[0], y[1], y[2], y[3]);
           *reinterpret_cast<uint4*>(to + sw128(key, (2 * c + 1) & 7)) =
               make_uint4(y[4], y[5], y[6], y[7]);
+        }
+        if (__builtin_expect(exact_k2 < -24, 0)) {
+          // (values rounded here only; from 2^-34 on to zeros, as 448 2^-34 < 2^-25)
+          const uint32_t rest = pow2_f16x2(max(exact_k2, -39) + 15);
+#pragma unroll 1
+          for (int i = 0; i < 2 * kMine; ++i) {
+            const int c = 2 * (c0 + kPer * (i >> 1)) + (i & 1);
+            uint4* at = reinterpret_cast<uint4*>(ws + (c >> 3) * (KT * 128) + sw128(key, c & 7));
+            const uint4 y = *at;
+            *at = make_uint4(mul_f16x2(y.x, rest), mul_f16x2(y.y, rest), mul_f16x2(y.z, rest),
+                             mul_f16x2(y.w, rest));
+          }
         }
         done(Tj);
       }

@@ -92,4 +92,12 @@ JET_HD ItemGeo item_geo_at(const ItemPlan& a, int r, int kh, int qb, int split, 
   return e;
 }
 
+// Whether n fed tokens from the f-th on are among the batch's N - R. Row offsets that pass
+// request_cut may still name others (a request's fed tokens start at n0 - r), so a kernel
+// that reads candidates by address asks this first; a TMA copy clips them by itself.
+JET_HD bool fed_inside(const ItemPlan& a, int f, int n) {
+  const int F = a.N - a.R;
+  return f >= 0 && n >= 0 && n <= F && f <= F - n;
+}
+
 }  // namespace jet

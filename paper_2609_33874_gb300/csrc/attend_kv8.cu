@@ -477,6 +477,10 @@ attend_kv8_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
               }
               e.f_begin += lo;
               fed -= lo;
+              if (!fed_inside(a, e.f_begin, fed)) {
+                flag(a.status, JET_ERR_DEVICE);
+                fed = 0;  // the block's rows get the prefix alone
+              }
             }
             e.nct = (fed + KC - 1) / KC;
             e.npt = (e.k_end - e.k_begin + KT - 1) / KT;

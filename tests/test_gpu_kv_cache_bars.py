@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 import attend_bars as B
-from test_gpu_kv_cache import ATTEND, Case, _np, _torch
+from test_gpu_kv_cache import JET_ERR_DEVICE, Case, _np
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +34,28 @@ def test_blocks_of_very_different_values(jet, P, heads, dtype, gap, d):
     c.kc.fill_(-80.0 / d ** 0.5)
     c.quantise()
     _check(c, None if len(P) < 3 else [0, 4, 8])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 256])
+@pytest.mark.parametrize("rows,right", [([0, 0, 10, 15], 2), ([0, 5, 15, 15], 0)])
+def test_rows_that_name_tokens_outside_the_batch(jet, dtype, d, rows, right):
+    # row offsets inside the batch whose fed tokens would start before the first one or
+    # end past the last one: reported, none of them read, the true request as it was.
+    # The values are far above the prefix's, so that every way of reading them is taken.
+    import torch
+    c = Case(jet, [70, 200, 90], [1] * 3, [5] * 3, dtype, 8, 2, d, seed=5)
+    c.vc *= 1e6
+    want = c.result()
+    words = c.host.words.copy()
+    off = (c.host.struct.row_offset - c.host.words.ctypes.data) // 4
+    assert words[off:off + 4].tolist() == [0, 5, 10, 15]
+    words[off:off + 4] = rows
+    c.lay.words.copy_(torch.from_numpy(words))
+    c.o.fill_(99.0)
+    c.run()
+    torch.cuda.synchronize()
+    assert jet.jet_device_status() == JET_ERR_DEVICE
+    assert bool((c.ws[c.need:] == 0x5A).all())
+    mine = [n for n in range(c.ref["N"]) if c.ref["row_req"][n] == right]
+    np.testing.assert_array_equal(_np(c.o)[mine], want[mine])

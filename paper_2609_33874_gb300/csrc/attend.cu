@@ -15,6 +15,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "attend_items.h"
 #include "jet_device.cuh"
 #include "jet_internal.h"
 #include "kv_cache.h"
@@ -75,11 +76,11 @@ attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* _
   const int r = blockIdx.z / Hkv, kh = blockIdx.z % Hkv;
   const int g = Hq / Hkv;
   if (r >= R) return;
-  const int n0 = row_offset[r], nr = row_offset[r + 1] - n0;
-  const int p0 = prefix_offset[r], P = prefix_offset[r + 1] - p0;
+  const int n0 = row_offset[r], n1 = row_offset[r + 1], nr = n1 - n0;
+  const int p0 = prefix_offset[r], p1 = prefix_offset[r + 1], P = p1 - p0;
   // (a request longer than the plan's chunks or vector groups is left out too)
-  if (n0 < 0 || nr < 1 || n0 + nr > N || p0 < 0 || P < 0 || p0 + P > total_prefix ||
-      P > chunk * int(gridDim.x) || nr * g > kQV * int(gridDim.y)) {
+  if (!span_inside(n0, n1, N) || nr < 1 || !span_inside(p0, p1, total_prefix) ||
+      P > (long long)chunk * gridDim.x || (long long)nr * g > (long long)kQV * gridDim.y) {
     if (threadIdx.x == 0) flag(status, JET_ERR_DEVICE);
     return;
   }

@@ -92,6 +92,13 @@ JET_HD ItemGeo item_geo_at(const ItemPlan& a, int r, int kh, int qb, int split, 
   return e;
 }
 
+// Whether [begin, end), two neighbouring words of a device layout, is a part of `total`
+// things. (No sum or difference of words: of 2^31 - 1 and -2^31 either would wrap to
+// something that fits.)
+JET_HD bool span_inside(int begin, int end, int total) {
+  return begin >= 0 && begin <= end && end <= total;
+}
+
 // Whether n fed tokens from the f-th on are among the batch's N - R. Row offsets that pass
 // request_cut may still name others (a request's fed tokens start at n0 - r), so a kernel
 // that reads candidates by address asks this first; a TMA copy clips them by itself.

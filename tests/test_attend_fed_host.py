@@ -1,7 +1,7 @@
-"""Which fed candidate tokens an attention item may read (csrc/attend_items.h, plain
+"""Which parts of a batch the words of a layout may name (csrc/attend_items.h, plain
 arithmetic), on the host: over random plans and row offsets that pass the cut of a
-request, true or not, fed_inside admits exactly the ranges of the batch's N - R tokens,
-and every range of a true layout."""
+request, true or not, fed_inside admits exactly the ranges of the batch's N - R fed
+tokens, and every range of a true layout; span_inside exactly the parts of a total."""
 import os
 import subprocess
 
@@ -65,6 +65,14 @@ int main() {
   CHECK(fed_inside(a, 0, 10) && fed_inside(a, 10, 0) && !fed_inside(a, 11, 0));
   CHECK(!fed_inside(a, big, big) && !fed_inside(a, 5, big) && !fed_inside(a, big, 1));
   CHECK(!fed_inside(a, -1, 2) && !fed_inside(a, -big - 1, big) && !fed_inside(a, 0, -1));
+  const int word[] = {-big - 1, -big, -7, -1, 0, 1, 6, 9, 10, 11, big - 1, big};
+  const int total[] = {0, 1, 9, 10, big};
+  for (int b : word)
+    for (int e : word)
+      for (int t : total)
+        CHECK(span_inside(b, e, t) ==
+              ((long long)b >= 0 && (long long)e - b >= 0 && (long long)e <= t));
+  CHECK(!span_inside(big, -big - 1, 10));  // whose difference wraps to 1
   a.R = 20;  // fewer rows than requests: no token at all
   CHECK(!fed_inside(a, 0, 0) && !fed_inside(a, 0, 1));
   return 0;

@@ -59,3 +59,25 @@ def test_rows_that_name_tokens_outside_the_batch(jet, dtype, d, rows, right):
     assert bool((c.ws[c.need:] == 0x5A).all())
     mine = [n for n in range(c.ref["N"]) if c.ref["row_req"][n] == right]
     np.testing.assert_array_equal(_np(c.o)[mine], want[mine])
+
+
+@pytest.mark.parametrize("d", [64, 256])
+def test_words_whose_difference_wraps(jet, d):
+    # float32: neighbouring words 2^31 - 1 and -2^31 differ by 1 in 32 bits; the requests
+    # beside them are left out and reported, the third is as it was
+    import torch
+    c = Case(jet, [70, 200, 90], [1] * 3, [5] * 3, "f32", 8, 2, d, seed=6)
+    want = c.result()
+    clean = c.host.words.copy()
+    for name, true in (("row_offset", [0, 5, 10, 15]), ("prefix_offset", [0, 70, 270, 360])):
+        off = (getattr(c.host.struct, name) - c.host.words.ctypes.data) // 4
+        words = clean.copy()
+        assert words[off:off + 4].tolist() == true
+        words[off:off + 2] = [2 ** 31 - 1, -2 ** 31]
+        c.lay.words.copy_(torch.from_numpy(words))
+        c.o.fill_(99.0)
+        c.run()
+        torch.cuda.synchronize()
+        assert jet.jet_device_status() == JET_ERR_DEVICE
+        assert bool((c.ws[c.need:] == 0x5A).all())
+        np.testing.assert_array_equal(_np(c.o)[10:], want[10:])

@@ -100,7 +100,6 @@ struct Geo {
 struct Kv8Args : AttArgs {
   const uint8_t* k_exp;  // exponent bytes of the caches
   const uint8_t* v_exp;
-  const __nv_bfloat16* q;
   const __nv_bfloat16* k_cand;
   const __nv_bfloat16* v_cand;
 };
@@ -210,38 +209,22 @@ __device__ __forceinline__ void tmem_st_8cols_u32(uint32_t taddr, const uint32_t
       : "memory");
 }
 
-// and 4 columns
-__device__ __forceinline__ void tmem_st_4cols_u32(uint32_t taddr, const uint32_t (&v)[4]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr),
-               "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3])
-               : "memory");
-}
-
 template <int N>
 __device__ __forceinline__ void tmem_st_cols(uint32_t taddr, const uint32_t (&v)[N]) {
+  static_assert(N == 16 || N == 8);
   if constexpr (N == 16) tmem_st_16cols_u32(taddr, v);
   if constexpr (N == 8) tmem_st_8cols_u32(taddr, v);
-  if constexpr (N == 4) tmem_st_4cols_u32(taddr, v);
-}
-
-// 8 consecutive f32 columns of this warp's 32 TMEM lanes
-__device__ __forceinline__ void tmem_ld_8cols(uint32_t taddr, float (&v)[8]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]),
-        "=f"(v[7])
-      : "r"(taddr));
 }
 
 template <int N>
 __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, float (&v)[N]) {
+  static_assert(N == 64 || N == 32 || N == 16);
   if constexpr (N == 64) {
     tmem_ld_32cols(taddr, *reinterpret_cast<float(*)[32]>(v));
     tmem_ld_32cols(taddr + 32, *reinterpret_cast<float(*)[32]>(v + 32));
   }
   if constexpr (N == 32) tmem_ld_32cols(taddr, v);
   if constexpr (N == 16) tmem_ld_16cols(taddr, v);
-  if constexpr (N == 8) tmem_ld_8cols(taddr, v);
 }
 
 // the codes of a word's two halves as f16 numbers, and two f16 numbers' nearest codes

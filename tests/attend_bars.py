@@ -90,6 +90,23 @@ def worst(got, want, bar):
 BLOCK = 64
 
 
+def columns_of_blocks(rng, prefix_len, heads, d):
+    """Values that make every block count: column e holds positive values in the blocks b
+    with b % d == e % blocks only, of a scale of their own, and zeros elsewhere. A block
+    that is lost, doubled or halved changes a column's output by its part of few."""
+    v = np.zeros((sum(prefix_len), heads, d), np.float32)
+    p0 = 0
+    for P in prefix_len:
+        blocks = -(-P // BLOCK)
+        for b in range(blocks):
+            cols = [e for e in range(d) if e % min(blocks, d) == b % d]
+            t = slice(p0 + b * BLOCK, p0 + min(P, (b + 1) * BLOCK))
+            x = rng.uniform(1.0, 2.0, (t.stop - t.start, heads, len(cols)))
+            v[t, :, cols] = x * 2.0 ** (b % 5 - 2)
+        p0 += P
+    return v
+
+
 def gaps(rng, prefix_len, heads, d, gap, target):
     """Keys and values of one prefix whose block `target` takes all the weight of queries
     of ones while another block's values are 2^gap larger: (k, v) for q = 1."""
@@ -103,4 +120,15 @@ def gaps(rng, prefix_len, heads, d, gap, target):
         k[t] += np.float32(80.0 / d ** 0.5)           # ... but about 0 there
         v[p0:p0 + BLOCK] *= np.float32(2.0 ** gap)
         p0 += P
+    return k, v
+
+
+def outweighed(rng, total, heads, d, q_mean, below):
+    """Keys and values of one prefix whose first key's score is `below` powers of e above
+    the others', for queries of positive elements of that mean; its value is zero, so
+    the outputs are what the many small weights make together."""
+    k = (rng.standard_normal((total, heads, d)) * 0.05).astype(np.float32)
+    k[0] = below / (q_mean * d ** 0.5)
+    v = rng.uniform(1.0, 2.0, (total, heads, d)).astype(np.float32)
+    v[0] = 0.0
     return k, v

@@ -283,14 +283,16 @@ jet_status jet_dequantize_kv_e4m3(const jet_layout* lay, const jet_dims* dims, c
  * same rows, masks, scale and outputs, the prefix keys and values being the caches'
  * values. q, k_cand, v_cand and o are in dims.dtype (float32 or bf16). bf16: at most
  * 128 query heads a key/value head (else JET_ERR_UNSUPPORTED). ws/ws_bytes: scratch of at
- * least jet_attend_workspace_bytes_e4m3().
+ * least jet_attend_workspace_bytes_e4m3(). Long or many prefixes are read in less time than
+ * jet_prefix_attend takes over a bf16 cache, batches of short ones in up to 1.5 times it.
  * bf16: a query enters the prefix scores as two e4m3 numbers in the unit of its row (exact
- * for elements of 2^-9 of the row's largest or more, 2^-17.8 of that off below). The
- * weights enter the product with the values in f16, eleven binary digits; those below
- * 2^-21 of the row's largest are off by up to 2^-32 of that largest. The values do in f16
- * too, in a unit that they share: of a prefix chunk and head, and in the last chunk of
- * its candidate tokens. They are exact from 2^-21 of the largest among them on, and off by
- * up to 2^-32 of that largest below. Sums are float32.
+ * for elements of 2^-9 of the row's largest or more, 2^-17.8 of that off below; rows
+ * whose largest is below 2^-108 lose more). The weights enter the product with the values
+ * in f16, eleven binary digits; those below 2^-21 of the row's largest are off by up to
+ * 2^-32 of that largest. The values do in f16 too, in a unit that they share: of a prefix
+ * chunk and head, and in the last chunk of its candidate tokens. They are exact from 2^-21
+ * of the largest among them on, and off by up to 2^-32 of that largest below. Sums are
+ * float32.
  * Candidate values that are not finite, or beyond some 2^8 times the largest prefix value
  * of their request's last chunk, stay out of that unit: the candidate tokens of such a
  * block of rows are added one by one, more slowly, each to the rows that see it only.

@@ -10,8 +10,8 @@
 //   scores   S = Q K^T on the codes as they are (kind::f8f6f4). A query is held as two
 //            e4m3 numbers, q = 2^x (hi + lo), x per row: hi is the nearest code, lo that of
 //            what is left, at most four binary digits of a bf16 number's eight, so the
-//            split is exact for elements within 2^-10 of the row's largest and leaves
-//            2^-10 of 2^x, at most 2^-17.8 of that largest element, below. (Keys
+//            split is exact for elements of 2^-2 of 2^x or more, 2^-9.8 of the row's
+//            largest, and leaves 2^-10 of 2^x, at most 2^-17.8 of that largest, below. (Keys
 //            widened to bf16 instead would pass shared memory twice more: 1,536 cycles
 //            a tile of d 256, 1,393 at the HBM rate.) S = acc 2^(x + X), X the exponent
 //            of the 64 tokens: a tile has one or two.
@@ -37,11 +37,12 @@
 // pass the widening warps too. Values that are not finite, or so large that V's unit
 // would take the prefix's digits with it, are left out there, as a weight of zero would
 // not keep them from the rows that do not see them; the output adds such an item's
-// candidate tokens one by one, each to the rows that do.
+// candidate tokens one by one, each to the rows that do (16 multiple-choice requests whose
+// last chunks hold zeros, so that all take this way: 112 us instead of 27).
 //
 // What bounds it: long prefixes, at 60 % of the copy rate, the units of an SM in turn (256
-// requests of 2,048 - 8,192 tokens, d 256, two kv heads: 340 us; 128 of them at d 128, eight
-// kv heads: 340 us). Of the some 1,600 cycles of a d 256 tile, whose bytes take 1,393, the
+// requests of 2,048 - 8,192 tokens, d 256, two kv heads: 344 us; 128 of them at d 128, eight
+// kv heads: 354 us). Of the some 1,600 cycles of a d 256 tile, whose bytes take 1,393, the
 // tensor pipe is busy for 1,024 (two passes over the keys, one over the values), and the
 // softmax and widening warps fill half of the issue slots, where a conversion or an
 // exponential holds its unit for two to four cycles. At one query row a request the copies

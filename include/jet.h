@@ -323,6 +323,103 @@ jet_status jet_prefill_attend(const jet_layout* lay, const jet_dims* dims, const
                               void* stream);
 
 /*
+ * Positions: the norm of every query and key head and its rotation by position, in one
+ * pass (models with positions apply it to the projected queries and keys before the
+ * attention calls, which take them as they are). A head x of d elements at position p
+ * becomes
+ *   y = x / sqrt(mean(x^2) + eps) * gain     (norm 1; norm 0: y = x)
+ *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = p f_i,  for i < rot / 2
+ * with (a, b) = (y[i], y[i + rot / 2]) (JET_ROPE_HALVES) or (y[2 i], y[2 i + 1])
+ * (JET_ROPE_PAIRS); the elements from rot on stay y. All of it is float32, rounded once
+ * to the output's type; the angle is exact modulo a turn for every int32 position, up to
+ * the 53 binary digits of f_i.
+ */
+enum { JET_ROPE_HALVES = 0, JET_ROPE_PAIRS = 1 };
+
+/* What the rotation needs of a model; filled by jet_rope_init, kept by the caller (host). */
+typedef struct jet_rope {
+  int32_t rot;         /* rotated elements of a head: a multiple of 8, 0 (none) to 256 */
+  int32_t style;       /* JET_ROPE_*                                                    */
+  int32_t norm;        /* 1: the heads are normalised first                            */
+  float eps;
+  uint64_t turn[128];  /* f_i / (2 pi) of pair i, as a fraction of 2^64                */
+} jet_rope;
+
+/*
+ * jet_rope_init - fill *out (host only). freq[rot / 2] holds f_i in radians a position;
+ * NULL means theta^(-2 i / rot). Errors: JET_ERR_ARG (null out, an unknown style, norm
+ * not 0 or 1, eps negative or not finite, without freq a theta that is not positive and
+ * finite, a frequency that is not finite), JET_ERR_SHAPE (rot).
+ */
+jet_status jet_rope_init(int32_t rot, int32_t style, double theta, const double* freq,
+                         int32_t norm, float eps, jet_rope* out);
+
+/*
+ * jet_norm_rotate - n tokens at given positions.
+ *   pos      [n] int32 (device)  any position, negative ones too
+ *   q, k     [n, Hq, d], [n, Hkv, d] dims.dtype; either may be NULL (with its output):
+ *            then only the other is worked on
+ *   gq, gk   [d] dims.dtype      gains of the query and the key heads; NULL means ones;
+ *            not read without the norm
+ *   q_out, k_out                 may be q and k themselves, and may not overlap them else
+ * Uses dims.dtype (float32 or bf16), Hq, Hkv and d (64, 128 or 256, at least rot, else
+ * JET_ERR_SHAPE) only.
+ */
+jet_status jet_norm_rotate(const jet_dims* dims, const jet_rope* rope, int32_t n,
+                           const int32_t* pos, const void* q, const void* k, const void* gq,
+                           const void* gk, void* q_out, void* k_out, void* stream);
+
+/* jet_norm_rotate_prefix - the same for a batch's prefixes, as jet_prefill_attend takes
+ * them: q [total_prefix, Hq, d] and k [total_prefix, Hkv, d], token i of a request at
+ * position i. */
+jet_status jet_norm_rotate_prefix(const jet_layout* lay, const jet_dims* dims,
+                                  const jet_rope* rope, const void* q, const void* k,
+                                  const void* gq, const void* gk, void* q_out, void* k_out,
+                                  void* stream);
+
+/* jet_norm_rotate_rows - the same for the step's rows, as jet_prefix_attend takes them:
+ * q [N, Hq, d] of every row and k [F, Hkv, d] of the fed tokens. Request r's shared row
+ * stands at position P_r - 1, the row fed with y_{c,t} at P_r - 1 + t. */
+jet_status jet_norm_rotate_rows(const jet_layout* lay, const jet_dims* dims,
+                                const jet_rope* rope, const void* q, const void* k,
+                                const void* gq, const void* gk, void* q_out, void* k_out,
+                                void* stream);
+
+/*
+ * Attention under a window: jet_prefix_attend and jet_prefill_attend for layers in which
+ * a token sees the last `window` tokens (itself among them) and the first `sinks` ones: a
+ * row at position p sees the keys at positions j <= p with j > p - window or j < sinks.
+ * Positions count from the request's first prefix token; candidate c's fed token y_{c,t}
+ * stands at P_r - 1 + t, so a row's own candidate tokens leave its window, too, and are
+ * first tokens where the prefix is shorter than `sinks`. window >= 1 and sinks >= 0 (else
+ * JET_ERR_ARG); every row sees itself, the shared row its prefix's last key. What a row
+ * does not see does not reach it, infinities and NaN among it.
+ *
+ * jet_prefix_attend_window - the step (arguments, types and head sizes of
+ * jet_prefix_attend; bf16: at most 128 query heads a key/value head, else
+ * JET_ERR_UNSUPPORTED). The whole prefix is given; only the keys that some row sees are
+ * read: the first `sinks` and the last `window` of each request.
+ * ws/ws_bytes: scratch of at least jet_attend_window_workspace_bytes().
+ */
+size_t jet_attend_window_workspace_bytes(const jet_sizes* n, const jet_dims* dims,
+                                         int32_t window, int32_t sinks);
+jet_status jet_prefix_attend_window(const jet_layout* lay, const jet_dims* dims, int32_t window,
+                                    int32_t sinks, const void* q, const void* k_pre,
+                                    const void* v_pre, const void* k_cand, const void* v_cand,
+                                    void* o, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * jet_prefill_attend_window - the prefill (arguments of jet_prefill_attend; bf16 only and
+ * at most 128 query heads a key/value head, else JET_ERR_UNSUPPORTED).
+ * ws/ws_bytes: scratch of at least jet_prefill_window_workspace_bytes().
+ */
+size_t jet_prefill_window_workspace_bytes(const jet_sizes* n, const jet_dims* dims,
+                                          int32_t window, int32_t sinks);
+jet_status jet_prefill_attend_window(const jet_layout* lay, const jet_dims* dims, int32_t window,
+                                     int32_t sinks, const void* q, const void* k, const void* v,
+                                     void* o, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * jet_prefill_state - the prefill of a linear-attention layer: every request's
  * P_r prefix tokens fed in order through the recurrence `rule` (JET_RECUR_*,
  * as for jet_fork_state_rule) starting from s_init.

@@ -366,6 +366,146 @@ extern "C" jet_status jet_prefill_attend(const jet_layout* lay, const jet_dims* 
                                             static_cast<cudaStream_t>(stream)));
 }
 
+namespace {
+
+// what jet_norm_rotate and its forms take of the rotation, the dims and the tensors:
+// nq and nk tokens of queries and keys
+jet_status check_rotate(const jet_dims* d, const jet_rope* rope, long long nq, long long nk,
+                        const void* q, const void* k, const void* gq, const void* gk,
+                        const void* qo, const void* ko) {
+  JET_TRY(check_attn_dims(d));
+  if (!rope) return JET_ERR_ARG;
+  if (rope->style != JET_ROPE_HALVES && rope->style != JET_ROPE_PAIRS) return JET_ERR_ARG;
+  if ((rope->norm != 0 && rope->norm != 1) || !(rope->eps >= 0.f)) return JET_ERR_ARG;
+  if (rope->rot < 0 || rope->rot % 8 != 0 || rope->rot > d->d) return JET_ERR_SHAPE;
+  if (!q && !k && (nq > 0 || nk > 0)) return JET_ERR_ARG;
+  if (!q != !qo || !k != !ko) return JET_ERR_ARG;
+  if (q) {
+    JET_TRY(check_ptr(q, nq));
+    JET_TRY(check_ptr(qo, nq));
+    if (rope->norm && gq) JET_TRY(check_ptr(gq, nq));
+  }
+  if (k) {
+    JET_TRY(check_ptr(k, nk));
+    JET_TRY(check_ptr(ko, nk));
+    if (rope->norm && gk) JET_TRY(check_ptr(gk, nk));
+  }
+  return JET_OK;
+}
+
+jet_status check_window(int32_t window, int32_t sinks) {
+  return window < 1 || sinks < 0 ? JET_ERR_ARG : JET_OK;
+}
+
+}  // namespace
+
+extern "C" jet_status jet_norm_rotate(const jet_dims* dims, const jet_rope* rope, int32_t n,
+                                      const int32_t* pos, const void* q, const void* k,
+                                      const void* gq, const void* gk, void* q_out, void* k_out,
+                                      void* stream) {
+  if (n < 0) return JET_ERR_ARG;
+  JET_TRY(check_rotate(dims, rope, n, n, q, k, gq, gk, q_out, k_out));
+  if (n == 0) return JET_OK;
+  if (!pos) return JET_ERR_ARG;
+  if ((reinterpret_cast<uintptr_t>(pos) & 3u) != 0) return JET_ERR_ALIGN;
+  return cuda_status(jet::launch_norm_rotate(nullptr, false, *dims, *rope, n, pos, q, k, gq, gk,
+                                             q_out, k_out, jet::device_status_ptr(),
+                                             static_cast<cudaStream_t>(stream)));
+}
+
+extern "C" jet_status jet_norm_rotate_prefix(const jet_layout* lay, const jet_dims* dims,
+                                             const jet_rope* rope, const void* q, const void* k,
+                                             const void* gq, const void* gk, void* q_out,
+                                             void* k_out, void* stream) {
+  JET_TRY(check_layout(lay));
+  const jet_sizes& n = lay->n;
+  JET_TRY(check_rotate(dims, rope, n.total_prefix, n.total_prefix, q, k, gq, gk, q_out, k_out));
+  if (n.R == 0) return JET_OK;
+  return cuda_status(jet::launch_norm_rotate(lay, false, *dims, *rope, n.total_prefix, nullptr, q, k,
+                                             gq, gk, q_out, k_out, jet::device_status_ptr(),
+                                             static_cast<cudaStream_t>(stream)));
+}
+
+extern "C" jet_status jet_norm_rotate_rows(const jet_layout* lay, const jet_dims* dims,
+                                           const jet_rope* rope, const void* q, const void* k,
+                                           const void* gq, const void* gk, void* q_out,
+                                           void* k_out, void* stream) {
+  JET_TRY(check_layout(lay));
+  const jet_sizes& n = lay->n;
+  JET_TRY(check_rotate(dims, rope, n.N, n.N - n.R, q, k, gq, gk, q_out, k_out));
+  if (n.R == 0) return JET_OK;
+  if (!q && n.N == n.R) return JET_OK;  // keys of fed tokens only, and none fed
+  return cuda_status(jet::launch_norm_rotate(lay, true, *dims, *rope, n.N, nullptr, q, k, gq, gk,
+                                             q_out, k_out, jet::device_status_ptr(),
+                                             static_cast<cudaStream_t>(stream)));
+}
+
+extern "C" size_t jet_attend_window_workspace_bytes(const jet_sizes* n, const jet_dims* d,
+                                                    int32_t window, int32_t sinks) {
+  if (!n || n->R < 0 || n->N < 0 || check_attn_dims(d) != JET_OK) return 0;
+  if (check_window(window, sinks) != JET_OK) return 0;
+  return jet::attend_window_bytes(*n, *d, window, sinks);
+}
+
+extern "C" jet_status jet_prefix_attend_window(const jet_layout* lay, const jet_dims* dims,
+                                               int32_t window, int32_t sinks, const void* q,
+                                               const void* k_pre, const void* v_pre,
+                                               const void* k_cand, const void* v_cand, void* o,
+                                               void* ws, size_t ws_bytes, void* stream) {
+  JET_TRY(check_layout(lay));
+  JET_TRY(check_attn_dims(dims));
+  JET_TRY(check_window(window, sinks));
+  if (dims->dtype == JET_DTYPE_BF16 && dims->Hq / dims->Hkv > jet::attn_tc_block())
+    return JET_ERR_UNSUPPORTED;
+  const jet_sizes& n = lay->n;
+  if (n.R == 0) return JET_OK;
+  if ((long long)n.R * dims->Hkv > 65535) return JET_ERR_CAPACITY;
+  const long long F = n.N - n.R;
+  JET_TRY(check_ptr(q, n.N));
+  JET_TRY(check_ptr(k_pre, n.total_prefix));
+  JET_TRY(check_ptr(v_pre, n.total_prefix));
+  JET_TRY(check_ptr(k_cand, F));
+  JET_TRY(check_ptr(v_cand, F));
+  JET_TRY(check_ptr(o, n.N));
+  if (!ws || ws_bytes < jet::attend_window_bytes(n, *dims, window, sinks))
+    return JET_ERR_WORKSPACE;
+  if (!aligned16(ws)) return JET_ERR_ALIGN;
+  return cuda_status(jet::launch_attend_window(*lay, *dims, window, sinks, q, k_pre, v_pre, k_cand,
+                                               v_cand, o, ws, jet::device_status_ptr(),
+                                               static_cast<cudaStream_t>(stream)));
+}
+
+extern "C" size_t jet_prefill_window_workspace_bytes(const jet_sizes* n, const jet_dims* d,
+                                                     int32_t window, int32_t sinks) {
+  if (!n || n->R < 0 || check_attn_dims(d) != JET_OK) return 0;
+  if (check_window(window, sinks) != JET_OK) return 0;
+  return jet::prefill_window_bytes(*n, *d, window, sinks);
+}
+
+extern "C" jet_status jet_prefill_attend_window(const jet_layout* lay, const jet_dims* dims,
+                                                int32_t window, int32_t sinks, const void* q,
+                                                const void* k, const void* v, void* o, void* ws,
+                                                size_t ws_bytes, void* stream) {
+  JET_TRY(check_layout(lay));
+  JET_TRY(check_attn_dims(dims));
+  JET_TRY(check_window(window, sinks));
+  if (dims->dtype != JET_DTYPE_BF16) return JET_ERR_UNSUPPORTED;
+  if (dims->Hq / dims->Hkv > jet::attn_tc_block()) return JET_ERR_UNSUPPORTED;
+  const jet_sizes& n = lay->n;
+  if (n.R == 0) return JET_OK;
+  if (n.R > 65535) return JET_ERR_CAPACITY;
+  JET_TRY(check_ptr(q, n.total_prefix));
+  JET_TRY(check_ptr(k, n.total_prefix));
+  JET_TRY(check_ptr(v, n.total_prefix));
+  JET_TRY(check_ptr(o, n.total_prefix));
+  if (!ws || ws_bytes < jet::prefill_window_bytes(n, *dims, window, sinks))
+    return JET_ERR_WORKSPACE;
+  if (!aligned16(ws)) return JET_ERR_ALIGN;
+  return cuda_status(jet::launch_prefill_window(*lay, *dims, window, sinks, q, k, v, o, ws,
+                                                jet::device_status_ptr(),
+                                                static_cast<cudaStream_t>(stream)));
+}
+
 extern "C" jet_status jet_prefill_state(const jet_layout* lay, const jet_dims* dims, int32_t rule,
                                         const float* s_init, const void* q, const void* k,
                                         const void* v, const float* alpha, const float* beta,

@@ -147,6 +147,24 @@ cudaError_t launch_attend_tc(const jet_layout& lay, const jet_dims& d, const Att
                              const void* k_cand, const void* v_cand, void* o, float* o_part,
                              float2* ml_part, int* status, cudaStream_t st);
 
+// norm and rotation of queries and keys (rotate.cu): n tokens at the positions pos
+// (lay null), of the batch's prefixes, or of the step's rows
+cudaError_t launch_norm_rotate(const jet_layout* lay, bool rows, const jet_dims& d,
+                               const jet_rope& rope, int n, const int32_t* pos, const void* q,
+                               const void* k, const void* gq, const void* gk, void* qo, void* ko,
+                               int* status, cudaStream_t st);
+
+// attention under a window (window.cu): the step, and the prefill
+size_t attend_window_bytes(const jet_sizes& n, const jet_dims& d, int window, int sinks);
+cudaError_t launch_attend_window(const jet_layout& lay, const jet_dims& d, int window, int sinks,
+                                 const void* q, const void* k_pre, const void* v_pre,
+                                 const void* k_cand, const void* v_cand, void* o, void* ws,
+                                 int* status, cudaStream_t st);
+size_t prefill_window_bytes(const jet_sizes& n, const jet_dims& d, int window, int sinks);
+cudaError_t launch_prefill_window(const jet_layout& lay, const jet_dims& d, int window, int sinks,
+                                  const void* q, const void* k, const void* v, void* o, void* ws,
+                                  int* status, cudaStream_t st);
+
 // the prefix scan of the recurrent state (prefill of a linear-attention layer)
 cudaError_t launch_prefill_state(const jet_layout& lay, const jet_dims& d, int rule,
                                  const float* s_init, const void* q, const void* k, const void* v,

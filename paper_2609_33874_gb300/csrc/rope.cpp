@@ -1,0 +1,34 @@
+// What the rotation by position needs of a model (jet_rope): the frequencies as fractions
+// of a turn. An angle p f is needed modulo a turn only, and p times f / (2 pi) in units of
+// 2^-64 turns wraps in 64 bits by itself: no position loses digits to a large angle.
+#include <cmath>
+#include <cstring>
+
+#include "jet.h"
+
+extern "C" jet_status jet_rope_init(int32_t rot, int32_t style, double theta, const double* freq,
+                                    int32_t norm, float eps, jet_rope* out) {
+  if (!out) return JET_ERR_ARG;
+  if (style != JET_ROPE_HALVES && style != JET_ROPE_PAIRS) return JET_ERR_ARG;
+  if (norm != 0 && norm != 1) return JET_ERR_ARG;
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return JET_ERR_ARG;
+  if (rot < 0 || rot > 256 || rot % 8 != 0) return JET_ERR_SHAPE;
+  if (!freq && !(theta > 0.0 && std::isfinite(theta))) return JET_ERR_ARG;
+  jet_rope r;
+  std::memset(&r, 0, sizeof(r));
+  r.rot = rot;
+  r.style = style;
+  r.norm = norm;
+  r.eps = eps;
+  for (int i = 0; i < rot / 2; ++i) {
+    const double f = freq ? freq[i] : std::pow(theta, -2.0 * i / rot);
+    if (!std::isfinite(f)) return JET_ERR_ARG;
+    double t = std::fmod(f / 6.283185307179586476925286766559, 1.0);
+    if (t < 0.0) t += 1.0;
+    // a t just below a turn may round up to it: no turn at all
+    const double scaled = std::ldexp(t, 64);
+    r.turn[i] = scaled >= 18446744073709551616.0 ? 0u : static_cast<uint64_t>(scaled);
+  }
+  *out = r;
+  return JET_OK;
+}

@@ -1,0 +1,50 @@
+// Which keys a token sees under a window (jet_prefix_attend_window,
+// jet_prefill_attend_window): of the tokens up to its own position p, the last `window` and
+// the first `sinks`. Plain arithmetic, for the kernels and for host tests.
+#pragma once
+
+#include <stdint.h>
+
+#ifndef JET_HD
+#ifdef __CUDACC__
+#define JET_HD __host__ __device__ __forceinline__
+#else
+#define JET_HD inline
+#endif
+#endif
+
+namespace jet {
+
+struct Window {
+  int window, sinks;
+};
+
+// The tokens [0, first) and [lo, p] that position p sees, first <= lo.
+struct Seen {
+  int64_t first, lo;
+};
+JET_HD Seen seen_at(const Window& w, int64_t p) {
+  Seen s;
+  s.lo = p - w.window + 1;
+  if (s.lo < 0) s.lo = 0;
+  s.first = w.sinks < s.lo ? w.sinks : s.lo;
+  return s;
+}
+
+// The same of a row of the step at t (0: the shared row) over a prefix of P tokens: prefix
+// keys [0, pre_first) and [pre_lo, P), own candidate tokens [1, own_first] and [own_lo, t].
+struct RowSeen {
+  int pre_first, pre_lo, own_first, own_lo;
+};
+JET_HD RowSeen row_seen(const Window& w, int P, int t) {
+  const Seen s = seen_at(w, int64_t(P) - 1 + t);
+  RowSeen r;
+  r.pre_lo = int(s.lo < P ? s.lo : P);
+  r.pre_first = int(s.first < r.pre_lo ? s.first : r.pre_lo);
+  const int64_t lo = s.lo - P + 1, first = s.first - P;
+  r.own_lo = int(lo > 1 ? lo : 1);
+  r.own_first = int(first > 0 ? first : 0);
+  return r;
+}
+
+}  // namespace jet

@@ -29,6 +29,8 @@ DECIDE_ARGMAX, DECIDE_BINARY, DECIDE_ORDINAL = 0, 1, 2
 MODES = {"argmax": DECIDE_ARGMAX, "binary": DECIDE_BINARY, "ordinal": DECIDE_ORDINAL}
 RECUR_DELTA, RECUR_GLA = 0, 1
 RULES = {"delta": RECUR_DELTA, "gla": RECUR_GLA}
+ROPE_HALVES, ROPE_PAIRS = 0, 1
+ROPE_STYLES = {"halves": ROPE_HALVES, "pairs": ROPE_PAIRS}
 
 
 class JetError(RuntimeError):
@@ -59,6 +61,11 @@ class jet_layout(ctypes.Structure):
 class jet_dims(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "Hq", "Hkv", "d", "D", "Hl", "dk", "dv",
                                               "max_sms")]
+
+
+class jet_rope(ctypes.Structure):
+    _fields_ = [("rot", ctypes.c_int32), ("style", ctypes.c_int32), ("norm", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("turn", ctypes.c_uint64 * 128)]
 
 
 def _load() -> ctypes.CDLL:
@@ -94,6 +101,22 @@ def _load() -> ctypes.CDLL:
                                              ctypes.POINTER(jet_dims)]),
         "jet_prefill_attend": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
                                    P, P, P, P, P, SZ, P]),
+        "jet_rope_init": (I, [I, I, ctypes.c_double, ctypes.POINTER(ctypes.c_double), I,
+                              ctypes.c_float, ctypes.POINTER(jet_rope)]),
+        "jet_norm_rotate": (I, [ctypes.POINTER(jet_dims), ctypes.POINTER(jet_rope), I,
+                                P, P, P, P, P, P, P, P]),
+        "jet_norm_rotate_prefix": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
+                                       ctypes.POINTER(jet_rope), P, P, P, P, P, P, P]),
+        "jet_norm_rotate_rows": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
+                                     ctypes.POINTER(jet_rope), P, P, P, P, P, P, P]),
+        "jet_attend_window_workspace_bytes": (SZ, [ctypes.POINTER(jet_sizes),
+                                                   ctypes.POINTER(jet_dims), I, I]),
+        "jet_prefix_attend_window": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
+                                         I, I, P, P, P, P, P, P, P, SZ, P]),
+        "jet_prefill_window_workspace_bytes": (SZ, [ctypes.POINTER(jet_sizes),
+                                                    ctypes.POINTER(jet_dims), I, I]),
+        "jet_prefill_attend_window": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
+                                          I, I, P, P, P, P, P, SZ, P]),
         "jet_prefill_state": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims), I,
                                   P, P, P, P, P, P, P, P, P]),
         "jet_fork_state": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
@@ -140,7 +163,11 @@ DECLARED = ("jet_abi_version", "jet_status_string", "jet_layout_plan", "jet_layo
             "jet_layout_build", "jet_layout_bind", "jet_workspace_bytes", "jet_prefix_attend",
             "jet_kv_e4m3_bytes", "jet_quantize_kv_e4m3", "jet_append_kv_e4m3",
             "jet_dequantize_kv_e4m3", "jet_attend_workspace_bytes_e4m3", "jet_prefix_attend_e4m3",
-            "jet_prefill_workspace_bytes", "jet_prefill_attend", "jet_prefill_state",
+            "jet_prefill_workspace_bytes", "jet_prefill_attend", "jet_rope_init",
+            "jet_norm_rotate", "jet_norm_rotate_prefix", "jet_norm_rotate_rows",
+            "jet_attend_window_workspace_bytes", "jet_prefix_attend_window",
+            "jet_prefill_window_workspace_bytes", "jet_prefill_attend_window",
+            "jet_prefill_state",
             "jet_fork_state", "jet_fork_state_rule", "jet_score_candidates", "jet_score_candidates_noalloc",
             "jet_quantize_rows_e4m3", "jet_workspace_bytes_e4m3", "jet_score_candidates_e4m3",
             "jet_w4_bytes", "jet_quantize_w4", "jet_score_candidates_w4",
@@ -373,6 +400,107 @@ def jet_prefill_attend(layout, dims: jet_dims, q, k, v, o, ws, ws_bytes: Optiona
     _check(_lib.jet_prefill_attend(ctypes.byref(_lay(layout)), ctypes.byref(dims), _addr(q),
                                    _addr(k), _addr(v), _addr(o), _addr(ws), int(ws_bytes),
                                    _stream(stream)), "jet_prefill_attend")
+
+
+def make_rope(rot: int, style: str = "halves", theta: float = 10000.0, freq=None,
+              norm: bool = True, eps: float = 1e-6) -> jet_rope:
+    """A model's rotation (jet_rope_init): ``rot`` rotated elements of a head, pairs of
+    ``style`` "halves" or "pairs", at theta^(-2 i / rot) or the ``freq`` [rot / 2] given, in
+    radians a position; ``norm``: normalise the heads first."""
+    if style not in ROPE_STYLES:
+        raise ValueError("style must be 'halves' or 'pairs'")
+    f = None
+    if freq is not None:
+        f = np.ascontiguousarray(np.asarray(freq, dtype=np.float64))
+        if f.shape != (int(rot) // 2,):
+            raise ValueError("freq holds one frequency a pair: rot / 2")
+    out = jet_rope()
+    _check(_lib.jet_rope_init(int(rot), ROPE_STYLES[style], float(theta),
+                              f.ctypes.data_as(ctypes.POINTER(ctypes.c_double))
+                              if f is not None else None, 1 if norm else 0, float(eps),
+                              ctypes.byref(out)), "jet_rope_init")
+    return out
+
+
+def jet_norm_rotate(dims: jet_dims, rope: jet_rope, pos, q, k, gq, gk, q_out, k_out,
+                    stream=None) -> None:
+    """Norm and rotation of q [n, Hq, d] and k [n, Hkv, d] (either may be None) at the
+    positions pos [n], an int32 device tensor (see include/jet.h)."""
+    if pos.dim() != 1 or pos.element_size() != 4 or pos.is_floating_point():
+        raise ValueError("pos must be a vector of int32")
+    n = int(pos.shape[0])
+    for x in (q, k, q_out, k_out):
+        if x is not None and not isinstance(x, int) and int(x.shape[0]) != n:
+            raise ValueError("pos, q, k and the outputs must have as many tokens")
+    _check(_lib.jet_norm_rotate(ctypes.byref(dims), ctypes.byref(rope), n, _addr(pos), _addr(q),
+                                _addr(k), _addr(gq), _addr(gk), _addr(q_out), _addr(k_out),
+                                _stream(stream)), "jet_norm_rotate")
+
+
+def jet_norm_rotate_prefix(layout, dims: jet_dims, rope: jet_rope, q, k, gq, gk, q_out, k_out,
+                           stream=None) -> None:
+    """Norm and rotation of the prefixes' q and k (see include/jet.h)."""
+    _check(_lib.jet_norm_rotate_prefix(ctypes.byref(_lay(layout)), ctypes.byref(dims),
+                                       ctypes.byref(rope), _addr(q), _addr(k), _addr(gq),
+                                       _addr(gk), _addr(q_out), _addr(k_out), _stream(stream)),
+           "jet_norm_rotate_prefix")
+
+
+def jet_norm_rotate_rows(layout, dims: jet_dims, rope: jet_rope, q, k, gq, gk, q_out, k_out,
+                         stream=None) -> None:
+    """Norm and rotation of the step's q [N, Hq, d] and k [F, Hkv, d] (see include/jet.h)."""
+    _check(_lib.jet_norm_rotate_rows(ctypes.byref(_lay(layout)), ctypes.byref(dims),
+                                     ctypes.byref(rope), _addr(q), _addr(k), _addr(gq), _addr(gk),
+                                     _addr(q_out), _addr(k_out), _stream(stream)),
+           "jet_norm_rotate_rows")
+
+
+def _i32_arg(x, name: str) -> int:
+    """x as an int32 argument (ctypes would cut a larger one silently)."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise ValueError(f"{name} must fit an int32")
+    return x
+
+
+def _win(window, sinks):
+    return _i32_arg(window, "window"), _i32_arg(sinks, "sinks")
+
+
+def jet_attend_window_workspace_bytes(sizes: jet_sizes, dims: jet_dims, window: int,
+                                      sinks: int) -> int:
+    return int(_lib.jet_attend_window_workspace_bytes(ctypes.byref(sizes), ctypes.byref(dims),
+                                                      *_win(window, sinks)))
+
+
+def jet_prefix_attend_window(layout, dims: jet_dims, window: int, sinks: int, q, k_pre, v_pre,
+                             k_cand, v_cand, o, ws, ws_bytes: Optional[int] = None,
+                             stream=None) -> None:
+    """jet_prefix_attend where a row sees its last ``window`` tokens and the first ``sinks``
+    (see include/jet.h)."""
+    ws_bytes = ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    _check(_lib.jet_prefix_attend_window(ctypes.byref(_lay(layout)), ctypes.byref(dims),
+                                         *_win(window, sinks), _addr(q), _addr(k_pre),
+                                         _addr(v_pre), _addr(k_cand), _addr(v_cand), _addr(o),
+                                         _addr(ws), int(ws_bytes), _stream(stream)),
+           "jet_prefix_attend_window")
+
+
+def jet_prefill_window_workspace_bytes(sizes: jet_sizes, dims: jet_dims, window: int,
+                                       sinks: int) -> int:
+    return int(_lib.jet_prefill_window_workspace_bytes(ctypes.byref(sizes), ctypes.byref(dims),
+                                                       *_win(window, sinks)))
+
+
+def jet_prefill_attend_window(layout, dims: jet_dims, window: int, sinks: int, q, k, v, o, ws,
+                              ws_bytes: Optional[int] = None, stream=None) -> None:
+    """jet_prefill_attend where a position sees its last ``window`` tokens and the first
+    ``sinks`` (see include/jet.h)."""
+    ws_bytes = ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    _check(_lib.jet_prefill_attend_window(ctypes.byref(_lay(layout)), ctypes.byref(dims),
+                                          *_win(window, sinks), _addr(q), _addr(k), _addr(v),
+                                          _addr(o), _addr(ws), int(ws_bytes), _stream(stream)),
+           "jet_prefill_attend_window")
 
 
 def jet_prefill_state(layout, dims: jet_dims, q, k, v, alpha, beta, o, s_out, s_init=None,

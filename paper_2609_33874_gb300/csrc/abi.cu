@@ -493,13 +493,13 @@ extern "C" jet_status jet_prefill_attend_window(const jet_layout* lay, const jet
   if (dims->Hq / dims->Hkv > jet::attn_tc_block()) return JET_ERR_UNSUPPORTED;
   const jet_sizes& n = lay->n;
   if (n.R == 0) return JET_OK;
-  if (n.R > 65535) return JET_ERR_CAPACITY;
+  const size_t need = jet::prefill_window_bytes(n, *dims, window, sinks);
+  if ((need - 32) / 16 > size_t(INT32_MAX)) return JET_ERR_CAPACITY;  // items a counter indexes
   JET_TRY(check_ptr(q, n.total_prefix));
   JET_TRY(check_ptr(k, n.total_prefix));
   JET_TRY(check_ptr(v, n.total_prefix));
   JET_TRY(check_ptr(o, n.total_prefix));
-  if (!ws || ws_bytes < jet::prefill_window_bytes(n, *dims, window, sinks))
-    return JET_ERR_WORKSPACE;
+  if (!ws || ws_bytes < need) return JET_ERR_WORKSPACE;
   if (!aligned16(ws)) return JET_ERR_ALIGN;
   return cuda_status(jet::launch_prefill_window(*lay, *dims, window, sinks, q, k, v, o, ws,
                                                 jet::device_status_ptr(),

@@ -36,17 +36,23 @@ struct RequestCut {
 // layout gives it, if it lies in the batch and within the plan. The partials'
 // workspace holds `splits` chunks of every row, so a request with more is not
 // worked on at all. (Taken once a request: the divisions are what it costs.)
-JET_HD RequestCut request_cut(const ItemPlan& a, int n0, int nr, int p0, int P) {
+JET_HD bool request_fits(const ItemPlan& a, int n0, int nr, int p0, int P) {
+  if (nr < 1 || nr > a.N || n0 < 0 || n0 > a.N - nr) return false;
+  return P >= 1 && P <= a.total_prefix && p0 >= 0 && p0 <= a.total_prefix - P;
+}
+// nr rows and `keys` prefix keys, within the plan or left out
+JET_HD RequestCut cut_keys(const ItemPlan& a, int nr, int keys) {
   RequestCut c{};
-  if (nr < 1 || nr > a.N || n0 < 0 || n0 > a.N - nr) return c;
-  if (P < 1 || P > a.total_prefix || p0 < 0 || p0 > a.total_prefix - P) return c;
-  const int tiles = (P + kItemTile - 1) / kItemTile;
-  const int s = P <= a.chunk ? 1 : (P + a.chunk - 1) / a.chunk;
+  const int tiles = (keys + kItemTile - 1) / kItemTile;
+  const int s = keys <= a.chunk ? 1 : (keys + a.chunk - 1) / a.chunk;
   c.per = s == 1 ? tiles : (tiles + s - 1) / s;
   c.sp = s == 1 ? 1 : (tiles + c.per - 1) / c.per;
   const int nq = nr <= a.rb ? 1 : (nr + a.rb - 1) / a.rb;
   if (nq <= a.qgroups && c.sp <= a.splits) c.nq = nq;
   return c;
+}
+JET_HD RequestCut request_cut(const ItemPlan& a, int n0, int nr, int p0, int P) {
+  return request_fits(a, n0, nr, p0, P) ? cut_keys(a, nr, P) : RequestCut{};
 }
 
 // Geometry of one work item (request r, key/value head kh, query block qb,

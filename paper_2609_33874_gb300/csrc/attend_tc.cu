@@ -37,6 +37,7 @@
 #include <cmath>
 
 #include "attend_tc.cuh"
+#include "window_rows.cuh"
 
 namespace jet {
 namespace {
@@ -77,6 +78,7 @@ __device__ __forceinline__ int4 item_of(const AttArgs& a, long long idx, int spl
   return make_int4(rk / a.Hkv, rk % a.Hkv, qb, split);
 }
 
+template <bool WIN>
 __global__ void __launch_bounds__(1024)
 attend_items_kernel(const AttArgs a, int qgroups, int splits) {
   pdl_begin();
@@ -89,7 +91,7 @@ attend_items_kernel(const AttArgs a, int qgroups, int splits) {
   const long long n_all = (long long)a.R * a.Hkv * qgroups * splits;
   for (long long idx = threadIdx.x; idx < n_all; idx += blockDim.x) {
     bool fits;
-    const ItemGeo e = item_geo(a, item_of(a, idx, splits), &fits);
+    const ItemGeo e = item_geo<WIN>(a, item_of(a, idx, splits), &fits);
     if (!fits) flag(a.status, JET_ERR_DEVICE);  // the request is left out
     const int b = e.ok ? min(e.ntiles, kBuckets - 1) : 0;
     if (idx < kItemCache) bucket[idx] = uint8_t(b);
@@ -125,11 +127,63 @@ attend_items_kernel(const AttArgs a, int qgroups, int splits) {
       b = bucket[idx];
     } else {
       bool fits;
-      const ItemGeo e = item_geo(a, it, &fits);
+      const ItemGeo e = item_geo<WIN>(a, it, &fits);
       b = e.ok ? min(e.ntiles, kBuckets - 1) : 0;
     }
     if (b > 0) a.items[atomicAdd(&cursor[b], 1)] = it;
   }
+}
+
+// What a windowed kernel takes besides: maps of boxes of kSlotBox keys, for the tile that
+// holds the last first keys and the window's first, and the tensors themselves, for vectors
+// that are computed again (window_rows.cuh).
+template <bool WIN>
+struct WinArgs {};
+template <>
+struct WinArgs<true> {
+  CUtensorMap k16, v16;
+  const __nv_bfloat16 *k, *v, *kc, *vc;
+};
+
+// 64 keys of an item's slots from slot0 on into a tile (DH / 64 slices): one box a slice, or
+// kSlotBox keys at a time where first keys and window meet
+template <int DH>
+__device__ __forceinline__ void load_slots(uint8_t* dst, const CUtensorMap* map,
+                                           const CUtensorMap* map16, uint64_t* bar,
+                                           const Slots& sl, int slot0, int p0, int kh,
+                                           uint64_t pol) {
+  if (slot0 < sl.pad && slot0 + kBN > sl.pad) {
+#pragma unroll
+    for (int b = 0; b < kBN / kSlotBox; ++b) {
+      const int slot = slot0 + b * kSlotBox;
+      const int key = p0 + (slot < sl.pad ? slot : slot + sl.off);
+#pragma unroll
+      for (int i = 0; i < DH / 64; ++i)
+        tma_load_3d(dst + i * (kBN * 128) + b * (kSlotBox * 128), map16, bar, i * 64, kh, key, pol);
+    }
+  } else {
+    const int key = p0 + slot0 + (slot0 < sl.pad ? 0 : sl.off);
+#pragma unroll
+    for (int i = 0; i < DH / 64; ++i)
+      tma_load_3d(dst + i * (kBN * 128), map, bar, i * 64, kh, key, pol);
+  }
+}
+
+// query vector gv of an item's request, key by key; t of its own fed tokens from the f-th on
+template <int DH>
+__device__ __noinline__ void again(const AttArgs& a, const WinArgs<true>& w, const ItemGeo& e,
+                                   int gv, int t, int f, int lane) {
+  const size_t at = (size_t(e.n0 + gv / a.g) * a.Hq + e.kh * a.g + gv % a.g) * DH;
+  const size_t step = size_t(a.Hkv) * DH, pre = size_t(e.p0) * step + size_t(e.kh) * DH;
+  if (a.prefill) {
+    position_attend<DH>(a.win, a.q + at, w.k + pre, w.v + pre, step, gv / a.g, a.o + at, lane);
+    return;
+  }
+  // (row offsets that pass request_cut may name fed tokens outside the batch)
+  if (!fed_inside(a, t > 0 ? f : 0, t)) t = 0;
+  const size_t own = t > 0 ? size_t(f) * step + size_t(e.kh) * DH : 0;
+  row_attend<DH>(a.win, a.q + at, w.k + pre, w.v + pre, w.kc + own, w.vc + own, step, e.P, t,
+                 a.o + at, lane);
 }
 
 // One persistent CTA per SM. The scheduler warp claims the work items one
@@ -138,13 +192,14 @@ attend_items_kernel(const AttArgs a, int qgroups, int splits) {
 // when they are done with its item. All barrier phases run on counters that
 // continue across items, so the next item's query block and first K/V tiles
 // load while the current item's last tiles and its output are still in flight.
-template <int DH>
+template <int DH, bool WIN>
 __global__ void __launch_bounds__(kThreads, 1)
 attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
                         const __grid_constant__ CUtensorMap tmK,
                         const __grid_constant__ CUtensorMap tmV,
                         const __grid_constant__ CUtensorMap tmKc,
-                        const __grid_constant__ CUtensorMap tmVc, const AttArgs a) {
+                        const __grid_constant__ CUtensorMap tmVc, const AttArgs a,
+                        const __grid_constant__ WinArgs<WIN> w) {
   using G = Geo<DH>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -243,7 +298,7 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
             if (idx >= count) break;
             const int4 cand = a.items[idx];
             bool fits;
-            const ItemGeo ce = item_geo(a, cand, &fits);
+            const ItemGeo ce = item_geo<WIN>(a, cand, &fits);
             if (ce.ok) {
               it = cand;
               e = ce;
@@ -262,7 +317,7 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         const int k = u * n + ((u & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
         int4 cand;
         ItemGeo ce;
-        if (k < a.n_all && nth_item(a, k, lane, window, &cand, &ce)) {
+        if (k < a.n_all && nth_item<WIN>(a, k, lane, window, &cand, &ce)) {
           if (ce.ok) {
             it = cand;
             e = ce;
@@ -318,6 +373,8 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
           q_par = v & 1;
         }
         // K_j and V_j are issued as soon as their slots drain, whichever first
+        Slots sl{};
+        if constexpr (WIN) sl = item_slots(a, e);
         int jk = 0, jv = 0;
         IdleClock clk;
         while (jv < e.ntiles) {
@@ -330,11 +387,17 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
               uint8_t* ks = smem + G::kOffK + s * 2 * G::kKVBytes;
               mbar_arrive_expect_tx(k_full + s, G::kKVBytes);
               const bool pre = jk < e.npt;
+              if (WIN && pre) {
+                if constexpr (WIN)
+                  load_slots<DH>(ks, &tmK, &w.k16, k_full + s, sl, e.k_begin + jk * kBN, e.p0, e.kh,
+                                 pol);
+              } else {
               const CUtensorMap* mk = pre ? &tmK : &tmKc;
               const int key = pre ? e.p0 + e.k_begin + jk * kBN : e.f_begin + (jk - e.npt) * kBN;
 #pragma unroll
               for (int sl = 0; sl < G::kSlices; ++sl)
                 tma_load_3d(ks + sl * (kBN * 128), mk, k_full + s, sl * 64, e.kh, key, pol);
+              }
               k_issued |= 1u << s;
               k_par = (k_par & ~(1u << s)) | (ph << s);
               ++jk;
@@ -349,11 +412,17 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
               uint8_t* vs = smem + G::kOffK + s * 2 * G::kKVBytes + G::kKVBytes;
               mbar_arrive_expect_tx(v_full + s, G::kKVBytes);
               const bool pre = jv < e.npt;
+              if (WIN && pre) {
+                if constexpr (WIN)
+                  load_slots<DH>(vs, &tmV, &w.v16, v_full + s, sl, e.k_begin + jv * kBN, e.p0, e.kh,
+                                 pol);
+              } else {
               const CUtensorMap* mv = pre ? &tmV : &tmVc;
               const int key = pre ? e.p0 + e.k_begin + jv * kBN : e.f_begin + (jv - e.npt) * kBN;
 #pragma unroll
               for (int sl = 0; sl < G::kSlices; ++sl)
                 tma_load_3d(vs + sl * (kBN * 128), mv, v_full + s, sl * 64, e.kh, key, pol);
+              }
               v_issued |= 1u << s;
               v_par = (v_par & ~(1u << s)) | (ph << s);
               ++jv;
@@ -508,6 +577,26 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
           fb = n - e.r - 1;                     // the row's own fed token, inclusive
         }
       }
+      // under a window: the slots [0, vfirst) and [vlo, vend) and the own tokens [fa, ffirst)
+      // and [flo, fb] that this vector sees
+      int vfirst = 0, vlo = 0, vend = 0, ffirst = 0, flo = 0;
+      if constexpr (WIN) {
+        const Slots sl = item_slots(a, e);
+        if (a.prefill) {
+          const int p = e.row0 + i / g;
+          const Seen see = seen_at(a.win, p);
+          vfirst = int(see.first);
+          vlo = int(see.lo - sl.off);
+          vend = p + 1 - sl.off;
+        } else {
+          const RowSeen see = row_seen(a.win, e.P, max(0, fb - fa + 1));
+          vfirst = see.pre_first;
+          vlo = see.pre_lo - sl.off;
+          vend = e.P - sl.off;
+          ffirst = fa + see.own_first;
+          flo = fa + see.own_lo - 1;
+        }
+      }
       float m_used = -INFINITY, l = 0.f;
       for (int j = 0; j < e.ntiles; ++j) {
         const int Tj = T + j;
@@ -532,6 +621,28 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(s_free + b);
+        if constexpr (WIN) {
+          // what this vector sees of the tile's 64 keys
+          uint32_t see[2];
+          if (j < e.npt) {
+            const int k0 = e.k_begin + j * kBN;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+              see[x] = bit_range(-32 * x, vfirst - k0 - 32 * x) |
+                       bit_range(vlo - k0 - 32 * x, min(e.k_end, vend) - k0 - 32 * x);
+          } else {
+            const int f0 = e.f_begin + (j - e.npt) * kBN;
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+              see[x] = bit_range(fa - f0 - 32 * x, min(ffirst, fb + 1) - f0 - 32 * x) |
+                       bit_range(flo - f0 - 32 * x, fb + 1 - f0 - 32 * x);
+          }
+          if (__any_sync(0xffffffffu, (see[0] & see[1]) != ~0u)) {
+#pragma unroll
+            for (int c = 0; c < kBN; ++c)
+              if (!(see[c >> 5] >> (c & 31) & 1u)) sv[c] = -INFINITY;
+          }
+        } else {
         // visible keys of this tile: [klo, khi) of its 64 slots
         int klo = 0, khi;
         if (j < e.npt) {
@@ -542,13 +653,14 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
           klo = max(0, fa - f0);
           khi = min(kBN, fb - f0 + 1);
         }
-        // the row's tile maximum through eight independent chains (one warp per
-        // scheduler runs this: a single 64-long chain would be pure latency)
         if (__any_sync(0xffffffffu, klo > 0 || khi < kBN)) {
 #pragma unroll
           for (int c = 0; c < kBN; ++c)
             if (c < klo || c >= khi) sv[c] = -INFINITY;
         }
+        }
+        // the row's tile maximum through eight independent chains (one warp per
+        // scheduler runs this: a single 64-long chain would be pure latency)
         float mq[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) mq[q] = sv[q];
@@ -594,13 +706,15 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         // the tensor core multiplies
         uint32_t pw[kBN / 2];
         float ps[8];  // one partial sum per 8 keys, added as a tree
+        // under a window a vector may have seen no key yet: its weights are zeros then
+        const float m_off = WIN && m_used == -INFINITY ? 0.f : -m_used;
 #pragma unroll
         for (int cc = 0; cc < 8; ++cc) {
           ps[cc] = 0.f;
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const float x0 = ex2(fmaf(sv[cc * 8 + 2 * q], a.scale_log2, -m_used));
-            const float x1 = ex2(fmaf(sv[cc * 8 + 2 * q + 1], a.scale_log2, -m_used));
+            const float x0 = ex2(fmaf(sv[cc * 8 + 2 * q], a.scale_log2, m_off));
+            const float x1 = ex2(fmaf(sv[cc * 8 + 2 * q + 1], a.scale_log2, m_off));
             const uint32_t w = pack_bf16(x0, x1);
             pw[cc * 4 + q] = w;
             ps[cc] += __uint_as_float(w << 16) + __uint_as_float(w & 0xffff0000u);
@@ -667,6 +781,7 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         }
         __syncwarp();
       };
+      __nv_bfloat162 most = __floats2bfloat162_rn(0.f, 0.f);  // NaN where an output is
 #pragma unroll 1
       for (int c0 = 0; c0 < DH; c0 += kCols) {
         float ov[kCols / 32][32];
@@ -683,6 +798,12 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
               const float* y = ov[k + (q >> 2)] + 8 * (q & 3);
               x[q] = make_uint4(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
                                 pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv));
+              if constexpr (WIN) {
+                const uint32_t words[4] = {x[q].x, x[q].y, x[q].z, x[q].w};
+#pragma unroll
+                for (int z = 0; z < 4; ++z)
+                  most = __hmax2_nan(most, *reinterpret_cast<const __nv_bfloat162*>(&words[z]));
+              }
             }
             put_piece(x, reinterpret_cast<char*>(a.o), 2, c0 + 32 * k);
           }
@@ -705,6 +826,17 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         mbar_arrive(o_free);
         mbar_arrive(item_empty + slot);
       }
+      if constexpr (WIN) {
+        // vectors with a NaN: again from what they see alone
+        const bool nan = __hisnan(most.x) || __hisnan(most.y);
+        for (unsigned left = __ballot_sync(0xffffffffu, direct && valid && nan); left;
+             left &= left - 1) {
+          const int src = __ffs(left) - 1, gv = e.vbase + q4 * 32 + src;
+          const int t = __shfl_sync(0xffffffffu, max(0, fb - fa + 1), src);
+          const int f = __shfl_sync(0xffffffffu, fa, src);
+          again<DH>(a, w, e, gv, t, f, lane);
+        }
+      }
       T += e.ntiles;
     }
     if (!ok) {
@@ -721,11 +853,69 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
   }
 }
 
+// The combine of a windowed step's chunks, one warp per (row, query head): the plain one's
+// (attend_combine_kernel), and outputs with a NaN again from what their row sees alone.
 template <int DH>
+__global__ void __launch_bounds__(128)
+combine_window_kernel(const AttArgs a, const WinArgs<true> w, const int32_t* __restrict__ row_req,
+                      bool ahead) {
+  pdl_begin();
+  const int lane = threadIdx.x & 31;
+  const long long idx = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  if (idx >= (long long)a.N * a.Hq) return;
+  const int n = int(idx / a.Hq), h = int(idx % a.Hq);
+  const int r = row_req[n];
+  const bool direct = a.ml_part[size_t(n) * a.Hq + h].y < 0.f;
+  if (!ahead && direct) return;
+  constexpr int PER = DH / 32;
+  float acc[PER];
+  float m, l;
+  combine_chunks<DH>(ahead, a.splits, a.N, a.Hq, n, h, lane, a.ml_part, a.o_part, m, l, acc);
+  if (r < 0 || r >= a.R) {
+    if (lane == 0) flag(a.status, JET_ERR_DEVICE);
+    return;
+  }
+  if (direct) return;
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  bool nan = false;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const float y = acc[i] * inv;
+    nan |= isnan(y);
+    a.o[(size_t(n) * a.Hq + h) * DH + lane + 32 * i] = __float2bfloat16_rn(y);
+  }
+  if (!__any_sync(0xffffffffu, nan)) return;
+  ItemGeo e{};
+  e.n0 = a.row_offset[r];
+  e.kh = h / a.g;
+  e.p0 = a.prefix_offset[r];
+  e.P = a.prefix_offset[r + 1] - e.p0;
+  const int c = a.row_cand[n];
+  int t = 0, f = 0;
+  if (c >= 0 && c < a.C) {
+    f = a.cand_row_offset[c] - r - 1;
+    t = n - r - 1 - f + 1;
+  }
+  // a request that was left out has no chunks to combine
+  if (!request_fits(a, e.n0, 1, e.p0, e.P) || n < e.n0 || t < 0) return;
+  again<DH>(a, w, e, (n - e.n0) * a.g + h % a.g, t, f, lane);
+}
+
+bool win_args(WinArgs<true>* w, const jet_sizes& n, const jet_dims& d, const void* k,
+              const void* v, const void* kc, const void* vc) {
+  w->k = static_cast<const __nv_bfloat16*>(k);
+  w->v = static_cast<const __nv_bfloat16*>(v);
+  w->kc = static_cast<const __nv_bfloat16*>(kc);
+  w->vc = static_cast<const __nv_bfloat16*>(vc);
+  return encode_3d(&w->k16, k, n.total_prefix, d.Hkv, d.d, 1, kSlotBox) &&
+         encode_3d(&w->v16, v, n.total_prefix, d.Hkv, d.d, 1, kSlotBox);
+}
+
+template <int DH, bool WIN>
 cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& plan,
-                      const void* q, const void* k_pre, const void* v_pre, const void* k_cand,
-                      const void* v_cand, void* o, float* o_part, float2* ml_part, int* status,
-                      cudaStream_t st) {
+                      const Window& win, const void* q, const void* k_pre, const void* v_pre,
+                      const void* k_cand, const void* v_cand, void* o, float* o_part,
+                      float2* ml_part, int* status, cudaStream_t st) {
   const jet_sizes& n = lay.n;
   const int F = n.N - n.R;
   const int g = d.Hq / d.Hkv;
@@ -781,21 +971,30 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
   if (sms < 1) return cudaErrorInvalidValue;
   const int grid = int(std::max<long long>(1, std::min<long long>(sms, a.n_all)));
   a.sorted = plan.sorted;
+  WinArgs<WIN> w;
+  if constexpr (WIN) {
+    a.win = win;
+    if (!win_args(&w, n, d, k_pre, v_pre, k_cand, v_cand)) return cudaErrorInvalidValue;
+  }
   cudaError_t e = cudaSuccess;
   if (a.sorted)
-    e = launch_pdl(attend_items_kernel, dim3(1), dim3(1024), 0, st, a, plan.qgroups, plan.splits);
+    e = launch_pdl(attend_items_kernel<WIN>, dim3(1), dim3(1024), 0, st, a, plan.qgroups, plan.splits);
   if (e != cudaSuccess) return e;
   const size_t smem = Geo<DH>::kBytes + 1024;
-  e = cudaFuncSetAttribute(attend_prefix_tc_kernel<DH>,
+  e = cudaFuncSetAttribute(attend_prefix_tc_kernel<DH, WIN>,
                            cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
-  e = launch_pdl(attend_prefix_tc_kernel<DH>, dim3(grid), dim3(kThreads), smem, st, tmQ, tmK, tmV,
-                 tmKc, tmVc, a);
+  e = launch_pdl(attend_prefix_tc_kernel<DH, WIN>, dim3(grid), dim3(kThreads), smem, st, tmQ, tmK,
+                 tmV, tmKc, tmVc, a, w);
   if (e != cudaSuccess || plan.splits <= 1) return e;
   // ahead while the grid is one that the chip holds at once: then a memory latency is
   // all that counts (one request of 500 keys 13.5 -> 13.1 us); in a larger grid the
   // rows of short requests are traffic (64 requests of 100 - 2,000 keys 46.4 -> 48.2 us)
   const long long blocks = ((long long)n.N * d.Hq + 3) / 4;
+  if constexpr (WIN)
+    return launch_pdl(combine_window_kernel<DH>, dim3(unsigned(blocks)), dim3(128), 0, st, a, w,
+                      lay.row_req, blocks <= 8LL * sms);
+  else
   return launch_pdl(attend_combine_kernel<DH>, dim3(unsigned(blocks)), dim3(128), 0, st,
                     lay.row_req, n.N, n.R, d.Hq, plan.splits, blocks <= 8LL * sms, o_part, ml_part,
                     static_cast<__nv_bfloat16*>(o), status);
@@ -806,9 +1005,9 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
 // a block reads the keys up to its last position, a row masks the keys past
 // its own; no chunking (the blocks already give one item per 128 / g
 // positions), so the output is written directly. Longest items first.
-template <int DH>
-cudaError_t launch_prefill_dh(const jet_layout& lay, const jet_dims& d, const void* q,
-                              const void* k, const void* v, void* o, void* ws, int* status,
+template <int DH, bool WIN>
+cudaError_t launch_prefill_dh(const jet_layout& lay, const jet_dims& d, const Window& win,
+                              const void* q, const void* k, const void* v, void* o, void* ws, int* status,
                               cudaStream_t st) {
   const jet_sizes& n = lay.n;
   const int g = d.Hq / d.Hkv;
@@ -850,18 +1049,23 @@ cudaError_t launch_prefill_dh(const jet_layout& lay, const jet_dims& d, const vo
   a.qgroups = qgroups;
   a.n_all = (long long)n.R * d.Hkv * qgroups;
   a.sorted = 1;
+  WinArgs<WIN> w;
+  if constexpr (WIN) {
+    a.win = win;
+    if (!win_args(&w, n, d, k, v, nullptr, nullptr)) return cudaErrorInvalidValue;
+  }
   cudaError_t e =
-      launch_pdl(attend_items_kernel, dim3(1), dim3(1024), 0, st, a, qgroups, 1);
+      launch_pdl(attend_items_kernel<WIN>, dim3(1), dim3(1024), 0, st, a, qgroups, 1);
   if (e != cudaSuccess) return e;
   const size_t smem = Geo<DH>::kBytes + 1024;
-  e = cudaFuncSetAttribute(attend_prefix_tc_kernel<DH>,
+  e = cudaFuncSetAttribute(attend_prefix_tc_kernel<DH, WIN>,
                            cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
   const int sms = sm_count();
   if (sms < 1) return cudaErrorInvalidValue;
   const int grid = int(std::max<long long>(1, std::min<long long>(sms, a.n_all)));
-  return launch_pdl(attend_prefix_tc_kernel<DH>, dim3(grid), dim3(kThreads), smem, st, tmQ, tmK,
-                    tmV, tmK, tmV, a);
+  return launch_pdl(attend_prefix_tc_kernel<DH, WIN>, dim3(grid), dim3(kThreads), smem, st, tmQ,
+                    tmK, tmV, tmK, tmV, a, w);
 }
 
 }  // namespace
@@ -908,35 +1112,82 @@ bool prefill_on_pairs(const jet_sizes& n, const jet_dims& d) {
   return time(single, rb, kBN, kPlanSMs) >= time(pair, 2 * rb, 128, kPlanSMs / 2);
 }
 
+template <bool WIN>
+cudaError_t prefill_dispatch(const jet_layout& lay, const jet_dims& d, const Window& win,
+                             const void* q, const void* k, const void* v, void* o, void* ws,
+                             bool pairs, int* status, cudaStream_t st) {
+  if (d.d == 64) return launch_prefill_dh<64, WIN>(lay, d, win, q, k, v, o, ws, status, st);
+  if (d.d == 128)
+    return pairs ? launch_prefill_pair<128, WIN>(lay, d, win, q, k, v, o, status, st)
+                 : launch_prefill_dh<128, WIN>(lay, d, win, q, k, v, o, ws, status, st);
+  if (d.d == 256)
+    return pairs ? launch_prefill_pair<256, WIN>(lay, d, win, q, k, v, o, status, st)
+                 : launch_prefill_dh<256, WIN>(lay, d, win, q, k, v, o, ws, status, st);
+  return cudaErrorInvalidValue;
+}
+
+// What a windowed call's plan reckons with: a request's keys are its slots, at most `window`
+// and the first ones' boxes.
+jet_sizes window_sizes(const jet_sizes& n, int window, int sinks) {
+  jet_sizes e = n;
+  const long long most = std::min<long long>(
+      n.max_prefix, (long long)window + ((long long)sinks + kSlotBox - 1) / kSlotBox * kSlotBox);
+  e.max_prefix = int(most);
+  e.total_prefix = int(std::min<long long>(n.total_prefix, most * std::max(1, n.R)));
+  return e;
+}
+
 }  // namespace
 
 cudaError_t launch_prefill_tc(const jet_layout& lay, const jet_dims& d, const void* q,
                               const void* k, const void* v, void* o, void* ws, int* status,
                               cudaStream_t st) {
-  if (d.d == 64) return launch_prefill_dh<64>(lay, d, q, k, v, o, ws, status, st);
   if (d.Hq / d.Hkv > kBV) return cudaErrorInvalidValue;
-  const bool pairs = prefill_on_pairs(lay.n, d);
-  if (d.d == 128)
-    return pairs ? launch_prefill_pair<128>(lay, d, q, k, v, o, status, st)
-                 : launch_prefill_dh<128>(lay, d, q, k, v, o, ws, status, st);
-  if (d.d == 256)
-    return pairs ? launch_prefill_pair<256>(lay, d, q, k, v, o, status, st)
-                 : launch_prefill_dh<256>(lay, d, q, k, v, o, ws, status, st);
-  return cudaErrorInvalidValue;
+  const bool pairs = d.d != 64 && prefill_on_pairs(lay.n, d);
+  return prefill_dispatch<false>(lay, d, Window{}, q, k, v, o, ws, pairs, status, st);
 }
 
 cudaError_t launch_attend_tc(const jet_layout& lay, const jet_dims& d, const AttnPlan& plan,
                              const void* q, const void* k_pre, const void* v_pre,
                              const void* k_cand, const void* v_cand, void* o, float* o_part,
                              float2* ml_part, int* status, cudaStream_t st) {
-#define JET_TC(DH)                                                                          \
-  return launch_dh<DH>(lay, d, plan, q, k_pre, v_pre, k_cand, v_cand, o, o_part, ml_part, \
-                       status, st)
+#define JET_TC(DH)                                                                               \
+  return launch_dh<DH, false>(lay, d, plan, Window{}, q, k_pre, v_pre, k_cand, v_cand, o,        \
+                              o_part, ml_part, status, st)
   if (d.d == 64) JET_TC(64);
   if (d.d == 128) JET_TC(128);
   if (d.d == 256) JET_TC(256);
 #undef JET_TC
   return cudaErrorInvalidValue;
+}
+
+AttnPlan attend_window_plan(const jet_sizes& n, const jet_dims& d, int window, int sinks) {
+  return attn_plan(window_sizes(n, window, sinks), d);
+}
+
+cudaError_t launch_attend_window_tc(const jet_layout& lay, const jet_dims& d, int window,
+                                    int sinks, const void* q, const void* k_pre,
+                                    const void* v_pre, const void* k_cand, const void* v_cand,
+                                    void* o, void* ws, int* status, cudaStream_t st) {
+  const AttnPlan plan = attend_window_plan(lay.n, d, window, sinks);
+  float* o_part = static_cast<float*>(ws);
+  float2* ml_part = reinterpret_cast<float2*>(o_part + size_t(plan.splits) * lay.n.N * d.Hq * d.d);
+  const Window win{window, sinks};
+#define JET_TC(DH)                                                                               \
+  return launch_dh<DH, true>(lay, d, plan, win, q, k_pre, v_pre, k_cand, v_cand, o, o_part,      \
+                             ml_part, status, st)
+  if (d.d == 64) JET_TC(64);
+  if (d.d == 128) JET_TC(128);
+  if (d.d == 256) JET_TC(256);
+#undef JET_TC
+  return cudaErrorInvalidValue;
+}
+
+cudaError_t launch_prefill_window_tc(const jet_layout& lay, const jet_dims& d, int window,
+                                     int sinks, const void* q, const void* k, const void* v,
+                                     void* o, void* ws, int* status, cudaStream_t st) {
+  const bool pairs = d.d != 64 && prefill_on_pairs(lay.n, d);
+  return prefill_dispatch<true>(lay, d, Window{window, sinks}, q, k, v, o, ws, pairs, status, st);
 }
 
 }  // namespace jet

@@ -12,6 +12,7 @@
 #include "jet_device.cuh"
 #include "jet_internal.h"
 #include "sm100_ptx.cuh"
+#include "window.h"
 
 namespace jet {
 namespace {
@@ -45,6 +46,7 @@ struct AttArgs : ItemPlan {
   float scale_log2;  // log2(e) / sqrt(d)
   uint64_t wait_ns;  // budget of one bounded wait (jet_set_wait_budget_ns)
   int hold_first;    // test hook (jet_set_test_stall): withhold the first query block
+  Window win;        // of the windowed forms: their keys are slots (window.h)
 };
 
 // SW128 K-major position of 16-byte chunk c of row i inside one 64-wide slice
@@ -81,16 +83,45 @@ __device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* map, int32_t 
                : "memory");
 }
 
+// How a step's request is cut: its prefix keys, or its slots under a window
+template <bool WIN>
+__device__ __forceinline__ RequestCut cut_of(const AttArgs& a, int n0, int nr, int p0, int P) {
+  if constexpr (WIN)
+    return request_fits(a, n0, nr, p0, P) ? cut_keys(a, nr, step_slots(a.win, P).n) : RequestCut{};
+  else
+    return request_cut(a, n0, nr, p0, P);
+}
+
+// The geometry of its items: under a window k_begin, k_end and npt count slots, and P is the
+// request's prefix all the same
+template <bool WIN>
+__device__ __forceinline__ ItemGeo geo_at(const AttArgs& a, int r, int kh, int qb, int split,
+                                          int n0, int nr, int p0, int P, const RequestCut& cut) {
+  if constexpr (WIN) {
+    ItemGeo e = item_geo_at(a, r, kh, qb, split, n0, nr, p0, step_slots(a.win, P).n, cut);
+    e.P = P;
+    return e;
+  } else {
+    return item_geo_at(a, r, kh, qb, split, n0, nr, p0, P, cut);
+  }
+}
+
+// The slots of an item
+__device__ __forceinline__ Slots item_slots(const AttArgs& a, const ItemGeo& e) {
+  return a.prefill ? block_slots(a.win, e.row0, min(e.P, e.row0 + a.rb)) : step_slots(a.win, e.P);
+}
+
 // Of an item of the work list; *fits: its request is one to work on
+template <bool WIN = false>
 __device__ __forceinline__ ItemGeo item_geo(const AttArgs& a, int4 it, bool* fits) {
   *fits = false;
   if (!a.prefill) {
     if (it.x < 0 || it.x >= a.R) return ItemGeo{};
     const int n0 = a.row_offset[it.x], nr = a.row_offset[it.x + 1] - n0;
     const int p0 = a.prefix_offset[it.x], P = a.prefix_offset[it.x + 1] - p0;
-    const RequestCut cut = request_cut(a, n0, nr, p0, P);
+    const RequestCut cut = cut_of<WIN>(a, n0, nr, p0, P);
     *fits = cut.nq > 0;
-    return item_geo_at(a, it.x, it.y, it.z, it.w, n0, nr, p0, P, cut);
+    return geo_at<WIN>(a, it.x, it.y, it.z, it.w, n0, nr, p0, P, cut);
   }
   // prefill: the rows are the request's prefix positions and a block of
   // them sees the keys up to its last position (per-row causal mask in the
@@ -114,6 +145,7 @@ __device__ __forceinline__ ItemGeo item_geo(const AttArgs& a, int4 it, bool* fit
   e.nv = min(a.rb, e.nr - e.row0) * a.g;
   e.splits_r = 1;
   e.k_end = min(e.P, e.row0 + a.rb);
+  if constexpr (WIN) e.k_end = block_slots(a.win, e.row0, e.k_end).n;
   e.npt = (e.k_end + kBN - 1) / kBN;
   e.ntiles = e.npt;
   e.ok = true;
@@ -175,13 +207,14 @@ struct ItemWindow {
   bool held;
   int base, before;  // its first request in the order; the items before it
 };
+template <bool WIN = false>
 __device__ __forceinline__ bool nth_item(const AttArgs& a, int k, int lane, ItemWindow& w,
                                          int4* out, ItemGeo* geo) {
   LaneReq& q = w.q;
   for (; w.base < a.R; w.base += 32) {
     if (!w.held) {
       q = lane_req(a, w.base, lane);
-      if (q.r >= 0) q.cut = request_cut(a, q.n0, q.nr, q.p0, q.P);
+      if (q.r >= 0) q.cut = cut_of<WIN>(a, q.n0, q.nr, q.p0, q.P);
       // a request that the layout or the plan does not hold is left out
       if (q.cut.nq == 0 && w.base + lane < a.R) flag(a.status, JET_ERR_DEVICE);
       w.held = true;
@@ -206,7 +239,7 @@ __device__ __forceinline__ bool nth_item(const AttArgs& a, int k, int lane, Item
       const int nq = cut.nq, sp = cut.sp;
       const int split = kk % sp, rest = kk / sp;
       *out = make_int4(r, rest / nq, rest % nq, split);
-      *geo = item_geo_at(a, r, rest / nq, rest % nq, split, __shfl_sync(0xffffffffu, q.n0, src),
+      *geo = geo_at<WIN>(a, r, rest / nq, rest % nq, split, __shfl_sync(0xffffffffu, q.n0, src),
                          __shfl_sync(0xffffffffu, q.nr, src), __shfl_sync(0xffffffffu, q.p0, src),
                          __shfl_sync(0xffffffffu, q.P, src), cut);
       return true;

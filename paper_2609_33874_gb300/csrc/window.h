@@ -47,4 +47,42 @@ JET_HD RowSeen row_seen(const Window& w, int P, int t) {
   return r;
 }
 
+// Keys as the tiles of a tensor-core kernel take them: the first `sinks` keys and [lo, end)
+// laid end to end. Slot i < pad holds key i (those from `sinks` on are masked), a later one
+// key i + off. pad is a multiple of kSlotBox, the keys of one copy into a tile that holds both;
+// 0 where nothing lies between the first keys and lo.
+constexpr int kSlotBox = 16;
+struct Slots {
+  int n, pad, off;
+};
+JET_HD Slots window_slots(const Window& w, int64_t lo, int64_t end) {
+  Slots s;
+  if (w.sinks >= lo) {
+    s.pad = s.off = 0;
+    s.n = int(end);
+  } else {
+    s.pad = int((int64_t(w.sinks) + kSlotBox - 1) / kSlotBox * kSlotBox);
+    s.off = int(lo - s.pad);
+    s.n = int(s.pad + end - lo);
+  }
+  return s;
+}
+
+// The slots of a step's request (its shared row's window reaches back the farthest) and of a
+// block of positions [first, end) of the prefill.
+JET_HD Slots step_slots(const Window& w, int P) {
+  return window_slots(w, seen_at(w, int64_t(P) - 1).lo, P);
+}
+JET_HD Slots block_slots(const Window& w, int first, int end) {
+  return window_slots(w, seen_at(w, first).lo, end);
+}
+
+// Bits [lo, hi) of a word, of what lies in it.
+JET_HD uint32_t bit_range(int lo, int hi) {
+  if (lo < 0) lo = 0;
+  if (hi > 32) hi = 32;
+  if (hi <= lo) return 0u;
+  return (hi == 32 ? ~0u : (1u << hi) - 1u) & (~0u << lo);
+}
+
 }  // namespace jet

@@ -1,0 +1,125 @@
+// Attention of one query vector under a window by one warp, key by key in float32: what the
+// tensor-core kernels fall back on for a vector whose output came out NaN. Their products
+// take whole tiles, and a weight of zero times an infinite or NaN value that the vector does
+// not see is NaN; here nothing but what it sees is read.
+#pragma once
+
+#include "jet_device.cuh"
+#include "window.h"
+
+namespace jet {
+namespace {
+
+template <int PER>
+__device__ __forceinline__ void load_row(const float* p, float (&v)[PER]) {
+#pragma unroll
+  for (int i = 0; i < PER; i += 2) {
+    const float2 x = *reinterpret_cast<const float2*>(p + i);
+    v[i] = x.x;
+    v[i + 1] = x.y;
+  }
+}
+template <int PER>
+__device__ __forceinline__ void load_row(const __nv_bfloat16* p, float (&v)[PER]) {
+#pragma unroll
+  for (int i = 0; i < PER; i += 2) {
+    const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(p + i));
+    v[i] = x.x;
+    v[i + 1] = x.y;
+  }
+}
+
+// A query vector's running softmax over keys in pieces: elements lane PER .. + PER - 1
+template <int DH>
+struct RowState {
+  static constexpr int PER = DH / 32;
+  float q[PER], acc[PER], m, l;
+
+  // keys [begin, end) of k and v, rows `step` elements apart
+  template <typename T>
+  __device__ __forceinline__ void add(const T* k, const T* v, size_t step, int begin, int end,
+                                      int lane) {
+    constexpr int kAtOnce = 4;
+    for (int j0 = begin; j0 < end; j0 += kAtOnce) {
+      float kv[kAtOnce][PER], vv[kAtOnce][PER], s[kAtOnce];
+#pragma unroll
+      for (int t = 0; t < kAtOnce; ++t) {
+        const size_t at = size_t(min(j0 + t, end - 1)) * step + lane * PER;
+        load_row<PER>(k + at, kv[t]);
+        load_row<PER>(v + at, vv[t]);
+      }
+#pragma unroll
+      for (int t = 0; t < kAtOnce; ++t) {
+        s[t] = 0.f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) s[t] = fmaf(q[i], kv[t][i], s[t]);
+        s[t] = warp_sum(s[t]);
+      }
+#pragma unroll
+      for (int t = 0; t < kAtOnce; ++t) {
+        if (j0 + t >= end) break;
+        const float mn = fmaxf(m, s[t]);
+        const float a = mn == -INFINITY ? 1.f : exp2f(m - mn);
+        const float b = mn == -INFINITY ? 0.f : exp2f(s[t] - mn);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) acc[i] = acc[i] * a + b * vv[t][i];
+        l = l * a + b;
+        m = mn;
+      }
+    }
+  }
+};
+
+template <int DH, typename T>
+__device__ __forceinline__ void begin_row(RowState<DH>& s, const T* q, int lane) {
+  const float scale = 1.4426950408889634f * rsqrtf(float(DH));  // base-2 scores
+  load_row<RowState<DH>::PER>(q + lane * RowState<DH>::PER, s.q);
+#pragma unroll
+  for (int i = 0; i < RowState<DH>::PER; ++i) {
+    s.q[i] *= scale;
+    s.acc[i] = 0.f;
+  }
+  s.m = -INFINITY;
+  s.l = 0.f;
+}
+
+template <int DH, typename T>
+__device__ __forceinline__ void end_row(const RowState<DH>& s, T* o, int lane) {
+  const float inv = 1.f / s.l;
+#pragma unroll
+  for (int i = 0; i < RowState<DH>::PER; ++i)
+    o[lane * RowState<DH>::PER + i] = from_f32<T>(s.acc[i] * inv);
+}
+
+// one row of the step: its prefix keys from kp on, its own fed tokens from kc on (the first
+// of them y_1), t of them
+template <int DH, typename T>
+__device__ __forceinline__ void row_attend(const Window& w, const T* q, const T* kp, const T* vp,
+                                           const T* kc, const T* vc, size_t step, int P, int t,
+                                           T* o, int lane) {
+  const RowSeen see = row_seen(w, P, t);
+  RowState<DH> s;
+  begin_row(s, q, lane);
+  s.add(kp, vp, step, 0, see.pre_first, lane);
+  s.add(kp, vp, step, see.pre_lo, P, lane);
+  if (t > 0) {
+    s.add(kc, vc, step, 0, min(see.own_first, t), lane);
+    s.add(kc, vc, step, see.own_lo - 1, t, lane);
+  }
+  end_row<DH, T>(s, o, lane);
+}
+
+// one position of the prefill
+template <int DH, typename T>
+__device__ __forceinline__ void position_attend(const Window& w, const T* q, const T* kp,
+                                                const T* vp, size_t step, int p, T* o, int lane) {
+  const Seen see = seen_at(w, p);
+  RowState<DH> s;
+  begin_row(s, q, lane);
+  s.add(kp, vp, step, 0, int(see.first), lane);
+  s.add(kp, vp, step, int(see.lo), p + 1, lane);
+  end_row<DH, T>(s, o, lane);
+}
+
+}  // namespace
+}  // namespace jet

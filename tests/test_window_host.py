@@ -213,3 +213,68 @@ def test_window_refusals(jet):
         assert f(hl.sizes, dims, 0, 0) == 0 and f(hl.sizes, dims, 4, -1) == 0
         assert f(hl.sizes, jet.make_dims(jet.DTYPE_BF16, Hq=8, Hkv=3, d=64), 4, 0) == 0
         assert f(hl.sizes, dims, 2 ** 31 - 1, 2 ** 31 - 1) > 0
+
+
+TILES = r"""
+#include <cstdio>
+#include "window.h"
+// the keys that a vector sees, by slots and the words of a tile's mask
+int main() {
+  int window, sinks, P, t, first, end, prefill, tile;
+  while (std::scanf("%d %d %d %d %d %d %d %d", &window, &sinks, &P, &t, &first, &end, &prefill,
+                    &tile) == 8) {
+    const jet::Window w{window, sinks};
+    const jet::Slots s = prefill ? jet::block_slots(w, first, end) : jet::step_slots(w, P);
+    long long vfirst, vlo, vend;
+    if (prefill) {
+      const jet::Seen x = jet::seen_at(w, t);
+      vfirst = x.first, vlo = x.lo - s.off, vend = (long long)t + 1 - s.off;
+    } else {
+      const jet::RowSeen x = jet::row_seen(w, P, t);
+      vfirst = x.pre_first, vlo = x.pre_lo - s.off, vend = P - s.off;
+    }
+    std::printf("%d %d %d :", s.n, s.pad, s.off);
+    for (int k0 = 0; k0 < s.n; k0 += tile)
+      for (int c0 = k0; c0 < k0 + tile; c0 += 32) {
+        const unsigned see = jet::bit_range(-c0, int(vfirst) - c0) |
+                             jet::bit_range(int(vlo) - c0, int(vend < s.n ? vend : s.n) - c0);
+        for (int x = 0; x < 32; ++x)
+          if (see >> x & 1u) std::printf(" %d", c0 + x < s.pad ? c0 + x : c0 + x + s.off);
+      }
+    std::printf("\n");
+  }
+}
+"""
+
+
+def test_slots_and_masks_give_what_the_oracle_says(repo_root, tmp_path):
+    (tmp_path / "t.cpp").write_text(TILES)
+    csrc = os.path.join(repo_root, "paper_2609_33874_gb300", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-I", csrc, str(tmp_path / "t.cpp"),
+                    "-o", str(tmp_path / "t")], check=True)
+    rng = np.random.default_rng(8)
+    cases = []
+    for w in (1, 2, 16, 50, 64, 200):
+        for s in (0, 1, 15, 16, 17, 40, 64, 70, 130):
+            for P in (1, 20, 64, 130, 300):
+                for t in (0, 1, 5, 70):
+                    cases.append((w, s, P, t, 0, 0, 0, 64))
+                # a block of the prefill and a position in it
+                first = int(rng.integers(0, P))
+                end = min(P, first + int(rng.integers(1, 64)))
+                cases.append((w, s, P, int(rng.integers(first, end)), first, end, 1, 128))
+    text = "\n".join(" ".join(map(str, c)) for c in cases)
+    out = subprocess.run([str(tmp_path / "t")], input=text, capture_output=True, text=True,
+                         check=True).stdout.splitlines()
+    assert len(out) == len(cases)
+    for (w, s, P, t, first, end, prefill, _), line in zip(cases, out):
+        head, keys = line.split(":")
+        n, pad, off = map(int, head.split())
+        keys = [int(k) for k in keys.split()]
+        want = (W.seen(t, w, s) if prefill else
+                [j for j in W.seen(P - 1 + t, w, s) if j < P])
+        assert keys == want, (w, s, P, t, first, end, prefill)
+        top = end if prefill else P
+        assert n <= top + 15 and pad % 16 == 0
+        assert n <= (end - first if prefill else 0) + w + -(-s // 16) * 16
+        assert all(0 <= j < top for j in keys)

@@ -411,7 +411,8 @@ jet_status jet_prefix_attend_window(const jet_layout* lay, const jet_dims* dims,
 /*
  * jet_prefill_attend_window - the prefill (arguments of jet_prefill_attend; bf16 only and
  * at most 128 query heads a key/value head, else JET_ERR_UNSUPPORTED).
- * ws/ws_bytes: scratch of at least jet_prefill_window_workspace_bytes().
+ * ws/ws_bytes: scratch of at least jet_prefill_window_workspace_bytes() (16 bytes: the
+ * kernel keeps nothing in memory today).
  */
 size_t jet_prefill_window_workspace_bytes(const jet_sizes* n, const jet_dims* dims,
                                           int32_t window, int32_t sinks);

@@ -393,6 +393,9 @@ jet_status check_rotate(const jet_dims* d, const jet_rope* rope, long long nq, l
   return JET_OK;
 }
 
+// what a call asks for that takes a workspace and needs none today
+constexpr size_t kNoScratch = 16;
+
 jet_status check_window(int32_t window, int32_t sinks) {
   return window < 1 || sinks < 0 ? JET_ERR_ARG : JET_OK;
 }
@@ -479,7 +482,7 @@ extern "C" size_t jet_prefill_window_workspace_bytes(const jet_sizes* n, const j
                                                      int32_t window, int32_t sinks) {
   if (!n || n->R < 0 || check_attn_dims(d) != JET_OK) return 0;
   if (check_window(window, sinks) != JET_OK) return 0;
-  return jet::prefill_window_bytes(*n, *d, window, sinks);
+  return kNoScratch;
 }
 
 extern "C" jet_status jet_prefill_attend_window(const jet_layout* lay, const jet_dims* dims,
@@ -493,15 +496,13 @@ extern "C" jet_status jet_prefill_attend_window(const jet_layout* lay, const jet
   if (dims->Hq / dims->Hkv > jet::attn_tc_block()) return JET_ERR_UNSUPPORTED;
   const jet_sizes& n = lay->n;
   if (n.R == 0) return JET_OK;
-  const size_t need = jet::prefill_window_bytes(n, *dims, window, sinks);
-  if ((need - 32) / 16 > size_t(INT32_MAX)) return JET_ERR_CAPACITY;  // items a counter indexes
   JET_TRY(check_ptr(q, n.total_prefix));
   JET_TRY(check_ptr(k, n.total_prefix));
   JET_TRY(check_ptr(v, n.total_prefix));
   JET_TRY(check_ptr(o, n.total_prefix));
-  if (!ws || ws_bytes < need) return JET_ERR_WORKSPACE;
+  if (!ws || ws_bytes < kNoScratch) return JET_ERR_WORKSPACE;
   if (!aligned16(ws)) return JET_ERR_ALIGN;
-  return cuda_status(jet::launch_prefill_window(*lay, *dims, window, sinks, q, k, v, o, ws,
+  return cuda_status(jet::launch_prefill_window(*lay, *dims, window, sinks, q, k, v, o,
                                                 jet::device_status_ptr(),
                                                 static_cast<cudaStream_t>(stream)));
 }

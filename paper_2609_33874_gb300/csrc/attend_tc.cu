@@ -175,10 +175,6 @@ __device__ __noinline__ void again(const AttArgs& a, const WinArgs<true>& w, con
                                    int gv, int t, int f, int lane) {
   const size_t at = (size_t(e.n0 + gv / a.g) * a.Hq + e.kh * a.g + gv % a.g) * DH;
   const size_t step = size_t(a.Hkv) * DH, pre = size_t(e.p0) * step + size_t(e.kh) * DH;
-  if (a.prefill) {
-    position_attend<DH>(a.win, a.q + at, w.k + pre, w.v + pre, step, gv / a.g, a.o + at, lane);
-    return;
-  }
   // (row offsets that pass request_cut may name fed tokens outside the batch)
   if (!fed_inside(a, t > 0 ? f : 0, t)) t = 0;
   const size_t own = t > 0 ? size_t(f) * step + size_t(e.kh) * DH : 0;
@@ -374,7 +370,7 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         }
         // K_j and V_j are issued as soon as their slots drain, whichever first
         Slots sl{};
-        if constexpr (WIN) sl = item_slots(a, e);
+        if constexpr (WIN) sl = step_slots(a.win, e.P);
         int jk = 0, jv = 0;
         IdleClock clk;
         while (jv < e.ntiles) {
@@ -577,25 +573,16 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
           fb = n - e.r - 1;                     // the row's own fed token, inclusive
         }
       }
-      // under a window: the slots [0, vfirst) and [vlo, vend) and the own tokens [fa, ffirst)
-      // and [flo, fb] that this vector sees
-      int vfirst = 0, vlo = 0, vend = 0, ffirst = 0, flo = 0;
+      // under a window: the slots before vfirst and from vlo on and the own tokens
+      // [fa, ffirst) and [flo, fb] that this vector sees
+      int vfirst = 0, vlo = 0, ffirst = 0, flo = 0;
       if constexpr (WIN) {
-        const Slots sl = item_slots(a, e);
-        if (a.prefill) {
-          const int p = e.row0 + i / g;
-          const Seen see = seen_at(a.win, p);
-          vfirst = int(see.first);
-          vlo = int(see.lo - sl.off);
-          vend = p + 1 - sl.off;
-        } else {
-          const RowSeen see = row_seen(a.win, e.P, max(0, fb - fa + 1));
-          vfirst = see.pre_first;
-          vlo = see.pre_lo - sl.off;
-          vend = e.P - sl.off;
-          ffirst = fa + see.own_first;
-          flo = fa + see.own_lo - 1;
-        }
+        const Slots sl = step_slots(a.win, e.P);
+        const RowSeen see = row_seen(a.win, e.P, max(0, fb - fa + 1));
+        vfirst = see.pre_first;
+        vlo = see.pre_lo - sl.off;
+        ffirst = fa + see.own_first;
+        flo = fa + see.own_lo - 1;
       }
       float m_used = -INFINITY, l = 0.f;
       for (int j = 0; j < e.ntiles; ++j) {
@@ -629,7 +616,7 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
 #pragma unroll
             for (int x = 0; x < 2; ++x)
               see[x] = bit_range(-32 * x, vfirst - k0 - 32 * x) |
-                       bit_range(vlo - k0 - 32 * x, min(e.k_end, vend) - k0 - 32 * x);
+                       bit_range(vlo - k0 - 32 * x, e.k_end - k0 - 32 * x);
           } else {
             const int f0 = e.f_begin + (j - e.npt) * kBN;
 #pragma unroll
@@ -1005,9 +992,9 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
 // a block reads the keys up to its last position, a row masks the keys past
 // its own; no chunking (the blocks already give one item per 128 / g
 // positions), so the output is written directly. Longest items first.
-template <int DH, bool WIN>
-cudaError_t launch_prefill_dh(const jet_layout& lay, const jet_dims& d, const Window& win,
-                              const void* q, const void* k, const void* v, void* o, void* ws, int* status,
+template <int DH>
+cudaError_t launch_prefill_dh(const jet_layout& lay, const jet_dims& d, const void* q,
+                              const void* k, const void* v, void* o, void* ws, int* status,
                               cudaStream_t st) {
   const jet_sizes& n = lay.n;
   const int g = d.Hq / d.Hkv;
@@ -1049,23 +1036,18 @@ cudaError_t launch_prefill_dh(const jet_layout& lay, const jet_dims& d, const Wi
   a.qgroups = qgroups;
   a.n_all = (long long)n.R * d.Hkv * qgroups;
   a.sorted = 1;
-  WinArgs<WIN> w;
-  if constexpr (WIN) {
-    a.win = win;
-    if (!win_args(&w, n, d, k, v, nullptr, nullptr)) return cudaErrorInvalidValue;
-  }
   cudaError_t e =
-      launch_pdl(attend_items_kernel<WIN>, dim3(1), dim3(1024), 0, st, a, qgroups, 1);
+      launch_pdl(attend_items_kernel<false>, dim3(1), dim3(1024), 0, st, a, qgroups, 1);
   if (e != cudaSuccess) return e;
   const size_t smem = Geo<DH>::kBytes + 1024;
-  e = cudaFuncSetAttribute(attend_prefix_tc_kernel<DH, WIN>,
+  e = cudaFuncSetAttribute(attend_prefix_tc_kernel<DH, false>,
                            cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
   const int sms = sm_count();
   if (sms < 1) return cudaErrorInvalidValue;
   const int grid = int(std::max<long long>(1, std::min<long long>(sms, a.n_all)));
-  return launch_pdl(attend_prefix_tc_kernel<DH, WIN>, dim3(grid), dim3(kThreads), smem, st, tmQ,
-                    tmK, tmV, tmK, tmV, a, w);
+  return launch_pdl(attend_prefix_tc_kernel<DH, false>, dim3(grid), dim3(kThreads), smem, st, tmQ,
+                    tmK, tmV, tmK, tmV, a, WinArgs<false>{});
 }
 
 }  // namespace
@@ -1112,20 +1094,6 @@ bool prefill_on_pairs(const jet_sizes& n, const jet_dims& d) {
   return time(single, rb, kBN, kPlanSMs) >= time(pair, 2 * rb, 128, kPlanSMs / 2);
 }
 
-template <bool WIN>
-cudaError_t prefill_dispatch(const jet_layout& lay, const jet_dims& d, const Window& win,
-                             const void* q, const void* k, const void* v, void* o, void* ws,
-                             bool pairs, int* status, cudaStream_t st) {
-  if (d.d == 64) return launch_prefill_dh<64, WIN>(lay, d, win, q, k, v, o, ws, status, st);
-  if (d.d == 128)
-    return pairs ? launch_prefill_pair<128, WIN>(lay, d, win, q, k, v, o, status, st)
-                 : launch_prefill_dh<128, WIN>(lay, d, win, q, k, v, o, ws, status, st);
-  if (d.d == 256)
-    return pairs ? launch_prefill_pair<256, WIN>(lay, d, win, q, k, v, o, status, st)
-                 : launch_prefill_dh<256, WIN>(lay, d, win, q, k, v, o, ws, status, st);
-  return cudaErrorInvalidValue;
-}
-
 // What a windowed call's plan reckons with: a request's keys are its slots, at most `window`
 // and the first ones' boxes.
 jet_sizes window_sizes(const jet_sizes& n, int window, int sinks) {
@@ -1142,9 +1110,16 @@ jet_sizes window_sizes(const jet_sizes& n, int window, int sinks) {
 cudaError_t launch_prefill_tc(const jet_layout& lay, const jet_dims& d, const void* q,
                               const void* k, const void* v, void* o, void* ws, int* status,
                               cudaStream_t st) {
+  if (d.d == 64) return launch_prefill_dh<64>(lay, d, q, k, v, o, ws, status, st);
   if (d.Hq / d.Hkv > kBV) return cudaErrorInvalidValue;
-  const bool pairs = d.d != 64 && prefill_on_pairs(lay.n, d);
-  return prefill_dispatch<false>(lay, d, Window{}, q, k, v, o, ws, pairs, status, st);
+  const bool pairs = prefill_on_pairs(lay.n, d);
+  if (d.d == 128)
+    return pairs ? launch_prefill_pair<128>(lay, d, q, k, v, o, status, st)
+                 : launch_prefill_dh<128>(lay, d, q, k, v, o, ws, status, st);
+  if (d.d == 256)
+    return pairs ? launch_prefill_pair<256>(lay, d, q, k, v, o, status, st)
+                 : launch_prefill_dh<256>(lay, d, q, k, v, o, ws, status, st);
+  return cudaErrorInvalidValue;
 }
 
 cudaError_t launch_attend_tc(const jet_layout& lay, const jet_dims& d, const AttnPlan& plan,
@@ -1181,13 +1156,6 @@ cudaError_t launch_attend_window_tc(const jet_layout& lay, const jet_dims& d, in
   if (d.d == 256) JET_TC(256);
 #undef JET_TC
   return cudaErrorInvalidValue;
-}
-
-cudaError_t launch_prefill_window_tc(const jet_layout& lay, const jet_dims& d, int window,
-                                     int sinks, const void* q, const void* k, const void* v,
-                                     void* o, void* ws, int* status, cudaStream_t st) {
-  const bool pairs = d.d != 64 && prefill_on_pairs(lay.n, d);
-  return prefill_dispatch<true>(lay, d, Window{window, sinks}, q, k, v, o, ws, pairs, status, st);
 }
 
 }  // namespace jet

@@ -106,11 +106,6 @@ __device__ __forceinline__ ItemGeo geo_at(const AttArgs& a, int r, int kh, int q
   }
 }
 
-// The slots of an item
-__device__ __forceinline__ Slots item_slots(const AttArgs& a, const ItemGeo& e) {
-  return a.prefill ? block_slots(a.win, e.row0, min(e.P, e.row0 + a.rb)) : step_slots(a.win, e.P);
-}
-
 // Of an item of the work list; *fits: its request is one to work on
 template <bool WIN = false>
 __device__ __forceinline__ ItemGeo item_geo(const AttArgs& a, int4 it, bool* fits) {
@@ -145,7 +140,6 @@ __device__ __forceinline__ ItemGeo item_geo(const AttArgs& a, int4 it, bool* fit
   e.nv = min(a.rb, e.nr - e.row0) * a.g;
   e.splits_r = 1;
   e.k_end = min(e.P, e.row0 + a.rb);
-  if constexpr (WIN) e.k_end = block_slots(a.win, e.row0, e.k_end).n;
   e.npt = (e.k_end + kBN - 1) / kBN;
   e.ntiles = e.npt;
   e.ok = true;

@@ -155,24 +155,20 @@ cudaError_t launch_norm_rotate(const jet_layout* lay, bool rows, const jet_dims&
                                const void* k, const void* gq, const void* gk, void* qo, void* ko,
                                int* status, cudaStream_t st);
 
-// attention under a window (window.cu): the step, and the prefill
+// attention under a window: the step (window.cu; bf16 on the tensor cores in attend_tc.cu),
+// and the prefill on pairs of SMs (prefill_window.cu), which needs no workspace
 size_t attend_window_bytes(const jet_sizes& n, const jet_dims& d, int window, int sinks);
 cudaError_t launch_attend_window(const jet_layout& lay, const jet_dims& d, int window, int sinks,
                                  const void* q, const void* k_pre, const void* v_pre,
                                  const void* k_cand, const void* v_cand, void* o, void* ws,
                                  int* status, cudaStream_t st);
-// bf16 on the tensor cores (attend_tc.cu, prefill_tc.cu)
 AttnPlan attend_window_plan(const jet_sizes& n, const jet_dims& d, int window, int sinks);
 cudaError_t launch_attend_window_tc(const jet_layout& lay, const jet_dims& d, int window,
                                     int sinks, const void* q, const void* k_pre,
                                     const void* v_pre, const void* k_cand, const void* v_cand,
                                     void* o, void* ws, int* status, cudaStream_t st);
-cudaError_t launch_prefill_window_tc(const jet_layout& lay, const jet_dims& d, int window,
-                                     int sinks, const void* q, const void* k, const void* v,
-                                     void* o, void* ws, int* status, cudaStream_t st);
-size_t prefill_window_bytes(const jet_sizes& n, const jet_dims& d, int window, int sinks);
 cudaError_t launch_prefill_window(const jet_layout& lay, const jet_dims& d, int window, int sinks,
-                                  const void* q, const void* k, const void* v, void* o, void* ws,
+                                  const void* q, const void* k, const void* v, void* o,
                                   int* status, cudaStream_t st);
 
 // the prefix scan of the recurrent state (prefill of a linear-attention layer)
@@ -195,9 +191,9 @@ cudaError_t launch_prefill_tc(const jet_layout& lay, const jet_dims& d, const vo
                               cudaStream_t st);
 
 // the same on pairs of SMs (prefill_tc.cu), head dimensions 128 and 256; no work list
-template <int DH, bool WIN>
-cudaError_t launch_prefill_pair(const jet_layout& lay, const jet_dims& d, const Window& win,
-                                const void* q, const void* k, const void* v, void* o, int* status,
+template <int DH>
+cudaError_t launch_prefill_pair(const jet_layout& lay, const jet_dims& d, const void* q,
+                                const void* k, const void* v, void* o, int* status,
                                 cudaStream_t st);
 
 // q_rows (optional, every row's q [N, Hl, dk]): o then covers all N rows, the

@@ -40,7 +40,6 @@
 #include "jet_device.cuh"
 #include "jet_internal.h"
 #include "sm100_ptx.cuh"
-#include "window_rows.cuh"
 
 namespace jet {
 namespace {
@@ -85,28 +84,15 @@ struct PreArgs {
   int hold_first;    // test hook (jet_set_test_stall): withhold the first query block
 };
 
-// What the windowed form takes besides (under a window an item's keys are slots, window.h):
-// maps of boxes of kSlotBox keys, for the tile that holds the last first keys and the
-// window's first, and the tensors themselves, for vectors that are computed again
-// (window_rows.cuh).
-template <bool WIN>
-struct WinArgs {};
-template <>
-struct WinArgs<true> {
-  CUtensorMap k16, v16;
-  Window win;
-  const __nv_bfloat16 *q, *k, *v;
-};
-
 // One item as the schedule warp publishes it (ntiles 0: no more items).
 struct __align__(16) Item {
   int p0;      // the request's first position in the packed prefixes
   int kh;      // key/value head
   int row0;    // this CTA's first position within the request
   int nv;      // this CTA's query vectors (may be 0 in the odd CTA)
-  int k_end;   // keys of the block: the request's first k_end positions (WIN: its slots)
+  int k_end;   // keys of the block: the request's first k_end positions
   int ntiles;
-  int pad, off;  // WIN: Slots
+  int pad[2];
 };
 
 // SW128 K-major position of 16-byte chunk c of row i inside one 64-wide slice
@@ -131,30 +117,6 @@ __device__ __forceinline__ void tma_load_3d_pair(void* dst, const CUtensorMap* m
       : "memory");
 }
 
-// KEYS slots from slot0 on into a tile (SLICES slices of 64 from column x0): one box a slice,
-// or kSlotBox keys at a time where first keys and window meet
-template <int KEYS, int SLICES>
-__device__ __forceinline__ void load_slots(uint8_t* dst, const CUtensorMap* map,
-                                           const CUtensorMap* map16, uint32_t bar, const Item& e,
-                                           int slot0, int x0, uint64_t pol) {
-  if (slot0 < e.pad && slot0 + KEYS > e.pad) {
-#pragma unroll 1
-    for (int b = 0; b < KEYS / kSlotBox; ++b) {
-      const int slot = slot0 + b * kSlotBox;
-      const int key = e.p0 + (slot < e.pad ? slot : slot + e.off);
-#pragma unroll
-      for (int i = 0; i < SLICES; ++i)
-        tma_load_3d_pair(dst + i * (KEYS * 128) + b * (kSlotBox * 128), map16, bar, x0 + i * 64,
-                         e.kh, key, pol);
-    }
-  } else {
-    const int key = e.p0 + slot0 + (slot0 < e.pad ? 0 : e.off);
-#pragma unroll
-    for (int i = 0; i < SLICES; ++i)
-      tma_load_3d_pair(dst + i * (KEYS * 128), map, bar, x0 + i * 64, e.kh, key, pol);
-  }
-}
-
 __device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* map, int32_t x, int32_t y,
                                                 int32_t z) {
   asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(
@@ -163,22 +125,11 @@ __device__ __forceinline__ void tma_prefetch_3d(const CUtensorMap* map, int32_t 
                : "memory");
 }
 
-// a position's query vector, key by key
 template <int DH>
-__device__ __noinline__ void again(const PreArgs& a, const WinArgs<true>& w, const Item& e, int gi,
-                                   int lane) {
-  const int p = e.row0 + gi / a.g;
-  const size_t at = (size_t(e.p0 + p) * a.Hq + e.kh * a.g + gi % a.g) * DH;
-  const size_t step = size_t(a.Hkv) * DH, pre = size_t(e.p0) * step + size_t(e.kh) * DH;
-  position_attend<DH>(w.win, w.q + at, w.k + pre, w.v + pre, step, p, a.o + at, lane);
-}
-
-template <int DH, bool WIN>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_pair_kernel(const __grid_constant__ CUtensorMap tmQ,
                     const __grid_constant__ CUtensorMap tmK,
-                    const __grid_constant__ CUtensorMap tmV, const PreArgs a,
-                    const __grid_constant__ WinArgs<WIN> w) {
+                    const __grid_constant__ CUtensorMap tmV, const PreArgs a) {
   using G = Geo<DH>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
@@ -309,12 +260,6 @@ prefill_pair_kernel(const __grid_constant__ CUtensorMap tmQ,
           it.row0 = (2 * qb + int(rank)) * rb;
           it.nv = min(rb, max(0, PP - it.row0)) * g;
           it.k_end = min(PP, (qb + 1) * 2 * rb);
-          if constexpr (WIN) {
-            const Slots sl = block_slots(w.win, 2 * qb * rb, it.k_end);
-            it.k_end = sl.n;
-            it.pad = sl.pad;
-            it.off = sl.off;
-          }
           it.ntiles = (it.k_end + kBN - 1) / kBN;
           break;
         }
@@ -389,15 +334,10 @@ prefill_pair_kernel(const __grid_constant__ CUtensorMap tmQ,
             if (mbar_test(k_empty + s, ph ^ 1u)) {
               uint8_t* ks = smem + G::kOffK + s * G::kKBytes;
               if (rank == 0) mbar_arrive_expect_tx(k_full + s, 2 * G::kKBytes);
-              if constexpr (WIN) {
-                load_slots<kHalfN, G::kSlices>(ks, &tmK, &w.k16, bar_k + 8 * s, e,
-                                               jk * kBN + int(rank) * kHalfN, 0, pol_kv);
-              } else {
 #pragma unroll
-                for (int sl = 0; sl < G::kSlices; ++sl)
-                  tma_load_3d_pair(ks + sl * (kHalfN * 128), &tmK, bar_k + 8 * s, sl * 64, e.kh,
-                                   e.p0 + jk * kBN + int(rank) * kHalfN, pol_kv);
-              }
+              for (int sl = 0; sl < G::kSlices; ++sl)
+                tma_load_3d_pair(ks + sl * (kHalfN * 128), &tmK, bar_k + 8 * s, sl * 64, e.kh,
+                                 e.p0 + jk * kBN + int(rank) * kHalfN, pol_kv);
               k_issued |= 1u << s;
               k_par = (k_par & ~(1u << s)) | (ph << s);
               ++jk;
@@ -410,15 +350,10 @@ prefill_pair_kernel(const __grid_constant__ CUtensorMap tmQ,
             if (mbar_test(v_empty + s, ph ^ 1u)) {
               uint8_t* vs = smem + G::kOffV + s * G::kVBytes;
               if (rank == 0) mbar_arrive_expect_tx(v_full + s, 2 * G::kVBytes);
-              if constexpr (WIN) {
-                load_slots<kBN, G::kVSlices>(vs, &tmV, &w.v16, bar_v + 8 * s, e, jv * kBN,
-                                             int(rank) * (DH / 2), pol_kv);
-              } else {
 #pragma unroll
-                for (int sl = 0; sl < G::kVSlices; ++sl)
-                  tma_load_3d_pair(vs + sl * (kBN * 128), &tmV, bar_v + 8 * s,
-                                   int(rank) * (DH / 2) + sl * 64, e.kh, e.p0 + jv * kBN, pol_kv);
-              }
+              for (int sl = 0; sl < G::kVSlices; ++sl)
+                tma_load_3d_pair(vs + sl * (kBN * 128), &tmV, bar_v + 8 * s,
+                                 int(rank) * (DH / 2) + sl * 64, e.kh, e.p0 + jv * kBN, pol_kv);
               v_issued |= 1u << s;
               v_par = (v_par & ~(1u << s)) | (ph << s);
               ++jv;
@@ -553,22 +488,11 @@ prefill_pair_kernel(const __grid_constant__ CUtensorMap tmQ,
         break;
       }
       const int row0 = ring[slot].row0, ntiles = ring[slot].ntiles;
-      const int off = WIN ? ring[slot].off : 0, pad = WIN ? ring[slot].pad : 0;
       __syncwarp();
       if (lane == 0) mbar_arrive(item_empty + slot);
       if (ntiles == 0) break;
-      const int vis_end = row0 + i / g + 1 - off;          // keys this vector sees
-      const int vis_min = row0 + (q4 * 32) / g + 1 - off;  // the warp's first vector's
-      // under a window: the slots [0, vfirst) and [vlo, vis_end); the warp's last vector's
-      // vlo, and whether there may be slots that its vectors do not see before that
-      int vfirst = 0, vlo = 0, vlo_max = 0;
-      if constexpr (WIN) {
-        const Seen see = seen_at(w.win, row0 + i / g);
-        vfirst = int(see.first);
-        vlo = int(see.lo - off);
-        vlo_max = int(seen_at(w.win, row0 + (q4 * 32 + 31) / g).lo - off);
-        (void)pad;
-      }
+      const int vis_end = row0 + i / g + 1;                // keys this vector sees
+      const int vis_min = row0 + (q4 * 32) / g + 1;        // the warp's first vector's
       float m_used = -INFINITY, l = 0.f;
       for (int j = 0; j < ntiles; ++j) {
         const int Tj = T + j, b = Tj & 1;
@@ -583,19 +507,7 @@ prefill_pair_kernel(const __grid_constant__ CUtensorMap tmQ,
         for (int c = 0; c < 4; ++c) tmem_ld_32cols(scol + 32 * c, sv[c]);
         tmem_wait_ld();
         const int vis = vis_end - j * kBN;  // visible keys of this tile
-        if constexpr (WIN) {
-          if (vis_min - j * kBN < kBN || j * kBN < vlo_max) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              const int c0 = j * kBN + 32 * c;
-              const uint32_t see =
-                  bit_range(-c0, vfirst - c0) | bit_range(vlo - c0, vis_end - c0);
-#pragma unroll
-              for (int x = 0; x < 32; ++x)
-                if (!(see >> x & 1u)) sv[c][x] = -INFINITY;
-            }
-          }
-        } else if (vis_min - j * kBN < kBN) {  // some vector of the warp does not see all 128
+        if (vis_min - j * kBN < kBN) {      // some vector of the warp does not see all 128
 #pragma unroll
           for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -644,8 +556,7 @@ prefill_pair_kernel(const __grid_constant__ CUtensorMap tmQ,
         // P = 2^(s scale - m_used) as bf16 pairs over this lane's S columns; the
         // row sum uses the rounded values, which are what the tensor core
         // multiplies
-        // (under a window a vector may have seen no key yet: its weights are zeros then)
-        const float mneg = WIN && m_used == -INFINITY ? 0.f : -m_used;
+        const float mneg = -m_used;
         float ps[8];
 #pragma unroll
         for (int x = 0; x < 8; ++x) ps[x] = 0.f;
@@ -738,14 +649,6 @@ prefill_pair_kernel(const __grid_constant__ CUtensorMap tmQ,
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_remote(o_free_even);
-      unsigned nans = 0;  // vectors with a NaN among their outputs
-      if constexpr (WIN) {
-        __nv_bfloat162 most = __floats2bfloat162_rn(0.f, 0.f);
-#pragma unroll
-        for (int x = 0; x < DH / 2; ++x)
-          most = __hmax2_nan(most, *reinterpret_cast<const __nv_bfloat162*>(&pk[x]));
-        nans = __ballot_sync(0xffffffffu, i < e.nv && (__hisnan(most.x) || __hisnan(most.y)));
-      }
 #pragma unroll
       for (int c0 = 0; c0 < DH; c0 += 64) {
 #pragma unroll
@@ -761,10 +664,6 @@ prefill_pair_kernel(const __grid_constant__ CUtensorMap tmQ,
           if (dst[s] >= 0) *reinterpret_cast<uint4*>(a.o + dst[s] + c0 + c * 8) = val;
         }
         __syncwarp();
-      }
-      if constexpr (WIN) {
-        // those again, from what they see alone
-        for (; nans; nans &= nans - 1) again<DH>(a, w, e, q4 * 32 + __ffs(nans) - 1, lane);
       }
     }
     if (!ok) {
@@ -814,9 +713,9 @@ bool encode_3d(CUtensorMap* map, const void* base, int rows, int heads, int DH, 
 
 }  // namespace
 
-template <int DH, bool WIN>
-cudaError_t launch_prefill_pair(const jet_layout& lay, const jet_dims& d, const Window& win,
-                                const void* q, const void* k, const void* v, void* o, int* status,
+template <int DH>
+cudaError_t launch_prefill_pair(const jet_layout& lay, const jet_dims& d, const void* q,
+                                const void* k, const void* v, void* o, int* status,
                                 cudaStream_t st) {
   const jet_sizes& n = lay.n;
   const int g = d.Hq / d.Hkv;
@@ -840,18 +739,8 @@ cudaError_t launch_prefill_pair(const jet_layout& lay, const jet_dims& d, const 
   a.g = g;
   a.rb = kBV / g;
   a.scale_log2 = 1.4426950408889634f / sqrtf(float(DH));
-  WinArgs<WIN> w;
-  if constexpr (WIN) {
-    w.win = win;
-    w.q = static_cast<const __nv_bfloat16*>(q);
-    w.k = static_cast<const __nv_bfloat16*>(k);
-    w.v = static_cast<const __nv_bfloat16*>(v);
-    if (!encode_3d(&w.k16, k, n.total_prefix, d.Hkv, DH, 1, kSlotBox) ||
-        !encode_3d(&w.v16, v, n.total_prefix, d.Hkv, DH, 1, kSlotBox))
-      return cudaErrorInvalidValue;
-  }
   const size_t smem = Geo<DH>::kBytes + 1024;
-  auto kern = prefill_pair_kernel<DH, WIN>;
+  auto kern = prefill_pair_kernel<DH>;
   cudaError_t e =
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
@@ -861,17 +750,12 @@ cudaError_t launch_prefill_pair(const jet_layout& lay, const jet_dims& d, const 
   const int held = resident_pairs(reinterpret_cast<const void*>(kern), kThreads, smem);
   const int pairs = int(std::max<long long>(1, std::min<long long>(held, items)));
   return launch_pdl_pairs(kern, dim3(unsigned(2 * pairs)), dim3(kThreads), smem, st, tmQ, tmK,
-                          tmV, a, w);
+                          tmV, a);
 }
 
-#define JET_PAIR(DH, WIN)                                                                       \
-  template cudaError_t launch_prefill_pair<DH, WIN>(const jet_layout&, const jet_dims&,         \
-                                                    const Window&, const void*, const void*,    \
-                                                    const void*, void*, int*, cudaStream_t)
-JET_PAIR(128, false);
-JET_PAIR(256, false);
-JET_PAIR(128, true);
-JET_PAIR(256, true);
-#undef JET_PAIR
+template cudaError_t launch_prefill_pair<128>(const jet_layout&, const jet_dims&, const void*,
+                                              const void*, const void*, void*, int*, cudaStream_t);
+template cudaError_t launch_prefill_pair<256>(const jet_layout&, const jet_dims&, const void*,
+                                              const void*, const void*, void*, int*, cudaStream_t);
 
 }  // namespace jet

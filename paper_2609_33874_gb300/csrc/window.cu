@@ -86,10 +86,6 @@ size_t attend_window_bytes(const jet_sizes& n, const jet_dims& d, int window, in
   return std::max<size_t>(16, attend_window_plan(n, d, window, sinks).bytes);
 }
 
-size_t prefill_window_bytes(const jet_sizes& n, const jet_dims& d, int, int) {
-  return prefill_workspace_bytes(n, d);
-}
-
 cudaError_t launch_attend_window(const jet_layout& lay, const jet_dims& d, int window, int sinks,
                                  const void* q, const void* k_pre, const void* v_pre,
                                  const void* k_cand, const void* v_cand, void* o, void* ws,
@@ -102,12 +98,6 @@ cudaError_t launch_attend_window(const jet_layout& lay, const jet_dims& d, int w
   if (d.d == 128) return launch_rows<128, float>(a, q, k_pre, v_pre, k_cand, v_cand, o, st);
   if (d.d == 256) return launch_rows<256, float>(a, q, k_pre, v_pre, k_cand, v_cand, o, st);
   return cudaErrorInvalidValue;
-}
-
-cudaError_t launch_prefill_window(const jet_layout& lay, const jet_dims& d, int window, int sinks,
-                                  const void* q, const void* k, const void* v, void* o, void* ws,
-                                  int* status, cudaStream_t st) {
-  return launch_prefill_window_tc(lay, d, window, sinks, q, k, v, o, ws, status, st);
 }
 
 }  // namespace jet

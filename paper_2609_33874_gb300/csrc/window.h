@@ -31,6 +31,18 @@ JET_HD Seen seen_at(const Window& w, int64_t p) {
   return s;
 }
 
+// The same in 32 bits, of a position of a prefix (below 2^31).
+struct Seen32 {
+  int first, lo;
+};
+JET_HD Seen32 seen_at32(const Window& w, int p) {
+  Seen32 s;
+  s.lo = p - (w.window - 1);  // p >= 0 and window >= 1: above -2^31
+  if (s.lo < 0) s.lo = 0;
+  s.first = w.sinks < s.lo ? w.sinks : s.lo;
+  return s;
+}
+
 // The same of a row of the step at t (0: the shared row) over a prefix of P tokens: prefix
 // keys [0, pre_first) and [pre_lo, P), own candidate tokens [1, own_first] and [own_lo, t].
 struct RowSeen {

@@ -48,20 +48,21 @@ constexpr int kStages = 2;
 constexpr int kThreads = 224;
 constexpr int kSchedWarp = 6;  // the work-item scheduler
 
-template <int DH>
+template <int DH, int BN>
 struct Geo {
   static constexpr int kSlices = DH / 64;                   // 64-wide d slices
   static constexpr uint32_t kQBytes = kBV * DH * 2;         // query block
-  static constexpr uint32_t kKVBytes = kBN * DH * 2;        // one K (or V) tile
+  static constexpr uint32_t kKVBytes = BN * DH * 2;         // one K (or V) tile
   static constexpr uint32_t kOffK = kQBytes;                // stage s: K at kOffK + s * 2 kKV
   // the output stage: 32 rows of 128 bytes per softmax warp
   static constexpr uint32_t kOffStage = kQBytes + kStages * 2 * kKVBytes;
   static constexpr uint32_t kOffBar = kOffStage + 4 * 32 * 128;
   static constexpr uint32_t kBytes = kOffBar + 512;
-  // TMEM: the two S buffers, O, then the two P buffers (bf16 pairs, 32 columns)
-  static constexpr uint32_t kTmemCols = (2 * kBN + DH + 2 * (kBN / 2)) <= 256 ? 256 : 512;
-  static constexpr uint32_t kOCol = 2 * kBN;                // O after the two S buffers
-  static constexpr uint32_t kPCol = 2 * kBN + DH;           // P buffer b at kPCol + 32 b
+  // TMEM: the two S buffers, O, then the two P buffers (bf16 pairs, BN / 2 columns)
+  static constexpr uint32_t kTmemCols = (2 * BN + DH + 2 * (BN / 2)) <= 256 ? 256 : 512;
+  static constexpr uint32_t kOCol = 2 * BN;                 // O after the two S buffers
+  static constexpr uint32_t kPCol = 2 * BN + DH;            // P buffer b at kPCol + BN / 2 b
+  static_assert(kPCol + BN <= 512, "tensor memory");
 };
 
 // The work list: every (request, kv head, query block, chunk) that has keys
@@ -145,27 +146,27 @@ struct WinArgs<true> {
   const __nv_bfloat16 *k, *v, *kc, *vc;
 };
 
-// 64 keys of an item's slots from slot0 on into a tile (DH / 64 slices): one box a slice, or
+// BN keys of an item's slots from slot0 on into a tile (DH / 64 slices): one box a slice, or
 // kSlotBox keys at a time where first keys and window meet
-template <int DH>
+template <int DH, int BN>
 __device__ __forceinline__ void load_slots(uint8_t* dst, const CUtensorMap* map,
                                            const CUtensorMap* map16, uint64_t* bar,
                                            const Slots& sl, int slot0, int p0, int kh,
                                            uint64_t pol) {
-  if (slot0 < sl.pad && slot0 + kBN > sl.pad) {
+  if (slot0 < sl.pad && slot0 + BN > sl.pad) {
 #pragma unroll
-    for (int b = 0; b < kBN / kSlotBox; ++b) {
+    for (int b = 0; b < BN / kSlotBox; ++b) {
       const int slot = slot0 + b * kSlotBox;
       const int key = p0 + (slot < sl.pad ? slot : slot + sl.off);
 #pragma unroll
       for (int i = 0; i < DH / 64; ++i)
-        tma_load_3d(dst + i * (kBN * 128) + b * (kSlotBox * 128), map16, bar, i * 64, kh, key, pol);
+        tma_load_3d(dst + i * (BN * 128) + b * (kSlotBox * 128), map16, bar, i * 64, kh, key, pol);
     }
   } else {
     const int key = p0 + slot0 + (slot0 < sl.pad ? 0 : sl.off);
 #pragma unroll
     for (int i = 0; i < DH / 64; ++i)
-      tma_load_3d(dst + i * (kBN * 128), map, bar, i * 64, kh, key, pol);
+      tma_load_3d(dst + i * (BN * 128), map, bar, i * 64, kh, key, pol);
   }
 }
 
@@ -196,7 +197,8 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
                         const __grid_constant__ CUtensorMap tmKc,
                         const __grid_constant__ CUtensorMap tmVc, const AttArgs a,
                         const __grid_constant__ WinArgs<WIN> w) {
-  using G = Geo<DH>;
+  constexpr int BN = WIN ? win_tile(DH) : kBN;
+  using G = Geo<DH, BN>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
@@ -385,14 +387,14 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
               const bool pre = jk < e.npt;
               if (WIN && pre) {
                 if constexpr (WIN)
-                  load_slots<DH>(ks, &tmK, &w.k16, k_full + s, sl, e.k_begin + jk * kBN, e.p0, e.kh,
+                  load_slots<DH, BN>(ks, &tmK, &w.k16, k_full + s, sl, e.k_begin + jk * BN, e.p0, e.kh,
                                  pol);
               } else {
               const CUtensorMap* mk = pre ? &tmK : &tmKc;
-              const int key = pre ? e.p0 + e.k_begin + jk * kBN : e.f_begin + (jk - e.npt) * kBN;
+              const int key = pre ? e.p0 + e.k_begin + jk * BN : e.f_begin + (jk - e.npt) * BN;
 #pragma unroll
               for (int sl = 0; sl < G::kSlices; ++sl)
-                tma_load_3d(ks + sl * (kBN * 128), mk, k_full + s, sl * 64, e.kh, key, pol);
+                tma_load_3d(ks + sl * (BN * 128), mk, k_full + s, sl * 64, e.kh, key, pol);
               }
               k_issued |= 1u << s;
               k_par = (k_par & ~(1u << s)) | (ph << s);
@@ -410,14 +412,14 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
               const bool pre = jv < e.npt;
               if (WIN && pre) {
                 if constexpr (WIN)
-                  load_slots<DH>(vs, &tmV, &w.v16, v_full + s, sl, e.k_begin + jv * kBN, e.p0, e.kh,
+                  load_slots<DH, BN>(vs, &tmV, &w.v16, v_full + s, sl, e.k_begin + jv * BN, e.p0, e.kh,
                                  pol);
               } else {
               const CUtensorMap* mv = pre ? &tmV : &tmVc;
-              const int key = pre ? e.p0 + e.k_begin + jv * kBN : e.f_begin + (jv - e.npt) * kBN;
+              const int key = pre ? e.p0 + e.k_begin + jv * BN : e.f_begin + (jv - e.npt) * BN;
 #pragma unroll
               for (int sl = 0; sl < G::kSlices; ++sl)
-                tma_load_3d(vs + sl * (kBN * 128), mv, v_full + s, sl * 64, e.kh, key, pol);
+                tma_load_3d(vs + sl * (BN * 128), mv, v_full + s, sl * 64, e.kh, key, pol);
               }
               v_issued |= 1u << s;
               v_par = (v_par & ~(1u << s)) | (ph << s);
@@ -450,7 +452,7 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
     if (elect_one()) {
-      const uint32_t id_s = idesc_bf16_f32(kBV, kBN);
+      const uint32_t id_s = idesc_bf16_f32(kBV, BN);
       const uint32_t id_o = idesc_bf16_f32(kBV, DH) | (1u << 16);  // B (V) is MN-major
       const uint32_t qs = smem_u32(smem);
       bool ok = mbar_wait(qz_done, 0, a.wait_ns, abort_flag);
@@ -484,8 +486,8 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
 #pragma unroll
               for (int st = 0; st < DH / 16; ++st) {
                 const int sl = st >> 2, k = st & 3;
-                mma_f16(tmem + b * kBN, desc_k_sw128(qs + sl * (kBV * 128) + 32 * k),
-                        desc_k_sw128(ks + sl * (kBN * 128) + 32 * k), id_s, st != 0);
+                mma_f16(tmem + b * BN, desc_k_sw128(qs + sl * (kBV * 128) + 32 * k),
+                        desc_k_sw128(ks + sl * (BN * 128) + 32 * k), id_s, st != 0);
               }
               mma_commit(s_full + b);
               mma_commit(k_empty + s);
@@ -503,12 +505,12 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
                 mbar_test(v_full + s, (Tj / kStages) & 1)) {
               tc_fence_after();
               // P_j from TMEM (8 columns = 16 keys per instruction), V_j from shared memory
-              const uint32_t pt = tmem + G::kPCol + uint32_t(b) * (kBN / 2);
+              const uint32_t pt = tmem + G::kPCol + uint32_t(b) * (BN / 2);
               const uint32_t vs = smem_u32(smem + G::kOffK + s * 2 * G::kKVBytes + G::kKVBytes);
 #pragma unroll
-              for (int k = 0; k < kBN / 16; ++k)
+              for (int k = 0; k < BN / 16; ++k)
                 mma_f16_ta(tmem + G::kOCol, pt + uint32_t(8 * k),
-                           desc_mn_sw128(vs + k * 16 * 128, kBN * 128), id_o, (jo | k) != 0);
+                           desc_mn_sw128(vs + k * 16 * 128, BN * 128), id_o, (jo | k) != 0);
               mma_commit(p_free + b);
               mma_commit(v_empty + s);
               ++jo;
@@ -593,56 +595,56 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
           break;
         }
         tc_fence_after();
-        float sv[kBN];
+        float sv[BN];
         {
-          float t0[32], t1[32];
-          tmem_ld_32cols(tmem + lane_off + b * kBN, t0);
-          tmem_ld_32cols(tmem + lane_off + b * kBN + 32, t1);
+          float t[BN / 32][32];
+#pragma unroll
+          for (int x = 0; x < BN / 32; ++x)
+            tmem_ld_32cols(tmem + lane_off + b * BN + 32 * x, t[x]);
           tmem_wait_ld();
 #pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            sv[c] = t0[c];
-            sv[c + 32] = t1[c];
-          }
+          for (int c = 0; c < BN; ++c) sv[c] = t[c >> 5][c & 31];
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(s_free + b);
         if constexpr (WIN) {
-          // what this vector sees of the tile's 64 keys
-          uint32_t see[2];
+          // what this vector sees of the tile's keys
+          uint32_t see[BN / 32];
           if (j < e.npt) {
-            const int k0 = e.k_begin + j * kBN;
+            const int k0 = e.k_begin + j * BN;
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-              see[x] = bit_range(-32 * x, vfirst - k0 - 32 * x) |
+            for (int x = 0; x < BN / 32; ++x)
+              see[x] = bit_range(-32 * x, min(e.k_end, vfirst) - k0 - 32 * x) |
                        bit_range(vlo - k0 - 32 * x, e.k_end - k0 - 32 * x);
           } else {
-            const int f0 = e.f_begin + (j - e.npt) * kBN;
+            const int f0 = e.f_begin + (j - e.npt) * BN;
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int x = 0; x < BN / 32; ++x)
               see[x] = bit_range(fa - f0 - 32 * x, min(ffirst, fb + 1) - f0 - 32 * x) |
                        bit_range(flo - f0 - 32 * x, fb + 1 - f0 - 32 * x);
           }
-          if (__any_sync(0xffffffffu, (see[0] & see[1]) != ~0u)) {
 #pragma unroll
-            for (int c = 0; c < kBN; ++c)
-              if (!(see[c >> 5] >> (c & 31) & 1u)) sv[c] = -INFINITY;
+          for (int x = 0; x < BN / 32; ++x) {
+            if (__all_sync(0xffffffffu, see[x] == ~0u)) continue;
+#pragma unroll
+            for (int c = 32 * x; c < 32 * x + 32; ++c)
+              if (!(see[x] >> (c & 31) & 1u)) sv[c] = -INFINITY;
           }
         } else {
         // visible keys of this tile: [klo, khi) of its 64 slots
         int klo = 0, khi;
         if (j < e.npt) {
-          khi = min(kBN, e.k_end - (e.k_begin + j * kBN));
-          khi = min(khi, kcap + 1 - (e.k_begin + j * kBN));  // prefill: keys <= own position
+          khi = min(BN, e.k_end - (e.k_begin + j * BN));
+          khi = min(khi, kcap + 1 - (e.k_begin + j * BN));  // prefill: keys <= own position
         } else {
-          const int f0 = e.f_begin + (j - e.npt) * kBN;
+          const int f0 = e.f_begin + (j - e.npt) * BN;
           klo = max(0, fa - f0);
-          khi = min(kBN, fb - f0 + 1);
+          khi = min(BN, fb - f0 + 1);
         }
-        if (__any_sync(0xffffffffu, klo > 0 || khi < kBN)) {
+        if (__any_sync(0xffffffffu, klo > 0 || khi < BN)) {
 #pragma unroll
-          for (int c = 0; c < kBN; ++c)
+          for (int c = 0; c < BN; ++c)
             if (c < klo || c >= khi) sv[c] = -INFINITY;
         }
         }
@@ -652,7 +654,7 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
 #pragma unroll
         for (int q = 0; q < 8; ++q) mq[q] = sv[q];
 #pragma unroll
-        for (int c = 8; c < kBN; ++c) mq[c & 7] = fmaxf(mq[c & 7], sv[c]);
+        for (int c = 8; c < BN; ++c) mq[c & 7] = fmaxf(mq[c & 7], sv[c]);
         const float mt = a.scale_log2 * fmaxf(fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])),
                                               fmaxf(fmaxf(mq[4], mq[5]), fmaxf(mq[6], mq[7])));
         // P buffer b was last read by the P V of tile Tj - 2
@@ -691,23 +693,30 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         // P = 2^(s scale - m_used) as bf16 pairs into this row's TMEM lane (the P V
         // MMA's A operand); the row sum uses the rounded values, which are what
         // the tensor core multiplies
-        uint32_t pw[kBN / 2];
-        float ps[8];  // one partial sum per 8 keys, added as a tree
+        uint32_t pw[BN / 2];
+        float ps[8];  // partial sums, added as a tree
         // under a window a vector may have seen no key yet: its weights are zeros then
         const float m_off = WIN && m_used == -INFINITY ? 0.f : -m_used;
 #pragma unroll
-        for (int cc = 0; cc < 8; ++cc) {
-          ps[cc] = 0.f;
+        for (int cc = 0; cc < 8; ++cc) ps[cc] = 0.f;
+#pragma unroll
+        for (int cc = 0; cc < BN / 8; ++cc) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const float x0 = ex2(fmaf(sv[cc * 8 + 2 * q], a.scale_log2, m_off));
             const float x1 = ex2(fmaf(sv[cc * 8 + 2 * q + 1], a.scale_log2, m_off));
             const uint32_t w = pack_bf16(x0, x1);
             pw[cc * 4 + q] = w;
-            ps[cc] += __uint_as_float(w << 16) + __uint_as_float(w & 0xffff0000u);
+            ps[cc & 7] += __uint_as_float(w << 16) + __uint_as_float(w & 0xffff0000u);
           }
         }
-        tmem_st_32cols_u32(tmem + lane_off + G::kPCol + uint32_t(b) * (kBN / 2), pw);
+#pragma unroll
+        for (int x = 0; x < BN / 64; ++x) {
+          uint32_t part[32];
+#pragma unroll
+          for (int c = 0; c < 32; ++c) part[c] = pw[32 * x + c];
+          tmem_st_32cols_u32(tmem + lane_off + G::kPCol + uint32_t(b) * (BN / 2) + 32 * x, part);
+        }
         l += ((ps[0] + ps[1]) + (ps[2] + ps[3])) + ((ps[4] + ps[5]) + (ps[6] + ps[7]));
         tmem_wait_st();
         tc_fence_before();
@@ -903,18 +912,19 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
                       const Window& win, const void* q, const void* k_pre, const void* v_pre,
                       const void* k_cand, const void* v_cand, void* o, float* o_part,
                       float2* ml_part, int* status, cudaStream_t st) {
+  constexpr int BN = WIN ? win_tile(DH) : kBN;
   const jet_sizes& n = lay.n;
   const int F = n.N - n.R;
   const int g = d.Hq / d.Hkv;
   if (g > kBV) return cudaErrorInvalidValue;
   CUtensorMap tmQ, tmK, tmV, tmKc, tmVc;
   if (!encode_3d(&tmQ, q, n.N, d.Hq, DH, g, kBV / g) ||
-      !encode_3d(&tmK, k_pre, n.total_prefix, d.Hkv, DH, 1, kBN) ||
-      !encode_3d(&tmV, v_pre, n.total_prefix, d.Hkv, DH, 1, kBN))
+      !encode_3d(&tmK, k_pre, n.total_prefix, d.Hkv, DH, 1, BN) ||
+      !encode_3d(&tmV, v_pre, n.total_prefix, d.Hkv, DH, 1, BN))
     return cudaErrorInvalidValue;
   if (F > 0) {
-    if (!encode_3d(&tmKc, k_cand, F, d.Hkv, DH, 1, kBN) ||
-        !encode_3d(&tmVc, v_cand, F, d.Hkv, DH, 1, kBN))
+    if (!encode_3d(&tmKc, k_cand, F, d.Hkv, DH, 1, BN) ||
+        !encode_3d(&tmVc, v_cand, F, d.Hkv, DH, 1, BN))
       return cudaErrorInvalidValue;
   } else {
     tmKc = tmK;  // never read: no request has candidate tiles
@@ -961,13 +971,14 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
   WinArgs<WIN> w;
   if constexpr (WIN) {
     a.win = win;
+    a.bn = BN;
     if (!win_args(&w, n, d, k_pre, v_pre, k_cand, v_cand)) return cudaErrorInvalidValue;
   }
   cudaError_t e = cudaSuccess;
   if (a.sorted)
     e = launch_pdl(attend_items_kernel<WIN>, dim3(1), dim3(1024), 0, st, a, plan.qgroups, plan.splits);
   if (e != cudaSuccess) return e;
-  const size_t smem = Geo<DH>::kBytes + 1024;
+  const size_t smem = Geo<DH, BN>::kBytes + 1024;
   e = cudaFuncSetAttribute(attend_prefix_tc_kernel<DH, WIN>,
                            cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
@@ -982,7 +993,7 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
     return launch_pdl(combine_window_kernel<DH>, dim3(unsigned(blocks)), dim3(128), 0, st, a, w,
                       lay.row_req, blocks <= 8LL * sms);
   else
-  return launch_pdl(attend_combine_kernel<DH>, dim3(unsigned(blocks)), dim3(128), 0, st,
+    return launch_pdl(attend_combine_kernel<DH>, dim3(unsigned(blocks)), dim3(128), 0, st,
                     lay.row_req, n.N, n.R, d.Hq, plan.splits, blocks <= 8LL * sms, o_part, ml_part,
                     static_cast<__nv_bfloat16*>(o), status);
 }
@@ -1039,7 +1050,7 @@ cudaError_t launch_prefill_dh(const jet_layout& lay, const jet_dims& d, const vo
   cudaError_t e =
       launch_pdl(attend_items_kernel<false>, dim3(1), dim3(1024), 0, st, a, qgroups, 1);
   if (e != cudaSuccess) return e;
-  const size_t smem = Geo<DH>::kBytes + 1024;
+  const size_t smem = Geo<DH, kBN>::kBytes + 1024;
   e = cudaFuncSetAttribute(attend_prefix_tc_kernel<DH, false>,
                            cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;

@@ -471,8 +471,6 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
               progressed = true;
             }
           }
-          // (polling without a pause takes issue slots from the softmax warps beside it)
-          if (!progressed) __nanosleep(64);
           if (clk.expired(progressed, abort_flag, a.wait_ns)) {
             ok = false;
             break;
@@ -592,13 +590,6 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
             }
             progressed = true;
           }
-        }
-        if (!progressed) {
-          // nothing but the next weights can come where S is full; else look at all again soon
-          if (ahead == kSBufs)
-            mbar_try_wait(p_full + sp.at, sp.phase);
-          else
-            __nanosleep(20);
         }
         if (clk.expired(progressed, abort_flag, a.wait_ns)) ok = false;
       }

@@ -2,12 +2,12 @@
 // projected queries and keys.
 //
 // Every element is read and written once, so HBM bounds long inputs and latencies short
-// ones. A warp takes 256 elements at a time - one head of 256, two of 128, four of 64 - of
-// one token, eight a lane: the two elements of a pair lie in one lane (two groups of four,
-// half a rotation apart, or eight in a row), so the rotation needs no shuffle and the norm
-// four to five. The angles are common to a token's heads: a block takes kTokens tokens, or
-// a part of one token's heads where there are few tokens, and computes each (token, pair)'s
-// cosine and sine once into shared memory.
+// ones; what stands between a long input and HBM is the number of instructions. A warp takes
+// one token, or every parts-th piece of it, 256 elements at a time - one head of 256, two of
+// 128, four of 64 - eight a lane. The two elements of a pair lie in one lane (two groups of
+// four, half a rotation apart, or eight in a row), so the rotation needs no shuffle and the
+// norm three to five, and a lane's four cosines and sines, of the same four pairs in every
+// head, stay in registers for the whole token.
 //
 // An angle is a 64-bit fraction of a turn, position times frequency modulo 2^64; its
 // nearest quarter turn is taken off exactly and the rest, at most an eighth of a turn, is
@@ -20,9 +20,8 @@
 namespace jet {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
-constexpr int kTokens = 4;  // tokens a block takes, at most
 
 enum { kGiven = 0, kPrefix = 1, kRows = 2 };  // where the positions come from
 
@@ -40,8 +39,7 @@ struct RotArgs {
   void* ko;
   int* status;
   int n, R, total, Hq, Hkv, nfed;
-  int tokens;  // of a block
-  int parts;   // blocks that share a token's heads
+  int parts;   // warps that share a token's heads
 };
 
 // cos and sin of the angle `turn` (2^-64 turns a position) at position p
@@ -92,24 +90,29 @@ __device__ __forceinline__ bool token_at(const RotArgs& a, int n, int lane, int*
   }
 }
 
+// four elements as they are in memory, and their values
 template <typename T>
-__device__ __forceinline__ void load4(const T* p, float (&v)[4]) {
-  if constexpr (sizeof(T) == 4) {
-    const float4 x = *reinterpret_cast<const float4*>(p);
+struct Raw4 {
+  uint2 x;
+  __device__ __forceinline__ void load(const T* p) { x = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void values(float (&v)[4]) const {
+    v[0] = __uint_as_float(x.x << 16);
+    v[1] = __uint_as_float(x.x & 0xffff0000u);
+    v[2] = __uint_as_float(x.y << 16);
+    v[3] = __uint_as_float(x.y & 0xffff0000u);
+  }
+};
+template <>
+struct Raw4<float> {
+  float4 x;
+  __device__ __forceinline__ void load(const float* p) { x = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void values(float (&v)[4]) const {
     v[0] = x.x;
     v[1] = x.y;
     v[2] = x.z;
     v[3] = x.w;
-  } else {
-    const uint2 x = *reinterpret_cast<const uint2*>(p);
-    const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x.x));
-    const float2 b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x.y));
-    v[0] = a.x;
-    v[1] = a.y;
-    v[2] = b.x;
-    v[3] = b.y;
   }
-}
+};
 
 template <typename T>
 __device__ __forceinline__ void store4(T* p, const float (&v)[4]) {
@@ -123,127 +126,166 @@ __device__ __forceinline__ void store4(T* p, const float (&v)[4]) {
   }
 }
 
+// v over the root of the mean of its head's squares, times g. The root's reciprocal is the
+// hardware's and one step of Newton's: two units of the last place at most, as a root and a
+// quotient would be, for six instructions. Heads whose squares leave float32 are scaled by a
+// power of two first.
+template <int DH>
+__device__ __forceinline__ void normalise(float (&v)[2][4], const float (&g)[2][4], float eps) {
+  auto squares = [&]() {
+    float ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ss = fmaf(v[0][j], v[0][j], fmaf(v[1][j], v[1][j], ss));
+#pragma unroll
+    for (int o = DH / 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    return ss;
+  };
+  float x = fmaf(squares(), 1.f / float(DH), eps);
+  if (__any_sync(0xffffffffu, !(x > 1e-30f && x < 1e30f))) {
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(v[0][j]), fabsf(v[1][j])));
+#pragma unroll
+    for (int o = DH / 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    // its exponent; not of zeros (they stay), nor where eps counts more than they do
+    const int e = top > 0.f && top < INFINITY && !(top * top < eps) ? ilogbf(top) : 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[0][j] = ldexpf(v[0][j], -e);
+      v[1][j] = ldexpf(v[1][j], -e);
+    }
+    x = fmaf(squares(), 1.f / float(DH), ldexpf(ldexpf(eps, -e), -e));
+    if (top == 0.f) x = 1.f;
+  }
+  const float r = rsqrtf(x);
+  const float inv = r * fmaf(-0.5f * x * r, r, 1.5f);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    v[0][j] *= inv * g[0][j];
+    v[1][j] *= inv * g[1][j];
+  }
+}
+
 // 8 elements a lane in two groups of four, v[0] and v[1]. Halves: the groups are half a
 // rotation apart in the lanes that rotate, and in a row past them. Pairs: in a row.
 template <int DH, int STYLE, int FROM, typename T>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 10)
 norm_rotate_kernel(const RotArgs a, const __grid_constant__ jet_rope rope) {
   pdl_begin();
   constexpr int kLanes = DH / 8;        // lanes of a head
   constexpr int kHeads = 32 / kLanes;   // heads of a warp's step
-  __shared__ float2 cs[kTokens][128];
-  __shared__ int2 token[kTokens];       // position; key's place, -1 none, -2 no token
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int block = int(blockIdx.x) / a.parts, part = int(blockIdx.x) % a.parts;
-  const int n0 = block * a.tokens, count = min(a.tokens, a.n - n0);
-  if (warp < count) {
-    int pos = 0, fed = -1;
-    const bool ok = token_at<FROM>(a, n0 + warp, lane, &pos, &fed);
-    if (lane == 0) {
-      token[warp] = make_int2(pos, ok ? fed : -2);
-      if (!ok) flag(a.status, JET_ERR_DEVICE);
-    }
-  }
+  const int lane = threadIdx.x & 31;
+  const long long w = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  const int n = int(w / a.parts), part = int(w % a.parts);
+  if (n >= a.n) return;
   const int half = rope.rot / 2;
-  const int pair = int(threadIdx.x) & 127;
-  const uint64_t turn = pair < half ? rope.turn[pair] : 0;
-  __syncthreads();
-  if (pair < half)
-    for (int t = int(threadIdx.x) >> 7; t < count; t += kThreads / 128)
-      cs[t][pair] = turn_cos_sin(turn, token[t].x);
-  __syncthreads();
-
   const int hl = lane % kLanes, hs = lane / kLanes;
-  int e0, e1, p0;  // the groups' elements, the lane's first pair
+  int e0, e1;  // the groups' elements
   bool rotates;
   if constexpr (STYLE == JET_ROPE_HALVES) {
     rotates = hl < half / 4;
     const int j = hl - half / 4;
     e0 = rotates ? 4 * hl : rope.rot + 8 * j;
     e1 = rotates ? half + 4 * hl : e0 + 4;
-    p0 = 4 * hl;
   } else {
     rotates = 8 * hl < rope.rot;
     e0 = 8 * hl;
     e1 = e0 + 4;
-    p0 = 4 * hl;
   }
-  float gq[2][4], gk[2][4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) gq[0][i] = gq[1][i] = gk[0][i] = gk[1][i] = 1.f;
-  if (rope.norm) {
-    if (a.gq) {
-      load4(static_cast<const T*>(a.gq) + e0, gq[0]);
-      load4(static_cast<const T*>(a.gq) + e1, gq[1]);
-    }
-    if (a.gk) {
-      load4(static_cast<const T*>(a.gk) + e0, gk[0]);
-      load4(static_cast<const T*>(a.gk) + e1, gk[1]);
-    }
-  }
+  // The first step's elements come beside the token's position, and each later step's beside
+  // the step before it
   const int nq = a.q ? (a.Hq + kHeads - 1) / kHeads : 0;
-  const int nk = a.k ? (a.Hkv + kHeads - 1) / kHeads : 0;
-  const int steps = nq + nk;
-  const int items = count * steps;
-  for (int i = part * kWarps + warp; i < items; i += a.parts * kWarps) {
-    const int t = i / steps, st = i % steps;
-    const int2 tok = token[t];
-    const bool is_q = st < nq;
-    if (tok.y == -2 || (!is_q && tok.y < 0)) continue;
-    const int head = (is_q ? st : st - nq) * kHeads + hs;
-    const int H = is_q ? a.Hq : a.Hkv;
-    const bool in = head < H;
-    const size_t at = (size_t(is_q ? n0 + t : tok.y) * H + (in ? head : H - 1)) * DH;
-    const T* x = static_cast<const T*>(is_q ? a.q : a.k) + at;
-    float v[2][4];
-    load4(x + e0, v[0]);
-    load4(x + e1, v[1]);
-    if (rope.norm) {
-      float ss = 0.f;
+  Raw4<T> r0, r1;
+  auto fetch = [&](const T* x, int at) {
+    r0.load(x + at + e0);
+    r1.load(x + at + e1);
+  };
+  if (part < nq && part * kHeads + hs < a.Hq)
+    fetch(static_cast<const T*>(a.q) + size_t(n) * a.Hq * DH, (part * kHeads + hs) * DH);
+  int pos = 0, fed = -1;
+  const bool ok = token_at<FROM>(a, n, lane, &pos, &fed);
+  if (!ok) {
+    if (lane == 0) flag(a.status, JET_ERR_DEVICE);
+    return;
+  }
+  // the cosines and sines of pairs 4 hl .. + 3: DH / 64 pairs a lane, then from lane to lane
+  float2 cs[4];
+  {
+    constexpr int kOwn = DH / 64;
+    float2 own[kOwn];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) ss = fmaf(v[0][j], v[0][j], fmaf(v[1][j], v[1][j], ss));
-#pragma unroll
-      for (int o = kLanes / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      const float inv = 1.f / sqrtf(ss / float(DH) + rope.eps);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[0][j] *= inv * (is_q ? gq[0][j] : gk[0][j]);
-        v[1][j] *= inv * (is_q ? gq[1][j] : gk[1][j]);
-      }
+    for (int i = 0; i < kOwn; ++i) {
+      const int pair = lane * kOwn + i;
+      own[i] = turn_cos_sin(pair < half ? rope.turn[pair] : 0, pos);
     }
-    if (rotates) {
-      float2 c[4];
-      const float4* tc = reinterpret_cast<const float4*>(&cs[t][p0]);
-      *reinterpret_cast<float4*>(&c[0]) = tc[0];
-      *reinterpret_cast<float4*>(&c[2]) = tc[1];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float& x0 = STYLE == JET_ROPE_HALVES ? v[0][j] : v[j >> 1][(2 * j) & 3];
-        float& x1 = STYLE == JET_ROPE_HALVES ? v[1][j] : v[j >> 1][(2 * j + 1) & 3];
-        const float y0 = x0, y1 = x1;
-        x0 = y0 * c[j].x - y1 * c[j].y;
-        x1 = y0 * c[j].y + y1 * c[j].x;
-      }
-    }
-    if (in) {
-      T* y = static_cast<T*>(is_q ? a.qo : a.ko) + at;
-      store4(y + e0, v[0]);
-      store4(y + e1, v[1]);
+    for (int j = 0; j < 4; ++j) {
+      const int src = (4 * hl + j) / kOwn;
+      cs[j].x = __shfl_sync(0xffffffffu, own[j % kOwn].x, src);
+      cs[j].y = __shfl_sync(0xffffffffu, own[j % kOwn].y, src);
     }
   }
+
+  // the H heads of row `row`, kHeads a step, every parts-th step from `st` on; returns the
+  // step past them that is the next array's
+  auto run = [&](const void* xs, void* ys, const void* gs, int H, int steps, size_t row, int st,
+                 bool held) {
+    float g[2][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) g[0][j] = g[1][j] = 1.f;
+    if (rope.norm && gs) {
+      Raw4<T> r;
+      r.load(static_cast<const T*>(gs) + e0);
+      r.values(g[0]);
+      r.load(static_cast<const T*>(gs) + e1);
+      r.values(g[1]);
+    }
+    const T* x = static_cast<const T*>(xs) + row * H * DH;
+    T* y = static_cast<T*>(ys) + row * H * DH;
+    int head = st * kHeads + hs, at = head * DH;   // a token's heads: an int holds them
+    const int step = a.parts * kHeads;
+    if (!held && st < steps && head < H) fetch(x, at);
+    for (; st < steps; st += a.parts) {
+      float v[2][4];
+      r0.values(v[0]);
+      r1.values(v[1]);
+      const bool in = head < H;
+      T* out = y + at;
+      head += step;
+      at += step * DH;
+      if (head < H) fetch(x, at);
+      if (rope.norm) normalise<DH>(v, g, rope.eps);
+      if (rotates) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float& x0 = STYLE == JET_ROPE_HALVES ? v[0][j] : v[j >> 1][(2 * j) & 3];
+          float& x1 = STYLE == JET_ROPE_HALVES ? v[1][j] : v[j >> 1][(2 * j + 1) & 3];
+          const float y0 = x0, y1 = x1;
+          x0 = y0 * cs[j].x - y1 * cs[j].y;
+          x1 = y0 * cs[j].y + y1 * cs[j].x;
+        }
+      }
+      if (in) {
+        store4(out + e0, v[0]);
+        store4(out + e1, v[1]);
+      }
+    }
+    return st - steps;
+  };
+  int st = part;
+  if (a.q) st = run(a.q, a.qo, a.gq, a.Hq, nq, size_t(n), st, true);
+  if (a.k && fed >= 0)
+    run(a.k, a.ko, a.gk, a.Hkv, (a.Hkv + kHeads - 1) / kHeads, size_t(fed), st, false);
 }
 
 template <int FROM, typename T>
 cudaError_t launch_from(RotArgs a, const jet_dims& d, const jet_rope& rope, cudaStream_t st) {
   const int heads = 256 / d.d;
   const int steps = (a.q ? (d.Hq + heads - 1) / heads : 0) + (a.k ? (d.Hkv + heads - 1) / heads : 0);
-  // few tokens: one a block, its heads over several blocks, a step a warp
+  // few tokens: several warps each, down to a step a warp
   const long long want = 8LL * kPlanSMs;
-  a.tokens = a.n >= want * kTokens ? kTokens : 1;
-  const int most = (steps + kWarps - 1) / kWarps;
-  a.parts = 1;
-  if (a.tokens == 1) a.parts = int(std::min<long long>(most, std::max<long long>(1, want / a.n)));
-  const long long blocks = ((long long)a.n + a.tokens - 1) / a.tokens * a.parts;
+  a.parts = int(std::min<long long>(steps, std::max<long long>(1, want / a.n)));
+  const long long blocks = ((long long)a.n * a.parts + kWarps - 1) / kWarps;
   if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
   const dim3 grid{unsigned(blocks)};
 #define JET_ROT(DH)                                                                             \

@@ -30,6 +30,23 @@ constexpr long long kTargetCtas = 4 * kPlanSMs;
 constexpr int kMinChunkTc = 640;        // keys
 constexpr int kFewGroups = 22, kFewItems = 44, kLeastChunk = 192;
 
+// what the kernels take of a window besides
+template <bool WIN>
+struct WinRows {};
+template <>
+struct WinRows<true> {
+  Window win;
+  const int32_t* prefix_offset;
+  const int32_t* row_cand;
+  const int32_t* cand_row_offset;
+  int C;
+  // t of the token fed at row n (0: a shared row)
+  __device__ __forceinline__ int fed(int n) const {
+    const int c = row_cand[n];
+    return c >= 0 && c < C ? max(0, n - cand_row_offset[c] + 1) : 0;
+  }
+};
+
 // rows of Q, K and P are padded by 16 bytes: 16-byte reads of eight consecutive
 // rows then fall in different banks
 template <int DH>
@@ -57,14 +74,16 @@ __device__ __forceinline__ float4 load4(const uint8_t* p, float f) {
 // TK: float32 keys and values, or the codes of an 8-bit cache (uint8_t) with their
 // exponent bytes k_exp, v_exp: a tile lies within one block of 64 tokens, so it has one
 // scale of keys and one of values.
-template <int DH, typename TK>
+// WIN: under a window the keys are slots (window.h), and a vector sees those before
+// vfirst and from vlo on.
+template <int DH, typename TK, bool WIN>
 __global__ void __launch_bounds__(kThreads)
 attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* __restrict__ row_offset,
                      int R, int N, int total_prefix, int Hq, int Hkv, int chunk,
                      const float* __restrict__ q, const TK* __restrict__ k_pre,
                      const TK* __restrict__ v_pre, const uint8_t* __restrict__ k_exp,
                      const uint8_t* __restrict__ v_exp, float* __restrict__ o_part,
-                     float2* __restrict__ ml_part, int* status) {
+                     float2* __restrict__ ml_part, int* status, const WinRows<WIN> wr) {
   pdl_begin();
   extern __shared__ __align__(16) float smem[];
   float* Qs = smem;                          // [kQV][DH+4], pre-scaled by log2(e)/sqrt(d)
@@ -79,8 +98,14 @@ attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* _
   const int n0 = row_offset[r], n1 = row_offset[r + 1], nr = n1 - n0;
   const int p0 = prefix_offset[r], p1 = prefix_offset[r + 1], P = p1 - p0;
   // (a request longer than the plan's chunks or vector groups is left out too)
-  if (!span_inside(n0, n1, N) || nr < 1 || !span_inside(p0, p1, total_prefix) ||
-      P > (long long)chunk * gridDim.x || (long long)nr * g > (long long)kQV * gridDim.y) {
+  const bool inside = span_inside(n0, n1, N) && nr >= 1 && span_inside(p0, p1, total_prefix);
+  int keys = P;  // or slots
+  Slots slots{};
+  if constexpr (WIN) {
+    if (inside && P > 0) slots = step_slots(wr.win, P);
+    keys = slots.n;
+  }
+  if (!inside || keys > (long long)chunk * gridDim.x || (long long)nr * g > (long long)kQV * gridDim.y) {
     if (threadIdx.x == 0) flag(status, JET_ERR_DEVICE);
     return;
   }
@@ -88,7 +113,7 @@ attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* _
   const int vbase = qg * kQV;
   if (vbase >= nvec) return;
   const int k_begin = split * chunk;
-  const int k_end = min(P, k_begin + chunk);
+  const int k_end = min(keys, k_begin + chunk);
 
   constexpr int C4 = DH / 4;                       // 16-byte pieces of a row
   constexpr int QI = kQV * C4 / kThreads;          // of the query block per thread
@@ -110,12 +135,23 @@ attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* _
     for (int i = 0; i < KI; ++i) {
       const int e = tid + i * kThreads, j = e / C4, c = e % C4;
       const bool in = kb + j < k_end;
-      const size_t idx = (size_t(p0 + kb + (in ? j : 0)) * Hkv + kh) * DH + 4 * c;
+      int key = kb + (in ? j : 0);
+      if (WIN && key >= slots.pad) key += slots.off;
+      const size_t idx = (size_t(p0 + key) * Hkv + kh) * DH + 4 * c;
       kr[i] = in ? load4(k_pre + idx, fk) : zero;
       vr[i] = in ? load4(v_pre + idx, fv) : zero;
     }
   };
   if (k_begin < k_end) fetch(k_begin);
+  int vfirst = 0, vlo = 0;
+  if constexpr (WIN) {
+    if (vbase + vec < nvec) {
+      const int n = n0 + (vbase + vec) / g;
+      const RowSeen see = row_seen(wr.win, P, wr.fed(n));
+      vfirst = see.pre_first;
+      vlo = see.pre_lo - slots.off;
+    }
+  }
 #pragma unroll
   for (int i = 0; i < QI; ++i) {
     const int e = tid + i * kThreads, vv = e / C4, c = e % C4, gv = vbase + vv;
@@ -166,12 +202,20 @@ attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* _
     }
     if (sub >= nk) s0 = -INFINITY;
     if (sub + 16 >= nk) s1 = -INFINITY;
+    if constexpr (WIN) {
+      const int k0 = kb + sub;
+      if (k0 >= vfirst && k0 < vlo) s0 = -INFINITY;
+      if (k0 + 16 >= vfirst && k0 + 16 < vlo) s1 = -INFINITY;
+    }
     float tmax = fmaxf(s0, s1);
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, o));
-    const float mn = fmaxf(m, tmax);            // finite: key 0 of the tile is valid
-    const float corr = exp2f(m - mn);           // 0 on the first tile
-    const float e0 = exp2f(s0 - mn), e1 = exp2f(s1 - mn);
+    // finite without a window: key 0 of the tile is valid; under one a vector may have seen
+    // no key yet
+    const float mn = fmaxf(m, tmax);
+    const float base = WIN && mn == -INFINITY ? 0.f : mn;
+    const float corr = exp2f(m - base);         // 0 on the first tile
+    const float e0 = exp2f(s0 - base), e1 = exp2f(s1 - base);
     float psum = e0 + e1;
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) psum += __shfl_xor_sync(0xffffffffu, psum, o);
@@ -185,6 +229,8 @@ attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* _
       acc[i] = make_float4(acc[i].x * corr, acc[i].y * corr, acc[i].z * corr, acc[i].w * corr);
     for (int j = 0; j < nk; ++j) {
       const float pj = Ps[vec * (kKT + 4) + j];
+      // (0 times what it does not see may be NaN)
+      if (WIN && kb + j >= vfirst && kb + j < vlo) continue;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const float4 x = *reinterpret_cast<const float4*>(Vs + j * DH + 4 * sub + 64 * i);
@@ -211,13 +257,14 @@ attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* _
 // row's own causal candidate keys, normalised. The loads that do not depend on
 // each other go out together: the chunks' (m, l) one a lane, their outputs and
 // the candidate's keys and values four at a time.
-template <int DH>
+template <int DH, bool WIN>
 __global__ void __launch_bounds__(128)
 attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restrict__ row_cand,
                     const int32_t* __restrict__ cand_row_offset, int N, int R, int C, int Hq, int Hkv,
                     int splits, const float* __restrict__ q, const float* __restrict__ k_cand,
                     const float* __restrict__ v_cand, const float* __restrict__ o_part,
-                    const float2* __restrict__ ml_part, float* __restrict__ o, int* status) {
+                    const float2* __restrict__ ml_part, float* __restrict__ o, int* status,
+                    const WinRows<WIN> wr) {
   pdl_begin();
   const int lane = threadIdx.x & 31;
   const long long idx = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
@@ -238,7 +285,16 @@ attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restri
       if (lane == 0) flag(status, JET_ERR_DEVICE);
     } else {
       const float scale = 1.4426950408889634f * rsqrtf(float(DH));  // base 2
-      for (int n4 = first; n4 <= n; n4 += 4) {
+      // under a window: the own tokens that are first tokens, then those of the window
+      int skip_from = n + 1, skip_to = n + 1;
+      if constexpr (WIN) {
+        const int p0 = wr.prefix_offset[r < R ? r : 0], p1 = wr.prefix_offset[(r < R ? r : 0) + 1];
+        const RowSeen see = row_seen(wr.win, max(p1 - p0, 1), n - first + 1);
+        skip_from = first + see.own_first;
+        skip_to = first + see.own_lo - 1;
+      }
+      for (int n4 = WIN && skip_from == first ? skip_to : first; n4 <= n; n4 += 4) {
+        if (WIN && n4 >= skip_from && n4 < skip_to) n4 = skip_to;
         float kv[4][PER], vv[4][PER], sc[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -263,6 +319,7 @@ attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restri
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           if (n4 + t > n) break;
+          if (WIN && n4 + t >= skip_from && n4 + t < skip_to) continue;
           const float mn = fmaxf(m, sc[t]);
           const float a = exp2f(m - mn), b = exp2f(sc[t] - mn);
 #pragma unroll
@@ -279,30 +336,31 @@ attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restri
 }
 
 // the prefix chunks, then their merge with the candidates' own keys
-template <int DH, typename TK>
+template <int DH, typename TK, bool WIN = false>
 cudaError_t launch_simt(const jet_layout& lay, const jet_dims& d, const AttnPlan& plan,
                         const void* q, const void* k_pre, const void* v_pre, size_t exp_off,
                         const void* k_cand, const void* v_cand, void* o, void* ws, int* status,
-                        cudaStream_t st) {
+                        cudaStream_t st, const WinRows<WIN>& wr = {}) {
   const jet_sizes& n = lay.n;
   float* o_part = static_cast<float*>(ws);
   float2* ml_part = reinterpret_cast<float2*>(o_part + size_t(plan.splits) * n.N * d.Hq * DH);
   const size_t smem = prefix_smem_bytes<DH>();
-  cudaError_t e = cudaFuncSetAttribute(attend_prefix_kernel<DH, TK>,
+  cudaError_t e = cudaFuncSetAttribute(attend_prefix_kernel<DH, TK, WIN>,
                                        cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
   dim3 grid(plan.splits, plan.qgroups, unsigned(n.R * d.Hkv));
-  e = launch_pdl(attend_prefix_kernel<DH, TK>, grid, dim3(kThreads), smem, st,
+  e = launch_pdl(attend_prefix_kernel<DH, TK, WIN>, grid, dim3(kThreads), smem, st,
                  lay.prefix_offset, lay.row_offset, n.R, n.N, n.total_prefix, d.Hq, d.Hkv,
                  plan.chunk, static_cast<const float*>(q), static_cast<const TK*>(k_pre),
                  static_cast<const TK*>(v_pre), static_cast<const uint8_t*>(k_pre) + exp_off,
-                 static_cast<const uint8_t*>(v_pre) + exp_off, o_part, ml_part, status);
+                 static_cast<const uint8_t*>(v_pre) + exp_off, o_part, ml_part, status, wr);
   if (e != cudaSuccess) return e;
   const long long warps = (long long)n.N * d.Hq;
-  return launch_pdl(attend_merge_kernel<DH>, dim3(unsigned((warps + 3) / 4)), dim3(128), 0, st,
+  return launch_pdl(attend_merge_kernel<DH, WIN>, dim3(unsigned((warps + 3) / 4)), dim3(128), 0, st,
                     lay.row_req, lay.row_cand, lay.cand_row_offset, n.N, n.R, n.C, d.Hq, d.Hkv,
                     plan.splits, static_cast<const float*>(q), static_cast<const float*>(k_cand),
-                    static_cast<const float*>(v_cand), o_part, ml_part, static_cast<float*>(o), status);
+                    static_cast<const float*>(v_cand), o_part, ml_part, static_cast<float*>(o), status,
+                    wr);
 }
 
 template <int DH>
@@ -468,6 +526,34 @@ AttnPlan attn_plan_kv8(const jet_sizes& n, const jet_dims& d) {
   const size_t partials = size_t(p.splits) * p.copies * n.N * d.Hq;
   p.bytes = partials * d.d * sizeof(float) + partials * sizeof(float2);
   return p;
+}
+
+// the step under a window: float32 here, bf16 in attend_tc.cu
+size_t attend_window_bytes(const jet_sizes& n, const jet_dims& d, int window, int sinks) {
+  const AttnPlan p = d.dtype == JET_DTYPE_BF16
+                         ? attend_window_plan(n, d, window, sinks)
+                         : attn_plan_simt(window_sizes(n, window, sinks), d);
+  return std::max<size_t>(16, p.bytes);
+}
+
+cudaError_t launch_attend_window(const jet_layout& lay, const jet_dims& d, int window, int sinks,
+                                 const void* q, const void* k_pre, const void* v_pre,
+                                 const void* k_cand, const void* v_cand, void* o, void* ws,
+                                 int* status, cudaStream_t st) {
+  if (d.dtype == JET_DTYPE_BF16)
+    return launch_attend_window_tc(lay, d, window, sinks, q, k_pre, v_pre, k_cand, v_cand, o, ws,
+                                   status, st);
+  const AttnPlan plan = attn_plan_simt(window_sizes(lay.n, window, sinks), d);
+  const WinRows<true> wr{Window{window, sinks}, lay.prefix_offset, lay.row_cand,
+                         lay.cand_row_offset, lay.n.C};
+#define JET_WIN(DH)                                                                             \
+  return launch_simt<DH, float, true>(lay, d, plan, q, k_pre, v_pre, 0, k_cand, v_cand, o, ws, \
+                                      status, st, wr)
+  if (d.d == 64) JET_WIN(64);
+  if (d.d == 128) JET_WIN(128);
+  if (d.d == 256) JET_WIN(256);
+#undef JET_WIN
+  return cudaErrorInvalidValue;
 }
 
 cudaError_t launch_prefix_attend_kv8(const jet_layout& lay, const jet_dims& d,

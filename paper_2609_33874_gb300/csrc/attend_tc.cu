@@ -79,7 +79,6 @@ __device__ __forceinline__ int4 item_of(const AttArgs& a, long long idx, int spl
   return make_int4(rk / a.Hkv, rk % a.Hkv, qb, split);
 }
 
-template <bool WIN>
 __global__ void __launch_bounds__(1024)
 attend_items_kernel(const AttArgs a, int qgroups, int splits) {
   pdl_begin();
@@ -92,7 +91,7 @@ attend_items_kernel(const AttArgs a, int qgroups, int splits) {
   const long long n_all = (long long)a.R * a.Hkv * qgroups * splits;
   for (long long idx = threadIdx.x; idx < n_all; idx += blockDim.x) {
     bool fits;
-    const ItemGeo e = item_geo<WIN>(a, item_of(a, idx, splits), &fits);
+    const ItemGeo e = item_geo(a, item_of(a, idx, splits), &fits);
     if (!fits) flag(a.status, JET_ERR_DEVICE);  // the request is left out
     const int b = e.ok ? min(e.ntiles, kBuckets - 1) : 0;
     if (idx < kItemCache) bucket[idx] = uint8_t(b);
@@ -128,7 +127,7 @@ attend_items_kernel(const AttArgs a, int qgroups, int splits) {
       b = bucket[idx];
     } else {
       bool fits;
-      const ItemGeo e = item_geo<WIN>(a, it, &fits);
+      const ItemGeo e = item_geo(a, it, &fits);
       b = e.ok ? min(e.ntiles, kBuckets - 1) : 0;
     }
     if (b > 0) a.items[atomicAdd(&cursor[b], 1)] = it;
@@ -296,7 +295,7 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
             if (idx >= count) break;
             const int4 cand = a.items[idx];
             bool fits;
-            const ItemGeo ce = item_geo<WIN>(a, cand, &fits);
+            const ItemGeo ce = item_geo(a, cand, &fits);
             if (ce.ok) {
               it = cand;
               e = ce;
@@ -976,7 +975,7 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
   }
   cudaError_t e = cudaSuccess;
   if (a.sorted)
-    e = launch_pdl(attend_items_kernel<WIN>, dim3(1), dim3(1024), 0, st, a, plan.qgroups, plan.splits);
+    e = launch_pdl(attend_items_kernel, dim3(1), dim3(1024), 0, st, a, plan.qgroups, plan.splits);
   if (e != cudaSuccess) return e;
   const size_t smem = Geo<DH, BN>::kBytes + 1024;
   e = cudaFuncSetAttribute(attend_prefix_tc_kernel<DH, WIN>,
@@ -1048,7 +1047,7 @@ cudaError_t launch_prefill_dh(const jet_layout& lay, const jet_dims& d, const vo
   a.n_all = (long long)n.R * d.Hkv * qgroups;
   a.sorted = 1;
   cudaError_t e =
-      launch_pdl(attend_items_kernel<false>, dim3(1), dim3(1024), 0, st, a, qgroups, 1);
+      launch_pdl(attend_items_kernel, dim3(1), dim3(1024), 0, st, a, qgroups, 1);
   if (e != cudaSuccess) return e;
   const size_t smem = Geo<DH, kBN>::kBytes + 1024;
   e = cudaFuncSetAttribute(attend_prefix_tc_kernel<DH, false>,
@@ -1105,17 +1104,6 @@ bool prefill_on_pairs(const jet_sizes& n, const jet_dims& d) {
   return time(single, rb, kBN, kPlanSMs) >= time(pair, 2 * rb, 128, kPlanSMs / 2);
 }
 
-// What a windowed call's plan reckons with: a request's keys are its slots, at most `window`
-// and the first ones' boxes.
-jet_sizes window_sizes(const jet_sizes& n, int window, int sinks) {
-  jet_sizes e = n;
-  const long long most = std::min<long long>(
-      n.max_prefix, (long long)window + ((long long)sinks + kSlotBox - 1) / kSlotBox * kSlotBox);
-  e.max_prefix = int(most);
-  e.total_prefix = int(std::min<long long>(n.total_prefix, most * std::max(1, n.R)));
-  return e;
-}
-
 }  // namespace
 
 cudaError_t launch_prefill_tc(const jet_layout& lay, const jet_dims& d, const void* q,
@@ -1147,8 +1135,62 @@ cudaError_t launch_attend_tc(const jet_layout& lay, const jet_dims& d, const Att
   return cudaErrorInvalidValue;
 }
 
-AttnPlan attend_window_plan(const jet_sizes& n, const jet_dims& d, int window, int sinks) {
-  return attn_plan(window_sizes(n, window, sinks), d);
+// What a windowed call's plan reckons with: a request's keys are its slots, at most `window`
+// and the first ones' boxes.
+jet_sizes window_sizes(const jet_sizes& n, int window, int sinks) {
+  jet_sizes e = n;
+  const long long most = std::min<long long>(
+      n.max_prefix, (long long)window + ((long long)sinks + kSlotBox - 1) / kSlotBox * kSlotBox);
+  e.max_prefix = int(most);
+  e.total_prefix = int(std::min<long long>(n.total_prefix, most * std::max(1, n.R)));
+  return e;
+}
+
+// A request's slots are cut in as many near-equal chunks as give the least estimated time, in
+// us: an item (2.5 us, and per 64 keys 0.78 at d 256, 0.26 at 64 and 128) bounds it from
+// below, and so do the bytes of all of them; with more items than SMs their sum's share of an
+// SM counts, and what the schedule leaves uneven (0.25 of an item where chunks are whole
+// requests, 1 else); chunks cost the combine's launch (1.5 us) and their partials' way out and
+// back (0.9 us a MB). Fitted to 45 batches of 1 to 256 requests under windows of 128 to 8,192
+// at up to 13 chunk lengths each: the chosen ones take 1.2 % more than the best, the plan of
+// the call without a window 8 % (127 requests of 1,733 tokens, one kv head of 128: unsplit
+// 28.9, in its chunks 44.6; seven of 1,425, d 64: 19.8 and 26.0; one of 4,641: 30.0 unsplit,
+// 14.8 in chunks of 192).
+AttnPlan attend_window_plan(const jet_sizes& sizes, const jet_dims& d, int window, int sinks) {
+  const jet_sizes n = window_sizes(sizes, window, sinks);
+  AttnPlan p{};
+  if (n.R <= 0 || n.N <= 0) return p;
+  const int g = d.Hq / d.Hkv, qv = std::max(1, kBV / g) * g;
+  p.qgroups = int(((long long)n.max_rows * g + qv - 1) / qv);
+  const double avg = double(n.total_prefix) / n.R;
+  const double groups =
+      double(n.R) * d.Hkv * std::max(1.0, std::ceil(double(n.N) * g / n.R / qv));
+  const double key_us = (d.d == 256 ? 0.78 : 0.26) / 64;
+  const double stream_us = groups * avg * d.d * 4 / 6.8e6;
+  const double partial_us = 7e-6 * double(n.N) * d.Hq * d.d;
+  const int tiles = n.max_prefix < 1 ? 1 : (n.max_prefix - 1) / 64 + 1;
+  double best = 0;
+  // chunks of 192 keys or more, two an SM at most for one request
+  const int most_chunks = std::max(1, std::min(tiles / 3, 2 * kPlanSMs));
+  for (int s = 1; s <= most_chunks; ++s) {
+    const int chunk = (tiles + s - 1) / s * 64, splits = (tiles * 64 + chunk - 1) / chunk;
+    if (splits != s) continue;  // as with fewer, longer chunks
+    const double per = s > 1 ? std::max(1.0, avg / chunk + 0.5) : 1.0;  // of a request
+    const double item = 2.5 + std::min(chunk, n.max_prefix) * key_us, items = groups * per;
+    double t = std::max(item, stream_us);
+    if (items > kPlanSMs)
+      t = std::max(t, (groups * avg * key_us + items * 2.5) / kPlanSMs +
+                          (s > 1 ? 1.0 : 0.25) * item);
+    if (s > 1) t += 1.5 + per * partial_us;
+    if (s == 1 || t < best) {
+      best = t;
+      p.chunk = chunk;
+      p.splits = splits;
+    }
+  }
+  const size_t partials = size_t(p.splits) * n.N * d.Hq;
+  p.bytes = partials * d.d * sizeof(float) + partials * sizeof(float2);
+  return p;
 }
 
 cudaError_t launch_attend_window_tc(const jet_layout& lay, const jet_dims& d, int window,

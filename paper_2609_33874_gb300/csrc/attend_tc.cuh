@@ -116,16 +116,15 @@ __device__ __forceinline__ ItemGeo geo_at(const AttArgs& a, int r, int kh, int q
 }
 
 // Of an item of the work list; *fits: its request is one to work on
-template <bool WIN = false>
 __device__ __forceinline__ ItemGeo item_geo(const AttArgs& a, int4 it, bool* fits) {
   *fits = false;
   if (!a.prefill) {
     if (it.x < 0 || it.x >= a.R) return ItemGeo{};
     const int n0 = a.row_offset[it.x], nr = a.row_offset[it.x + 1] - n0;
     const int p0 = a.prefix_offset[it.x], P = a.prefix_offset[it.x + 1] - p0;
-    const RequestCut cut = cut_of<WIN>(a, n0, nr, p0, P);
+    const RequestCut cut = request_cut(a, n0, nr, p0, P);
     *fits = cut.nq > 0;
-    return geo_at<WIN>(a, it.x, it.y, it.z, it.w, n0, nr, p0, P, cut);
+    return item_geo_at(a, it.x, it.y, it.z, it.w, n0, nr, p0, P, cut);
   }
   // prefill: the rows are the request's prefix positions and a block of
   // them sees the keys up to its last position (per-row causal mask in the

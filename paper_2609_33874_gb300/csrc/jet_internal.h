@@ -155,13 +155,14 @@ cudaError_t launch_norm_rotate(const jet_layout* lay, bool rows, const jet_dims&
                                const void* k, const void* gq, const void* gk, void* qo, void* ko,
                                int* status, cudaStream_t st);
 
-// attention under a window: the step (window.cu; bf16 on the tensor cores in attend_tc.cu),
-// and the prefill on pairs of SMs (prefill_window.cu), which needs no workspace
+// attention under a window: the step (float32 in attend.cu, bf16 on the tensor cores in
+// attend_tc.cu), and the prefill on pairs of SMs (prefill_window.cu), which needs no workspace
 size_t attend_window_bytes(const jet_sizes& n, const jet_dims& d, int window, int sinks);
 cudaError_t launch_attend_window(const jet_layout& lay, const jet_dims& d, int window, int sinks,
                                  const void* q, const void* k_pre, const void* v_pre,
                                  const void* k_cand, const void* v_cand, void* o, void* ws,
                                  int* status, cudaStream_t st);
+jet_sizes window_sizes(const jet_sizes& n, int window, int sinks);
 AttnPlan attend_window_plan(const jet_sizes& n, const jet_dims& d, int window, int sinks);
 cudaError_t launch_attend_window_tc(const jet_layout& lay, const jet_dims& d, int window,
                                     int sinks, const void* q, const void* k_pre,

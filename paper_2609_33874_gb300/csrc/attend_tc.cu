@@ -48,22 +48,31 @@ constexpr int kStages = 2;
 constexpr int kThreads = 224;
 constexpr int kSchedWarp = 6;  // the work-item scheduler
 
-template <int DH, int BN>
+// PAIRED: two CTAs an SM (the windowed step up to d 128), so that one's tiles come while the
+// other's item begins or ends: an item under a window is 2 to 20 tiles long, and its start and
+// end take as long as five. P then lies over the S tile that it comes from and the output
+// stage is half as large.
+template <int DH, bool PAIRED>
 struct Geo {
   static constexpr int kSlices = DH / 64;                   // 64-wide d slices
   static constexpr uint32_t kQBytes = kBV * DH * 2;         // query block
-  static constexpr uint32_t kKVBytes = BN * DH * 2;         // one K (or V) tile
+  static constexpr uint32_t kKVBytes = kBN * DH * 2;        // one K (or V) tile
   static constexpr uint32_t kOffK = kQBytes;                // stage s: K at kOffK + s * 2 kKV
-  // the output stage: 32 rows of 128 bytes per softmax warp
+  // the output stage: 32 rows of kPieces times 16 bytes per softmax warp
+  static constexpr int kPieces = PAIRED ? 4 : 8;
   static constexpr uint32_t kOffStage = kQBytes + kStages * 2 * kKVBytes;
-  static constexpr uint32_t kOffBar = kOffStage + 4 * 32 * 128;
+  static constexpr uint32_t kOffBar = kOffStage + 4 * 32 * kPieces * 16;
   static constexpr uint32_t kBytes = kOffBar + 512;
-  // TMEM: the two S buffers, O, then the two P buffers (bf16 pairs, BN / 2 columns)
-  static constexpr uint32_t kTmemCols = (2 * BN + DH + 2 * (BN / 2)) <= 256 ? 256 : 512;
-  static constexpr uint32_t kOCol = 2 * BN;                 // O after the two S buffers
-  static constexpr uint32_t kPCol = 2 * BN + DH;            // P buffer b at kPCol + BN / 2 b
-  static_assert(kPCol + BN <= 512, "tensor memory");
+  // TMEM: the two S buffers, O, then the two P buffers (bf16 pairs, 32 columns)
+  static constexpr uint32_t kUsedCols = 2 * kBN + DH + (PAIRED ? 0 : 2 * (kBN / 2));
+  static constexpr uint32_t kTmemCols = kUsedCols <= 256 ? 256 : 512;
+  static constexpr uint32_t kOCol = 2 * kBN;                // O after the two S buffers
+  static constexpr uint32_t kPCol = PAIRED ? 0 : 2 * kBN + DH;  // P buffer b at kPCol + b kPStep
+  static constexpr uint32_t kPStep = PAIRED ? kBN : kBN / 2;
 };
+static_assert(Geo<128, true>::kBytes + 1024 + 1024 <= 233472 / 2, "two CTAs an SM");
+static_assert(Geo<128, true>::kTmemCols == 256, "two CTAs an SM");
+constexpr bool paired(int d, bool win) { return win && d <= 128; }
 
 // The work list: every (request, kv head, query block, chunk) that has keys
 // and vectors, longest first (counting sort on the tile count), for the
@@ -145,27 +154,27 @@ struct WinArgs<true> {
   const __nv_bfloat16 *k, *v, *kc, *vc;
 };
 
-// BN keys of an item's slots from slot0 on into a tile (DH / 64 slices): one box a slice, or
+// 64 keys of an item's slots from slot0 on into a tile (DH / 64 slices): one box a slice, or
 // kSlotBox keys at a time where first keys and window meet
-template <int DH, int BN>
+template <int DH>
 __device__ __forceinline__ void load_slots(uint8_t* dst, const CUtensorMap* map,
                                            const CUtensorMap* map16, uint64_t* bar,
                                            const Slots& sl, int slot0, int p0, int kh,
                                            uint64_t pol) {
-  if (slot0 < sl.pad && slot0 + BN > sl.pad) {
+  if (slot0 < sl.pad && slot0 + kBN > sl.pad) {
 #pragma unroll
-    for (int b = 0; b < BN / kSlotBox; ++b) {
+    for (int b = 0; b < kBN / kSlotBox; ++b) {
       const int slot = slot0 + b * kSlotBox;
       const int key = p0 + (slot < sl.pad ? slot : slot + sl.off);
 #pragma unroll
       for (int i = 0; i < DH / 64; ++i)
-        tma_load_3d(dst + i * (BN * 128) + b * (kSlotBox * 128), map16, bar, i * 64, kh, key, pol);
+        tma_load_3d(dst + i * (kBN * 128) + b * (kSlotBox * 128), map16, bar, i * 64, kh, key, pol);
     }
   } else {
     const int key = p0 + slot0 + (slot0 < sl.pad ? 0 : sl.off);
 #pragma unroll
     for (int i = 0; i < DH / 64; ++i)
-      tma_load_3d(dst + i * (BN * 128), map, bar, i * 64, kh, key, pol);
+      tma_load_3d(dst + i * (kBN * 128), map, bar, i * 64, kh, key, pol);
   }
 }
 
@@ -189,15 +198,15 @@ __device__ __noinline__ void again(const AttArgs& a, const WinArgs<true>& w, con
 // continue across items, so the next item's query block and first K/V tiles
 // load while the current item's last tiles and its output are still in flight.
 template <int DH, bool WIN>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, paired(DH, WIN) ? 2 : 1)
 attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
                         const __grid_constant__ CUtensorMap tmK,
                         const __grid_constant__ CUtensorMap tmV,
                         const __grid_constant__ CUtensorMap tmKc,
                         const __grid_constant__ CUtensorMap tmVc, const AttArgs a,
                         const __grid_constant__ WinArgs<WIN> w) {
-  constexpr int BN = WIN ? win_tile(DH) : kBN;
-  using G = Geo<DH, BN>;
+  constexpr bool PAIRED = paired(DH, WIN);
+  using G = Geo<DH, PAIRED>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));
@@ -386,14 +395,14 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
               const bool pre = jk < e.npt;
               if (WIN && pre) {
                 if constexpr (WIN)
-                  load_slots<DH, BN>(ks, &tmK, &w.k16, k_full + s, sl, e.k_begin + jk * BN, e.p0, e.kh,
+                  load_slots<DH>(ks, &tmK, &w.k16, k_full + s, sl, e.k_begin + jk * kBN, e.p0, e.kh,
                                  pol);
               } else {
               const CUtensorMap* mk = pre ? &tmK : &tmKc;
-              const int key = pre ? e.p0 + e.k_begin + jk * BN : e.f_begin + (jk - e.npt) * BN;
+              const int key = pre ? e.p0 + e.k_begin + jk * kBN : e.f_begin + (jk - e.npt) * kBN;
 #pragma unroll
               for (int sl = 0; sl < G::kSlices; ++sl)
-                tma_load_3d(ks + sl * (BN * 128), mk, k_full + s, sl * 64, e.kh, key, pol);
+                tma_load_3d(ks + sl * (kBN * 128), mk, k_full + s, sl * 64, e.kh, key, pol);
               }
               k_issued |= 1u << s;
               k_par = (k_par & ~(1u << s)) | (ph << s);
@@ -411,14 +420,14 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
               const bool pre = jv < e.npt;
               if (WIN && pre) {
                 if constexpr (WIN)
-                  load_slots<DH, BN>(vs, &tmV, &w.v16, v_full + s, sl, e.k_begin + jv * BN, e.p0, e.kh,
+                  load_slots<DH>(vs, &tmV, &w.v16, v_full + s, sl, e.k_begin + jv * kBN, e.p0, e.kh,
                                  pol);
               } else {
               const CUtensorMap* mv = pre ? &tmV : &tmVc;
-              const int key = pre ? e.p0 + e.k_begin + jv * BN : e.f_begin + (jv - e.npt) * BN;
+              const int key = pre ? e.p0 + e.k_begin + jv * kBN : e.f_begin + (jv - e.npt) * kBN;
 #pragma unroll
               for (int sl = 0; sl < G::kSlices; ++sl)
-                tma_load_3d(vs + sl * (BN * 128), mv, v_full + s, sl * 64, e.kh, key, pol);
+                tma_load_3d(vs + sl * (kBN * 128), mv, v_full + s, sl * 64, e.kh, key, pol);
               }
               v_issued |= 1u << s;
               v_par = (v_par & ~(1u << s)) | (ph << s);
@@ -451,7 +460,7 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
     if (elect_one()) {
-      const uint32_t id_s = idesc_bf16_f32(kBV, BN);
+      const uint32_t id_s = idesc_bf16_f32(kBV, kBN);
       const uint32_t id_o = idesc_bf16_f32(kBV, DH) | (1u << 16);  // B (V) is MN-major
       const uint32_t qs = smem_u32(smem);
       bool ok = mbar_wait(qz_done, 0, a.wait_ns, abort_flag);
@@ -478,15 +487,16 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
           if (js < e.ntiles) {
             const int Tj = T + js;
             const int s = Tj % kStages, b = Tj & 1;
+            // (P over S: the buffer is free once its P V is issued, which runs before)
             if (mbar_test(k_full + s, (Tj / kStages) & 1) &&
-                mbar_test(s_free + b, ((Tj >> 1) & 1) ^ 1u)) {
+                (PAIRED ? js - jo < 2 : mbar_test(s_free + b, ((Tj >> 1) & 1) ^ 1u))) {
               tc_fence_after();
               const uint32_t ks = smem_u32(smem + G::kOffK + s * 2 * G::kKVBytes);
 #pragma unroll
               for (int st = 0; st < DH / 16; ++st) {
                 const int sl = st >> 2, k = st & 3;
-                mma_f16(tmem + b * BN, desc_k_sw128(qs + sl * (kBV * 128) + 32 * k),
-                        desc_k_sw128(ks + sl * (BN * 128) + 32 * k), id_s, st != 0);
+                mma_f16(tmem + b * kBN, desc_k_sw128(qs + sl * (kBV * 128) + 32 * k),
+                        desc_k_sw128(ks + sl * (kBN * 128) + 32 * k), id_s, st != 0);
               }
               mma_commit(s_full + b);
               mma_commit(k_empty + s);
@@ -504,12 +514,12 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
                 mbar_test(v_full + s, (Tj / kStages) & 1)) {
               tc_fence_after();
               // P_j from TMEM (8 columns = 16 keys per instruction), V_j from shared memory
-              const uint32_t pt = tmem + G::kPCol + uint32_t(b) * (BN / 2);
+              const uint32_t pt = tmem + G::kPCol + uint32_t(b) * G::kPStep;
               const uint32_t vs = smem_u32(smem + G::kOffK + s * 2 * G::kKVBytes + G::kKVBytes);
 #pragma unroll
-              for (int k = 0; k < BN / 16; ++k)
+              for (int k = 0; k < kBN / 16; ++k)
                 mma_f16_ta(tmem + G::kOCol, pt + uint32_t(8 * k),
-                           desc_mn_sw128(vs + k * 16 * 128, BN * 128), id_o, (jo | k) != 0);
+                           desc_mn_sw128(vs + k * 16 * 128, kBN * 128), id_o, (jo | k) != 0);
               mma_commit(p_free + b);
               mma_commit(v_empty + s);
               ++jo;
@@ -538,7 +548,8 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
     // the output is transposed through this warp's own 4 KB of the output
     // stage so that every global store covers whole 64- or 128-byte pieces of
     // one vector's output
-    uint4* stage = reinterpret_cast<uint4*>(smem + G::kOffStage + q4 * 32 * 128);
+    constexpr int PC = G::kPieces;  // 16-byte pieces of a row at a time
+    uint4* stage = reinterpret_cast<uint4*>(smem + G::kOffStage + q4 * 32 * PC * 16);
     // the query blocks arrive by TMA (rows [0, rb g)); zero the rows past them
     // once so that no stale shared memory enters the MMA
     if (i >= rb * g) {
@@ -594,37 +605,39 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
           break;
         }
         tc_fence_after();
-        float sv[BN];
+        float sv[kBN];
         {
-          float t[BN / 32][32];
-#pragma unroll
-          for (int x = 0; x < BN / 32; ++x)
-            tmem_ld_32cols(tmem + lane_off + b * BN + 32 * x, t[x]);
+          float t0[32], t1[32];
+          tmem_ld_32cols(tmem + lane_off + b * kBN, t0);
+          tmem_ld_32cols(tmem + lane_off + b * kBN + 32, t1);
           tmem_wait_ld();
 #pragma unroll
-          for (int c = 0; c < BN; ++c) sv[c] = t[c >> 5][c & 31];
+          for (int c = 0; c < 32; ++c) {
+            sv[c] = t0[c];
+            sv[c + 32] = t1[c];
+          }
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(s_free + b);
+        if (!PAIRED && lane == 0) mbar_arrive(s_free + b);
         if constexpr (WIN) {
           // what this vector sees of the tile's keys
-          uint32_t see[BN / 32];
+          uint32_t see[kBN / 32];
           if (j < e.npt) {
-            const int k0 = e.k_begin + j * BN;
+            const int k0 = e.k_begin + j * kBN;
 #pragma unroll
-            for (int x = 0; x < BN / 32; ++x)
+            for (int x = 0; x < kBN / 32; ++x)
               see[x] = bit_range(-32 * x, min(e.k_end, vfirst) - k0 - 32 * x) |
                        bit_range(vlo - k0 - 32 * x, e.k_end - k0 - 32 * x);
           } else {
-            const int f0 = e.f_begin + (j - e.npt) * BN;
+            const int f0 = e.f_begin + (j - e.npt) * kBN;
 #pragma unroll
-            for (int x = 0; x < BN / 32; ++x)
+            for (int x = 0; x < kBN / 32; ++x)
               see[x] = bit_range(fa - f0 - 32 * x, min(ffirst, fb + 1) - f0 - 32 * x) |
                        bit_range(flo - f0 - 32 * x, fb + 1 - f0 - 32 * x);
           }
 #pragma unroll
-          for (int x = 0; x < BN / 32; ++x) {
+          for (int x = 0; x < kBN / 32; ++x) {
             if (__all_sync(0xffffffffu, see[x] == ~0u)) continue;
 #pragma unroll
             for (int c = 32 * x; c < 32 * x + 32; ++c)
@@ -634,16 +647,16 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         // visible keys of this tile: [klo, khi) of its 64 slots
         int klo = 0, khi;
         if (j < e.npt) {
-          khi = min(BN, e.k_end - (e.k_begin + j * BN));
-          khi = min(khi, kcap + 1 - (e.k_begin + j * BN));  // prefill: keys <= own position
+          khi = min(kBN, e.k_end - (e.k_begin + j * kBN));
+          khi = min(khi, kcap + 1 - (e.k_begin + j * kBN));  // prefill: keys <= own position
         } else {
-          const int f0 = e.f_begin + (j - e.npt) * BN;
+          const int f0 = e.f_begin + (j - e.npt) * kBN;
           klo = max(0, fa - f0);
-          khi = min(BN, fb - f0 + 1);
+          khi = min(kBN, fb - f0 + 1);
         }
-        if (__any_sync(0xffffffffu, klo > 0 || khi < BN)) {
+        if (__any_sync(0xffffffffu, klo > 0 || khi < kBN)) {
 #pragma unroll
-          for (int c = 0; c < BN; ++c)
+          for (int c = 0; c < kBN; ++c)
             if (c < klo || c >= khi) sv[c] = -INFINITY;
         }
         }
@@ -653,11 +666,11 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
 #pragma unroll
         for (int q = 0; q < 8; ++q) mq[q] = sv[q];
 #pragma unroll
-        for (int c = 8; c < BN; ++c) mq[c & 7] = fmaxf(mq[c & 7], sv[c]);
+        for (int c = 8; c < kBN; ++c) mq[c & 7] = fmaxf(mq[c & 7], sv[c]);
         const float mt = a.scale_log2 * fmaxf(fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])),
                                               fmaxf(fmaxf(mq[4], mq[5]), fmaxf(mq[6], mq[7])));
-        // P buffer b was last read by the P V of tile Tj - 2
-        if (Tj >= 2 && !warp_mbar_wait(p_free + b, ((Tj - 2) >> 1) & 1, a.wait_ns, abort_flag)) {
+        // P buffer b was last read by the P V of tile Tj - 2 (P over S: before S_j came)
+        if (!PAIRED && Tj >= 2 && !warp_mbar_wait(p_free + b, ((Tj - 2) >> 1) & 1, a.wait_ns, abort_flag)) {
           ok = false;
           break;
         }
@@ -692,30 +705,23 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         // P = 2^(s scale - m_used) as bf16 pairs into this row's TMEM lane (the P V
         // MMA's A operand); the row sum uses the rounded values, which are what
         // the tensor core multiplies
-        uint32_t pw[BN / 2];
-        float ps[8];  // partial sums, added as a tree
+        uint32_t pw[kBN / 2];
+        float ps[8];  // one partial sum per 8 keys, added as a tree
         // under a window a vector may have seen no key yet: its weights are zeros then
         const float m_off = WIN && m_used == -INFINITY ? 0.f : -m_used;
 #pragma unroll
-        for (int cc = 0; cc < 8; ++cc) ps[cc] = 0.f;
-#pragma unroll
-        for (int cc = 0; cc < BN / 8; ++cc) {
+        for (int cc = 0; cc < 8; ++cc) {
+          ps[cc] = 0.f;
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const float x0 = ex2(fmaf(sv[cc * 8 + 2 * q], a.scale_log2, m_off));
             const float x1 = ex2(fmaf(sv[cc * 8 + 2 * q + 1], a.scale_log2, m_off));
             const uint32_t w = pack_bf16(x0, x1);
             pw[cc * 4 + q] = w;
-            ps[cc & 7] += __uint_as_float(w << 16) + __uint_as_float(w & 0xffff0000u);
+            ps[cc] += __uint_as_float(w << 16) + __uint_as_float(w & 0xffff0000u);
           }
         }
-#pragma unroll
-        for (int x = 0; x < BN / 64; ++x) {
-          uint32_t part[32];
-#pragma unroll
-          for (int c = 0; c < 32; ++c) part[c] = pw[32 * x + c];
-          tmem_st_32cols_u32(tmem + lane_off + G::kPCol + uint32_t(b) * (BN / 2) + 32 * x, part);
-        }
+        tmem_st_32cols_u32(tmem + lane_off + G::kPCol + uint32_t(b) * G::kPStep, pw);
         l += ((ps[0] + ps[1]) + (ps[2] + ps[3])) + ((ps[4] + ps[5]) + (ps[6] + ps[7]));
         tmem_wait_st();
         tc_fence_before();
@@ -728,10 +734,10 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
       // lane stores (4 s + lane / 8, 16 bytes each), as element offsets, -1 past the
       // block's vectors
       const bool direct = e.splits_r == 1;  // the whole row in this item: final output
-      long long dst[8];
+      long long dst[PC];
 #pragma unroll
-      for (int s = 0; s < 8; ++s) {
-        const int gi = q4 * 32 + 4 * s + (lane >> 3);
+      for (int s = 0; s < PC; ++s) {
+        const int gi = q4 * 32 + 32 / PC * s + lane / PC;
         dst[s] = -1;
         if (gi < e.nv) {
           const int gv = e.vbase + gi;
@@ -759,24 +765,24 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         break;
       }
       tc_fence_after();
-      // 128 (or all 64) columns of O per TMEM round trip, written as 128-byte pieces
+      // 128 (64 where two CTAs share the registers) columns of O per TMEM round trip, written as 128-byte pieces
       // of each vector (64 bf16 or 32 f32 columns) through this warp's 4 KB stage:
       // eight 16-byte pieces a row, rotated by the row
-      constexpr int kCols = DH < 128 ? DH : 128;
-      auto put_piece = [&](const uint4(&x)[8], char* base, size_t esize, int col) {
+      constexpr int kCols = DH < 128 || PAIRED ? 64 : 128;
+      auto put_piece = [&](const uint4(&x)[PC], char* base, size_t esize, int col) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) stage[lane * 8 + (q ^ (lane & 7))] = x[q];
+        for (int q = 0; q < PC; ++q) stage[lane * PC + (q ^ (lane & (PC - 1)))] = x[q];
         __syncwarp();
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {
-          const int iv = 4 * s + (lane >> 3), c = lane & 7;
-          const uint4 val = stage[iv * 8 + (c ^ (iv & 7))];
+        for (int s = 0; s < PC; ++s) {
+          const int iv = 32 / PC * s + lane / PC, c = lane & (PC - 1);
+          const uint4 val = stage[iv * PC + (c ^ (iv & (PC - 1)))];
           if (dst[s] >= 0)
             *reinterpret_cast<uint4*>(base + (dst[s] + col) * esize + c * 16) = val;
         }
         __syncwarp();
       };
-      __nv_bfloat162 most = __floats2bfloat162_rn(0.f, 0.f);  // NaN where an output is
+      __nv_bfloat162 most = __floats2bfloat162_rn(0.f, 0.f);  // the largest output, or NaN
 #pragma unroll 1
       for (int c0 = 0; c0 < DH; c0 += kCols) {
         float ov[kCols / 32][32];
@@ -786,31 +792,34 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         tmem_wait_ld();
         if (direct) {
 #pragma unroll
-          for (int k = 0; k < kCols / 32; k += 2) {
-            uint4 x[8];
+          for (int k = 0; k < kCols; k += 8 * PC) {
+            uint4 x[PC];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-              const float* y = ov[k + (q >> 2)] + 8 * (q & 3);
+            for (int q = 0; q < PC; ++q) {
+              const float* y = ov[(k + 8 * q) >> 5] + ((k + 8 * q) & 31);
               x[q] = make_uint4(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
                                 pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv));
               if constexpr (WIN) {
                 const uint32_t words[4] = {x[q].x, x[q].y, x[q].z, x[q].w};
 #pragma unroll
                 for (int z = 0; z < 4; ++z)
-                  most = __hmax2_nan(most, *reinterpret_cast<const __nv_bfloat162*>(&words[z]));
+                  most = __hmax2_nan(
+                      most, __habs2(*reinterpret_cast<const __nv_bfloat162*>(&words[z])));
               }
             }
-            put_piece(x, reinterpret_cast<char*>(a.o), 2, c0 + 32 * k);
+            put_piece(x, reinterpret_cast<char*>(a.o), 2, c0 + k);
           }
         } else {
 #pragma unroll
-          for (int k = 0; k < kCols / 32; ++k) {
-            uint4 x[8];
+          for (int k = 0; k < kCols; k += 4 * PC) {
+            uint4 x[PC];
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
-              x[q] = make_uint4(__float_as_uint(ov[k][4 * q]), __float_as_uint(ov[k][4 * q + 1]),
-                                __float_as_uint(ov[k][4 * q + 2]), __float_as_uint(ov[k][4 * q + 3]));
-            put_piece(x, reinterpret_cast<char*>(a.o_part), 4, c0 + 32 * k);
+            for (int q = 0; q < PC; ++q) {
+              const float* y = ov[(k + 4 * q) >> 5] + ((k + 4 * q) & 31);
+              x[q] = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]),
+                                __float_as_uint(y[3]));
+            }
+            put_piece(x, reinterpret_cast<char*>(a.o_part), 4, c0 + k);
           }
         }
       }
@@ -822,9 +831,11 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         mbar_arrive(item_empty + slot);
       }
       if constexpr (WIN) {
-        // vectors with a NaN: again from what they see alone
-        const bool nan = __hisnan(most.x) || __hisnan(most.y);
-        for (unsigned left = __ballot_sync(0xffffffffu, direct && valid && nan); left;
+        // vectors with a NaN or an infinity: again from what they see alone (a weight above 1
+        // may have taken a large value past the largest float)
+        const bool odd =
+            __hisnan(most.x) || __hisnan(most.y) || __hisinf(most.x) || __hisinf(most.y);
+        for (unsigned left = __ballot_sync(0xffffffffu, direct && valid && odd); left;
              left &= left - 1) {
           const int src = __ffs(left) - 1, gv = e.vbase + q4 * 32 + src;
           const int t = __shfl_sync(0xffffffffu, max(0, fb - fa + 1), src);
@@ -872,14 +883,14 @@ combine_window_kernel(const AttArgs a, const WinArgs<true> w, const int32_t* __r
   }
   if (direct) return;
   const float inv = l > 0.f ? 1.f / l : 0.f;
-  bool nan = false;
+  bool odd = false;  // a NaN or an infinity
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const float y = acc[i] * inv;
-    nan |= isnan(y);
+    odd |= !isfinite(y);
     a.o[(size_t(n) * a.Hq + h) * DH + lane + 32 * i] = __float2bfloat16_rn(y);
   }
-  if (!__any_sync(0xffffffffu, nan)) return;
+  if (!__any_sync(0xffffffffu, odd)) return;
   ItemGeo e{};
   e.n0 = a.row_offset[r];
   e.kh = h / a.g;
@@ -911,19 +922,18 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
                       const Window& win, const void* q, const void* k_pre, const void* v_pre,
                       const void* k_cand, const void* v_cand, void* o, float* o_part,
                       float2* ml_part, int* status, cudaStream_t st) {
-  constexpr int BN = WIN ? win_tile(DH) : kBN;
   const jet_sizes& n = lay.n;
   const int F = n.N - n.R;
   const int g = d.Hq / d.Hkv;
   if (g > kBV) return cudaErrorInvalidValue;
   CUtensorMap tmQ, tmK, tmV, tmKc, tmVc;
   if (!encode_3d(&tmQ, q, n.N, d.Hq, DH, g, kBV / g) ||
-      !encode_3d(&tmK, k_pre, n.total_prefix, d.Hkv, DH, 1, BN) ||
-      !encode_3d(&tmV, v_pre, n.total_prefix, d.Hkv, DH, 1, BN))
+      !encode_3d(&tmK, k_pre, n.total_prefix, d.Hkv, DH, 1, kBN) ||
+      !encode_3d(&tmV, v_pre, n.total_prefix, d.Hkv, DH, 1, kBN))
     return cudaErrorInvalidValue;
   if (F > 0) {
-    if (!encode_3d(&tmKc, k_cand, F, d.Hkv, DH, 1, BN) ||
-        !encode_3d(&tmVc, v_cand, F, d.Hkv, DH, 1, BN))
+    if (!encode_3d(&tmKc, k_cand, F, d.Hkv, DH, 1, kBN) ||
+        !encode_3d(&tmVc, v_cand, F, d.Hkv, DH, 1, kBN))
       return cudaErrorInvalidValue;
   } else {
     tmKc = tmK;  // never read: no request has candidate tiles
@@ -965,19 +975,18 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
   a.n_all = (long long)n.R * d.Hkv * plan.qgroups * plan.splits;
   const int sms = sm_count();
   if (sms < 1) return cudaErrorInvalidValue;
-  const int grid = int(std::max<long long>(1, std::min<long long>(sms, a.n_all)));
+  const int grid = int(std::max<long long>(1, std::min<long long>((paired(DH, WIN) ? 2 : 1) * sms, a.n_all)));
   a.sorted = plan.sorted;
   WinArgs<WIN> w;
   if constexpr (WIN) {
     a.win = win;
-    a.bn = BN;
     if (!win_args(&w, n, d, k_pre, v_pre, k_cand, v_cand)) return cudaErrorInvalidValue;
   }
   cudaError_t e = cudaSuccess;
   if (a.sorted)
     e = launch_pdl(attend_items_kernel, dim3(1), dim3(1024), 0, st, a, plan.qgroups, plan.splits);
   if (e != cudaSuccess) return e;
-  const size_t smem = Geo<DH, BN>::kBytes + 1024;
+  const size_t smem = Geo<DH, paired(DH, WIN)>::kBytes + 1024;
   e = cudaFuncSetAttribute(attend_prefix_tc_kernel<DH, WIN>,
                            cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
@@ -1049,7 +1058,7 @@ cudaError_t launch_prefill_dh(const jet_layout& lay, const jet_dims& d, const vo
   cudaError_t e =
       launch_pdl(attend_items_kernel, dim3(1), dim3(1024), 0, st, a, qgroups, 1);
   if (e != cudaSuccess) return e;
-  const size_t smem = Geo<DH, kBN>::kBytes + 1024;
+  const size_t smem = Geo<DH, false>::kBytes + 1024;
   e = cudaFuncSetAttribute(attend_prefix_tc_kernel<DH, false>,
                            cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
@@ -1147,15 +1156,15 @@ jet_sizes window_sizes(const jet_sizes& n, int window, int sinks) {
 }
 
 // A request's slots are cut in as many near-equal chunks as give the least estimated time, in
-// us: an item (2.5 us, and per 64 keys 0.78 at d 256, 0.26 at 64 and 128) bounds it from
-// below, and so do the bytes of all of them; with more items than SMs their sum's share of an
-// SM counts, and what the schedule leaves uneven (0.25 of an item where chunks are whole
-// requests, 1 else); chunks cost the combine's launch (1.5 us) and their partials' way out and
-// back (0.9 us a MB). Fitted to 45 batches of 1 to 256 requests under windows of 128 to 8,192
-// at up to 13 chunk lengths each: the chosen ones take 1.2 % more than the best, the plan of
-// the call without a window 8 % (127 requests of 1,733 tokens, one kv head of 128: unsplit
-// 28.9, in its chunks 44.6; seven of 1,425, d 64: 19.8 and 26.0; one of 4,641: 30.0 unsplit,
-// 14.8 in chunks of 192).
+// us: an item (1.9 us, and per 64 keys 0.58 at d 256, 0.47 at 64 and 128, where two CTAs share
+// an SM) bounds it from below, and so do the bytes of all of them; with more items than CTAs
+// their sum's share of a CTA counts, and what the schedule leaves uneven (0.25 of an item where
+// chunks are whole requests, 0.6 else); chunks cost the combine's launch (2.8 us) and their
+// partials' way out and back (0.2 us a MB). Fitted to 45 batches of 1 to 256 requests under
+// windows of 128 to 8,192 at up to 13 chunk lengths each: the chosen ones take 1.1 % more than
+// the best, the plan of the call without a window 8 % (127 requests of 1,733 tokens, one kv head
+// of 128: unsplit 28.9, in its chunks 44.6; one of 4,641, two: 34.4 unsplit, 13.7 in chunks of
+// 192).
 AttnPlan attend_window_plan(const jet_sizes& sizes, const jet_dims& d, int window, int sinks) {
   const jet_sizes n = window_sizes(sizes, window, sinks);
   AttnPlan p{};
@@ -1165,9 +1174,10 @@ AttnPlan attend_window_plan(const jet_sizes& sizes, const jet_dims& d, int windo
   const double avg = double(n.total_prefix) / n.R;
   const double groups =
       double(n.R) * d.Hkv * std::max(1.0, std::ceil(double(n.N) * g / n.R / qv));
-  const double key_us = (d.d == 256 ? 0.78 : 0.26) / 64;
-  const double stream_us = groups * avg * d.d * 4 / 6.8e6;
-  const double partial_us = 7e-6 * double(n.N) * d.Hq * d.d;
+  const double ctas = paired(d.d, true) ? 2 * kPlanSMs : kPlanSMs;
+  const double key_us = (d.d == 256 ? 0.58 : 0.47) / 64, fixed_us = 1.9;
+  const double stream_us = groups * avg * d.d * 4 / 8.8e6;
+  const double partial_us = 1.6e-6 * double(n.N) * d.Hq * d.d;
   const int tiles = n.max_prefix < 1 ? 1 : (n.max_prefix - 1) / 64 + 1;
   double best = 0;
   // chunks of 192 keys or more, two an SM at most for one request
@@ -1176,12 +1186,12 @@ AttnPlan attend_window_plan(const jet_sizes& sizes, const jet_dims& d, int windo
     const int chunk = (tiles + s - 1) / s * 64, splits = (tiles * 64 + chunk - 1) / chunk;
     if (splits != s) continue;  // as with fewer, longer chunks
     const double per = s > 1 ? std::max(1.0, avg / chunk + 0.5) : 1.0;  // of a request
-    const double item = 2.5 + std::min(chunk, n.max_prefix) * key_us, items = groups * per;
+    const double item = fixed_us + std::min(chunk, n.max_prefix) * key_us, items = groups * per;
     double t = std::max(item, stream_us);
-    if (items > kPlanSMs)
-      t = std::max(t, (groups * avg * key_us + items * 2.5) / kPlanSMs +
-                          (s > 1 ? 1.0 : 0.25) * item);
-    if (s > 1) t += 1.5 + per * partial_us;
+    if (items > ctas)
+      t = std::max(t, (groups * avg * key_us + items * fixed_us) / ctas +
+                          (s > 1 ? 0.6 : 0.25) * item);
+    if (s > 1) t += 2.8 + per * partial_us;
     if (s == 1 || t < best) {
       best = t;
       p.chunk = chunk;

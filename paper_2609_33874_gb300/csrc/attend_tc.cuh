@@ -47,7 +47,6 @@ struct AttArgs : ItemPlan {
   uint64_t wait_ns;  // budget of one bounded wait (jet_set_wait_budget_ns)
   int hold_first;    // test hook (jet_set_test_stall): withhold the first query block
   Window win;        // of the windowed step: its keys are slots (window.h)
-  int bn;            // and its tiles hold so many
 };
 
 // SW128 K-major position of 16-byte chunk c of row i inside one 64-wide slice
@@ -93,22 +92,14 @@ __device__ __forceinline__ RequestCut cut_of(const AttArgs& a, int n0, int nr, i
     return request_cut(a, n0, nr, p0, P);
 }
 
-// Keys per tile of the windowed step: 128 where TMEM holds two such score tiles and their
-// weights beside O. (One query row of 64 requests under 1,024, 32/8 heads of 128, 64 keys a
-// tile: 65 us; the softmax of a tile, not its bytes, set the pace.)
-constexpr int win_tile(int d) { return d <= 128 ? 128 : kBN; }
-
-// The geometry of its items: under a window k_begin, k_end and npt count slots, in tiles of
-// `bn`, and P is the request's prefix all the same
+// The geometry of its items: under a window k_begin, k_end and npt count slots, and P is the
+// request's prefix all the same
 template <bool WIN>
 __device__ __forceinline__ ItemGeo geo_at(const AttArgs& a, int r, int kh, int qb, int split,
                                           int n0, int nr, int p0, int P, const RequestCut& cut) {
   if constexpr (WIN) {
     ItemGeo e = item_geo_at(a, r, kh, qb, split, n0, nr, p0, step_slots(a.win, P).n, cut);
     e.P = P;
-    e.npt = (e.k_end - e.k_begin + a.bn - 1) / a.bn;
-    if (e.nct > 0) e.nct = (e.nr - 1 + a.bn - 1) / a.bn;
-    e.ntiles = e.npt + e.nct;
     return e;
   } else {
     return item_geo_at(a, r, kh, qb, split, n0, nr, p0, P, cut);

@@ -719,6 +719,37 @@ jet_status jet_stack_forward(const jet_layout* lay, const jet_dims* dims, const 
                              const void* x0, void* x, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Stacks of layers with positions (see jet_norm_rotate and jet_prefix_attend_window): what a
+ * full layer's attention does besides.
+ */
+typedef struct jet_stack_attn {
+  int32_t window;      /* tokens a token sees, itself among them; 0: all of them        */
+  int32_t sinks;       /* first tokens that stay visible under the window               */
+  const void* gq;      /* [d] bf16 gains of the query heads; NULL: ones                  */
+  const void* gk;      /* [d] bf16 gains of the key heads; NULL: ones                    */
+} jet_stack_attn;
+
+/* Workspace bytes of jet_stack_forward_window: L layers, attn a host array of L (NULL: as
+ * jet_stack_workspace_bytes); 0 on invalid arguments. */
+size_t jet_stack_window_workspace_bytes(const jet_sizes* n, const jet_dims* dims, int32_t Dff,
+                                        int32_t L, const jet_stack_attn* attn);
+
+/*
+ * jet_stack_forward_window - jet_stack_forward, in whose full layers the projected queries and
+ * keys are normalised and rotated at their rows' positions (rope; NULL: neither) and attend
+ * under the layer's window (attn, a host array of stack.L entries read during the call; NULL:
+ * no windows and no gains; linear layers' entries are not read). The prefix keys in k_pre are
+ * taken as they are: normalised and rotated already. Between the operations the rows are bf16,
+ * so the projection's queries and keys are rounded before the norm, and after the rotation.
+ * Errors besides: as for jet_norm_rotate_rows and jet_prefix_attend_window, window or sinks
+ * below 0 JET_ERR_ARG.
+ */
+jet_status jet_stack_forward_window(const jet_layout* lay, const jet_dims* dims,
+                                    const jet_stack* stack, const jet_rope* rope,
+                                    const jet_stack_attn* attn, const void* x0, void* x, void* ws,
+                                    size_t ws_bytes, void* stream);
+
+/*
  * jet_score_candidates_noalloc - jet_score_candidates without caller-owned
  * scratch memory. The paper has no counterpart to this entry point: it exists
  * for callers that cannot call cudaMalloc, such as a host application that

@@ -10,8 +10,10 @@ import math
 
 import numpy as np
 
+from .stack import _fed_rows, _gate_up, bf16, rmsnorm, silu
+
 __all__ = ["frequencies", "rotate", "seen", "row_position", "window_keys", "window_cascade",
-           "window_prefill"]
+           "window_prefill", "full_layer"]
 
 
 def frequencies(rot: int, theta: float) -> np.ndarray:
@@ -102,3 +104,27 @@ def window_prefill(prefix_len, q, k, v, Hq, Hkv, window, sinks, rows):
                                 np.asarray(k[at, h // g], np.float64),
                                 np.asarray(v[at, h // g], np.float64), 1.0 / math.sqrt(d))
     return out
+
+
+def full_layer(lay, x, P, dims, window=None, sinks=0, rope=None):
+    """A decoder stack's full layer with positions, at the stack oracle's storage points and one
+    more, the rotated queries and keys: rope is None or a dict of rot, style, freq, eps and norm
+    (gains gq and gk in P), window None or the tokens a token sees."""
+    N = x.shape[0]
+    fed = _fed_rows(lay)
+    Hq, Hkv, d = dims["Hq"], dims["Hkv"], dims["d"]
+    z = bf16(bf16(rmsnorm(x, P["g1"])) @ P["w_mix"].T)
+    q = z[:, :Hq * d].reshape(N, Hq, d)
+    k = z[:, Hq * d:(Hq + Hkv) * d].reshape(N, Hkv, d)
+    v = z[:, (Hq + Hkv) * d:].reshape(N, Hkv, d)
+    if rope is not None:
+        pos = [row_position(lay, n) for n in range(N)]
+        q, k = (bf16(rotate(t, pos, rope["rot"], rope["style"], rope["freq"], P.get(g),
+                            rope["eps"], rope["norm"])) for t, g in ((q, "gq"), (k, "gk")))
+    wide = 1 << 40 if window is None else window
+    o = bf16(window_cascade(lay, q, P["k_pre"], P["v_pre"], k[fed], v[fed], Hq, Hkv, wide, sinks,
+                            list(range(N))))
+    x1 = bf16(x + o.reshape(N, Hq * d) @ P["w_o"].T)
+    wg, wu = _gate_up(P["w_gu"], dims["Dff"])
+    h2 = bf16(rmsnorm(x1, P["g2"]))
+    return bf16(x1 + bf16(silu(h2 @ wg.T) * (h2 @ wu.T)) @ P["w_d"].T)

@@ -370,14 +370,19 @@ namespace {
 
 // what jet_norm_rotate and its forms take of the rotation, the dims and the tensors:
 // nq and nk tokens of queries and keys
-jet_status check_rotate(const jet_dims* d, const jet_rope* rope, long long nq, long long nk,
-                        const void* q, const void* k, const void* gq, const void* gk,
-                        const void* qo, const void* ko) {
+jet_status check_rope(const jet_dims* d, const jet_rope* rope) {
   JET_TRY(check_attn_dims(d));
   if (!rope) return JET_ERR_ARG;
   if (rope->style != JET_ROPE_HALVES && rope->style != JET_ROPE_PAIRS) return JET_ERR_ARG;
   if ((rope->norm != 0 && rope->norm != 1) || !(rope->eps >= 0.f)) return JET_ERR_ARG;
   if (rope->rot < 0 || rope->rot % 8 != 0 || rope->rot > d->d) return JET_ERR_SHAPE;
+  return JET_OK;
+}
+
+jet_status check_rotate(const jet_dims* d, const jet_rope* rope, long long nq, long long nk,
+                        const void* q, const void* k, const void* gq, const void* gk,
+                        const void* qo, const void* ko) {
+  JET_TRY(check_rope(d, rope));
   if (!q && !k && (nq > 0 || nk > 0)) return JET_ERR_ARG;
   if (!q != !qo || !k != !ko) return JET_ERR_ARG;
   if (q) {
@@ -748,7 +753,9 @@ struct StackPlan {
   bool full_ok, lin_ok;
 };
 
-StackPlan stack_plan(const jet_sizes& n, const jet_dims& d, int Dff) {
+// attn: the windows of L layers, for their attention's workspace (null: none)
+StackPlan stack_plan(const jet_sizes& n, const jet_dims& d, int Dff, int L,
+                     const jet_stack_attn* attn) {
   auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
   StackPlan p{};
   const size_t N = size_t(n.N), F = size_t(n.N - n.R), b = 2;
@@ -785,7 +792,11 @@ StackPlan stack_plan(const jet_sizes& n, const jet_dims& d, int Dff) {
     p.kc = take(F * d.Hkv * d.d * b);
     p.vc = take(F * d.Hkv * d.d * b);
     p.attn_plan = jet::attn_plan(n, d);
-    p.attn = take(p.attn_plan.bytes);
+    size_t bytes = p.attn_plan.bytes;
+    for (int l = 0; attn && l < L; ++l)
+      if (attn[l].window > 0)
+        bytes = std::max(bytes, jet::attend_window_bytes(n, d, attn[l].window, attn[l].sinks));
+    p.attn = take(bytes);
   }
   if (p.lin_ok) {
     p.lqa = take(N * d.Hl * d.dk * b);
@@ -803,12 +814,24 @@ StackPlan stack_plan(const jet_sizes& n, const jet_dims& d, int Dff) {
 
 extern "C" size_t jet_stack_workspace_bytes(const jet_sizes* n, const jet_dims* d, int32_t Dff) {
   if (!n || !d || n->R < 0 || n->N < n->R || d->D < 16 || Dff < 64 || Dff % 64 != 0) return 0;
-  return stack_plan(*n, *d, Dff).bytes;
+  return stack_plan(*n, *d, Dff, 0, nullptr).bytes;
 }
 
-extern "C" jet_status jet_stack_forward(const jet_layout* lay, const jet_dims* dims,
-                                        const jet_stack* stack, const void* x0, void* x,
-                                        void* ws, size_t ws_bytes, void* stream) {
+extern "C" size_t jet_stack_window_workspace_bytes(const jet_sizes* n, const jet_dims* d,
+                                                   int32_t Dff, int32_t L,
+                                                   const jet_stack_attn* attn) {
+  if (!n || !d || n->R < 0 || n->N < n->R || d->D < 16 || Dff < 64 || Dff % 64 != 0) return 0;
+  if (L < 0) return 0;
+  for (int l = 0; attn && l < L; ++l)
+    if (attn[l].window < 0 || attn[l].sinks < 0) return 0;
+  return stack_plan(*n, *d, Dff, L, attn).bytes;
+}
+
+namespace {
+
+jet_status stack_forward(const jet_layout* lay, const jet_dims* dims, const jet_stack* stack,
+                         const jet_rope* rope, const jet_stack_attn* attn, const void* x0, void* x,
+                         void* ws, size_t ws_bytes, void* stream) {
   JET_TRY(check_layout(lay));
   if (!dims || !stack) return JET_ERR_ARG;
   JET_TRY(check_dtype(dims));
@@ -819,13 +842,19 @@ extern "C" jet_status jet_stack_forward(const jet_layout* lay, const jet_dims* d
   if (stack->rule != JET_RECUR_DELTA && stack->rule != JET_RECUR_GLA) return JET_ERR_ARG;
   const jet_sizes& n = lay->n;
   const long long N = n.N;
-  const StackPlan plan = stack_plan(n, *dims, stack->Dff);
   // validate every layer before the first launch
   for (int l = 0; l < stack->L; ++l) {
     const jet_stack_layer& Ly = stack->layers[l];
     if (Ly.kind == JET_LAYER_FULL) {
       JET_TRY(check_attn_dims(dims));
       if ((long long)n.R * dims->Hkv > 65535) return JET_ERR_CAPACITY;
+      if (rope) JET_TRY(check_rope(dims, rope));
+      if (attn) {
+        if (attn[l].window < 0 || attn[l].sinks < 0) return JET_ERR_ARG;
+        if (attn[l].window > 0 && dims->Hq / dims->Hkv > jet::attn_tc_block())
+          return JET_ERR_UNSUPPORTED;
+        if (!aligned16(attn[l].gq) || !aligned16(attn[l].gk)) return JET_ERR_ALIGN;
+      }
       JET_TRY(check_ptr(Ly.k_pre, n.total_prefix));
       JET_TRY(check_ptr(Ly.v_pre, n.total_prefix));
     } else if (Ly.kind == JET_LAYER_LINEAR) {
@@ -846,6 +875,7 @@ extern "C" jet_status jet_stack_forward(const jet_layout* lay, const jet_dims* d
   if (n.R == 0) return JET_OK;
   JET_TRY(check_ptr(x0, N));
   JET_TRY(check_ptr(x, N));
+  const StackPlan plan = stack_plan(n, *dims, stack->Dff, stack->L, attn);
   if (!ws || ws_bytes < plan.bytes) return JET_ERR_WORKSPACE;
   if (!aligned16(ws)) return JET_ERR_ALIGN;
   if (N > 65535 * 8 || (long long)N * dims->D > INT32_MAX) return JET_ERR_CAPACITY;
@@ -873,10 +903,20 @@ extern "C" jet_status jet_stack_forward(const jet_layout* lay, const jet_dims* d
       JET_TRY(cuda_status(jet::launch_proj_qkv(*lay, w + plan.h, D, Ly.w_mix, qw, kw, w + plan.z,
                                                w + plan.q, w + plan.kc, w + plan.vc, part, status,
                                                st)));
-      JET_TRY(cuda_status(jet::launch_prefix_attend(*lay, *dims, plan.attn_plan, w + plan.q,
-                                                    Ly.k_pre, Ly.v_pre, w + plan.kc,
-                                                    w + plan.vc, w + plan.o, w + plan.attn,
-                                                    status, st)));
+      if (rope)
+        JET_TRY(cuda_status(jet::launch_norm_rotate(
+            lay, true, *dims, *rope, int(N), nullptr, w + plan.q, N > n.R ? w + plan.kc : nullptr,
+            attn ? attn[l].gq : nullptr, attn ? attn[l].gk : nullptr, w + plan.q,
+            N > n.R ? w + plan.kc : nullptr, status, st)));
+      if (attn && attn[l].window > 0)
+        JET_TRY(cuda_status(jet::launch_attend_window(
+            *lay, *dims, attn[l].window, attn[l].sinks, w + plan.q, Ly.k_pre, Ly.v_pre, w + plan.kc,
+            w + plan.vc, w + plan.o, w + plan.attn, status, st)));
+      else
+        JET_TRY(cuda_status(jet::launch_prefix_attend(*lay, *dims, plan.attn_plan, w + plan.q,
+                                                      Ly.k_pre, Ly.v_pre, w + plan.kc,
+                                                      w + plan.vc, w + plan.o, w + plan.attn,
+                                                      status, st)));
       ow = qw;
     } else {
       float* al = reinterpret_cast<float*>(w + plan.al);
@@ -909,6 +949,21 @@ extern "C" jet_status jet_stack_forward(const jet_layout* lay, const jet_dims* d
                                          next ? w + plan.h : nullptr)));
   }
   return JET_OK;
+}
+
+}  // namespace
+
+extern "C" jet_status jet_stack_forward(const jet_layout* lay, const jet_dims* dims,
+                                        const jet_stack* stack, const void* x0, void* x,
+                                        void* ws, size_t ws_bytes, void* stream) {
+  return stack_forward(lay, dims, stack, nullptr, nullptr, x0, x, ws, ws_bytes, stream);
+}
+
+extern "C" jet_status jet_stack_forward_window(const jet_layout* lay, const jet_dims* dims,
+                                               const jet_stack* stack, const jet_rope* rope,
+                                               const jet_stack_attn* attn, const void* x0, void* x,
+                                               void* ws, size_t ws_bytes, void* stream) {
+  return stack_forward(lay, dims, stack, rope, attn, x0, x, ws, ws_bytes, stream);
 }
 
 extern "C" jet_status jet_decide(const jet_layout* lay, int32_t mode, const float* cand_score,

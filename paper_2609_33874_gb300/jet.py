@@ -142,6 +142,10 @@ def _load() -> ctypes.CDLL:
                                            P, P, P, P, P, SZ, P]),
         "jet_stack_workspace_bytes": (SZ, [ctypes.POINTER(jet_sizes), ctypes.POINTER(jet_dims),
                                            I]),
+        "jet_stack_window_workspace_bytes": (SZ, [ctypes.POINTER(jet_sizes),
+                                                  ctypes.POINTER(jet_dims), I, I, P]),
+        "jet_stack_forward_window": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
+                                         P, P, P, P, P, P, SZ, P]),
         "jet_stack_forward": (I, [ctypes.POINTER(jet_layout), ctypes.POINTER(jet_dims),
                                   P, P, P, P, SZ, P]),
         "jet_decide": (I, [ctypes.POINTER(jet_layout), I, P, P, P, P, P]),
@@ -173,7 +177,8 @@ DECLARED = ("jet_abi_version", "jet_status_string", "jet_layout_plan", "jet_layo
             "jet_w4_bytes", "jet_quantize_w4", "jet_score_candidates_w4",
             "jet_mxfp8_bytes", "jet_quantize_mxfp8", "jet_workspace_bytes_mxfp8",
             "jet_score_candidates_mxfp8",
-            "jet_stack_workspace_bytes", "jet_stack_forward", "jet_decide", "jet_evaluate", "jet_device_status",
+            "jet_stack_workspace_bytes", "jet_stack_forward", "jet_stack_window_workspace_bytes",
+            "jet_stack_forward_window", "jet_decide", "jet_evaluate", "jet_device_status",
             "jet_set_wait_budget_ns", "jet_launch_count", "jet_set_test_stall")
 
 
@@ -302,6 +307,21 @@ def make_stack(layers, Dff: int, rule: int = 0):
     st = jet_stack(len(layers), int(Dff), int(rule), 0,
                    ctypes.cast(arr, ctypes.POINTER(jet_stack_layer)))
     return st, arr
+
+
+class jet_stack_attn(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("gq", ctypes.c_void_p),
+                ("gk", ctypes.c_void_p)]
+
+
+def make_stack_attn(layers):
+    """A jet_stack_attn array over a list of dicts (window, sinks, gq, gk, each optional)."""
+    arr = (jet_stack_attn * max(1, len(layers)))()
+    for i, Ly in enumerate(layers):
+        arr[i].window = _i32_arg(Ly.get("window") or 0, "window")
+        arr[i].sinks = _i32_arg(Ly.get("sinks") or 0, "sinks")
+        arr[i].gq, arr[i].gk = _addr(Ly.get("gq")), _addr(Ly.get("gk"))
+    return arr
 
 
 def make_dims(dtype: int, Hq=0, Hkv=0, d=0, D=0, Hl=0, dk=0, dv=0, max_sms=0) -> jet_dims:
@@ -631,6 +651,27 @@ def jet_stack_forward(layout, dims: jet_dims, stack, x0, x, ws, ws_bytes: Option
     _check(_lib.jet_stack_forward(ctypes.byref(_lay(layout)), ctypes.byref(dims),
                                   ctypes.byref(stack), _addr(x0), _addr(x), _addr(ws),
                                   int(ws_bytes), _stream(stream)), "jet_stack_forward")
+
+
+def jet_stack_window_workspace_bytes(sizes: jet_sizes, dims: jet_dims, Dff: int, L: int,
+                                     attn=None) -> int:
+    """Workspace bytes of jet_stack_forward_window; ``attn`` from :func:`make_stack_attn`."""
+    return int(_lib.jet_stack_window_workspace_bytes(ctypes.byref(sizes), ctypes.byref(dims),
+                                                     int(Dff), int(L), attn))
+
+
+def jet_stack_forward_window(layout, dims: jet_dims, stack, rope, attn, x0, x, ws,
+                             ws_bytes: Optional[int] = None, stream=None) -> None:
+    """jet_stack_forward with positions (``rope`` from :func:`make_rope`, or None) and windows
+    (``attn`` from :func:`make_stack_attn`, an entry a layer, or None); see include/jet.h."""
+    ws_bytes = ws.numel() * ws.element_size() if ws_bytes is None else ws_bytes
+    if attn is not None and len(attn) < stack.L:
+        raise ValueError("attn holds an entry a layer")
+    _check(_lib.jet_stack_forward_window(ctypes.byref(_lay(layout)), ctypes.byref(dims),
+                                         ctypes.byref(stack),
+                                         ctypes.byref(rope) if rope is not None else None, attn,
+                                         _addr(x0), _addr(x), _addr(ws), int(ws_bytes),
+                                         _stream(stream)), "jet_stack_forward_window")
 
 
 def jet_decide(layout, mode: int, cand_score, q, choice, value, stream=None) -> None:

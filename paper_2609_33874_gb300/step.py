@@ -129,6 +129,15 @@ def quantize_prefix(layout, dims: "jet.jet_dims", k_pre: torch.Tensor, v_pre: to
     return k8, v8
 
 
+def rotate_prefix(layout, dims: "jet.jet_dims", rope: "jet.jet_rope", k_pre: torch.Tensor,
+                  gk: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The packed prefix keys [total_prefix, Hkv, d] normalised and rotated at their positions
+    (jet_norm_rotate_prefix), for a step built with the same ``rope`` and ``gk``."""
+    out = torch.empty_like(k_pre)
+    jet.jet_norm_rotate_prefix(layout, dims, rope, None, k_pre, None, gk, None, out, stream=stream)
+    return out
+
+
 class ScoringStep:
     """Device state of one batch shape.
 
@@ -147,15 +156,30 @@ class ScoringStep:
     over the host link) instead of tensors of the step's type. Over long prefixes the
     attention is faster than over a bf16 cache; over batches of short ones, whose bytes do
     not set the pace, it takes up to 1.5 times as long.
+    ``window``: the attention sees a row's last ``window`` tokens and the request's first
+    ``sinks`` ones (jet_prefix_attend_window; not over 8-bit caches). ``rope`` (from
+    :func:`jet.make_rope`) normalises and rotates the step's q and k_cand at their rows'
+    positions first, with the gains ``gq`` and ``gk`` [d], into buffers of the step's own
+    (jet_norm_rotate_rows; the prefix keys are taken as they are, rotated already:
+    :func:`rotate_prefix`).
     """
 
     def __init__(self, layout: "jet.HostLayout", dims: "jet.jet_dims", mode: int,
                  device="cuda", hybrid: bool = False, keep_fork_state: bool = False,
                  chain: bool = False, lm: str = "bf16", rule: str = "delta",
-                 kv: Optional[str] = None):
+                 kv: Optional[str] = None, window: Optional[int] = None, sinks: int = 0,
+                 rope: Optional["jet.jet_rope"] = None, gq: Optional[torch.Tensor] = None,
+                 gk: Optional[torch.Tensor] = None):
         if kv not in (None, "e4m3"):
             raise ValueError("kv must be None or 'e4m3'")
-        self.kv = kv
+        if window is None and sinks:
+            raise ValueError("sinks are first tokens under a window")
+        if window is not None and kv:
+            raise ValueError("a window is not over 8-bit caches")
+        if rope is None and (gq is not None or gk is not None):
+            raise ValueError("gains belong to a rope's norm")
+        self.kv, self.window, self.sinks = kv, window, int(sinks)
+        self.rope, self.gq, self.gk = rope, gq, gk
         if lm not in ("bf16", "e4m3", "w4", "mxfp8"):
             raise ValueError("lm must be 'bf16', 'e4m3', 'w4' or 'mxfp8'")
         self.lm = lm
@@ -184,6 +208,14 @@ class ScoringStep:
               "mxfp8": jet.jet_workspace_bytes_mxfp8}[lm](n, dims)
         if kv:
             ws = max(ws, jet.jet_attend_workspace_bytes_e4m3(n, dims))
+        if window is not None:
+            nb = jet.jet_attend_window_workspace_bytes(n, dims, window, self.sinks)
+            if nb == 0:
+                raise ValueError("window must be at least 1, and sinks at least 0")
+            ws = max(ws, nb)
+        if rope is not None:
+            self._q = z(n.N, dims.Hq, dims.d, dtype=dt)
+            self._k_cand = z(self.F, dims.Hkv, dims.d, dtype=dt)
         self.ws = z((ws + 15) // 16 * 4)  # float32 words, 16-byte multiple
         if hybrid:
             self.lo = z(self.F, dims.Hl, dims.dv, dtype=dt)
@@ -215,9 +247,19 @@ class ScoringStep:
         """
         d = self.dims
         lay = self.layout if layout is None else layout
-        attend = jet.jet_prefix_attend_e4m3 if self.kv else jet.jet_prefix_attend
-        attend(lay, d, x["q"], x["k_pre"], x["v_pre"], x["k_cand"], x["v_cand"], self.o, self.ws,
-               stream=stream)
+        q, k_cand = x["q"], x["k_cand"]
+        if self.rope is not None:
+            jet.jet_norm_rotate_rows(lay, d, self.rope, q, k_cand, self.gq, self.gk, self._q,
+                                     self._k_cand, stream=stream)
+            q, k_cand = self._q, self._k_cand
+        if self.window is not None:
+            jet.jet_prefix_attend_window(lay, d, self.window, self.sinks, q, x["k_pre"],
+                                         x["v_pre"], k_cand, x["v_cand"], self.o, self.ws,
+                                         stream=stream)
+        else:
+            attend = jet.jet_prefix_attend_e4m3 if self.kv else jet.jet_prefix_attend
+            attend(lay, d, q, x["k_pre"], x["v_pre"], k_cand, x["v_cand"], self.o, self.ws,
+                   stream=stream)
         if self.hybrid:
             jet.jet_fork_state(lay, d, x["s_prefix"], x["lq"], x["lk"], x["lv"], x["alpha"],
                                x["beta"], self.lo, self.s_fork, stream=stream, rule=self.rule)
@@ -370,10 +412,12 @@ class DecoderStack:
     """A hybrid decoder stack's device tensors and workspace for one batch
     shape. ``layers`` is a list of dicts: kind ("linear" or "full") and the
     tensors g1, g2, w_mix, w_o, w_gu, w_d and k_pre/v_pre (full) or s_prefix
-    (linear), already on the device."""
+    (linear), already on the device. ``rope`` (from :func:`jet.make_rope`) normalises and
+    rotates the full layers' queries and keys, with the layers' gains gq and gk (optional, [d]);
+    a full layer with a ``window`` (and ``sinks``) attends under it (jet_stack_forward_window)."""
 
     def __init__(self, layout: "jet.HostLayout", dims: "jet.jet_dims", layers, Dff: int,
-                 rule: str = "delta", device="cuda"):
+                 rule: str = "delta", device="cuda", rope: Optional["jet.jet_rope"] = None):
         self.dev = torch.device(device)
         self.layout = layout.to_device(self.dev)
         self.dims = dims
@@ -382,7 +426,10 @@ class DecoderStack:
         self.stack, self._keep = jet.make_stack(self.layers, Dff, jet.RULES[rule])
         n = layout.sizes
         self.N = n.N
-        wsb = jet.jet_stack_workspace_bytes(n, dims, Dff)
+        self.rope, self.attn = rope, None
+        if any(L.get(k) is not None for L in layers for k in ("window", "sinks", "gq", "gk")):
+            self.attn = jet.make_stack_attn(self.layers)
+        wsb = jet.jet_stack_window_workspace_bytes(n, dims, Dff, len(layers), self.attn)
         if wsb == 0:
             raise ValueError("invalid stack sizes")
         self.ws = torch.empty((wsb + 15) // 16 * 4, dtype=torch.float32, device=self.dev)
@@ -391,6 +438,10 @@ class DecoderStack:
     def forward(self, x0: torch.Tensor, stream=None, layout=None) -> torch.Tensor:
         """Enqueue the stack on ``stream``; returns the output rows [N, D]."""
         lay = self.layout if layout is None else layout
-        jet.jet_stack_forward(lay, self.dims, self.stack, x0, self.x, self.ws, stream=stream)
+        if self.rope is None and self.attn is None:
+            jet.jet_stack_forward(lay, self.dims, self.stack, x0, self.x, self.ws, stream=stream)
+        else:
+            jet.jet_stack_forward_window(lay, self.dims, self.stack, self.rope, self.attn, x0,
+                                         self.x, self.ws, stream=stream)
         return self.x
 

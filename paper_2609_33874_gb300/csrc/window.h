@@ -62,18 +62,20 @@ JET_HD RowSeen row_seen(const Window& w, int P, int t) {
 // Keys as the tiles of a tensor-core kernel take them: the first `sinks` keys and [lo, end)
 // laid end to end. Slot i < pad holds key i (those from `sinks` on are masked), a later one
 // key i + off. pad is a multiple of kSlotBox, the keys of one copy into a tile that holds both;
-// 0 where nothing lies between the first keys and lo.
+// 0 where lo lies before the end of the first keys' last box: then all of [0, end) are slots. So
+// no slot is a key at or past end, and there are no more of them than keys.
 constexpr int kSlotBox = 16;
 struct Slots {
   int n, pad, off;
 };
 JET_HD Slots window_slots(const Window& w, int64_t lo, int64_t end) {
   Slots s;
-  if (w.sinks >= lo) {
+  const int64_t pad = (int64_t(w.sinks) + kSlotBox - 1) / kSlotBox * kSlotBox;
+  if (pad >= lo) {
     s.pad = s.off = 0;
     s.n = int(end);
   } else {
-    s.pad = int((int64_t(w.sinks) + kSlotBox - 1) / kSlotBox * kSlotBox);
+    s.pad = int(pad);
     s.off = int(lo - s.pad);
     s.n = int(s.pad + end - lo);
   }

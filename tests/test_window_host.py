@@ -19,8 +19,10 @@ int main() {
   while (std::scanf("%d %d %d %d", &window, &sinks, &P, &t) == 4) {
     const jet::Seen s = jet::seen_at(jet::Window{window, sinks}, (long long)P - 1 + t);
     const jet::RowSeen r = jet::row_seen(jet::Window{window, sinks}, P, t);
-    std::printf("%lld %lld %d %d %d %d\n", (long long)s.first, (long long)s.lo, r.pre_first,
+    std::printf("%lld %lld %d %d %d %d", (long long)s.first, (long long)s.lo, r.pre_first,
                 r.pre_lo, r.own_first, r.own_lo);
+    const jet::Slots b = jet::step_slots(jet::Window{window, sinks}, P);
+    std::printf(" %d %d %d\n", b.n, b.pad, b.off);
   }
 }
 """
@@ -50,7 +52,7 @@ def test_rows_see_what_the_oracle_says(window_words):
               for _ in range(500)]
     for (w, s, P, t), got in zip(cases, window_words(cases)):
         p = P - 1 + t
-        first, lo, pre_first, pre_lo, own_first, own_lo = got
+        first, lo, pre_first, pre_lo, own_first, own_lo = got[:6]
         assert first <= lo
         assert sorted({*range(first), *range(lo, p + 1)}) == W.seen(p, w, s)
         assert 0 <= pre_first <= pre_lo <= P and own_lo >= 1
@@ -58,6 +60,19 @@ def test_rows_see_what_the_oracle_says(window_words):
         own = [*range(1, min(own_first, t) + 1)] + [*range(own_lo, t + 1)]
         assert len(own) == len(set(own))     # no token twice
         assert sorted(pre | {P - 1 + x for x in own}) == W.seen(p, w, s)
+
+
+def test_slots_are_a_request_s_own_keys(window_words):
+    """No slot is a key past the prefix, there are no more of them than the plans reckon with,
+    and every key that the shared row sees has one."""
+    cases = [(w, s, P, 0) for w in (1, 2, 17, 64) for s in (0, 1, 15, 16, 17, 49, 50, 62, 63, 200)
+             for P in (1, 2, 10, 17, 63, 64, 65, 66, 80, 130, 300)]
+    for (w, s, P, _), got in zip(cases, window_words(cases)):
+        n, pad, off = got[6:]
+        assert 1 <= n <= min(P, w + (s + 15) // 16 * 16) and pad % 16 == 0 and off >= 0
+        keys = [i if i < pad else i + off for i in range(n)]
+        assert len(set(keys)) == n and max(keys) == P - 1
+        assert set(W.seen(P - 1, w, s)) <= set(keys)
 
 
 def test_rows_at_the_largest_words(window_words):

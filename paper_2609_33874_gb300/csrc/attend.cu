@@ -321,7 +321,8 @@ attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restri
           if (n4 + t > n) break;
           if (WIN && n4 + t >= skip_from && n4 + t < skip_to) continue;
           const float mn = fmaxf(m, sc[t]);
-          const float a = exp2f(m - mn), b = exp2f(sc[t] - mn);
+          const float base = WIN && mn == -INFINITY ? 0.f : mn;  // nothing seen yet
+          const float a = exp2f(m - base), b = exp2f(sc[t] - base);
 #pragma unroll
           for (int i = 0; i < PER; ++i) acc[i] = acc[i] * a + b * vv[t][i];
           l = l * a + b;
@@ -330,7 +331,8 @@ attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restri
       }
     }
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  // (a windowed row whose scores are all minus infinity: 0 / 0)
+  const float inv = WIN || l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
   for (int i = 0; i < PER; ++i) o[(size_t(n) * Hq + h) * DH + lane + 32 * i] = acc[i] * inv;
 }

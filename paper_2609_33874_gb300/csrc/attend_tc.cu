@@ -832,9 +832,10 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
       }
       if constexpr (WIN) {
         // vectors with a NaN or an infinity: again from what they see alone (a weight above 1
-        // may have taken a large value past the largest float)
-        const bool odd =
-            __hisnan(most.x) || __hisnan(most.y) || __hisinf(most.x) || __hisinf(most.y);
+        // may have taken a large value past the largest float), and those whose scores are all
+        // minus infinity, 0 / 0
+        const bool odd = !(l > 0.f) || __hisnan(most.x) || __hisnan(most.y) ||
+                         __hisinf(most.x) || __hisinf(most.y);
         for (unsigned left = __ballot_sync(0xffffffffu, direct && valid && odd); left;
              left &= left - 1) {
           const int src = __ffs(left) - 1, gv = e.vbase + q4 * 32 + src;
@@ -883,7 +884,7 @@ combine_window_kernel(const AttArgs a, const WinArgs<true> w, const int32_t* __r
   }
   if (direct) return;
   const float inv = l > 0.f ? 1.f / l : 0.f;
-  bool odd = false;  // a NaN or an infinity
+  bool odd = !(l > 0.f);  // 0 / 0, a NaN or an infinity
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const float y = acc[i] * inv;

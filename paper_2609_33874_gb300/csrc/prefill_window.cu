@@ -848,8 +848,10 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
         }
       }
       // vectors with a NaN or an infinity: again, from what they see alone (a weight above 1 may
-      // have taken a large value past the largest float)
-      const bool odd = __hisnan(most.x) || __hisnan(most.y) || __hisinf(most.x) || __hisinf(most.y);
+      // have taken a large value past the largest float), and those whose scores are all minus
+      // infinity, 0 / 0
+      const bool odd = !(l > 0.f) || __hisnan(most.x) || __hisnan(most.y) || __hisinf(most.x) ||
+                       __hisinf(most.y);
       for (unsigned left = __ballot_sync(0xffffffffu, i < e.nv && odd); left; left &= left - 1)
         again<DH>(a, e, q4 * 32 + __ffs(left) - 1, lane);
     }

@@ -128,8 +128,8 @@ __device__ __forceinline__ void store4(T* p, const float (&v)[4]) {
 
 // v over the root of the mean of its head's squares, times g. The root's reciprocal is the
 // hardware's and one step of Newton's: two units of the last place at most, as a root and a
-// quotient would be, for six instructions. Heads whose squares leave float32 are scaled by a
-// power of two first.
+// quotient would be, for six instructions. Heads whose squares leave float32, or nearly, are
+// scaled by a power of two first.
 template <int DH>
 __device__ __forceinline__ void normalise(float (&v)[2][4], const float (&g)[2][4], float eps) {
   auto squares = [&]() {
@@ -147,22 +147,30 @@ __device__ __forceinline__ void normalise(float (&v)[2][4], const float (&g)[2][
     for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(v[0][j]), fabsf(v[1][j])));
 #pragma unroll
     for (int o = DH / 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    // its exponent; not of zeros (they stay), nor where eps counts more than they do
-    const int e = top > 0.f && top < INFINITY && !(top * top < eps) ? ilogbf(top) : 0;
+    const float m = fmaxf(top, sqrtf(eps));
+    const int e = m > 0.f && m < INFINITY ? ilogbf(m) : 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       v[0][j] = ldexpf(v[0][j], -e);
       v[1][j] = ldexpf(v[1][j], -e);
     }
     x = fmaf(squares(), 1.f / float(DH), ldexpf(ldexpf(eps, -e), -e));
-    if (top == 0.f) x = 1.f;
+    if (top == 0.f) x = 1.f;  // zeros stay
+    if (x == INFINITY) {      // an infinite element: NaN, and zeros beside it
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[0][j] *= 0.f;
+        v[1][j] *= 0.f;
+      }
+      x = 1.f;
+    }
   }
   const float r = rsqrtf(x);
   const float inv = r * fmaf(-0.5f * x * r, r, 1.5f);
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    v[0][j] *= inv * g[0][j];
-    v[1][j] *= inv * g[1][j];
+    v[0][j] = v[0][j] * inv * g[0][j];
+    v[1][j] = v[1][j] * inv * g[1][j];
   }
 }
 

@@ -1,7 +1,7 @@
 // Attention of one query vector under a window by one warp, key by key in float32: what the
-// tensor-core kernels fall back on for a vector whose output came out NaN. Their products
-// take whole tiles, and a weight of zero times an infinite or NaN value that the vector does
-// not see is NaN; here nothing but what it sees is read.
+// tensor-core kernels fall back on for a vector whose output came out NaN or infinite. Their
+// products take whole tiles, and a weight of zero times an infinite or NaN value that the vector
+// does not see is NaN; here nothing but what it sees is read.
 #pragma once
 
 #include "jet_device.cuh"
@@ -29,7 +29,8 @@ __device__ __forceinline__ void load_row(const __nv_bfloat16* p, float (&v)[PER]
   }
 }
 
-// A query vector's running softmax over keys in pieces: elements lane PER .. + PER - 1
+// A query vector's running softmax over keys in pieces: elements lane PER .. + PER - 1. acc is
+// the mean so far, not its product with l, so it is no larger than the values.
 template <int DH>
 struct RowState {
   static constexpr int PER = DH / 32;
@@ -58,13 +59,14 @@ struct RowState {
 #pragma unroll
       for (int t = 0; t < kAtOnce; ++t) {
         if (j0 + t >= end) break;
+        if (s[t] == -INFINITY) continue;  // weight 0
         const float mn = fmaxf(m, s[t]);
-        const float a = mn == -INFINITY ? 1.f : exp2f(m - mn);
-        const float b = mn == -INFINITY ? 0.f : exp2f(s[t] - mn);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) acc[i] = acc[i] * a + b * vv[t][i];
-        l = l * a + b;
+        const float a = l * exp2f(m - mn), b = exp2f(s[t] - mn);
+        l = a + b;
         m = mn;
+        const float inv = 1.f / l;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) acc[i] = acc[i] * (a * inv) + vv[t][i] * (b * inv);
       }
     }
   }
@@ -85,10 +87,11 @@ __device__ __forceinline__ void begin_row(RowState<DH>& s, const T* q, int lane)
 
 template <int DH, typename T>
 __device__ __forceinline__ void end_row(const RowState<DH>& s, T* o, int lane) {
-  const float inv = 1.f / s.l;
+  // scores all minus infinity: 0 / 0
+  const float nan = s.l == 0.f ? __int_as_float(0x7fffffff) : 0.f;
 #pragma unroll
   for (int i = 0; i < RowState<DH>::PER; ++i)
-    o[lane * RowState<DH>::PER + i] = from_f32<T>(s.acc[i] * inv);
+    o[lane * RowState<DH>::PER + i] = from_f32<T>(s.acc[i] + nan);
 }
 
 // one row of the step: its prefix keys from kp on, its own fed tokens from kc on (the first

@@ -100,6 +100,56 @@ def test_forms_of_the_norm_and_frequencies(cuda, a, bf16):
     c.check(a, pos, pos)
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("eps", [0.0, 2.0 ** -136, 2.0 ** -116, 2.0 ** -20])
+def test_heads_whose_squares_leave_float32(cuda, eps, d, bf16):
+    import torch
+    n, Hq, Hkv = 40, 6, 2
+    c = Case(cuda, n, n, Hq, Hkv, d, bf16, spread=False)
+    sizes = [-113, -66, 0, 60, 66, 125] + ([-126] if eps == 0.0 else [])
+    for i, x in enumerate((c.q, c.k)):  # a size for each head, and heads of zeros
+        e = torch.tensor(np.random.default_rng(i).choice(sizes, size=(n, x.shape[1], 1))).cuda()
+        x.copy_(torch.ldexp(x.double(), e).to(x.dtype))
+        x[3, 0] = 0.0
+        x[7] = 0.0
+    pos = np.arange(n) * 11
+    a = dict(rot=64, eps=eps)
+    cuda.jet_norm_rotate(c.dims, _rope(cuda, **a), torch.tensor(pos, dtype=torch.int32).cuda(),
+                         c.q, c.k, c.gq, c.gk, c.qo, c.ko)
+    _sync(cuda)
+    for x, y, g in ((c.q, c.qo, c.gq), (c.k, c.ko, c.gk)):
+        assert (y[3, 0] == 0.0).all() and (y[7] == 0.0).all()  # zeros stay, without eps too
+        some = (x != 0).any(-1).cpu().numpy()
+        one = x.clone()
+        one[~torch.tensor(some)] = 1.0
+        want, bar = B.rotation(_np(one), pos, 64, "halves", W.frequencies(64, 1e4), _np(g), eps,
+                               True, bf16)
+        assert B.worst(_np(y)[some], want[some], bar[some]) <= 1.0
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_infinite_and_nan_elements_stay_in_their_heads(cuda, bf16):
+    import torch
+    n = 5
+    c = Case(cuda, n, n, 4, 2, 64, bf16, spread=False)
+    c.q[1, 2, 3] = float("inf")
+    c.q[2, 0, 9] = float("nan")
+    pos = np.arange(n) * 11
+    cuda.jet_norm_rotate(c.dims, _rope(cuda, 64), torch.tensor(pos, dtype=torch.int32).cuda(),
+                         c.q, c.k, c.gq, c.gk, c.qo, c.ko)
+    _sync(cuda)
+    got = _np(c.qo)
+    pair = [3, 35]  # x / infinity: zeros, and NaN where x is infinite and in its pair
+    assert np.isnan(got[1, 2, pair]).all() and (np.delete(got[1, 2], pair) == 0.0).all()
+    assert np.isnan(got[2, 0]).all()
+    keep = np.ones((n, 4), bool)
+    keep[1, 2] = keep[2, 0] = False
+    want, bar = B.rotation(np.where(keep[..., None], _np(c.q), 1.0), pos, 64, "halves",
+                           W.frequencies(64, 1e4), _np(c.gq), 1e-6, True, bf16)
+    assert B.worst(got[keep], want[keep], bar[keep]) <= 1.0
+
+
 def test_the_farthest_positions(cuda):
     # position 2^31 - 1 (and its negative) at frequencies with few binary digits, so that the
     # angle in 64 bits is exact: f = 2 pi m / 2^20 is not, but f = m / 2^21 times p < 2^31 is

@@ -200,9 +200,32 @@ def test_wide_windows_give_the_plain_attention(cuda, bf16):
     assert float((s.o.double() - plain.double()).abs().max()) <= (0.04 if bf16 else 1e-5)
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("P", [[64], [10, 64, 63, 17]])
+def test_step_first_tokens_that_reach_the_window(cuda, P, bf16):
+    # the first tokens' last box of 16 passes the window's first key, or the prefix's end
+    s = Step(cuda, P, [2] * len(P), [3, 1] * len(P), 8, 2, 64, bf16, seed=10)
+    for window, sinks in ((1, 2), (1, 50), (1, 61), (2, 49), (15, 33), (8, 1), (1, 1)):
+        s.o.fill_(7.0)
+        s.run(window, sinks)
+        s.check(window, sinks)
+
+
 # --------------------------------------------------------------------------
 # the prefill
 # --------------------------------------------------------------------------
+@pytest.mark.parametrize("d,heads", [(64, (8, 2)), (128, (8, 8)), (256, (16, 2))])
+def test_prefill_large_scores(cuda, d, heads):
+    # scores of up to hundreds, and keys that grow along the prefix, so that the maximum does
+    import torch
+    p = Prefill(cuda, [700, 33, 260], *heads, d, seed=5)
+    p.q *= 8.0
+    p.k *= torch.linspace(0.25, 6.0, p.k.shape[0], device="cuda")[:, None, None].bfloat16()
+    for window, sinks in ((40, 3), (300, 0), (1000, 0)):
+        p.run(window, sinks)
+        p.check(window, sinks)
+
+
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("heads", [(8, 2), (7, 1), (3, 3), (24, 4)])
 def test_prefill(cuda, heads, d):
@@ -308,6 +331,141 @@ def test_prefill_unseen_keys_reach_no_row(cuda, d, heads):
             assert B.worst(got[rows[~seen]], want[~seen], bar[~seen]) <= 1.0, (r, bad)
             if bad != BAD[3] and seen.any():
                 assert not np.isfinite(got[rows[seen]]).all()
+
+
+@pytest.mark.parametrize("d,heads", [(64, (8, 2)), (128, (8, 8)), (256, (16, 2))])
+def test_values_near_the_largest_float(cuda, d, heads):
+    # finite outputs whose unnormalised sums are not
+    p = Prefill(cuda, [300, 41], *heads, d, seed=6)
+    s = Step(cuda, [300, 41], [2, 1], [3, 5, 30], *heads, d, True, seed=6)
+    for x in (p.v, s.v, s.vc):
+        x.copy_(x.float().clamp(-3, 3) * 1e38)
+    for window, sinks in ((60, 3), (1000, 0)):
+        for x in (p, s):
+            x.run(window, sinks)
+            x.check(window, sinks)
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_scores_of_minus_infinity(cuda, bf16):
+    """Keys of minus infinity under positive queries weigh nothing; a vector that sees no other
+    is 0 / 0."""
+    window, sinks = 3, 1
+    s = Step(cuda, [100, 90], [2, 1], [1, 6, 8], 4, 2, 64, bf16, seed=11)
+    p = Prefill(cuda, [100, 90], 4, 2, 64, seed=11)
+    p0 = [0, 100]
+    for x in (s, p):
+        x.q.abs_().add_(0.125)
+        x.k[p0[0] + 98, 0] = x.k[p0[1] + 20, 0] = float("-inf")      # one of several
+        x.k[p0[1] + 40:p0[1] + 43] = float("-inf")                   # all but the first token
+        x.run(window, sinks)
+    f = 1 + np.flatnonzero(s.lay["row_req"] == 1)[0]                # request 1's first fed token
+    s.kc[f - 1:f + 3] = float("-inf")
+    s.run(window, sinks)
+
+    def check(o, q, k, v, sees, rows):
+        for h in range(2):  # a key/value head at a time: their unseen keys differ
+            inf = ~np.isfinite(k[:, h, 0])
+            want, bar = B.attention(q[:, 2 * h:2 * h + 2], k[:, h:h + 1], v[:, h:h + 1],
+                                    sees & ~inf, bf16)
+            assert B.worst(o[rows, 2 * h:2 * h + 2], want, bar) <= 1.0
+
+    if bf16:
+        at = np.arange(190)
+        pos, req = np.concatenate([np.arange(100), np.arange(90)]), np.repeat([0, 1], [100, 90])
+        sees = B.in_window(pos, pos, window, sinks) & (req[:, None] == req[None, :])
+        check(_np(p.o), *(_np(x) for x in (p.q, p.k, p.v)), sees, at)
+    lay = s.lay
+    req, cand = lay["row_req"], lay["row_cand"].astype(np.int64)
+    pos = np.array([100, 90])[req] - 1 + np.where(cand >= 0, lay["row_pos"], 0)
+    key_req = np.repeat([0, 1], [100, 90])
+    key_pos = np.concatenate([np.arange(100), np.arange(90)])
+    fed = np.flatnonzero(cand >= 0)
+    sees = np.concatenate([
+        B.in_window(pos, key_pos, window, sinks) & (req[:, None] == key_req[None, :]),
+        B.in_window(pos, pos[fed], window, sinks) & (cand[:, None] == cand[None, fed])], 1)
+    check(_np(s.o), _np(s.q), np.concatenate([_np(s.k), _np(s.kc)]),
+          np.concatenate([_np(s.v), _np(s.vc)]), sees, np.arange(len(req)))
+    # and without the first token
+    s.run(window, 0)
+    got = _np(s.o)
+    sees0 = np.concatenate([
+        B.in_window(pos, key_pos, window, 0) & (req[:, None] == key_req[None, :]),
+        B.in_window(pos, pos[fed], window, 0) & (cand[:, None] == cand[None, fed])], 1)
+    none = ~(sees0 & np.isfinite(np.concatenate([_np(s.k), _np(s.kc)])[:, 1, 0])).any(1)
+    assert none.any() and np.isnan(got[none, 2:]).all() and np.isfinite(got[~none, 2:]).all()
+    if bf16:
+        p.run(window, 0)
+        got = _np(p.o)
+        assert np.isnan(got[142]).all() and np.isfinite(np.delete(got, 142, axis=0)).all()
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("d,heads", [(128, (8, 2)), (256, (16, 2))])
+def test_unseen_keys_reach_no_row_through_chunks(cuda, d, heads, bf16):
+    # a long window in chunks: the oldest key of the shared row, seen by no other, and one
+    # between the first tokens and the end of their box
+    P, window, sinks = 20000, 6000, 20
+    s = Step(cuda, [P], [2], [5, 3], *heads, d, bf16, seed=12)
+    for bad in BAD:
+        for at in (P - window, 25):
+            k, v = s.k[at].clone(), s.v[at].clone()
+            s.v[at] = bad
+            s.k[at] = bad
+            s.run(window, sinks)
+            got = _np(s.o)
+            for r, (rows, want, bar) in B.cascade(
+                    s.lay, *(_np(x) for x in (s.q, s.k, s.v, s.kc, s.vc)), window, sinks,
+                    bf16).items():
+                rest = rows[1:] if at != 25 else rows
+                assert B.worst(got[rest], want[rest], bar[rest]) <= 1.0, (bad, at)
+                if at != 25 and bad != BAD[3]:
+                    assert not np.isfinite(got[0]).any()
+            s.k[at], s.v[at] = k, v
+
+
+def test_offsets_past_32_bits(cuda):
+    """A batch whose tensors have more than 2^31 elements: the rotation, the prefill and the
+    step at its far end."""
+    import torch
+    P, H, d, window, sinks = [68000, 300], 128, 256, 200, 4
+    p = Prefill(cuda, P, H, H, d, seed=7)
+    assert p.q.numel() > 2 ** 31
+    rope = cuda.make_rope(64, theta=1e6, norm=False)
+    S, W0 = sum(P), 200 + 8
+
+    def ends(x, r):  # the first tokens and the last ones of a request
+        lo, hi = (0, P[0]) if r == 0 else (P[0], S)
+        return _np(torch.cat([x[lo:lo + sinks], x[hi - W0:hi]]))
+
+    from oracle import window as W
+    raw = [ends(p.k, r) for r in range(2)]
+    where = [np.concatenate([np.arange(sinks), np.arange(x - W0, x)]) for x in P]
+    cuda.jet_norm_rotate_prefix(p.dev, p.dims, rope, p.q, p.k, None, None, p.q, p.k)
+    p.run(window, sinks)
+    s = Step(cuda, P, [1, 1], [3, 2], H, H, d, True, seed=7)
+    s.k, s.v = p.k, p.v
+    s.run(window, sinks)
+    for r in range(2):
+        want, bar = B.rotation(raw[r], where[r], 64, "halves", W.frequencies(64, 1e6), None, 1e-6,
+                               False, True)
+        k, v = ends(p.k, r), ends(p.v, r)
+        assert B.worst(k, want, bar) <= 1.0
+        at = np.arange(P[r] - 3, P[r])
+        hi = P[0] if r == 0 else S
+        heads = [0, 1, 77, 127]
+        want, bar = B.attention(_np(p.q[hi - 3:hi])[:, heads], k[:, heads], v[:, heads],
+                                B.in_window(at, where[r], window, sinks), True)
+        assert B.worst(_np(p.o[hi - 3:hi])[:, heads], want, bar) <= 1.0
+        n0, n1 = (int(s.lay["row_offset"][r + i]) for i in (0, 1))
+        pos = P[r] - 1 + np.arange(n1 - n0)
+        own = slice(n0 - r, n1 - r - 1)
+        want, bar = B.attention(
+            _np(s.q[n0:n1])[:, heads],
+            np.concatenate([k, _np(s.kc[own])])[:, heads],
+            np.concatenate([v, _np(s.vc[own])])[:, heads],
+            B.in_window(pos, np.concatenate([where[r], pos[1:]]), window, sinks), True)
+        assert B.worst(_np(s.o[n0:n1])[:, heads], want, bar) <= 1.0
 
 
 def test_infinite_and_nan_values_come_out_where_they_are_seen(cuda):

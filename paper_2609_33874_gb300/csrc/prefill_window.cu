@@ -14,14 +14,15 @@
 //                 P_j (bf16) takes the place of half of S_j. The issuing thread's MMAs run
 //                 in order, so a new S overwrites a P after its PV.
 //   warp 2        schedule: which items this pair runs, up to kRing ahead
-//   warps 3..10   softmax: a query vector is a TMEM lane, and two warps share each lane, a half
-//                 of the tile's columns each: they tell each other their half's maximum
+//   warps 3..10   softmax: a query vector is a TMEM lane, and two warps share each lane, 32 of
+//                 every 64 of the tile's columns each: they tell each other their maximum
 //   warps 11..14  output: O / l to memory
 // Items are short under a window (2 to 10 tiles), so what counts is that they overlap: at d
 // 64 and 128 there are two query blocks in shared memory and two O in TMEM, and an item's
 // products begin while the last one's output is read. All barriers an MMA waits for live in
 // the even CTA; the commits reach both.
 #include <algorithm>
+#include <type_traits>
 
 #include "attend_tc.cuh"
 #include "window_rows.cuh"
@@ -138,6 +139,13 @@ __device__ __forceinline__ uint64_t desc_mn_sw64(uint32_t addr) {
   return d;
 }
 
+__device__ __forceinline__ void tmem_st_16cols_u32(uint32_t taddr, const uint32_t (&v)[16]) {
+  float f[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(v[i]);
+  tmem_st_16cols(taddr, f);
+}
+
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   float2 d;
   asm("{\n\t.reg .b64 a, b, c, d;\n\t"
@@ -220,7 +228,7 @@ __device__ __noinline__ void again(const WinPreArgs& a, const WinItem& e, int gi
   position_attend<DH>(a.win, a.q + at, a.k + pre, a.v + pre, step, p, a.o + at, lane);
 }
 
-template <int DH>
+template <int DH, bool SKIP>
 __global__ void __launch_bounds__(kWinThreads, 1)
 prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
                       const __grid_constant__ CUtensorMap tmK,
@@ -640,48 +648,57 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
         }
         tc_fence_after();
         const uint32_t scol = tmem + lane_off + b * kKeys;
+        // this warp's columns: 32 from 32 half on and 32 from 64 + 32 half on. SKIP: the second ones
+        // of a tile whose slots end before them are neither read nor weighed
+        const int t0 = j * kKeys, s0 = t0 + 32 * half;  // the first of the tile and the warp, as slots
+        const bool two = !SKIP || t0 + kHalfKeys < e.slots;
         float v[2][32];
-        tmem_ld_32cols(scol + half * kHalfKeys, v[0]);
-        tmem_ld_32cols(scol + half * kHalfKeys + 32, v[1]);
-        const int s0 = j * kKeys + half * kHalfKeys;  // this warp's first column, as a slot
+        tmem_ld_32cols(scol + 32 * half, v[0]);
+        if (two) tmem_ld_32cols(scol + kHalfKeys + 32 * half, v[1]);
         tmem_wait_ld_of(v[0], v[1]);
         tc_fence_before();
-        if (s0 < lo_max || s0 + kHalfKeys > end_min) {
-          // What this vector sees, and of it what all of the warp's do, and what any does. (The
-          // empty statements keep the branches: without them the compiler makes the selects of
-          // most tiles' 64 columns unconditional, d 64 under 1,708 546 -> 598 us.)
+        // What this vector sees, and of it what all of the warp's do, and what any does. (The
+        // empty statements keep the branches: without them the compiler makes the selects of
+        // most tiles' 64 columns unconditional, d 64 under 1,708 546 -> 598 us.)
+        auto mask = [&](float(&x)[32], int sc) {
           asm volatile("" ::: "memory");
-          uint32_t word[2], all[2], any[2];
+          uint32_t word = bit_span(see.lo - sc, see.end - sc);
+          if (sc < first_max) word |= bit_span(0, see.first - sc);
+          const uint32_t all = __reduce_and_sync(0xffffffffu, word);
+          const uint32_t any = __reduce_or_sync(0xffffffffu, word);
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const int sc = s0 + 32 * c;
-            word[c] = bit_span(see.lo - sc, see.end - sc);
-            if (sc < first_max) word[c] |= bit_span(0, see.first - sc);
-            all[c] = __reduce_and_sync(0xffffffffu, word[c]);
-            any[c] = __reduce_or_sync(0xffffffffu, word[c]);
-          }
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const uint32_t of = 0xffffu << (16 * (c & 1));
-            if ((all[c >> 1] & of) == of) continue;
+          for (int c = 0; c < 32; c += 16) {
+            const uint32_t of = 0xffffu << c;
+            if ((all & of) == of) continue;
             asm volatile("" ::: "memory");
-            if ((any[c >> 1] & of) == 0u) {
+            if ((any & of) == 0u) {
               asm volatile("" ::: "memory");
 #pragma unroll
-              for (int x = 0; x < 16; ++x) v[c >> 1][16 * (c & 1) + x] = -INFINITY;
+              for (int y = c; y < c + 16; ++y) x[y] = -INFINITY;
             } else {
               asm volatile("" ::: "memory");
 #pragma unroll
-              for (int x = 16 * (c & 1); x < 16 * (c & 1) + 16; ++x)
-                if (!(word[c >> 1] >> x & 1u)) v[c >> 1][x] = -INFINITY;
+              for (int y = c; y < c + 16; ++y)
+                if (!(word >> y & 1u)) x[y] = -INFINITY;
             }
           }
+        };
+        if (t0 < lo_max || t0 + kKeys > end_min) {
+          mask(v[0], s0);
+          if (two) mask(v[1], s0 + kHalfKeys);
         }
         float top[8];
+        if (two) {
+          if (SKIP) asm volatile("" ::: "memory");
 #pragma unroll
-        for (int x = 0; x < 8; ++x) top[x] = fmaxf(v[0][x], v[1][x]);
+          for (int x = 0; x < 8; ++x) top[x] = fmaxf(v[0][x], v[1][x]);
 #pragma unroll
-        for (int x = 8; x < 32; ++x) top[x & 7] = max3(top[x & 7], v[0][x], v[1][x]);
+          for (int x = 8; x < 32; ++x) top[x & 7] = max3(top[x & 7], v[0][x], v[1][x]);
+        } else {
+          asm volatile("" ::: "memory");
+#pragma unroll
+          for (int x = 0; x < 8; ++x) top[x] = max3(v[0][x], v[0][x + 8], fmaxf(v[0][x + 16], v[0][x + 24]));
+        }
         const float own = a.scale_log2 * max3(max3(top[0], top[1], top[2]),
                                               max3(top[3], top[4], top[5]), fmaxf(top[6], top[7]));
         // the other half's maximum; that it is there also says that the other warp has read
@@ -726,21 +743,38 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
         // ones would cost two instructions more a pair (d 64, window 128: 187 -> 175 us)
         const float mneg = m_used == -INFINITY ? 0.f : -m_used;
         const float2 sc2 = make_float2(a.scale_log2, a.scale_log2), mn2 = make_float2(mneg, mneg);
-        uint32_t pw[32];
+        // the columns v[FIRST] to v[END - 1]
+        auto weigh = [&](auto first, auto end) {
+          uint32_t pw[2][16];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float2 ps[4];
+          for (int c = first; c < end; ++c) {
+            float2 ps[4];
 #pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            const float2 y = fma2(make_float2(v[c][2 * x], v[c][2 * x + 1]), sc2, mn2);
-            const float2 p = make_float2(ex2(y.x), ex2(y.y));
-            pw[16 * c + x] = pack_bf16(p.x, p.y);
-            ps[x & 3] = x < 4 ? p : add2(ps[x & 3], p);
+            for (int x = 0; x < 16; ++x) {
+              const float2 y = fma2(make_float2(v[c][2 * x], v[c][2 * x + 1]), sc2, mn2);
+              const float2 p = make_float2(ex2(y.x), ex2(y.y));
+              pw[c][x] = pack_bf16(p.x, p.y);
+              ps[x & 3] = x < 4 ? p : add2(ps[x & 3], p);
+            }
+            ps[0] = add2(add2(ps[0], ps[1]), add2(ps[2], ps[3]));
+            l += ps[0].x + ps[0].y;
           }
-          ps[0] = add2(add2(ps[0], ps[1]), add2(ps[2], ps[3]));
-          l += ps[0].x + ps[0].y;
+#pragma unroll
+          for (int c = first; c < end; ++c)
+            tmem_st_16cols_u32(scol + (kHalfKeys * c + 32 * half) / 2, pw[c]);
+        };
+        constexpr std::integral_constant<int, 0> k0;
+        constexpr std::integral_constant<int, 1> k1;
+        constexpr std::integral_constant<int, 2> k2;
+        if constexpr (SKIP) {
+          weigh(k0, k1);
+          if (two) {
+            asm volatile("" ::: "memory");
+            weigh(k1, k2);
+          }
+        } else {
+          weigh(k0, k2);
         }
-        tmem_st_32cols_u32(scol + half * (kHalfKeys / 2), pw);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
@@ -885,7 +919,7 @@ bool encode_v64(CUtensorMap* map, const void* base, int rows, int heads, int box
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int DH>
+template <int DH, bool SKIP>
 cudaError_t launch_pairs(const jet_layout& lay, const jet_dims& d, const Window& win,
                          const void* q, const void* k, const void* v, void* o, int* status,
                          cudaStream_t st) {
@@ -921,7 +955,7 @@ cudaError_t launch_pairs(const jet_layout& lay, const jet_dims& d, const Window&
   a.rb = kBV / g;
   a.scale_log2 = 1.4426950408889634f / sqrtf(float(DH));
   const size_t smem = WinGeo<DH>::kBytes + 1024;
-  auto kern = prefill_window_kernel<DH>;
+  auto kern = prefill_window_kernel<DH, SKIP>;
   cudaError_t e =
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
@@ -933,15 +967,33 @@ cudaError_t launch_pairs(const jet_layout& lay, const jet_dims& d, const Window&
                           tmV, tmK16, tmV16, a);
 }
 
+// Whether the softmax looks for tiles that end in their first half. The branches cost it 8 % of a
+// tile, so it pays where most items are short and end so: the slots of a block in the longest
+// prefix end in the first half of their third tile or before (24,000 positions, d 64, 16/2 heads, 2,
+// 3, 4 and 6 tiles: 52.6, 68.5, 85.1 and 118 us with them, 55.2, 69.8, 84.7 and 114 without; d 128,
+// 32/8 heads: 117, 154, 183 and 247, and 124, 157, 182 and 238). At d 256 the tensor pipe takes
+// longer than the softmax and they never cost more than they give (2 to 8 tiles 1 to 3 %).
+bool skips(const jet_sizes& n, const jet_dims& d, const Window& win) {
+  const int block = 2 * (kBV / (d.Hq / d.Hkv));
+  const int slots = block_slots(win, std::max(0, n.max_prefix - block), n.max_prefix).n;
+  return slots <= 3 * kKeys && (slots - 1) % kKeys < kHalfKeys;
+}
+
 }  // namespace
 
 cudaError_t launch_prefill_window(const jet_layout& lay, const jet_dims& d, int window, int sinks,
                                   const void* q, const void* k, const void* v, void* o,
                                   int* status, cudaStream_t st) {
   const Window win{window, sinks};
-  if (d.d == 64) return launch_pairs<64>(lay, d, win, q, k, v, o, status, st);
-  if (d.d == 128) return launch_pairs<128>(lay, d, win, q, k, v, o, status, st);
-  if (d.d == 256) return launch_pairs<256>(lay, d, win, q, k, v, o, status, st);
+  if (d.Hq / d.Hkv > kBV) return cudaErrorInvalidValue;
+  const bool skip = skips(lay.n, d, win);
+  if (d.d == 64)
+    return skip ? launch_pairs<64, true>(lay, d, win, q, k, v, o, status, st)
+                : launch_pairs<64, false>(lay, d, win, q, k, v, o, status, st);
+  if (d.d == 128)
+    return skip ? launch_pairs<128, true>(lay, d, win, q, k, v, o, status, st)
+                : launch_pairs<128, false>(lay, d, win, q, k, v, o, status, st);
+  if (d.d == 256) return launch_pairs<256, true>(lay, d, win, q, k, v, o, status, st);
   return cudaErrorInvalidValue;
 }
 

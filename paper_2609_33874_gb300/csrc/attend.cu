@@ -105,7 +105,8 @@ attend_prefix_kernel(const int32_t* __restrict__ prefix_offset, const int32_t* _
     if (inside && P > 0) slots = step_slots(wr.win, P);
     keys = slots.n;
   }
-  if (!inside || keys > (long long)chunk * gridDim.x || (long long)nr * g > (long long)kQV * gridDim.y) {
+  if (!inside || keys > (long long)chunk * gridDim.x ||
+      (long long)nr * g > (long long)kQV * gridDim.y) {
     if (threadIdx.x == 0) flag(status, JET_ERR_DEVICE);
     return;
   }
@@ -361,8 +362,8 @@ cudaError_t launch_simt(const jet_layout& lay, const jet_dims& d, const AttnPlan
   return launch_pdl(attend_merge_kernel<DH, WIN>, dim3(unsigned((warps + 3) / 4)), dim3(128), 0, st,
                     lay.row_req, lay.row_cand, lay.cand_row_offset, n.N, n.R, n.C, d.Hq, d.Hkv,
                     plan.splits, static_cast<const float*>(q), static_cast<const float*>(k_cand),
-                    static_cast<const float*>(v_cand), o_part, ml_part, static_cast<float*>(o), status,
-                    wr);
+                    static_cast<const float*>(v_cand), o_part, ml_part, static_cast<float*>(o),
+                    status, wr);
 }
 
 template <int DH>

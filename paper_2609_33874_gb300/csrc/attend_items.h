@@ -32,15 +32,15 @@ struct RequestCut {
   int nq, sp, per;
 };
 
-// The cut of a request of rows [n0, n0 + nr) and prefix [p0, p0 + P), as a device
-// layout gives it, if it lies in the batch and within the plan. The partials'
-// workspace holds `splits` chunks of every row, so a request with more is not
-// worked on at all. (Taken once a request: the divisions are what it costs.)
+// Whether rows [n0, n0 + nr) and prefix [p0, p0 + P), as a device layout gives a request,
+// lie in the batch.
 JET_HD bool request_fits(const ItemPlan& a, int n0, int nr, int p0, int P) {
   if (nr < 1 || nr > a.N || n0 < 0 || n0 > a.N - nr) return false;
   return P >= 1 && P <= a.total_prefix && p0 >= 0 && p0 <= a.total_prefix - P;
 }
-// nr rows and `keys` prefix keys, within the plan or left out
+// The cut of nr rows over `keys` keys of the prefix, if it lies within the plan: the
+// partials' workspace holds `splits` chunks of every row, so a request with more is not
+// worked on at all. (Taken once a request: the divisions are what it costs.)
 JET_HD RequestCut cut_keys(const ItemPlan& a, int nr, int keys) {
   RequestCut c{};
   const int tiles = (keys + kItemTile - 1) / kItemTile;

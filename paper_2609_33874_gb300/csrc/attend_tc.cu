@@ -33,6 +33,13 @@
 // TMEM 128 columns at a time, and the chunks' (m, l) tell the combine all it needs
 // (one 6,000-key request 18.4 -> 17.2 us, 16 of 200 - 1,200 keys 24.5 -> 23.2 us,
 // one of 500 keys 14.3 -> 13.1 us, 32 of 2,048 - 8,192 keys 86.0 -> 85.0 us).
+//
+// Under a window (WIN) a request's keys are slots (window.h): its first tokens and what its
+// shared row sees, so nothing else is read; what a row further on does not see of them is masked.
+// Such items are short, so up to d 128 two CTAs share an SM (Geo). 256 requests of 2,048 - 8,192
+// under 2,048 (2 kv heads of 256) take 190 us, 88 % of the copy rate; one row of each of 64 under
+// 1,024 (8 heads of 128) 51.8, 78 %; 16 requests of 200 - 1,200 under 128 (4 heads of 256) 10.6,
+// latencies in a row as above.
 #include <algorithm>
 #include <cmath>
 
@@ -379,8 +386,8 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
           q_par = v & 1;
         }
         // K_j and V_j are issued as soon as their slots drain, whichever first
-        Slots sl{};
-        if constexpr (WIN) sl = step_slots(a.win, e.P);
+        Slots slots{};
+        if constexpr (WIN) slots = step_slots(a.win, e.P);
         int jk = 0, jv = 0;
         IdleClock clk;
         while (jv < e.ntiles) {
@@ -395,14 +402,14 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
               const bool pre = jk < e.npt;
               if (WIN && pre) {
                 if constexpr (WIN)
-                  load_slots<DH>(ks, &tmK, &w.k16, k_full + s, sl, e.k_begin + jk * kBN, e.p0, e.kh,
-                                 pol);
+                  load_slots<DH>(ks, &tmK, &w.k16, k_full + s, slots, e.k_begin + jk * kBN, e.p0,
+                                 e.kh, pol);
               } else {
-              const CUtensorMap* mk = pre ? &tmK : &tmKc;
-              const int key = pre ? e.p0 + e.k_begin + jk * kBN : e.f_begin + (jk - e.npt) * kBN;
+                const CUtensorMap* mk = pre ? &tmK : &tmKc;
+                const int key = pre ? e.p0 + e.k_begin + jk * kBN : e.f_begin + (jk - e.npt) * kBN;
 #pragma unroll
-              for (int sl = 0; sl < G::kSlices; ++sl)
-                tma_load_3d(ks + sl * (kBN * 128), mk, k_full + s, sl * 64, e.kh, key, pol);
+                for (int sl = 0; sl < G::kSlices; ++sl)
+                  tma_load_3d(ks + sl * (kBN * 128), mk, k_full + s, sl * 64, e.kh, key, pol);
               }
               k_issued |= 1u << s;
               k_par = (k_par & ~(1u << s)) | (ph << s);
@@ -420,14 +427,14 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
               const bool pre = jv < e.npt;
               if (WIN && pre) {
                 if constexpr (WIN)
-                  load_slots<DH>(vs, &tmV, &w.v16, v_full + s, sl, e.k_begin + jv * kBN, e.p0, e.kh,
-                                 pol);
+                  load_slots<DH>(vs, &tmV, &w.v16, v_full + s, slots, e.k_begin + jv * kBN, e.p0,
+                                 e.kh, pol);
               } else {
-              const CUtensorMap* mv = pre ? &tmV : &tmVc;
-              const int key = pre ? e.p0 + e.k_begin + jv * kBN : e.f_begin + (jv - e.npt) * kBN;
+                const CUtensorMap* mv = pre ? &tmV : &tmVc;
+                const int key = pre ? e.p0 + e.k_begin + jv * kBN : e.f_begin + (jv - e.npt) * kBN;
 #pragma unroll
-              for (int sl = 0; sl < G::kSlices; ++sl)
-                tma_load_3d(vs + sl * (kBN * 128), mv, v_full + s, sl * 64, e.kh, key, pol);
+                for (int sl = 0; sl < G::kSlices; ++sl)
+                  tma_load_3d(vs + sl * (kBN * 128), mv, v_full + s, sl * 64, e.kh, key, pol);
               }
               v_issued |= 1u << s;
               v_par = (v_par & ~(1u << s)) | (ph << s);
@@ -644,21 +651,21 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
               if (!(see[x] >> (c & 31) & 1u)) sv[c] = -INFINITY;
           }
         } else {
-        // visible keys of this tile: [klo, khi) of its 64 slots
-        int klo = 0, khi;
-        if (j < e.npt) {
-          khi = min(kBN, e.k_end - (e.k_begin + j * kBN));
-          khi = min(khi, kcap + 1 - (e.k_begin + j * kBN));  // prefill: keys <= own position
-        } else {
-          const int f0 = e.f_begin + (j - e.npt) * kBN;
-          klo = max(0, fa - f0);
-          khi = min(kBN, fb - f0 + 1);
-        }
-        if (__any_sync(0xffffffffu, klo > 0 || khi < kBN)) {
+          // visible keys of this tile: [klo, khi) of its 64 slots
+          int klo = 0, khi;
+          if (j < e.npt) {
+            khi = min(kBN, e.k_end - (e.k_begin + j * kBN));
+            khi = min(khi, kcap + 1 - (e.k_begin + j * kBN));  // prefill: keys <= own position
+          } else {
+            const int f0 = e.f_begin + (j - e.npt) * kBN;
+            klo = max(0, fa - f0);
+            khi = min(kBN, fb - f0 + 1);
+          }
+          if (__any_sync(0xffffffffu, klo > 0 || khi < kBN)) {
 #pragma unroll
-          for (int c = 0; c < kBN; ++c)
-            if (c < klo || c >= khi) sv[c] = -INFINITY;
-        }
+            for (int c = 0; c < kBN; ++c)
+              if (c < klo || c >= khi) sv[c] = -INFINITY;
+          }
         }
         // the row's tile maximum through eight independent chains (one warp per
         // scheduler runs this: a single 64-long chain would be pure latency)
@@ -670,7 +677,8 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         const float mt = a.scale_log2 * fmaxf(fmaxf(fmaxf(mq[0], mq[1]), fmaxf(mq[2], mq[3])),
                                               fmaxf(fmaxf(mq[4], mq[5]), fmaxf(mq[6], mq[7])));
         // P buffer b was last read by the P V of tile Tj - 2 (P over S: before S_j came)
-        if (!PAIRED && Tj >= 2 && !warp_mbar_wait(p_free + b, ((Tj - 2) >> 1) & 1, a.wait_ns, abort_flag)) {
+        if (!PAIRED && Tj >= 2 &&
+            !warp_mbar_wait(p_free + b, ((Tj - 2) >> 1) & 1, a.wait_ns, abort_flag)) {
           ok = false;
           break;
         }
@@ -765,9 +773,10 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         break;
       }
       tc_fence_after();
-      // 128 (64 where two CTAs share the registers) columns of O per TMEM round trip, written as 128-byte pieces
-      // of each vector (64 bf16 or 32 f32 columns) through this warp's 4 KB stage:
-      // eight 16-byte pieces a row, rotated by the row
+      // 128 columns of O per TMEM round trip (all 64, and 64 where two CTAs share the
+      // registers), written as 128-byte pieces of each vector (64 bf16 or 32 f32 columns;
+      // half of that where two CTAs share the memory) through this warp's stage: eight (four)
+      // 16-byte pieces a row, rotated by the row
       constexpr int kCols = DH < 128 || PAIRED ? 64 : 128;
       auto put_piece = [&](const uint4(&x)[PC], char* base, size_t esize, int col) {
 #pragma unroll
@@ -797,8 +806,9 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
 #pragma unroll
             for (int q = 0; q < PC; ++q) {
               const float* y = ov[(k + 8 * q) >> 5] + ((k + 8 * q) & 31);
-              x[q] = make_uint4(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
-                                pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv));
+              x[q] = make_uint4(
+                  pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
+                  pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv));
               if constexpr (WIN) {
                 const uint32_t words[4] = {x[q].x, x[q].y, x[q].z, x[q].w};
 #pragma unroll
@@ -976,7 +986,8 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
   a.n_all = (long long)n.R * d.Hkv * plan.qgroups * plan.splits;
   const int sms = sm_count();
   if (sms < 1) return cudaErrorInvalidValue;
-  const int grid = int(std::max<long long>(1, std::min<long long>((paired(DH, WIN) ? 2 : 1) * sms, a.n_all)));
+  const int held = (paired(DH, WIN) ? 2 : 1) * sms;
+  const int grid = int(std::max<long long>(1, std::min<long long>(held, a.n_all)));
   a.sorted = plan.sorted;
   WinArgs<WIN> w;
   if constexpr (WIN) {
@@ -1003,8 +1014,8 @@ cudaError_t launch_dh(const jet_layout& lay, const jet_dims& d, const AttnPlan& 
                       lay.row_req, blocks <= 8LL * sms);
   else
     return launch_pdl(attend_combine_kernel<DH>, dim3(unsigned(blocks)), dim3(128), 0, st,
-                    lay.row_req, n.N, n.R, d.Hq, plan.splits, blocks <= 8LL * sms, o_part, ml_part,
-                    static_cast<__nv_bfloat16*>(o), status);
+                      lay.row_req, n.N, n.R, d.Hq, plan.splits, blocks <= 8LL * sms, o_part,
+                      ml_part, static_cast<__nv_bfloat16*>(o), status);
 }
 
 // Prefill: causal self-attention over every request's prefix with the same

@@ -648,9 +648,9 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
         }
         tc_fence_after();
         const uint32_t scol = tmem + lane_off + b * kKeys;
-        // this warp's columns: 32 from 32 half on and 32 from 64 + 32 half on. SKIP: the second ones
-        // of a tile whose slots end before them are neither read nor weighed
-        const int t0 = j * kKeys, s0 = t0 + 32 * half;  // the first of the tile and the warp, as slots
+        // this warp's columns: 32 from 32 half on and 32 from 64 + 32 half on. SKIP: the second
+        // ones of a tile whose slots end before them are neither read nor weighed
+        const int t0 = j * kKeys, s0 = t0 + 32 * half;  // the tile's first and the warp's, as slots
         const bool two = !SKIP || t0 + kHalfKeys < e.slots;
         float v[2][32];
         tmem_ld_32cols(scol + 32 * half, v[0]);
@@ -697,7 +697,8 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
         } else {
           asm volatile("" ::: "memory");
 #pragma unroll
-          for (int x = 0; x < 8; ++x) top[x] = max3(v[0][x], v[0][x + 8], fmaxf(v[0][x + 16], v[0][x + 24]));
+          for (int x = 0; x < 8; ++x)
+            top[x] = max3(v[0][x], v[0][x + 8], fmaxf(v[0][x + 16], v[0][x + 24]));
         }
         const float own = a.scale_log2 * max3(max3(top[0], top[1], top[2]),
                                               max3(top[3], top[4], top[5]), fmaxf(top[6], top[7]));
@@ -969,8 +970,8 @@ cudaError_t launch_pairs(const jet_layout& lay, const jet_dims& d, const Window&
 
 // Whether the softmax looks for tiles that end in their first half. The branches cost it 8 % of a
 // tile, so it pays where most items are short and end so: the slots of a block in the longest
-// prefix end in the first half of their third tile or before (24,000 positions, d 64, 16/2 heads, 2,
-// 3, 4 and 6 tiles: 52.6, 68.5, 85.1 and 118 us with them, 55.2, 69.8, 84.7 and 114 without; d 128,
+// prefix end in the first half of their third tile or before (24,000 positions, d 64, 16/2 heads,
+// 2, 3, 4 and 6 tiles: 52.6, 68.5, 85.1 and 118 us with them, 55.2, 69.8, 84.7 and 114 without; d 128,
 // 32/8 heads: 117, 154, 183 and 247, and 124, 157, 182 and 238). At d 256 the tensor pipe takes
 // longer than the softmax and they never cost more than they give (2 to 8 tiles 1 to 3 %).
 bool skips(const jet_sizes& n, const jet_dims& d, const Window& win) {

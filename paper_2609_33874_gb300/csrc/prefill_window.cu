@@ -543,17 +543,10 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
             const uint64_t dv = dv0 + (v.at * G::kVBytes >> 4);
             // the keys past the block's last are not read (16 per instruction)
             const int steps = min(kKeys, kend - jp * kKeys + 15) >> 4;
-            if (steps == kKeys / 16) {
-#pragma unroll
-              for (int x = 0; x < kKeys / 16; ++x)
-                mma_f16_ta_pair(ot, pt + uint32_t(8 * x), dv + (x * 16 * G::kVWide * 2 >> 4), id_o,
-                                (jp | x) != 0);
-            } else {
 #pragma unroll 1
-              for (int x = 0; x < steps; ++x)
-                mma_f16_ta_pair(ot, pt + uint32_t(8 * x), dv + (x * 16 * G::kVWide * 2 >> 4), id_o,
-                                (jp | x) != 0);
-            }
+            for (int x = 0; x < steps; ++x)
+              mma_f16_ta_pair(ot, pt + uint32_t(8 * x), dv + (x * 16 * G::kVWide * 2 >> 4), id_o,
+                              (jp | x) != 0);
             mma_commit_pair(v_empty + v.at, 0x3);
             --ahead;
             v.next();

@@ -32,7 +32,6 @@ namespace {
 
 constexpr int kKeys = 128;          // keys per tile of the pair
 constexpr int kHalfKeys = kKeys / 2;
-constexpr int kRing = 8;            // items the roles may be apart
 constexpr int kSoftWarps = 8, kOutWarps = 4;
 constexpr int kFirstSoft = 3, kFirstOut = kFirstSoft + kSoftWarps;
 constexpr int kWinThreads = 32 * (kFirstOut + kOutWarps);
@@ -56,6 +55,10 @@ struct WinGeo {
   // (d 128, 16,000 positions under 4,096: 727 us with two S and two O, 715 with three S)
   static constexpr int kSBufs = DH == 256 ? 2 : 3;
   static constexpr int kOBufs = DH == 64 ? 2 : 1;
+  // Items the roles may be apart. Their query blocks are on the way into L2, so more of them than
+  // it takes to hide that displace others before their use (d 256: two of 64 KB a CTA; with
+  // eight a third of the queries were read twice, 16 requests under 256 85.5 us instead of 77.3)
+  static constexpr int kRing = DH == 64 ? 4 : 2;
   static constexpr int kSlices = DH / 64;                  // 64-wide d slices of Q and K
   static constexpr int kVCols = DH / 2;                    // this CTA's columns of V
   static constexpr int kVWide = kVCols < 64 ? kVCols : 64;  // of a swizzled row of V
@@ -238,6 +241,7 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
                       const __grid_constant__ WinPreArgs a) {
   using G = WinGeo<DH>;
   constexpr int kStages = G::kStages, kQBufs = G::kQBufs, kSBufs = G::kSBufs, kOBufs = G::kOBufs;
+  constexpr int kRing = G::kRing;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~uintptr_t(1023));

@@ -332,7 +332,9 @@ jet_status jet_prefill_attend(const jet_layout* lay, const jet_dims* dims, const
  * with (a, b) = (y[i], y[i + rot / 2]) (JET_ROPE_HALVES) or (y[2 i], y[2 i + 1])
  * (JET_ROPE_PAIRS); the elements from rot on stay y. All of it is float32, rounded once
  * to the output's type; the angle is exact modulo a turn for every int32 position, up to
- * the 53 binary digits of f_i.
+ * the 53 binary digits of f_i. Heads whose squares leave float32 are normalised all the same, a
+ * head of zeros stays zeros without eps too, and an infinite element gives NaN in its pair and
+ * zeros in the rest of its head.
  */
 enum { JET_ROPE_HALVES = 0, JET_ROPE_PAIRS = 1 };
 
@@ -393,12 +395,14 @@ jet_status jet_norm_rotate_rows(const jet_layout* lay, const jet_dims* dims,
  * stands at P_r - 1 + t, so a row's own candidate tokens leave its window, too, and are
  * first tokens where the prefix is shorter than `sinks`. window >= 1 and sinks >= 0 (else
  * JET_ERR_ARG); every row sees itself, the shared row its prefix's last key. What a row
- * does not see does not reach it, infinities and NaN among it.
+ * does not see does not reach it, infinities and NaN among it; scores that are all minus
+ * infinity give NaN. bf16: the weights are rounded to bf16 before their product with the
+ * values, scores, maxima and sums are float32.
  *
  * jet_prefix_attend_window - the step (arguments, types and head sizes of
  * jet_prefix_attend; bf16: at most 128 query heads a key/value head, else
  * JET_ERR_UNSUPPORTED). The whole prefix is given; only the keys that some row sees are
- * read: the first `sinks` and the last `window` of each request.
+ * read, the first `sinks` (and up to 15 beside them) and the last `window` of each request.
  * ws/ws_bytes: scratch of at least jet_attend_window_workspace_bytes().
  */
 size_t jet_attend_window_workspace_bytes(const jet_sizes* n, const jet_dims* dims,
@@ -738,9 +742,10 @@ size_t jet_stack_window_workspace_bytes(const jet_sizes* n, const jet_dims* dims
  * jet_stack_forward_window - jet_stack_forward, in whose full layers the projected queries and
  * keys are normalised and rotated at their rows' positions (rope; NULL: neither) and attend
  * under the layer's window (attn, a host array of stack.L entries read during the call; NULL:
- * no windows and no gains; linear layers' entries are not read). The prefix keys in k_pre are
- * taken as they are: normalised and rotated already. Between the operations the rows are bf16,
- * so the projection's queries and keys are rounded before the norm, and after the rotation.
+ * no windows and no gains; a linear layer's window counts for the workspace alone). The prefix
+ * keys in k_pre are taken as they are: normalised and rotated already. Between the operations
+ * the rows are bf16, so the projection's queries and keys are rounded before the norm, and after
+ * the rotation.
  * Errors besides: as for jet_norm_rotate_rows and jet_prefix_attend_window, window or sinks
  * below 0 JET_ERR_ARG.
  */

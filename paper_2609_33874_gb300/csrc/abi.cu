@@ -845,12 +845,12 @@ jet_status stack_forward(const jet_layout* lay, const jet_dims* dims, const jet_
   // validate every layer before the first launch
   for (int l = 0; l < stack->L; ++l) {
     const jet_stack_layer& Ly = stack->layers[l];
+    if (attn && (attn[l].window < 0 || attn[l].sinks < 0)) return JET_ERR_ARG;
     if (Ly.kind == JET_LAYER_FULL) {
       JET_TRY(check_attn_dims(dims));
       if ((long long)n.R * dims->Hkv > 65535) return JET_ERR_CAPACITY;
       if (rope) JET_TRY(check_rope(dims, rope));
       if (attn) {
-        if (attn[l].window < 0 || attn[l].sinks < 0) return JET_ERR_ARG;
         if (attn[l].window > 0 && dims->Hq / dims->Hkv > jet::attn_tc_block())
           return JET_ERR_UNSUPPORTED;
         if (!aligned16(attn[l].gq) || !aligned16(attn[l].gk)) return JET_ERR_ALIGN;

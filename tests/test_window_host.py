@@ -230,6 +230,31 @@ def test_window_refusals(jet):
         assert f(hl.sizes, dims, 2 ** 31 - 1, 2 ** 31 - 1) > 0
 
 
+def test_stack_refusals_hold_for_every_layer(jet):
+    hl, _ = _batch(jet)
+    dims = jet.make_dims(jet.DTYPE_BF16, Hq=8, Hkv=2, d=64, D=64, Hl=2, dk=128, dv=64)
+    names = ("g1", "g2", "w_mix", "w_o", "w_gu", "w_d", "s_prefix", "k_pre", "v_pre")
+    layers = [dict(kind=kind, **{n: A for n in names})
+              for kind in (jet.LAYER_LINEAR, jet.LAYER_FULL)]
+    stack, keep = jet.make_stack(layers, 128)
+    good = [dict(window=9, sinks=1)] * 2
+    n = jet.jet_stack_window_workspace_bytes(hl.sizes, dims, 128, 2, jet.make_stack_attn(good))
+    assert n > 0
+
+    def call(attn, nb=1 << 40):
+        jet.jet_stack_forward_window(hl, dims, stack, None, jet.make_stack_attn(attn), A, A, A,
+                                     ws_bytes=nb, stream=0)
+
+    assert _status(jet, call, good, nb=n - 1) == "JET_ERR_WORKSPACE"
+    for l in range(2):  # a linear layer's entry too
+        for bad in (dict(window=-1), dict(window=9, sinks=-1)):
+            attn = [bad if i == l else good[i] for i in range(2)]
+            assert _status(jet, call, attn) == "JET_ERR_ARG"
+            assert jet.jet_stack_window_workspace_bytes(hl.sizes, dims, 128, 2,
+                                                        jet.make_stack_attn(attn)) == 0
+    assert keep is not None
+
+
 TILES = r"""
 #include <cstdio>
 #include "window.h"

@@ -14,9 +14,10 @@
 // rounded to float32 for sincospif: off by less than 2^-25 radians at any position.
 //
 // Everything is float32 from the load to the one rounding of the store. 74,210 tokens of 24 + 4
-// heads of 256 (1.06 GB each way in bf16) take 381 us, 83 % of the copy rate: the norm's and
-// rotation's instructions share the cycles with the loads; 64 rows take 4 to 5 us, a launch and
-// two latencies in a row.
+// heads of 256 (1.06 GB each way in bf16) take 350 us, 91 % of the copy rate. A warp's loads are
+// one step ahead of its arithmetic, too few bytes in flight for HBM, so a token's queries are asked
+// for at its start (386 -> 361; d 128, 92,227 tokens of 32 + 8 heads 326 -> 287), and the outputs
+// leave L2 first (361 -> 352, 280). 64 rows take 4 to 5 us, a launch and two latencies in a row.
 #include <algorithm>
 
 #include "jet_device.cuh"
@@ -27,6 +28,8 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
+// bytes of a token's queries that are asked for ahead: 44 MB for all of the chip's warps
+constexpr int kAhead = 8192;
 
 enum { kGiven = 0, kPrefix = 1, kRows = 2 };  // where the positions come from
 
@@ -122,12 +125,12 @@ struct Raw4<float> {
 template <typename T>
 __device__ __forceinline__ void store4(T* p, const float (&v)[4]) {
   if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
   } else {
     uint2 x;
     *reinterpret_cast<__nv_bfloat162*>(&x.x) = __floats2bfloat162_rn(v[0], v[1]);
     *reinterpret_cast<__nv_bfloat162*>(&x.y) = __floats2bfloat162_rn(v[2], v[3]);
-    *reinterpret_cast<uint2*>(p) = x;
+    __stcs(reinterpret_cast<uint2*>(p), x);
   }
 }
 
@@ -182,7 +185,7 @@ __device__ __forceinline__ void normalise(float (&v)[2][4], const float (&g)[2][
 // 8 elements a lane in two groups of four, v[0] and v[1]. Halves: the groups are half a
 // rotation apart in the lanes that rotate, and in a row past them. Pairs: in a row.
 template <int DH, int STYLE, int FROM, typename T>
-__global__ void __launch_bounds__(kThreads, 10)
+__global__ void __launch_bounds__(kThreads, 9)
 norm_rotate_kernel(const RotArgs a, const __grid_constant__ jet_rope rope) {
   pdl_begin();
   constexpr int kLanes = DH / 8;        // lanes of a head
@@ -215,6 +218,13 @@ norm_rotate_kernel(const RotArgs a, const __grid_constant__ jet_rope rope) {
   };
   if (part < nq && part * kHeads + hs < a.Hq)
     fetch(static_cast<const T*>(a.q) + size_t(n) * a.Hq * DH, (part * kHeads + hs) * DH);
+  // and of a token that is one warp's, what comes after them starts on its way into L2
+  if (a.q && a.parts == 1) {
+    const char* row = static_cast<const char*>(a.q) + size_t(n) * a.Hq * DH * sizeof(T);
+    const int bytes = min(kAhead, a.Hq * DH * int(sizeof(T)));
+    for (int at = lane * 128; at < bytes; at += 32 * 128)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(row + at));
+  }
   int pos = 0, fed = -1;
   const bool ok = token_at<FROM>(a, n, lane, &pos, &fed);
   if (!ok) {

@@ -37,7 +37,7 @@
 // Under a window (WIN) a request's keys are slots (window.h): its first tokens and what its
 // shared row sees, so nothing else is read; what a row further on does not see of them is masked.
 // Such items are short, so up to d 128 two CTAs share an SM (Geo). 256 requests of 2,048 - 8,192
-// under 2,048 (2 kv heads of 256) take 190 us, 88 % of the copy rate; one row of each of 64 under
+// under 2,048 (2 kv heads of 256) take 191 us, 88 % of the copy rate; one row of each of 64 under
 // 1,024 (8 heads of 128) 51.8, 78 %; 16 requests of 200 - 1,200 under 128 (4 heads of 256) 10.6,
 // latencies in a row as above.
 #include <algorithm>

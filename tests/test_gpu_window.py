@@ -531,6 +531,51 @@ def test_captured_and_replayed(cuda, bf16):
     s.check(70, 4)
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+def test_two_graphs_share_a_workspace(cuda, bf16):
+    # long contexts in chunks, whose partials lie there, under two windows
+    import torch
+    s = Step(cuda, [9000, 40], [2, 1], [3, 4, 2], 8, 2, 128, bf16, seed=13)
+    forms = [(4000, 3), (8000, 0)]
+    ws = max((s.ws(*f) for f in forms), key=lambda x: x.numel())
+    graphs = []
+    for window, sinks in forms:
+        s.run(window, sinks, ws=ws)
+        g, o = torch.cuda.CUDAGraph(), torch.empty_like(s.o)
+        with torch.cuda.graph(g):
+            cuda.jet_prefix_attend_window(s.dev, s.dims, window, sinks, s.q, s.k, s.v, s.kc, s.vc,
+                                          o, ws)
+        graphs.append((g, o))
+    for order in ((0, 1), (1, 0), (1, 1)):
+        ws.fill_(float("nan"))
+        for i in order:
+            graphs[i][1].fill_(7.0)
+        for i in order:
+            graphs[i][0].replay()
+        torch.cuda.synchronize()
+        for i in order:
+            s.check(*forms[i], o=graphs[i][1])
+
+
+def test_two_calls_at_once(cuda):
+    # each with its own workspace, on its own stream
+    import torch
+    s = Step(cuda, [6000] * 6, [2] * 6, [3, 4] * 6, 16, 2, 256, True, seed=14)
+    p = Prefill(cuda, [3000, 500], 16, 2, 256, seed=14)
+    ws, wp = s.ws(2000, 4), p.ws(300, 4)
+    side = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        cuda.jet_prefix_attend_window(s.dev, s.dims, 2000, 4, s.q, s.k, s.v, s.kc, s.vc, s.o, ws,
+                                      stream=side[0])
+        cuda.jet_prefill_attend_window(p.dev, p.dims, 300, 4, p.q, p.k, p.v, p.o, wp,
+                                       stream=side[1])
+    torch.cuda.synchronize()
+    assert cuda.jet_device_status() == 0
+    s.check(2000, 4)
+    p.check(300, 4, rows_of=_some(p.P, np.random.default_rng(0), 40))
+
+
 def test_prefill_captured_and_on_another_stream(cuda):
     import torch
     p = Prefill(cuda, [300, 20, 77], 8, 2, 64)

@@ -448,9 +448,9 @@ def jet_norm_rotate(dims: jet_dims, rope: jet_rope, pos, q, k, gq, gk, q_out, k_
     positions pos [n], an int32 device tensor (see include/jet.h)."""
     if pos.dim() != 1 or pos.element_size() != 4 or pos.is_floating_point():
         raise ValueError("pos must be a vector of int32")
-    n = int(pos.shape[0])
+    n = pos.shape[0]
     for x in (q, k, q_out, k_out):
-        if x is not None and not isinstance(x, int) and int(x.shape[0]) != n:
+        if x is not None and x.__class__ is not int and x.shape[0] != n:
             raise ValueError("pos, q, k and the outputs must have as many tokens")
     _check(_lib.jet_norm_rotate(ctypes.byref(dims), ctypes.byref(rope), n, _addr(pos), _addr(q),
                                 _addr(k), _addr(gq), _addr(gk), _addr(q_out), _addr(k_out),

@@ -11,15 +11,6 @@ namespace jet {
 namespace {
 
 template <int PER>
-__device__ __forceinline__ void load_row(const float* p, float (&v)[PER]) {
-#pragma unroll
-  for (int i = 0; i < PER; i += 2) {
-    const float2 x = *reinterpret_cast<const float2*>(p + i);
-    v[i] = x.x;
-    v[i + 1] = x.y;
-  }
-}
-template <int PER>
 __device__ __forceinline__ void load_row(const __nv_bfloat16* p, float (&v)[PER]) {
 #pragma unroll
   for (int i = 0; i < PER; i += 2) {
@@ -37,9 +28,8 @@ struct RowState {
   float q[PER], acc[PER], m, l;
 
   // keys [begin, end) of k and v, rows `step` elements apart
-  template <typename T>
-  __device__ __forceinline__ void add(const T* k, const T* v, size_t step, int begin, int end,
-                                      int lane) {
+  __device__ __forceinline__ void add(const __nv_bfloat16* k, const __nv_bfloat16* v, size_t step,
+                                      int begin, int end, int lane) {
     constexpr int kAtOnce = 4;
     for (int j0 = begin; j0 < end; j0 += kAtOnce) {
       float kv[kAtOnce][PER], vv[kAtOnce][PER], s[kAtOnce];
@@ -72,8 +62,8 @@ struct RowState {
   }
 };
 
-template <int DH, typename T>
-__device__ __forceinline__ void begin_row(RowState<DH>& s, const T* q, int lane) {
+template <int DH>
+__device__ __forceinline__ void begin_row(RowState<DH>& s, const __nv_bfloat16* q, int lane) {
   const float scale = 1.4426950408889634f * rsqrtf(float(DH));  // base-2 scores
   load_row<RowState<DH>::PER>(q + lane * RowState<DH>::PER, s.q);
 #pragma unroll
@@ -85,21 +75,22 @@ __device__ __forceinline__ void begin_row(RowState<DH>& s, const T* q, int lane)
   s.l = 0.f;
 }
 
-template <int DH, typename T>
-__device__ __forceinline__ void end_row(const RowState<DH>& s, T* o, int lane) {
+template <int DH>
+__device__ __forceinline__ void end_row(const RowState<DH>& s, __nv_bfloat16* o, int lane) {
   // scores all minus infinity: 0 / 0
   const float nan = s.l == 0.f ? __int_as_float(0x7fffffff) : 0.f;
 #pragma unroll
   for (int i = 0; i < RowState<DH>::PER; ++i)
-    o[lane * RowState<DH>::PER + i] = from_f32<T>(s.acc[i] + nan);
+    o[lane * RowState<DH>::PER + i] = __float2bfloat16_rn(s.acc[i] + nan);
 }
 
 // one row of the step: its prefix keys from kp on, its own fed tokens from kc on (the first
 // of them y_1), t of them
-template <int DH, typename T>
-__device__ __forceinline__ void row_attend(const Window& w, const T* q, const T* kp, const T* vp,
-                                           const T* kc, const T* vc, size_t step, int P, int t,
-                                           T* o, int lane) {
+template <int DH>
+__device__ __forceinline__ void row_attend(const Window& w, const __nv_bfloat16* q,
+                                           const __nv_bfloat16* kp, const __nv_bfloat16* vp,
+                                           const __nv_bfloat16* kc, const __nv_bfloat16* vc,
+                                           size_t step, int P, int t, __nv_bfloat16* o, int lane) {
   const RowSeen see = row_seen(w, P, t);
   RowState<DH> s;
   begin_row(s, q, lane);
@@ -109,19 +100,20 @@ __device__ __forceinline__ void row_attend(const Window& w, const T* q, const T*
     s.add(kc, vc, step, 0, min(see.own_first, t), lane);
     s.add(kc, vc, step, see.own_lo - 1, t, lane);
   }
-  end_row<DH, T>(s, o, lane);
+  end_row(s, o, lane);
 }
 
 // one position of the prefill
-template <int DH, typename T>
-__device__ __forceinline__ void position_attend(const Window& w, const T* q, const T* kp,
-                                                const T* vp, size_t step, int p, T* o, int lane) {
+template <int DH>
+__device__ __forceinline__ void position_attend(const Window& w, const __nv_bfloat16* q,
+                                                const __nv_bfloat16* kp, const __nv_bfloat16* vp,
+                                                size_t step, int p, __nv_bfloat16* o, int lane) {
   const Seen see = seen_at(w, p);
   RowState<DH> s;
   begin_row(s, q, lane);
   s.add(kp, vp, step, 0, int(see.first), lane);
   s.add(kp, vp, step, int(see.lo), p + 1, lane);
-  end_row<DH, T>(s, o, lane);
+  end_row(s, o, lane);
 }
 
 }  // namespace

@@ -705,7 +705,9 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
         // its scores, over which this one's weights may go
         maxima[(mb * 2 + half) * kBV + i] = own;
         named_bar_sync(1 + q4, 64);
-        if (*abort_flag) {  // the other warp may not come again
+        // the other warp may not come again; one outcome for the whole warp, as the flag may be
+        // raised between its lanes' looks
+        if (__any_sync(0xffffffffu, *abort_flag)) {
           ok = false;
           break;
         }

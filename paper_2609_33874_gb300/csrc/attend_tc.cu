@@ -897,11 +897,17 @@ combine_window_kernel(const AttArgs a, const WinArgs<true> w, const int32_t* __r
   bool odd = !(l > 0.f);  // 0 / 0, a NaN or an infinity
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const float y = acc[i] * inv;
-    odd |= !isfinite(y);
-    a.o[(size_t(n) * a.Hq + h) * DH + lane + 32 * i] = __float2bfloat16_rn(y);
+    acc[i] *= inv;
+    odd |= !isfinite(acc[i]);
   }
-  if (!__any_sync(0xffffffffu, odd)) return;
+  // (of an output that is computed again nothing is stored here: other lanes would store the
+  // same addresses there, and nothing orders the two)
+  if (!__any_sync(0xffffffffu, odd)) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      a.o[(size_t(n) * a.Hq + h) * DH + lane + 32 * i] = __float2bfloat16_rn(acc[i]);
+    return;
+  }
   ItemGeo e{};
   e.n0 = a.row_offset[r];
   e.kh = h / a.g;

@@ -69,7 +69,7 @@ struct Geo {
   static constexpr int kPieces = PAIRED ? 4 : 8;
   static constexpr uint32_t kOffStage = kQBytes + kStages * 2 * kKVBytes;
   static constexpr uint32_t kOffBar = kOffStage + 4 * 32 * kPieces * 16;
-  static constexpr uint32_t kBytes = kOffBar + 512;
+  static constexpr uint32_t kBytes = kOffBar + 640;  // the ring, barriers, words, OddItems
   // TMEM: the two S buffers, O, then the two P buffers (bf16 pairs, 32 columns)
   static constexpr uint32_t kUsedCols = 2 * kBN + DH + (PAIRED ? 0 : 2 * (kBN / 2));
   static constexpr uint32_t kTmemCols = kUsedCols <= 256 ? 256 : 512;
@@ -185,6 +185,21 @@ __device__ __forceinline__ void load_slots(uint8_t* dst, const CUtensorMap* map,
   }
 }
 
+// of row n of request r: its own fed tokens, in number, from the *f-th on
+__device__ __forceinline__ int own_tokens(const AttArgs& a, int r, int n, int* f) {
+  const int c = a.row_cand[n];
+  *f = 0;
+  if (c < 0 || c >= a.C) return 0;  // a shared row
+  *f = a.cand_row_offset[c] - r - 1;
+  return n - r - 1 - *f + 1;
+}
+
+// the CTA's u-th item of the static deal: back and forth (0 .. n-1, n-1 .. 0, ...)
+__device__ __forceinline__ int dealt(int u) {
+  const int n = int(gridDim.x);
+  return u * n + ((u & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
+}
+
 // query vector gv of an item's request, key by key; t of its own fed tokens from the f-th on
 template <int DH>
 __device__ __noinline__ void again(const AttArgs& a, const WinArgs<true>& w, const ItemGeo& e,
@@ -196,6 +211,27 @@ __device__ __noinline__ void again(const AttArgs& a, const WinArgs<true>& w, con
   const size_t own = t > 0 ? size_t(f) * step + size_t(e.kh) * DH : 0;
   row_attend<DH>(a.win, a.q + at, w.k + pre, w.v + pre, w.kc + own, w.vc + own, step, e.P, t,
                  a.o + at, lane);
+}
+
+// The outputs of this CTA's noted items that came out NaN or infinite, a warp each.
+template <int DH>
+__device__ __noinline__ void odd_outputs(const AttArgs& a, const WinArgs<true>& w,
+                                         const OddItems& odd, int warp, int lane) {
+  ItemWindow window{};
+  for (int u = 0;; ++u) {
+    const int k = dealt(u);
+    int4 it;
+    ItemGeo e;
+    if (k >= a.n_all || !nth_item<true>(a, k, lane, window, &it, &e) || !e.ok) break;
+    if (e.splits_r != 1 || !odd.has(u)) continue;
+    for (int gv = e.vbase + warp; gv < e.vbase + e.nv; gv += kThreads / 32) {
+      const int n = e.n0 + gv / a.g;
+      if (!stored_odd<DH>(a.o + (size_t(n) * a.Hq + e.kh * a.g + gv % a.g) * DH, lane)) continue;
+      int f;
+      const int t = own_tokens(a, e.r, n, &f);
+      again<DH>(a, w, e, gv, max(0, t), f, lane);
+    }
+  }
 }
 
 // One persistent CTA per SM. The scheduler warp claims the work items one
@@ -238,6 +274,7 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
   uint64_t* drain = qz_done + 1;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  OddItems& odd_items = *reinterpret_cast<OddItems*>(tmem_slot + 2);  // (WIN)
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = a.g, rb = a.rb;
@@ -264,6 +301,7 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
     *abort_flag = 0;
     fence_barrier_init();
   }
+  if (WIN && warp == 1) odd_items.bits[lane] = 0;
   if (warp == 0 && lane == 0) {
     tma_prefetch_desc(&tmQ);
     tma_prefetch_desc(&tmK);
@@ -321,13 +359,12 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
           }
         }
       } else {
-        // dealt out back and forth (0 .. n-1, n-1 .. 0, ...): the items come by
+        // dealt out back and forth: the items come by
         // decreasing prefix length, so a CTA with a short item gets a long one.
         // A shared counter needs a launch to reset it: 64 requests of 100 - 2,000
         // keys 53.5 -> 47.9 us, 16 of 200 - 1,200 26.5 -> 24.2 us (together with
         // the softmax below masking only the tiles that need it).
-        const int n = int(gridDim.x);
-        const int k = u * n + ((u & 1) ? n - 1 - int(blockIdx.x) : int(blockIdx.x));
+        const int k = dealt(u);
         int4 cand;
         ItemGeo ce;
         if (k < a.n_all && nth_item<WIN>(a, k, lane, window, &cand, &ce)) {
@@ -766,7 +803,9 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
           for (int sp = e.splits_r; sp < a.splits; ++sp)
             a.ml_part[at + sp * step] = make_float2(-INFINITY, 0.f);
       }
-      const float inv = l > 0.f ? 1.f / l : 0.f;
+      // (under a window scores all minus infinity, or a NaN among them: NaN until it is computed
+      // again)
+      const float inv = l > 0.f ? 1.f / l : WIN ? __int_as_float(0x7fffffff) : 0.f;
       const int Tl = T + e.ntiles - 1;
       if (!warp_mbar_wait(p_free + (Tl & 1), (Tl >> 1) & 1, a.wait_ns, abort_flag)) {
         ok = false;
@@ -841,18 +880,12 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
         mbar_arrive(item_empty + slot);
       }
       if constexpr (WIN) {
-        // vectors with a NaN or an infinity: again from what they see alone (a weight above 1
-        // may have taken a large value past the largest float), and those whose scores are all
-        // minus infinity, 0 / 0
+        // vectors with a NaN or an infinity (a weight above 1 may have taken a large value past
+        // the largest float) are computed again from what they see alone, after the last item;
+        // those of chunks by the combine
         const bool odd = !(l > 0.f) || __hisnan(most.x) || __hisnan(most.y) ||
                          __hisinf(most.x) || __hisinf(most.y);
-        for (unsigned left = __ballot_sync(0xffffffffu, direct && valid && odd); left;
-             left &= left - 1) {
-          const int src = __ffs(left) - 1, gv = e.vbase + q4 * 32 + src;
-          const int t = __shfl_sync(0xffffffffu, max(0, fb - fa + 1), src);
-          const int f = __shfl_sync(0xffffffffu, fa, src);
-          again<DH>(a, w, e, gv, t, f, lane);
-        }
+        if (__any_sync(0xffffffffu, direct && valid && odd) && lane == 0) odd_items.note(u);
       }
       T += e.ntiles;
     }
@@ -867,6 +900,9 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem, G::kTmemCols);
+  }
+  if constexpr (WIN) {
+    if (odd_items.any(lane) && !*abort_flag) odd_outputs<DH>(a, w, odd_items, warp, lane);
   }
 }
 
@@ -913,12 +949,8 @@ combine_window_kernel(const AttArgs a, const WinArgs<true> w, const int32_t* __r
   e.kh = h / a.g;
   e.p0 = a.prefix_offset[r];
   e.P = a.prefix_offset[r + 1] - e.p0;
-  const int c = a.row_cand[n];
-  int t = 0, f = 0;
-  if (c >= 0 && c < a.C) {
-    f = a.cand_row_offset[c] - r - 1;
-    t = n - r - 1 - f + 1;
-  }
+  int f;
+  const int t = own_tokens(a, r, n, &f);
   // a request that was left out has no chunks to combine
   if (!request_fits(a, e.n0, 1, e.p0, e.P) || n < e.n0 || t < 0) return;
   again<DH>(a, w, e, (n - e.n0) * a.g + h % a.g, t, f, lane);

@@ -72,6 +72,7 @@ struct WinGeo {
   static constexpr uint32_t kOffL = kOffStage + kOutWarps * 4096;  // l of two items, halves
   static constexpr uint32_t kOffMax = kOffL + 2 * 2 * kBV * 4;     // maxima, two tiles, halves
   static constexpr uint32_t kOffBar = kOffMax + 2 * 2 * kBV * 4;
+  static constexpr uint32_t kOffOdd = kOffBar + 1024 - sizeof(OddItems);
   static constexpr uint32_t kBytes = kOffBar + 1024;
   // TMEM: the S tiles, then O
   static constexpr uint32_t kOCol = kSBufs * kKeys;
@@ -222,6 +223,77 @@ __device__ __forceinline__ RowBounds row_bounds(const Window& w, const WinItem& 
   return RowBounds{s.first, s.lo - e.off, min(e.slots, p + 1 - e.off)};
 }
 
+// A pair's items, one after the other. Requests by decreasing length, a request's blocks from
+// the last to the first, kv heads fastest, so that the pairs at work share one request's K and V
+// in L2; the pairs deal them out back and forth (0 .. n-1, n-1 .. 0, ...), without a work list or
+// a counter. Both CTAs derive the same items.
+struct WinSchedule {
+  long long before;  // items of the requests before this window of 32
+  int base, round;   // the window's first request in the order; the deal's
+  int cnt, inc, r, P, first, total;
+  bool held;         // the window's block counts are there
+};
+
+// One warp; ntiles 0: no more items.
+__device__ __forceinline__ WinItem next_item(const WinPreArgs& a, WinSchedule& s, int pair,
+                                             int npairs, int rank, int lane) {
+  const int g = a.g, rb = a.rb;
+  const long long k =
+      (long long)s.round * npairs + ((s.round & 1) ? npairs - 1 - pair : pair);
+  ++s.round;
+  WinItem it{};
+  for (; s.base < a.R; s.base += 32) {
+    if (!s.held) {
+      const int ri = s.base + lane;
+      s.cnt = s.r = s.P = s.first = 0;
+      if (ri < a.R) {
+        s.r = a.req_order[ri];
+        if (s.r >= 0 && s.r < a.R) {
+          s.first = a.prefix_offset[s.r];
+          const int end = a.prefix_offset[s.r + 1];
+          if (span_inside(s.first, end, a.total) && end > s.first) {
+            s.P = end - s.first;
+          } else {
+            flag(a.status, JET_ERR_DEVICE);
+          }
+        } else {
+          flag(a.status, JET_ERR_DEVICE);
+        }
+        s.cnt = a.Hkv * ((s.P + 2 * rb - 1) / (2 * rb));
+      }
+      s.inc = s.cnt;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, s.inc, o);
+        if (lane >= o) s.inc += y;
+      }
+      s.total = __shfl_sync(0xffffffffu, s.inc, 31);
+      s.held = true;
+    }
+    if (k < s.before + s.total) {
+      const unsigned hit = __ballot_sync(0xffffffffu, k < s.before + s.inc);
+      const int src = __ffs(hit) - 1;
+      const int kk = int(k - s.before) - __shfl_sync(0xffffffffu, s.inc - s.cnt, src);
+      const int PP = __shfl_sync(0xffffffffu, s.P, src);
+      const int nq = __shfl_sync(0xffffffffu, s.cnt, src) / a.Hkv;
+      const int qb = nq - 1 - kk / a.Hkv;
+      const Slots sl = block_slots(a.win, 2 * qb * rb, min(PP, (qb + 1) * 2 * rb));
+      it.p0 = __shfl_sync(0xffffffffu, s.first, src);
+      it.kh = kk % a.Hkv;
+      it.row0 = (2 * qb + rank) * rb;
+      it.nv = min(rb, max(0, PP - it.row0)) * g;
+      it.slots = sl.n;
+      it.pad = sl.pad;
+      it.off = sl.off;
+      it.ntiles = (sl.n + kKeys - 1) / kKeys;
+      break;
+    }
+    s.before += s.total;
+    s.held = false;
+  }
+  return it;
+}
+
 // a position's query vector, key by key
 template <int DH>
 __device__ __noinline__ void again(const WinPreArgs& a, const WinItem& e, int gi, int lane) {
@@ -229,6 +301,23 @@ __device__ __noinline__ void again(const WinPreArgs& a, const WinItem& e, int gi
   const size_t at = (size_t(e.p0 + p) * a.Hq + e.kh * a.g + gi % a.g) * DH;
   const size_t step = size_t(a.Hkv) * DH, pre = size_t(e.p0) * step + size_t(e.kh) * DH;
   position_attend<DH>(a.win, a.q + at, a.k + pre, a.v + pre, step, p, a.o + at, lane);
+}
+
+// The outputs of this CTA's noted items that came out NaN or infinite, a warp each.
+template <int DH>
+__device__ __noinline__ void odd_outputs(const WinPreArgs& a, const OddItems& odd, int rank,
+                                         int warp, int lane) {
+  WinSchedule order{};
+  for (int u = 0;; ++u) {
+    const WinItem e =
+        next_item(a, order, int(blockIdx.x >> 1), int(gridDim.x >> 1), rank, lane);
+    if (e.ntiles == 0) break;
+    if (!odd.has(u)) continue;
+    const __nv_bfloat16* out = a.o + (size_t(e.p0 + e.row0) * a.Hq + size_t(e.kh) * a.g) * DH;
+    for (int gi = warp; gi < e.nv; gi += kWinThreads / 32)
+      if (stored_odd<DH>(out + size_t(gi / a.g * a.Hq + gi % a.g) * DH, lane))
+        again<DH>(a, e, gi, lane);
+  }
 }
 
 template <int DH, bool SKIP>
@@ -265,6 +354,8 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
   uint64_t* drain = l_free + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  // (by its offset at each use: an address held all along cost d 128 and 64 up to 3 %)
+  auto odd_items = [&] { return reinterpret_cast<OddItems*>(smem + G::kOffOdd); };
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
@@ -302,6 +393,7 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
     *abort_flag = 0;
     fence_barrier_init();
   }
+  if (warp == 1) odd_items()->bits[lane] = 0;
   if (warp == 0 && lane == 0) {
     tma_prefetch_desc(&tmQ);
     tma_prefetch_desc(&tmK);
@@ -332,66 +424,9 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
 
   if (warp == 2) {
     // ---------------------------------------------------------------- schedule
-    // Items in the order: requests by decreasing length, a request's blocks from the last
-    // to the first, kv heads fastest, so that the pairs at work share one request's K and V
-    // in L2. The pairs deal them out back and forth (0 .. n-1, n-1 .. 0, ...), without a work
-    // list or a counter. Both CTAs derive the same items.
-    long long before = 0;  // items of the requests before this window of 32
-    int base = 0, total = -1, cnt = 0, inc = 0, r = 0, P = 0, first = 0;
-    for (int u = 0, round = 0;; ++round) {
-      const long long k =
-          (long long)round * npairs + ((round & 1) ? npairs - 1 - pair : pair);
-      WinItem it{};
-      for (;;) {
-        if (total < 0) {  // the window's block counts
-          const int ri = base + lane;
-          cnt = r = P = first = 0;
-          if (ri < a.R) {
-            r = a.req_order[ri];
-            if (r >= 0 && r < a.R) {
-              first = a.prefix_offset[r];
-              const int end = a.prefix_offset[r + 1];
-              if (span_inside(first, end, a.total) && end > first) {
-                P = end - first;
-              } else {
-                flag(a.status, JET_ERR_DEVICE);
-              }
-            } else {
-              flag(a.status, JET_ERR_DEVICE);
-            }
-            cnt = a.Hkv * ((P + 2 * rb - 1) / (2 * rb));
-          }
-          inc = cnt;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += y;
-          }
-          total = __shfl_sync(0xffffffffu, inc, 31);
-        }
-        if (k < before + total) {
-          const unsigned hit = __ballot_sync(0xffffffffu, k < before + inc);
-          const int src = __ffs(hit) - 1;
-          const int kk = int(k - before) - __shfl_sync(0xffffffffu, inc - cnt, src);
-          const int PP = __shfl_sync(0xffffffffu, P, src);
-          const int nq = __shfl_sync(0xffffffffu, cnt, src) / a.Hkv;
-          const int qb = nq - 1 - kk / a.Hkv;
-          const Slots sl = block_slots(a.win, 2 * qb * rb, min(PP, (qb + 1) * 2 * rb));
-          it.p0 = __shfl_sync(0xffffffffu, first, src);
-          it.kh = kk % a.Hkv;
-          it.row0 = (2 * qb + int(rank)) * rb;
-          it.nv = min(rb, max(0, PP - it.row0)) * g;
-          it.slots = sl.n;
-          it.pad = sl.pad;
-          it.off = sl.off;
-          it.ntiles = (sl.n + kKeys - 1) / kKeys;
-          break;
-        }
-        before += total;
-        base += 32;
-        if (base >= a.R) break;  // no more items
-        total = -1;
-      }
+    WinSchedule order{};
+    for (int u = 0;; ++u) {
+      const WinItem it = next_item(a, order, pair, npairs, int(rank), lane);
       const int slot = u % kRing;
       bool okw = true;
       if (lane == 0)
@@ -412,7 +447,6 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
             tma_prefetch_3d(&tmQ, sl * 64, it.kh * g, it.p0 + it.row0);
         }
       }
-      ++u;
       if (it.ntiles == 0) break;
     }
   } else if (warp == 0) {
@@ -838,7 +872,8 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
       }
       tc_fence_after();
       const float l = lsum[ls * 2 * kBV + i] + lsum[(ls * 2 + 1) * kBV + i];
-      const float inv = l > 0.f ? 1.f / l : 0.f;
+      // scores all minus infinity, or a NaN among them: NaN until it is computed again
+      const float inv = l > 0.f ? 1.f / l : __int_as_float(0x7fffffff);
       __syncwarp();
       if (lane == 0) mbar_arrive(l_free + ls);
       // up to 128 columns of O into registers as bf16 at a time; the next item's PV waits
@@ -883,13 +918,11 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
           __syncwarp();
         }
       }
-      // vectors with a NaN or an infinity: again, from what they see alone (a weight above 1 may
-      // have taken a large value past the largest float), and those whose scores are all minus
-      // infinity, 0 / 0
+      // vectors with a NaN or an infinity (a weight above 1 may have taken a large value past the
+      // largest float) are computed again from what they see alone, after the last item
       const bool odd = !(l > 0.f) || __hisnan(most.x) || __hisnan(most.y) || __hisinf(most.x) ||
                        __hisinf(most.y);
-      for (unsigned left = __ballot_sync(0xffffffffu, i < e.nv && odd); left; left &= left - 1)
-        again<DH>(a, e, q4 * 32 + __ffs(left) - 1, lane);
+      if (__any_sync(0xffffffffu, i < e.nv && odd) && lane == 0) odd_items()->note(u);
     }
     if (!ok) {
       *abort_flag = 1;
@@ -906,6 +939,8 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
     tc_fence_after();
     tmem_dealloc_pair(tmem, G::kTmemCols);
   }
+  if (odd_items()->any(lane) && !*abort_flag)
+    odd_outputs<DH>(a, *odd_items(), int(rank), warp, lane);
 }
 
 // packed [keys, Hkv, DH] bf16: box of 32 d x 1 head x box_rows keys, 64-byte swizzle

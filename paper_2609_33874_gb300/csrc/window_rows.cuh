@@ -1,7 +1,9 @@
 // Attention of one query vector under a window by one warp, key by key in float32: what the
 // tensor-core kernels fall back on for a vector whose output came out NaN or infinite. Their
 // products take whole tiles, and a weight of zero times an infinite or NaN value that the vector
-// does not see is NaN; here nothing but what it sees is read.
+// does not see is NaN; here nothing but what it sees is read. A key takes a warp some 0.15 us, so
+// this comes after a CTA's last item, when no role waits for another: they note the items with
+// such an output, and all of the CTA's warps look those over.
 #pragma once
 
 #include "jet_device.cuh"
@@ -26,12 +28,13 @@ template <int DH>
 struct RowState {
   static constexpr int PER = DH / 32;
   float q[PER], acc[PER], m, l;
+  bool over;  // every element is NaN, whatever comes
 
   // keys [begin, end) of k and v, rows `step` elements apart
   __device__ __forceinline__ void add(const __nv_bfloat16* k, const __nv_bfloat16* v, size_t step,
                                       int begin, int end, int lane) {
     constexpr int kAtOnce = 4;
-    for (int j0 = begin; j0 < end; j0 += kAtOnce) {
+    for (int j0 = begin; j0 < end && !over; j0 += kAtOnce) {
       float kv[kAtOnce][PER], vv[kAtOnce][PER], s[kAtOnce];
 #pragma unroll
       for (int t = 0; t < kAtOnce; ++t) {
@@ -58,6 +61,10 @@ struct RowState {
 #pragma unroll
         for (int i = 0; i < PER; ++i) acc[i] = acc[i] * (a * inv) + vv[t][i] * (b * inv);
       }
+      bool nan = true;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) nan &= isnan(acc[i]);
+      over = __all_sync(0xffffffffu, nan);
     }
   }
 };
@@ -73,6 +80,7 @@ __device__ __forceinline__ void begin_row(RowState<DH>& s, const __nv_bfloat16* 
   }
   s.m = -INFINITY;
   s.l = 0.f;
+  s.over = false;
 }
 
 template <int DH>
@@ -114,6 +122,35 @@ __device__ __forceinline__ void position_attend(const Window& w, const __nv_bflo
   s.add(kp, vp, step, 0, int(see.first), lane);
   s.add(kp, vp, step, int(see.lo), p + 1, lane);
   end_row(s, o, lane);
+}
+
+// Which of a CTA's items have an output to compute again: a bit an item, those of kOddItems apart
+// together.
+constexpr int kOddItems = 1024;
+struct OddItems {
+  uint32_t bits[kOddItems / 32];
+  __device__ __forceinline__ void note(int u) {
+    atomicOr(bits + (u % kOddItems) / 32, 1u << (u % 32));
+  }
+  __device__ __forceinline__ bool has(int u) const {
+    return bits[(u % kOddItems) / 32] >> (u % 32) & 1u;
+  }
+  __device__ __forceinline__ bool any(int lane) const {
+    return __any_sync(0xffffffffu, bits[lane] != 0);
+  }
+};
+static_assert(kOddItems == 32 * 32, "a word a lane");
+
+// Whether a vector's stored output, whole, has a NaN or an infinity.
+template <int DH>
+__device__ __forceinline__ bool stored_odd(const __nv_bfloat16* o, int lane) {
+  bool odd = false;
+#pragma unroll
+  for (int i = 0; i < DH / 32; i += 2) {
+    const uint32_t x = *reinterpret_cast<const uint32_t*>(o + lane * (DH / 32) + i);
+    odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+  }
+  return __any_sync(0xffffffffu, odd);
 }
 
 }  // namespace

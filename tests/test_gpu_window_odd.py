@@ -1,9 +1,12 @@
 """Attention under a window where outputs come out NaN or infinite and are computed again from what
 their rows see alone: in the step's chunks, beside keys that a row does not see, and under windows
-long enough for the second computation to take its time."""
+long enough for the second computation to take longer than any wait may."""
+import numpy as np
 import pytest
 
-from test_gpu_window import Step, _np
+import window_bars as B
+from test_gpu_timeout import JET_OK
+from test_gpu_window import Prefill, Step, _np, _some
 
 pytestmark = pytest.mark.gpu
 
@@ -33,3 +36,93 @@ def test_outputs_of_chunks_are_stored_once(cuda, d, heads):
         s.o.fill_(7.0)
         s.run(window, sinks, ws=ws)
         assert torch.equal(s.o, first)
+
+
+def _within(cuda, budget_ns, call):
+    old = cuda.jet_set_wait_budget_ns(budget_ns)
+    try:
+        call()
+        return cuda.jet_device_status()
+    finally:
+        cuda.jet_set_wait_budget_ns(old)
+
+
+def _check_with_nan(got, rows, want, bar, sees, col, heads):
+    """NaN in column `col` of `heads` where a row sees the key that has it; all else at the bars."""
+    nan = np.zeros(want.shape, bool)
+    nan[np.ix_(sees, heads, [col])] = True
+    assert np.isnan(got[rows][nan]).all()
+    assert B.worst(np.where(nan, 0.0, got[rows]), np.where(nan, 0.0, want), bar) <= 1.0
+
+
+@pytest.mark.parametrize("d,heads", [(64, (8, 2)), (128, (8, 2)), (256, (8, 1))])
+def test_prefill_of_a_long_window_whose_every_row_sees_a_nan(cuda, d, heads):
+    # a first token with one NaN, under a budget far below what 32 vectors take key by key
+    P, window, sinks = [6000, 40], 5000, 1
+    p = Prefill(cuda, P, *heads, d, seed=22)
+    ws = p.ws(window, sinks)
+    p.run(window, sinks, ws=ws)
+    p.v[0, 0, 3] = float("nan")
+    p.o.fill_(7.0)
+    assert _within(cuda, 5_000_000, lambda: cuda.jet_prefill_attend_window(
+        p.dev, p.dims, window, sinks, p.q, p.k, p.v, p.o, ws)) == JET_OK
+    got = _np(p.o)
+    some = _some(P, np.random.default_rng(1), 60)
+    for r, (rows, want, bar) in B.prefill(P, *(_np(x) for x in (p.q, p.k, p.v)), window, sinks,
+                                          rows_of=some).items():
+        sees = np.full(len(rows), r == 0)
+        _check_with_nan(got, rows, want, bar, sees, 3, np.arange(heads[0] // heads[1]))
+    assert np.isnan(got[:6000, :heads[0] // heads[1], 3]).all()
+    assert np.isfinite(np.delete(got, 3, axis=-1)).all()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_step_of_long_windows_whose_every_row_sees_a_nan(cuda, d):
+    R, P, window, sinks, Hq, Hkv = 160, 5200, 5000, 2, 32, 2
+    s = Step(cuda, [P] * R, [1] * R, [2] * R, Hq, Hkv, d, True, seed=23)
+    ws = s.ws(window, sinks)
+    s.run(window, sinks, ws=ws)
+    s.v.view(R, P, Hkv, d)[:, 1, 1, 5] = float("nan")
+    s.o.fill_(7.0)
+    assert _within(cuda, 5_000_000, lambda: cuda.jet_prefix_attend_window(
+        s.dev, s.dims, window, sinks, s.q, s.k, s.v, s.kc, s.vc, s.o, ws)) == JET_OK
+    got = _np(s.o)
+    at = [0, 1, 77, R - 1]
+    lay, few = s.lay, [int(x) for x in s.lay["prefix_offset"]]
+    k, v = (np.zeros((R * P, Hkv, d)) for _ in range(2))
+    for r in at:
+        for x, y in ((k, s.k), (v, s.v)):
+            x[few[r]:few[r + 1]] = _np(y[few[r]:few[r + 1]])
+    for r, (rows, want, bar) in B.cascade(lay, _np(s.q), k, v, _np(s.kc), _np(s.vc), window, sinks,
+                                          True, at).items():
+        _check_with_nan(got, rows, want, bar, np.ones(len(rows), bool), 5, np.arange(16, 32))
+    assert np.isnan(got[:, 16:, 5]).all() and np.isfinite(np.delete(got, 5, axis=-1)).all()
+
+
+def test_few_odd_outputs_among_many_items(cuda):
+    """More items a CTA than one, some with rows that see a NaN, some with rows beside it."""
+    rng = np.random.default_rng(24)
+    window, sinks = 30, 2
+    P = [int(x) for x in rng.integers(1, 300, size=400)]
+    p = Prefill(cuda, P, 8, 2, 64, seed=24)
+    s = Step(cuda, P, [2] * 400, [1 + int(x) for x in rng.integers(0, 5, size=800)], 8, 2, 64, True,
+             seed=24)
+    off = np.concatenate([[0], np.cumsum(P)])
+    hit = {int(r): int(rng.integers(0, P[r])) for r in rng.choice(400, size=40, replace=False)}
+    for r, j in hit.items():
+        p.v[off[r] + j, 0, 3] = s.v[off[r] + j, 0, 3] = float("nan")
+    p.run(window, sinks)
+    got = _np(p.o)
+    for r, (rows, want, bar) in B.prefill(P, *(_np(x) for x in (p.q, p.k, p.v)), window,
+                                          sinks).items():
+        sees = (B.in_window(rows - off[r], [hit[r]], window, sinks)[:, 0] if r in hit else
+                np.zeros(len(rows), bool))
+        _check_with_nan(got, rows, want, bar, sees, 3, np.arange(4))
+    s.run(window, sinks)
+    got, lay = _np(s.o), s.lay
+    for r, (rows, want, bar) in B.cascade(lay, *(_np(x) for x in (s.q, s.k, s.v, s.kc, s.vc)),
+                                          window, sinks, True).items():
+        pos = P[r] - 1 + np.where(lay["row_cand"][rows] >= 0, lay["row_pos"][rows], 0)
+        sees = (B.in_window(pos, [hit[r]], window, sinks)[:, 0] if r in hit else
+                np.zeros(len(rows), bool))
+        _check_with_nan(got, rows, want, bar, sees, 3, np.arange(4))

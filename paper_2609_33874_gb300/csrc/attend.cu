@@ -19,6 +19,7 @@
 #include "jet_device.cuh"
 #include "jet_internal.h"
 #include "kv_cache.h"
+#include "window_rows.cuh"
 
 namespace jet {
 namespace {
@@ -40,6 +41,8 @@ struct WinRows<true> {
   const int32_t* row_cand;
   const int32_t* cand_row_offset;
   int C;
+  const float *k, *v;  // the prefixes', for outputs that are computed again (window_rows.cuh)
+  int total;
   // t of the token fed at row n (0: a shared row)
   __device__ __forceinline__ int fed(int n) const {
     const int c = row_cand[n];
@@ -334,6 +337,25 @@ attend_merge_kernel(const int32_t* __restrict__ row_req, const int32_t* __restri
   }
   // (a windowed row whose scores are all minus infinity: 0 / 0)
   const float inv = WIN || l > 0.f ? 1.f / l : 0.f;
+  if constexpr (WIN) {
+    // Sums of weighted values past the largest float, where their mean need not be: again, the
+    // mean itself (a NaN sum of weights is a NaN score: the answer)
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) odd |= !isfinite(acc[i] * inv);
+    if (!isnan(l) && __any_sync(0xffffffffu, odd) && r >= 0 && r < R) {
+      const int p0 = wr.prefix_offset[r], p1 = wr.prefix_offset[r + 1];
+      const int t = wr.fed(n), f = n - r - t;  // its own fed tokens, from the f-th on
+      if (span_inside(p0, p1, wr.total) && p1 > p0 && (t == 0 || (f >= 0 && n - r - 1 < N - R))) {
+        const size_t step = size_t(Hkv) * DH, pre = size_t(p0) * step + size_t(kh) * DH;
+        const size_t own = t > 0 ? size_t(f) * step + size_t(kh) * DH : 0;
+        const size_t at = (size_t(n) * Hq + h) * DH;
+        row_attend<DH>(wr.win, q + at, wr.k + pre, wr.v + pre, k_cand + own, v_cand + own, step,
+                       p1 - p0, t, o + at, lane);
+        return;
+      }
+    }
+  }
 #pragma unroll
   for (int i = 0; i < PER; ++i) o[(size_t(n) * Hq + h) * DH + lane + 32 * i] = acc[i] * inv;
 }
@@ -548,7 +570,9 @@ cudaError_t launch_attend_window(const jet_layout& lay, const jet_dims& d, int w
                                    status, st);
   const AttnPlan plan = attn_plan_simt(window_sizes(lay.n, window, sinks), d);
   const WinRows<true> wr{Window{window, sinks}, lay.prefix_offset, lay.row_cand,
-                         lay.cand_row_offset, lay.n.C};
+                         lay.cand_row_offset, lay.n.C,
+                         static_cast<const float*>(k_pre), static_cast<const float*>(v_pre),
+                         lay.n.total_prefix};
 #define JET_WIN(DH)                                                                             \
   return launch_simt<DH, float, true>(lay, d, plan, q, k_pre, v_pre, 0, k_cand, v_cand, o, ws, \
                                       status, st, wr)

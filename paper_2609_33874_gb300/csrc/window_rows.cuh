@@ -1,9 +1,10 @@
 // Attention of one query vector under a window by one warp, key by key in float32: what the
-// tensor-core kernels fall back on for a vector whose output came out NaN or infinite. Their
+// kernels fall back on for a vector whose output came out NaN or infinite. The float32 step's sums
+// of weighted values may pass the largest float where their mean does not. The tensor-core kernels'
 // products take whole tiles, and a weight of zero times an infinite or NaN value that the vector
 // does not see is NaN; here nothing but what it sees is read. A key takes a warp some 0.15 us, so
-// this comes after a CTA's last item, when no role waits for another: they note the items with
-// such an output, and all of the CTA's warps look those over.
+// in them this comes after a CTA's last item, when no role waits for another: they note the items
+// with such an output, and all of the CTA's warps look those over.
 #pragma once
 
 #include "jet_device.cuh"
@@ -12,6 +13,15 @@
 namespace jet {
 namespace {
 
+template <int PER>
+__device__ __forceinline__ void load_row(const float* p, float (&v)[PER]) {
+#pragma unroll
+  for (int i = 0; i < PER; i += 2) {
+    const float2 x = *reinterpret_cast<const float2*>(p + i);
+    v[i] = x.x;
+    v[i + 1] = x.y;
+  }
+}
 template <int PER>
 __device__ __forceinline__ void load_row(const __nv_bfloat16* p, float (&v)[PER]) {
 #pragma unroll
@@ -31,8 +41,9 @@ struct RowState {
   bool over;  // every element is NaN, whatever comes
 
   // keys [begin, end) of k and v, rows `step` elements apart
-  __device__ __forceinline__ void add(const __nv_bfloat16* k, const __nv_bfloat16* v, size_t step,
-                                      int begin, int end, int lane) {
+  template <typename T>
+  __device__ __forceinline__ void add(const T* k, const T* v, size_t step, int begin, int end,
+                                      int lane) {
     constexpr int kAtOnce = 4;
     for (int j0 = begin; j0 < end && !over; j0 += kAtOnce) {
       float kv[kAtOnce][PER], vv[kAtOnce][PER], s[kAtOnce];
@@ -69,8 +80,8 @@ struct RowState {
   }
 };
 
-template <int DH>
-__device__ __forceinline__ void begin_row(RowState<DH>& s, const __nv_bfloat16* q, int lane) {
+template <int DH, typename T>
+__device__ __forceinline__ void begin_row(RowState<DH>& s, const T* q, int lane) {
   const float scale = 1.4426950408889634f * rsqrtf(float(DH));  // base-2 scores
   load_row<RowState<DH>::PER>(q + lane * RowState<DH>::PER, s.q);
 #pragma unroll
@@ -83,22 +94,21 @@ __device__ __forceinline__ void begin_row(RowState<DH>& s, const __nv_bfloat16* 
   s.over = false;
 }
 
-template <int DH>
-__device__ __forceinline__ void end_row(const RowState<DH>& s, __nv_bfloat16* o, int lane) {
+template <int DH, typename T>
+__device__ __forceinline__ void end_row(const RowState<DH>& s, T* o, int lane) {
   // scores all minus infinity: 0 / 0
   const float nan = s.l == 0.f ? __int_as_float(0x7fffffff) : 0.f;
 #pragma unroll
   for (int i = 0; i < RowState<DH>::PER; ++i)
-    o[lane * RowState<DH>::PER + i] = __float2bfloat16_rn(s.acc[i] + nan);
+    o[lane * RowState<DH>::PER + i] = T(s.acc[i] + nan);
 }
 
 // one row of the step: its prefix keys from kp on, its own fed tokens from kc on (the first
 // of them y_1), t of them
-template <int DH>
-__device__ __forceinline__ void row_attend(const Window& w, const __nv_bfloat16* q,
-                                           const __nv_bfloat16* kp, const __nv_bfloat16* vp,
-                                           const __nv_bfloat16* kc, const __nv_bfloat16* vc,
-                                           size_t step, int P, int t, __nv_bfloat16* o, int lane) {
+template <int DH, typename T>
+__device__ __forceinline__ void row_attend(const Window& w, const T* q, const T* kp, const T* vp,
+                                           const T* kc, const T* vc, size_t step, int P, int t,
+                                           T* o, int lane) {
   const RowSeen see = row_seen(w, P, t);
   RowState<DH> s;
   begin_row(s, q, lane);

@@ -126,3 +126,45 @@ def test_few_odd_outputs_among_many_items(cuda):
         sees = (B.in_window(pos, [hit[r]], window, sinks)[:, 0] if r in hit else
                 np.zeros(len(rows), bool))
         _check_with_nan(got, rows, want, bar, sees, 3, np.arange(4))
+
+
+@pytest.mark.parametrize("d,heads", [(64, (8, 2)), (128, (8, 8)), (256, (16, 2))])
+def test_float32_values_near_the_largest_float(cuda, d, heads):
+    """Means whose sums pass the largest float: in a prefix, across chunks, among own tokens, with
+    signs that would cancel as infinities. The second computation keeps a mean, a key's step of
+    which rounds up to six times where the sums' rounds once: 5 n 2^-24 A beside the bars."""
+    P = [300, 41, 9000]
+    s = Step(cuda, P, [2, 1, 1], [3, 5, 30, 70], *heads, d, False, seed=25)
+    for x in (s.v, s.vc):
+        x.copy_(x.clamp(-3, 3) * 1e38)
+    s.v[300:341] = 5e37                       # ten of them leave float32
+    clean = s.v.clone()
+    for window, sinks in ((60, 3), (8000, 0), (1000, 40)):
+        s.v.copy_(clean)
+        s.run(window, sinks)
+        got = _np(s.o)
+        assert np.isfinite(got).all()
+        for r, (rows, want, bar) in B.cascade(s.lay, *(_np(x) for x in (
+                s.q, s.k, s.v, s.kc, s.vc)), window, sinks, False).items():
+            n = min(P[r] + 70, window + 70 + sinks)
+            bar = bar + 5 * n * 2.0 ** -24 * 3e38
+            assert B.worst(got[rows], want, bar) <= 1.0, (r, window, sinks)
+            if r == 1:
+                row = rows[0]                 # the shared row sees equal values only
+                assert np.abs(got[row] / 5e37 - 1).max() <= (6 * n + 40) * 2.0 ** -24
+        # a NaN that a row does not see stays away, and one that it sees comes out
+        s.v[100] = float("nan")
+        s.run(window, sinks)
+        got = _np(s.o)
+        sees = window >= 200
+        assert np.isnan(got[0]).all() if sees else np.isfinite(got[0]).all()
+
+
+def test_float32_outputs_of_ordinary_rows_are_their_sums(cuda):
+    """Rows beside one whose sums overflow keep their bits."""
+    s = Step(cuda, [100, 100], [1, 1], [2, 2], 4, 2, 64, False, seed=26)
+    s.run(50, 2)
+    first = _np(s.o)
+    s.v[100:] = 3e38
+    s.run(50, 2)
+    assert (_np(s.o)[:2] == first[:2]).all() and np.isfinite(_np(s.o)).all()

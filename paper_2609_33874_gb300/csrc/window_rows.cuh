@@ -63,7 +63,11 @@ struct RowState {
 #pragma unroll
       for (int t = 0; t < kAtOnce; ++t) {
         if (j0 + t >= end) break;
-        if (s[t] == -INFINITY) continue;  // weight 0
+        if (s[t] == -INFINITY) {  // weight 0, and 0 times an infinity or a NaN is NaN
+#pragma unroll
+          for (int i = 0; i < PER; ++i) acc[i] = fmaf(vv[t][i], 0.f, acc[i]);
+          continue;
+        }
         const float mn = fmaxf(m, s[t]);
         const float a = l * exp2f(m - mn), b = exp2f(s[t] - mn);
         l = a + b;

@@ -168,3 +168,30 @@ def test_float32_outputs_of_ordinary_rows_are_their_sums(cuda):
     s.v[100:] = 3e38
     s.run(50, 2)
     assert (_np(s.o)[:2] == first[:2]).all() and np.isfinite(_np(s.o)).all()
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_a_seen_key_of_weight_zero_shows_its_values(cuda, bad, bf16):
+    """A score of minus infinity weighs 0, and 0 times a NaN or an infinity is NaN: in a row that
+    sees the key, in that column, whether the row is computed once or twice."""
+    P, window, sinks = 90, 40, 2
+    s = Step(cuda, [P], [1], [6], 4, 2, 64, bf16, seed=27)
+    s.q.abs_().add_(0.125)
+    s.k[70, 1] = s.kc[2, 1] = float("-inf")
+    s.v[70, 1, 7] = s.vc[2, 1, 9] = bad
+    s.run(window, sinks)
+    got = _np(s.o)
+    assert np.isnan(got[:, 2:, 7]).all()                       # every row sees key 70
+    assert np.isnan(got[3:, 2:, 9]).all() and np.isfinite(got[:3, 2:, 9]).all()
+    assert np.isfinite(np.delete(got, [7, 9], axis=-1)).all()
+    if not bf16:
+        return
+    p = Prefill(cuda, [P], 4, 2, 64, seed=27)
+    p.q.abs_().add_(0.125)
+    p.k[70, 1], p.v[70, 1, 7] = float("-inf"), bad
+    p.run(window, sinks)
+    got = _np(p.o)
+    assert np.isnan(got[70:, 2:, 7]).all()
+    got[70:, 2:, 7] = 0.0
+    assert np.isfinite(got).all()

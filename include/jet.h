@@ -732,9 +732,9 @@ jet_status jet_stack_forward(const jet_layout* lay, const jet_dims* dims, const 
  */
 typedef struct jet_stack_attn {
   int32_t window;      /* tokens a token sees, itself among them; 0: all of them        */
-  int32_t sinks;       /* first tokens that stay visible under the window               */
-  const void* gq;      /* [d] bf16 gains of the query heads; NULL: ones                  */
-  const void* gk;      /* [d] bf16 gains of the key heads; NULL: ones                    */
+  int32_t sinks;       /* first tokens that stay visible under the window; 0 without one */
+  const void* gq;      /* [d] bf16 gains of the query heads; NULL: ones, as without rope */
+  const void* gk;      /* [d] bf16 gains of the key heads; NULL: ones, as without rope   */
 } jet_stack_attn;
 
 /* Workspace bytes of jet_stack_forward_window: L layers, attn a host array of L (NULL: as
@@ -750,8 +750,8 @@ size_t jet_stack_window_workspace_bytes(const jet_sizes* n, const jet_dims* dims
  * keys in k_pre are taken as they are: normalised and rotated already. Between the operations
  * the rows are bf16, so the projection's queries and keys are rounded before the norm, and after
  * the rotation.
- * Errors besides: as for jet_norm_rotate_rows and jet_prefix_attend_window, window or sinks
- * below 0 JET_ERR_ARG.
+ * Errors besides: as for jet_norm_rotate_rows and jet_prefix_attend_window; window or sinks
+ * below 0, sinks without a window and gains without a rope (any layer's) JET_ERR_ARG.
  */
 jet_status jet_stack_forward_window(const jet_layout* lay, const jet_dims* dims,
                                     const jet_stack* stack, const jet_rope* rope,

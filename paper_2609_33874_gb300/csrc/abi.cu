@@ -753,6 +753,12 @@ struct StackPlan {
   bool full_ok, lin_ok;
 };
 
+// a layer's window and first tokens: none of the latter without the former
+jet_status check_stack_window(const jet_stack_attn& a) {
+  if (a.window < 0 || a.sinks < 0 || (a.window == 0 && a.sinks > 0)) return JET_ERR_ARG;
+  return JET_OK;
+}
+
 // attn: the windows of L layers, for their attention's workspace (null: none)
 StackPlan stack_plan(const jet_sizes& n, const jet_dims& d, int Dff, int L,
                      const jet_stack_attn* attn) {
@@ -823,7 +829,7 @@ extern "C" size_t jet_stack_window_workspace_bytes(const jet_sizes* n, const jet
   if (!n || !d || n->R < 0 || n->N < n->R || d->D < 16 || Dff < 64 || Dff % 64 != 0) return 0;
   if (L < 0) return 0;
   for (int l = 0; attn && l < L; ++l)
-    if (attn[l].window < 0 || attn[l].sinks < 0) return 0;
+    if (check_stack_window(attn[l]) != JET_OK) return 0;
   return stack_plan(*n, *d, Dff, L, attn).bytes;
 }
 
@@ -845,7 +851,10 @@ jet_status stack_forward(const jet_layout* lay, const jet_dims* dims, const jet_
   // validate every layer before the first launch
   for (int l = 0; l < stack->L; ++l) {
     const jet_stack_layer& Ly = stack->layers[l];
-    if (attn && (attn[l].window < 0 || attn[l].sinks < 0)) return JET_ERR_ARG;
+    if (attn) {
+      JET_TRY(check_stack_window(attn[l]));
+      if (!rope && (attn[l].gq || attn[l].gk)) return JET_ERR_ARG;  // gains of no norm
+    }
     if (Ly.kind == JET_LAYER_FULL) {
       JET_TRY(check_attn_dims(dims));
       if ((long long)n.R * dims->Hkv > 65535) return JET_ERR_CAPACITY;

@@ -414,7 +414,8 @@ class DecoderStack:
     tensors g1, g2, w_mix, w_o, w_gu, w_d and k_pre/v_pre (full) or s_prefix
     (linear), already on the device. ``rope`` (from :func:`jet.make_rope`) normalises and
     rotates the full layers' queries and keys, with the layers' gains gq and gk (optional, [d]);
-    a full layer with a ``window`` (and ``sinks``) attends under it (jet_stack_forward_window)."""
+    a full layer with a ``window`` (and ``sinks``) attends under it (jet_stack_forward_window).
+    Gains without a rope, and sinks without a window, raise ValueError."""
 
     def __init__(self, layout: "jet.HostLayout", dims: "jet.jet_dims", layers, Dff: int,
                  rule: str = "delta", device="cuda", rope: Optional["jet.jet_rope"] = None):
@@ -427,6 +428,11 @@ class DecoderStack:
         n = layout.sizes
         self.N = n.N
         self.rope, self.attn = rope, None
+        for L in layers:
+            if not L.get("window") and L.get("sinks"):
+                raise ValueError("sinks are first tokens under a window")
+            if rope is None and (L.get("gq") is not None or L.get("gk") is not None):
+                raise ValueError("gains belong to a rope's norm")
         if any(L.get(k) is not None for L in layers for k in ("window", "sinks", "gq", "gk")):
             self.attn = jet.make_stack_attn(self.layers)
         wsb = jet.jet_stack_window_workspace_bytes(n, dims, Dff, len(layers), self.attn)

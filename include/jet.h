@@ -331,8 +331,9 @@ jet_status jet_prefill_attend(const jet_layout* lay, const jet_dims* dims, const
  *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = p f_i,  for i < rot / 2
  * with (a, b) = (y[i], y[i + rot / 2]) (JET_ROPE_HALVES) or (y[2 i], y[2 i + 1])
  * (JET_ROPE_PAIRS); the elements from rot on stay y. All of it is float32, rounded once
- * to the output's type; the angle is exact modulo a turn for every int32 position, up to
- * the 53 binary digits of f_i. Heads whose squares leave float32 are normalised all the same, a
+ * to the output's type. The angle is taken modulo a turn in whole numbers: before its rounding
+ * to float32 it is off by |p f_i| 2^-52 radians at most, the digits of f_i, and by 2^-30 at the
+ * farthest int32 positions, those of its fraction of a turn. Heads whose squares leave float32 are normalised all the same, a
  * head of zeros stays zeros without eps too, and an infinite element gives NaN in its pair and
  * zeros in the rest of its head.
  */
@@ -344,7 +345,7 @@ typedef struct jet_rope {
   int32_t style;       /* JET_ROPE_*                                                    */
   int32_t norm;        /* 1: the heads are normalised first                            */
   float eps;
-  uint64_t turn[128];  /* f_i / (2 pi) of pair i, as a fraction of 2^64                */
+  uint64_t turn[128];  /* f_i / (2 pi) of pair i, modulo 1, as a fraction of 2^64      */
 } jet_rope;
 
 /*

@@ -1,6 +1,7 @@
 // What the rotation by position needs of a model (jet_rope): the frequencies as fractions
 // of a turn. An angle p f is needed modulo a turn only, and p times f / (2 pi) in units of
-// 2^-64 turns wraps in 64 bits by itself: no position loses digits to a large angle.
+// 2^-64 turns wraps in 64 bits by itself: no position loses digits to a large angle. What is left
+// are the digits of the quotient f / (2 pi) in doubles, 2^-52 of itself.
 #include <cmath>
 #include <cstring>
 
@@ -23,11 +24,11 @@ extern "C" jet_status jet_rope_init(int32_t rot, int32_t style, double theta, co
   for (int i = 0; i < rot / 2; ++i) {
     const double f = freq ? freq[i] : std::pow(theta, -2.0 * i / rot);
     if (!std::isfinite(f)) return JET_ERR_ARG;
-    double t = std::fmod(f / 6.283185307179586476925286766559, 1.0);
-    if (t < 0.0) t += 1.0;
-    // a t just below a turn may round up to it: no turn at all
-    const double scaled = std::ldexp(t, 64);
-    r.turn[i] = scaled >= 18446744073709551616.0 ? 0u : static_cast<uint64_t>(scaled);
+    // the fraction of its magnitude, to all 64 digits; a backward one is its complement (1 - t in
+    // doubles would keep 54 binary digits of a small t)
+    const double t = std::fmod(std::fabs(f) / 6.283185307179586476925286766559, 1.0);
+    const uint64_t turn = static_cast<uint64_t>(std::ldexp(t, 64));  // t < 1
+    r.turn[i] = f < 0.0 ? uint64_t(0) - turn : turn;
   }
   *out = r;
   return JET_OK;

@@ -11,7 +11,8 @@
 //
 // An angle is a 64-bit fraction of a turn, position times frequency modulo 2^64; its
 // nearest quarter turn is taken off exactly and the rest, at most an eighth of a turn, is
-// rounded to float32 for sincospif: off by less than 2^-25 radians at any position.
+// rounded to float32 for sincospif, by less than 2^-25 radians at any position. (The frequency's
+// own digits count |p f| 2^-52 beside that: 2^-21 at f = 1 and the farthest int32 positions.)
 //
 // Everything is float32 from the load to the one rounding of the store. 74,210 tokens of 24 + 4
 // heads of 256 (1.06 GB each way in bf16) take 350 us, 91 % of the copy rate. A warp's loads are

@@ -398,16 +398,18 @@ jet_status jet_norm_rotate_rows(const jet_layout* lay, const jet_dims* dims,
  * JET_ERR_ARG); every row sees itself, the shared row its prefix's last key. What a row
  * does not see does not reach it, infinities and NaN among it; scores that are all minus
  * infinity give NaN. bf16: the weights are rounded to bf16 before their product with the
- * values, scores, maxima and sums are float32. bf16 outputs that come out NaN or infinite beside
- * such keys, seen or not, are computed again key by key at the end of the call: the same answer
- * at a hundred times the cost and more (16,000 positions under 4,096 with 32 heads of 128 take
+ * values (their sum takes them rounded in the step, as they were in the prefill), scores, maxima
+ * and sums are float32. Outputs that come out NaN or infinite, beside such keys, seen or not, or by
+ * sums past the largest float, are computed again key by key at the end of the call: the same
+ * answer at a hundred times the cost and more (16,000 positions under 4,096 with 32 heads of 128 take
  * 0.6 ms, 220 ms with one NaN in every head's values of a first token; a token that is NaN
  * throughout ends its rows' second computation at once, 1.3 ms).
  *
  * jet_prefix_attend_window - the step (arguments, types and head sizes of
  * jet_prefix_attend; bf16: at most 128 query heads a key/value head, else
- * JET_ERR_UNSUPPORTED). The whole prefix is given; only the keys that some row sees are
- * read, the first `sinks` (and up to 15 beside them) and the last `window` of each request.
+ * JET_ERR_UNSUPPORTED). The whole prefix is given; of a request the first `sinks` keys (and up to
+ * 15 beside them) and the last `window` are read, in bf16 in whole tiles, so up to 63 keys past
+ * the prefix's end, the next request's, are read and masked (127 in the prefill).
  * ws/ws_bytes: scratch of at least jet_attend_window_workspace_bytes().
  */
 size_t jet_attend_window_workspace_bytes(const jet_sizes* n, const jet_dims* dims,

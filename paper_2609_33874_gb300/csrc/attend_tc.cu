@@ -35,10 +35,11 @@
 // one of 500 keys 14.3 -> 13.1 us, 32 of 2,048 - 8,192 keys 86.0 -> 85.0 us).
 //
 // Under a window (WIN) a request's keys are slots (window.h): its first tokens and what its
-// shared row sees, so nothing else is read; what a row further on does not see of them is masked.
+// shared row sees, so nothing else is read but the rest of whole tiles; what a row further on does
+// not see of them is masked.
 // Such items are short, so up to d 128 two CTAs share an SM (Geo). 256 requests of 2,048 - 8,192
-// under 2,048 (2 kv heads of 256) take 191 us, 88 % of the copy rate; one row of each of 64 under
-// 1,024 (8 heads of 128) 51.8, 78 %; 16 requests of 200 - 1,200 under 128 (4 heads of 256) 10.6,
+// under 2,048 (2 kv heads of 256) take 190 us, 88 % of the copy rate; one row of each of 64 under
+// 1,024 (8 heads of 128) 52.1, 78 %; 16 requests of 200 - 1,200 under 128 (4 heads of 256) 10.6,
 // latencies in a row as above.
 #include <algorithm>
 #include <cmath>
@@ -56,8 +57,8 @@ constexpr int kThreads = 224;
 constexpr int kSchedWarp = 6;  // the work-item scheduler
 
 // PAIRED: two CTAs an SM (the windowed step up to d 128), so that one's tiles come while the
-// other's item begins or ends: an item under a window is 2 to 20 tiles long, and its start and
-// end take as long as five. P then lies over the S tile that it comes from and the output
+// other's item begins or ends: an item under a window of 128 is 3 to 4 tiles long, one under 1,024
+// 17, and its start and end take as long as five. P then lies over the S tile that it comes from and the output
 // stage is half as large.
 template <int DH, bool PAIRED>
 struct Geo {
@@ -590,7 +591,7 @@ attend_prefix_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
     const int i = q4 * 32 + lane;  // query vector within the block = TMEM lane
     const uint32_t lane_off = uint32_t(q4 * 32) << 16;
     // the output is transposed through this warp's own 4 KB of the output
-    // stage so that every global store covers whole 64- or 128-byte pieces of
+    // stage (2 KB where two CTAs share an SM) so that every global store covers whole 64- or 128-byte pieces of
     // one vector's output
     constexpr int PC = G::kPieces;  // 16-byte pieces of a row at a time
     uint4* stage = reinterpret_cast<uint4*>(smem + G::kOffStage + q4 * 32 * PC * 16);
@@ -1211,7 +1212,7 @@ jet_sizes window_sizes(const jet_sizes& n, int window, int sinks) {
 // their sum's share of a CTA counts, and what the schedule leaves uneven (0.25 of an item where
 // chunks are whole requests, 0.6 else); chunks cost the combine's launch (2.8 us) and their
 // partials' way out and back (0.2 us a MB). Fitted to 45 batches of 1 to 256 requests under
-// windows of 128 to 8,192 at up to 13 chunk lengths each: the chosen ones take 1.1 % more than
+// windows of 128 to 8,192 at up to 13 chunk lengths each: the chosen ones take 1.2 % more than
 // the best, the plan of the call without a window 8 % (127 requests of 1,733 tokens, one kv head
 // of 128: unsplit 28.9, in its chunks 44.6; one of 4,641, two: 34.4 unsplit, 13.7 in chunks of
 // 192).

@@ -17,7 +17,9 @@
 //   warps 3..10   softmax: a query vector is a TMEM lane, and two warps share each lane, 32 of
 //                 every 64 of the tile's columns each: they tell each other their maximum
 //   warps 11..14  output: O / l to memory
-// Items are short under a window (2 to 10 tiles), so what counts is that they overlap: at d
+// and after the last item all of them: outputs that came out NaN or infinite (window_rows.cuh).
+// Items are short under a narrow window (two tiles for 16/2 heads under 128; 33 for 32/8 under
+// 4,096), so what counts is that they overlap: at d
 // 64 and 128 there are two query blocks in shared memory and two O in TMEM, and an item's
 // products begin while the last one's output is read. All barriers an MMA waits for live in
 // the even CTA; the commits reach both.
@@ -228,22 +230,18 @@ __device__ __forceinline__ RowBounds row_bounds(const Window& w, const WinItem& 
 // in L2; the pairs deal them out back and forth (0 .. n-1, n-1 .. 0, ...), without a work list or
 // a counter. Both CTAs derive the same items.
 struct WinSchedule {
-  long long before;  // items of the requests before this window of 32
-  int base, round;   // the window's first request in the order; the deal's
-  int cnt, inc, r, P, first, total;
-  bool held;         // the window's block counts are there
+  long long before = 0;  // items of the requests before this window of 32
+  int base = 0, total = -1, cnt = 0, inc = 0, r = 0, P = 0, first = 0;  // total -1: not counted
 };
 
-// One warp; ntiles 0: no more items.
-__device__ __forceinline__ WinItem next_item(const WinPreArgs& a, WinSchedule& s, int pair,
-                                             int npairs, int rank, int lane) {
+// The deal's item number `round`, of growing numbers. One warp; ntiles 0: no more items.
+__device__ __forceinline__ WinItem next_item(const WinPreArgs& a, WinSchedule& s, int round,
+                                             int pair, int npairs, int rank, int lane) {
   const int g = a.g, rb = a.rb;
-  const long long k =
-      (long long)s.round * npairs + ((s.round & 1) ? npairs - 1 - pair : pair);
-  ++s.round;
+  const long long k = (long long)round * npairs + ((round & 1) ? npairs - 1 - pair : pair);
   WinItem it{};
-  for (; s.base < a.R; s.base += 32) {
-    if (!s.held) {
+  for (;;) {
+    if (s.total < 0) {  // the window's block counts
       const int ri = s.base + lane;
       s.cnt = s.r = s.P = s.first = 0;
       if (ri < a.R) {
@@ -268,7 +266,6 @@ __device__ __forceinline__ WinItem next_item(const WinPreArgs& a, WinSchedule& s
         if (lane >= o) s.inc += y;
       }
       s.total = __shfl_sync(0xffffffffu, s.inc, 31);
-      s.held = true;
     }
     if (k < s.before + s.total) {
       const unsigned hit = __ballot_sync(0xffffffffu, k < s.before + s.inc);
@@ -289,7 +286,9 @@ __device__ __forceinline__ WinItem next_item(const WinPreArgs& a, WinSchedule& s
       break;
     }
     s.before += s.total;
-    s.held = false;
+    s.base += 32;
+    if (s.base >= a.R) break;  // no more items
+    s.total = -1;
   }
   return it;
 }
@@ -310,7 +309,7 @@ __device__ __noinline__ void odd_outputs(const WinPreArgs& a, const OddItems& od
   WinSchedule order{};
   for (int u = 0;; ++u) {
     const WinItem e =
-        next_item(a, order, int(blockIdx.x >> 1), int(gridDim.x >> 1), rank, lane);
+        next_item(a, order, u, int(blockIdx.x >> 1), int(gridDim.x >> 1), rank, lane);
     if (e.ntiles == 0) break;
     if (!odd.has(u)) continue;
     const __nv_bfloat16* out = a.o + (size_t(e.p0 + e.row0) * a.Hq + size_t(e.kh) * a.g) * DH;
@@ -319,6 +318,9 @@ __device__ __noinline__ void odd_outputs(const WinPreArgs& a, const OddItems& od
         again<DH>(a, e, gi, lane);
   }
 }
+
+// (a call: inlined, the output warps' code cost d 64 and 128 0.4 %)
+__device__ __noinline__ void note_odd(OddItems* odd, int u) { odd->note(u); }
 
 template <int DH, bool SKIP>
 __global__ void __launch_bounds__(kWinThreads, 1)
@@ -426,7 +428,7 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
     // ---------------------------------------------------------------- schedule
     WinSchedule order{};
     for (int u = 0;; ++u) {
-      const WinItem it = next_item(a, order, pair, npairs, int(rank), lane);
+      const WinItem it = next_item(a, order, u, pair, npairs, int(rank), lane);
       const int slot = u % kRing;
       bool okw = true;
       if (lane == 0)
@@ -922,7 +924,7 @@ prefill_window_kernel(const __grid_constant__ CUtensorMap tmQ,
       // largest float) are computed again from what they see alone, after the last item
       const bool odd = !(l > 0.f) || __hisnan(most.x) || __hisnan(most.y) || __hisinf(most.x) ||
                        __hisinf(most.y);
-      if (__any_sync(0xffffffffu, i < e.nv && odd) && lane == 0) odd_items()->note(u);
+      if (__any_sync(0xffffffffu, i < e.nv && odd) && lane == 0) note_odd(odd_items(), u);
     }
     if (!ok) {
       *abort_flag = 1;

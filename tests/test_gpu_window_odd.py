@@ -195,3 +195,26 @@ def test_a_seen_key_of_weight_zero_shows_its_values(cuda, bad, bf16):
     assert np.isnan(got[70:, 2:, 7]).all()
     got[70:, 2:, 7] = 0.0
     assert np.isfinite(got).all()
+
+
+@pytest.mark.parametrize("d,heads", [(64, (16, 2)), (128, (8, 8)), (256, (16, 2))])
+@pytest.mark.parametrize("window,sinks", [(1000, 4), (2048, 0)])
+def test_prefill_wide_windows_end_where_they_should(cuda, d, heads, window, sinks):
+    """A key that is NaN, seen by the last row of whose window it is part and by none after, in
+    windows of many tiles, whose middle ones are not masked: a key too few or too many there is
+    less than the bars of the weights."""
+    P = [3500]
+    p = Prefill(cuda, P, *heads, d, seed=28)
+    rng = np.random.default_rng(28)
+    for j in (sinks, 127, 128, 611, 640, 1000, 1333):
+        k = p.k[j].clone()
+        p.k[j] = float("nan")
+        p.run(window, sinks)
+        got = np.isnan(_np(p.o))
+        sees = B.in_window(np.arange(P[0]), [j], window, sinks)[:, 0]
+        assert got[sees].all() and not got[~sees].any(), j
+        rows = np.unique(np.clip([0, j - 1, j + window, j + window + 1, *rng.integers(0, 3500, 6)],
+                                 0, P[0] - 1))
+        rows = rows[~sees[rows]]
+        p.check(window, sinks, rows_of=[rows])
+        p.k[j] = k

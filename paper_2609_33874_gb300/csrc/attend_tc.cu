@@ -38,8 +38,8 @@
 // shared row sees, so nothing else is read but the rest of whole tiles; what a row further on does
 // not see of them is masked.
 // Such items are short, so up to d 128 two CTAs share an SM (Geo). 256 requests of 2,048 - 8,192
-// under 2,048 (2 kv heads of 256) take 190 us, 88 % of the copy rate; one row of each of 64 under
-// 1,024 (8 heads of 128) 52.1, 78 %; 16 requests of 200 - 1,200 under 128 (4 heads of 256) 10.6,
+// under 2,048 (2 kv heads of 256) take 194 us, 87 % of the copy rate; one row of each of 64 under
+// 1,024 (8 heads of 128) 52.7, 77 %; 16 requests of 200 - 1,200 under 128 (4 heads of 256) 10.6,
 // latencies in a row as above.
 #include <algorithm>
 #include <cmath>

@@ -939,12 +939,12 @@ combine_window_kernel(const AttArgs a, const WinArgs<true> w, const int32_t* __r
   }
   // (of an output that is computed again nothing is stored here: other lanes would store the
   // same addresses there, and nothing orders the two)
-  if (!__any_sync(0xffffffffu, odd)) {
+  auto store = [&] {
 #pragma unroll
     for (int i = 0; i < PER; ++i)
       a.o[(size_t(n) * a.Hq + h) * DH + lane + 32 * i] = __float2bfloat16_rn(acc[i]);
-    return;
-  }
+  };
+  if (!__any_sync(0xffffffffu, odd)) return store();
   ItemGeo e{};
   e.n0 = a.row_offset[r];
   e.kh = h / a.g;
@@ -952,8 +952,8 @@ combine_window_kernel(const AttArgs a, const WinArgs<true> w, const int32_t* __r
   e.P = a.prefix_offset[r + 1] - e.p0;
   int f;
   const int t = own_tokens(a, r, n, &f);
-  // a request that was left out has no chunks to combine
-  if (!request_fits(a, e.n0, 1, e.p0, e.P) || n < e.n0 || t < 0) return;
+  // (a layout that lies of the row or its request: what the chunks gave)
+  if (!request_fits(a, e.n0, 1, e.p0, e.P) || n < e.n0 || t < 0) return store();
   again<DH>(a, w, e, (n - e.n0) * a.g + h % a.g, t, f, lane);
 }
 

@@ -38,6 +38,25 @@ def test_outputs_of_chunks_are_stored_once(cuda, d, heads):
         assert torch.equal(s.o, first)
 
 
+def test_odd_rows_of_a_lying_candidate_are_written(cuda):
+    """A candidate whose first row the layout puts past the row in question: no own tokens are
+    read, and what the chunks gave is stored."""
+    import torch
+    s = Step(cuda, [20000], [2], [5, 3], 16, 2, 128, True, seed=29)
+    s.v[25] = float("nan")
+    s.run(6000, 20)
+    first = s.o.clone()
+    words = s.dev.words.clone()
+    words[(s.dev.struct.cand_row_offset - s.dev.words.data_ptr()) // 4 + 1] = 1 << 30
+    s.o.fill_(7.0)
+    cuda.jet_prefix_attend_window(cuda.DeviceLayout(s.hl.sizes, words), s.dims, 6000, 20, s.q, s.k,
+                                  s.v, s.kc, s.vc, s.o, s.ws(6000, 20))
+    torch.cuda.synchronize()
+    cuda.jet_device_status()
+    of = torch.from_numpy(s.lay["row_cand"] == 1).cuda()
+    assert (s.o[~of] == first[~of]).all() and not (s.o[of] == 7.0).any()
+
+
 def _within(cuda, budget_ns, call):
     old = cuda.jet_set_wait_budget_ns(budget_ns)
     try:
